@@ -375,6 +375,128 @@ lora_status lora_merge(int32_t num_layers, int32_t n, int32_t k, int32_t rank, f
                        int32_t variant, void* const* d_Wt_ptrs, int64_t ldw,
                        const void* const* d_At_ptrs, const void* const* d_Bt_ptrs, void* hip_stream);
 
+/*
+ * ATTENTION.  What runs between the projections that lora_fused_forward computes: attention of a batch of prompts, and a
+ * cache of keys and values in 4 bits with the attention that reads it.  dtype is that of queries, keys, values and outputs
+ * (LORA_BF16 or LORA_F32); head h of a token is at h * head_dim of its row, rows `ld` elements apart, so that q, k and v may be
+ * columns of one projection's output.  Query head h uses the keys and values of head h / (num_heads / num_kv_heads).
+ * head_dim is 1 .. LORA_MAX_HEAD_DIM.  Pointers have to be aligned to an element; the fast kernels want 16 bytes, leading
+ * dimensions and head_dim multiples of 8 (fp32: 4), anything else runs on a general kernel, one to two orders of magnitude
+ * slower for prompts and no slower for the cache.  Outputs must not share memory with inputs.
+ *
+ * Scores, softmax and sums are held in 32 bits; in bf16 the softmax weights are rounded to bf16 for the product with the
+ * values, as the output is.  What a query does not see has no effect on it, also where it holds infinities or NaN; a query
+ * that sees no key gets zeros.
+ */
+#define LORA_MAX_HEAD_DIM 256
+
+typedef struct lora_attention_plan lora_attention_plan;   /* opaque, library-owned; as lora_plan in all else */
+
+/* A batch of prompts, packed one behind the other.  HOST pointers, read during lora_attention_plan_create only. */
+typedef struct {
+    int32_t        num_seqs;       /* S >= 0 */
+    const int32_t* q_indptr;       /* [S+1] rows of q and o of each sequence: [0] = 0, non-decreasing */
+    const int32_t* kv_indptr;      /* [S+1] rows of k and v; NULL: q_indptr.  A sequence may have more keys than queries (they come
+                                      before its queries' own: a prefix, an earlier part of the prompt) or fewer */
+    int32_t        num_heads;      /* H >= 1 */
+    int32_t        num_kv_heads;   /* divides num_heads */
+    int32_t        head_dim;
+    int32_t        dtype;          /* lora_dtype */
+    int32_t        causal;         /* 1: of n queries and m keys, query i sees the keys j <= i + m - n; 0: every key */
+} lora_attention_desc;
+
+/* Pure host code: tiles of the queries, longest first.  One plan serves all layers of the batch.
+ * LORA_ERR_INVALID_ARG: null desc / out / q_indptr, offsets that do not start at 0 or decrease, heads < 1, num_heads no
+ * multiple of num_kv_heads, head_dim outside 1 .. LORA_MAX_HEAD_DIM, unknown dtype, causal other than 0 or 1.
+ * LORA_ERR_UNSUPPORTED: more than 2^30 rows. */
+lora_status lora_attention_plan_create(const lora_attention_desc* desc, lora_attention_plan** out);
+void        lora_attention_plan_destroy(lora_attention_plan* plan);
+lora_status lora_attention_plan_upload(lora_attention_plan* plan, void* hip_stream);
+
+/*
+ * lora_attention -- attention of the plan's prompts:
+ *     o[i,h,:] = sum_j p_ij v[j,h',:] / sum_j p_ij,   p_ij = exp(scale * q[i,h,:] . k[j,h',:] - max_j),   h' = h's kv head
+ * over the keys j of the query's own sequence that it sees.  scale: finite.
+ */
+lora_status lora_attention(lora_attention_plan* plan, const void* q, int64_t ldq, const void* k, int64_t ldk,
+                           const void* v, int64_t ldv, void* o, int64_t ldo, float scale, void* hip_stream);
+
+/*
+ * THE CACHE.  Keys and values of num_seqs sequences in pages of page_tokens tokens; page p of a sequence is
+ * page_table[s * table_stride + p], its tokens are slots p * page_tokens ...  A token's keys (and values) of one head are
+ * held as codes of 4 bits between their least element and 15 steps above it:
+ *     zero = least element, rounded down to bf16;  step = bf16(fp32(greatest - zero) * fp32(1/15)), 0 if below 2^-100
+ *     code = min(15, max(0, rint((x - zero) / step)))  (0 where step is 0);   value = code * step + zero
+ * A token with an infinite element or NaN, or whose range is no number of 32 bits, has NaN for values.
+ * Format of a page of one kv head (lora_cache_page_bytes; heads of a page one behind the other, pages too), with DP the
+ * head_dim padded to 64, 128 or 256 (padded codes are 0; a step's bf16 is in the low and a zero's in the high half of a word):
+ *     codes of the keys     [page_tokens][DP/2]           dims 2b (low nibble) and 2b+1 in byte b
+ *     codes of the values   [page_tokens/32][4][16][8][DP/32]   token 32 i + 8 g + t, dims (DP/16) r ...: at [i][g][r][t]
+ *     words of the keys     [page_tokens], words of the values [page_tokens]
+ * so that lora_cache_attention's loads of 16 bytes a lane are operands of the matrix cores as they are.
+ * The descriptor is the caller's; it is read during a call only.  All pointers in it are device memory.  Lengths, page tables and
+ * offsets are read on the device when the call runs (a captured graph replays with what they hold then): the host cannot check
+ * them, so the kernels keep to the bounds that the descriptor gives.  Lengths are cut to max_length; slots whose page is outside
+ * [0, num_pages) count as not there: they are not written, not seen, and read as zeros.
+ */
+typedef struct {
+    void*          pages;          /* [num_pages][num_kv_heads] pages, 16-byte aligned */
+    float*         weight;         /* accumulated weights [num_pages][num_kv_heads][page_tokens], or NULL: none kept */
+    const int32_t* page_table;     /* [num_seqs][table_stride] */
+    int32_t*       length;         /* [num_seqs] tokens held, those of the call at hand included (written by lora_cache_evict only) */
+    int64_t        num_pages;
+    int32_t        num_seqs;
+    int32_t        table_stride;
+    int32_t        max_length;     /* no sequence is longer; <= table_stride * page_tokens */
+    int32_t        page_tokens;    /* multiple of 32, at most 1024 */
+    int32_t        num_kv_heads;
+    int32_t        head_dim;
+} lora_cache;
+
+/* bytes of a page of one head; 0 for page_tokens or head_dim that no cache has */
+size_t lora_cache_page_bytes(int32_t page_tokens, int32_t head_dim);
+
+/*
+ * The calls below take the last tokens of every sequence, packed: sequence s has the rows d_indptr[s] .. d_indptr[s+1] - 1 (device
+ * array [num_seqs + 1]; NULL: one token a sequence, row s), the last of them being slot length[s] - 1.  num_tokens: rows in all;
+ * max_new: no sequence has more (a bound: more are left out).  Rows outside [0, num_tokens) are left out, too.
+ *
+ * lora_cache_append -- the tokens' keys and values into the cache; accumulated weights of their slots start at 0.
+ * No two sequences may write one page.
+ */
+lora_status lora_cache_append(const lora_cache* cache, int32_t dtype, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr,
+                              const void* k, int64_t ldk, const void* v, int64_t ldv, void* hip_stream);
+
+/* lora_cache_read -- the values that the cache holds of the tokens (code * step + zero in 32 bits, rounded to dtype). */
+lora_status lora_cache_read(const lora_cache* cache, int32_t dtype, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr,
+                            void* k, int64_t ldk, void* v, int64_t ldv, void* hip_stream);
+
+/*
+ * lora_cache_attention -- the tokens attend to their sequences' caches: token i of n of a sequence of length L sees the slots
+ * 0 .. L - n + i (single tokens: all).  Output as lora_attention's, over the values that the cache holds.
+ * decay in [0, 1]: accumulated weights of every sequence that has a token in the call are carried on,
+ *     weight[slot] = decay * weight[slot] + sum over its tokens and the kv head's query heads of p / sum p
+ * (0: what was there is not read); negative: weights are left alone.
+ * workspace: lora_cache_workspace's bytes for these arguments (weights: 1 where decay >= 0; 0 bytes: none needed), 256-byte
+ * aligned.  Nothing in it is kept from one call to the next.  Deterministic: no atomics.
+ */
+lora_status lora_cache_workspace(const lora_cache* cache, int32_t num_heads, int32_t num_tokens, int32_t max_new, int32_t weights,
+                                 size_t* bytes);
+lora_status lora_cache_attention(const lora_cache* cache, int32_t dtype, int32_t num_heads, int32_t num_tokens, int32_t max_new,
+                                 const int32_t* d_indptr, const void* q, int64_t ldq, void* o, int64_t ldo, float scale, float decay,
+                                 void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * lora_cache_evict -- every sequence's cache down to `budget` tokens, head by head, into pages of its own: where a sequence of
+ * `source` is longer, the last `recent` (0 .. budget) slots are kept and, of the others, those with the largest accumulated
+ * weights (ties: the lower slot; NaN counts as largest).  Kept tokens keep their order; target->length[s] = min(length, budget).
+ * kept: device, [num_seqs][num_kv_heads][budget] int32, the slots kept, -1 behind them.  target: same num_seqs, num_kv_heads,
+ * head_dim and page_tokens, max_length >= budget, a length array of its own; weights of both (they move along); its tables' pages must not
+ * be pages of source's tables.  source is left as it was (its pages may be shared with other caches).
+ */
+lora_status lora_cache_evict(const lora_cache* source, const lora_cache* target, int32_t budget, int32_t recent, int32_t* kept,
+                             void* hip_stream);
+
 const char* lora_status_str(lora_status s);
 
 /*

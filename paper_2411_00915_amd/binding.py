@@ -41,6 +41,7 @@ LORA_TUNING_COUNT = 17
 LORA_EXPAND_BY_ROUNDS = 1 << 30
 LORA_STATIC_V_BYTES = 16 << 20
 LORA_STATIC_MAX_GROUPS = 4096
+LORA_MAX_HEAD_DIM = 256
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _f32p = ctypes.POINTER(ctypes.c_float)
@@ -79,6 +80,17 @@ class PlanView(ctypes.Structure):
                 ("unmerge_expand_tiles", ctypes.POINTER(Tile)), ("num_unmerge_expand_tiles", ctypes.c_int32)]
 
 
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [("num_seqs", ctypes.c_int32), ("q_indptr", _i32p), ("kv_indptr", _i32p), ("num_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32)]
+
+
+class CacheDesc(ctypes.Structure):
+    _fields_ = [("pages", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("length", ctypes.c_void_p),
+                ("num_pages", ctypes.c_int64), ("num_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("max_length", ctypes.c_int32),
+                ("page_tokens", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
 _vp = ctypes.c_void_p
 _lib.lora_plan_create.restype = ctypes.c_int
 _lib.lora_plan_create.argtypes = [ctypes.POINTER(BatchDesc), ctypes.POINTER(_vp)]
@@ -107,6 +119,14 @@ _lib.lora_fused_forward.argtypes = [_vp, _vp, ctypes.c_int64, _vp, ctypes.c_int6
 _lib.lora_merge.restype = ctypes.c_int
 _lib.lora_merge.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_float, ctypes.c_int32,
                             ctypes.c_int32, _vp, ctypes.c_int64, _vp, _vp, _vp]
+_lib.lora_attention_plan_create.restype = ctypes.c_int
+_lib.lora_attention_plan_create.argtypes = [ctypes.POINTER(AttentionDesc), ctypes.POINTER(_vp)]
+_lib.lora_attention_plan_destroy.restype = None
+_lib.lora_attention_plan_destroy.argtypes = [_vp]
+_lib.lora_cache_page_bytes.restype = ctypes.c_size_t
+_lib.lora_cache_page_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32]
+_lib.lora_cache_workspace.restype = ctypes.c_int
+_lib.lora_cache_workspace.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
 _lib.lora_status_str.restype = ctypes.c_char_p
 _lib.lora_status_str.argtypes = [ctypes.c_int]
 _lib.lora_tuning_set.restype = None
@@ -145,6 +165,8 @@ EXPORTED = ["lora_timing_begin", "lora_timing_end", "lora_timing_read", "lora_ke
             "lora_plan_create", "lora_plan_destroy", "lora_plan_query", "lora_plan_export",
             "lora_plan_upload", "lora_shrink", "lora_expand", "lora_delta", "lora_delta_static", "lora_base_gemm",
             "lora_fused_forward", "lora_merge", "lora_status_str", "lora_tuning_set", "lora_tuning_get",
+            "lora_attention_plan_create", "lora_attention_plan_destroy", "lora_attention_plan_upload", "lora_attention",
+            "lora_cache_page_bytes", "lora_cache_append", "lora_cache_read", "lora_cache_workspace", "lora_cache_attention", "lora_cache_evict",
             "lora_tuning_table_set", "lora_tuning_table_get", "lora_probe", "lora_trace_set", "lora_trace_tick_khz"]
 
 TUNING_FIELDS = ["shrink_waves", "shrink_tb2_min_rows", "shrink_max_jb", "expand_wave_bytes",
@@ -381,6 +403,90 @@ def lora_plan_export(plan: Plan) -> dict:
                 unmerge_expand_tiles=tiles(v.unmerge_expand_tiles, v.num_unmerge_expand_tiles))
 
 
+class AttentionPlan:
+    """Owner of a lora_attention_plan handle."""
+
+    def __init__(self, handle: int):
+        self._h = handle
+
+    @property
+    def handle(self) -> int:
+        return self._h
+
+    def destroy(self):
+        if self._h:
+            _lib.lora_attention_plan_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def lora_attention_plan(q_indptr, kv_indptr, num_heads, num_kv_heads, head_dim, dtype, causal=True) -> AttentionPlan:
+    """lora_attention_plan_create; offsets are host arrays (numpy or sequences).  kv_indptr None: as q_indptr."""
+    qi = np.ascontiguousarray(q_indptr, dtype=np.int32)
+    ki = qi if kv_indptr is None else np.ascontiguousarray(kv_indptr, dtype=np.int32)
+    if qi.ndim != 1 or qi.shape != ki.shape or qi.shape[0] < 1:
+        raise ValueError("q_indptr and kv_indptr: one offset for every sequence and one behind the last")
+    desc = AttentionDesc(qi.shape[0] - 1, qi.ctypes.data_as(_i32p), ki.ctypes.data_as(_i32p), int(num_heads), int(num_kv_heads), int(head_dim),
+                         int(dtype), int(causal))
+    out = _vp()
+    _check(_lib.lora_attention_plan_create(ctypes.byref(desc), ctypes.byref(out)), "lora_attention_plan_create")
+    return AttentionPlan(out.value)
+
+
+def lora_attention_plan_create_raw(desc: Optional[AttentionDesc]):
+    """Direct call for error-path tests: returns (status, handle)."""
+    out = _vp()
+    st = _lib.lora_attention_plan_create(ctypes.byref(desc) if desc is not None else None, ctypes.byref(out))
+    return st, out.value
+
+
+def lora_cache_page_bytes(page_tokens: int, head_dim: int) -> int:
+    return int(_lib.lora_cache_page_bytes(int(page_tokens), int(head_dim)))
+
+
+class Cache:
+    """A lora_cache descriptor and the device tensors that it names (kept alive by it)."""
+
+    def __init__(self, desc: CacheDesc, keepalive):
+        self.desc = desc
+        self.handle = ctypes.addressof(desc)
+        self._keep = keepalive
+
+
+def lora_cache(pages, page_table, length, page_tokens, num_kv_heads, head_dim, max_length, weight=None) -> Cache:
+    """Descriptor over device tensors: pages (uint8, [num_pages][num_kv_heads][lora_cache_page_bytes]), page_table (int32, [num_seqs,
+    table_stride]), length (int32, [num_seqs]), weight (float32, [num_pages, num_kv_heads, page_tokens], or None)."""
+    import torch
+    page_bytes = lora_cache_page_bytes(page_tokens, head_dim) * int(num_kv_heads)
+    if page_bytes <= 0:
+        raise ValueError(f"no cache has pages of {page_tokens} tokens, {num_kv_heads} heads of {head_dim}")
+    for name, x, dtype in (("pages", pages, torch.uint8), ("page_table", page_table, torch.int32), ("length", length, torch.int32),
+                           ("weight", weight, torch.float32)):
+        if x is not None and (x.dtype != dtype or not x.is_contiguous()):
+            raise ValueError(f"{name}: a contiguous tensor of {dtype}")
+    num_pages = pages.numel() // page_bytes
+    if page_table.dim() != 2 or length.dim() != 1 or page_table.shape[0] != length.shape[0] or pages.numel() != num_pages * page_bytes:
+        raise ValueError("page_table [num_seqs, table_stride], length [num_seqs], whole pages")
+    if weight is not None and weight.numel() != num_pages * num_kv_heads * page_tokens:
+        raise ValueError("weight: one for every slot of every page and head")
+    desc = CacheDesc(_ptr(pages), _ptr(weight), _ptr(page_table), _ptr(length), num_pages, int(length.shape[0]), int(page_table.shape[1]),
+                     int(max_length), int(page_tokens), int(num_kv_heads), int(head_dim))
+    return Cache(desc, (pages, weight, page_table, length))
+
+
+def lora_cache_workspace(cache: Cache, num_heads, num_tokens, max_new, weights=False) -> int:
+    """Bytes that lora_cache_attention needs with these arguments"""
+    n = ctypes.c_size_t()
+    _check(_lib.lora_cache_workspace(cache.handle, int(num_heads), int(num_tokens), int(max_new), int(bool(weights)), ctypes.byref(n)),
+           "lora_cache_workspace")
+    return int(n.value)
+
+
 def _first_stream():
     """torch's current stream, and the functions that give the current device and a device's current stream once torch is
     initialised"""
@@ -408,3 +514,16 @@ _calls.bind(_check, _first_stream, *(_address(f) for f in (
 (lora_plan_upload, lora_shrink, lora_expand, lora_delta, lora_delta_static, lora_base_gemm, lora_fused_forward, lora_merge) = (
     _calls.lora_plan_upload, _calls.lora_shrink, _calls.lora_expand, _calls.lora_delta, _calls.lora_delta_static,
     _calls.lora_base_gemm, _calls.lora_fused_forward, _calls.lora_merge)
+
+_calls.bind_attention(*(_address(f) for f in (_lib.lora_attention_plan_upload, _lib.lora_attention, _lib.lora_cache_append, _lib.lora_cache_read,
+                                              _lib.lora_cache_attention, _lib.lora_cache_evict)))
+
+# lora_attention_plan_upload(plan, stream=None),
+# lora_attention(plan, q, ldq, k, ldk, v, ldv, o, ldo, scale, stream=None),
+# lora_cache_append(cache, dtype, num_tokens, max_new, d_indptr, k, ldk, v, ldv, stream=None),
+# lora_cache_read(cache, dtype, num_tokens, max_new, d_indptr, k, ldk, v, ldv, stream=None),
+# lora_cache_attention(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, o, ldo, scale, decay, workspace, workspace_bytes, stream=None),
+# lora_cache_evict(cache, target, budget, recent, d_kept, stream=None)
+(lora_attention_plan_upload, lora_attention, lora_cache_append, lora_cache_read, lora_cache_attention, lora_cache_evict) = (
+    _calls.lora_attention_plan_upload, _calls.lora_attention, _calls.lora_cache_append, _calls.lora_cache_read, _calls.lora_cache_attention,
+    _calls.lora_cache_evict)

@@ -8,6 +8,10 @@ _PROTOTYPES = [ctypes.CFUNCTYPE(ctypes.c_int, *a) for a in (
     (_P, _P, _L, _P, _P, _P, _L, _F, _P), (_I, _I, _I, _I, _P, _L, _P, _L, _P, _L, _P),
     (_P, _P, _L, _P, _L, _P, _P, _P, _L, _P, _Z, _P), (_I, _I, _I, _I, _F, _I, _I, _P, _L, _P, _P, _P))]
 
+_ATTENTION_PROTOTYPES = [ctypes.CFUNCTYPE(ctypes.c_int, *a) for a in (
+    (_P, _P), (_P, _P, _L, _P, _L, _P, _L, _P, _L, _F, _P), (_P, _I, _I, _I, _P, _P, _L, _P, _L, _P), (_P, _I, _I, _I, _P, _P, _L, _P, _L, _P),
+    (_P, _I, _I, _I, _I, _P, _P, _L, _P, _L, _F, _F, _P, _Z, _P), (_P, _P, _I, _I, _P, _P))]
+
 
 def bind(check, first_stream, *addresses):
     """As that of _calls: check(status, name) raises; first_stream()[0] is torch's current stream; the functions' addresses in
@@ -63,3 +67,39 @@ def lora_merge(num_layers, n, k, rank, scale, dtype, d_Wt_ptrs, ldw, d_At_ptrs, 
 def lora_fused_forward(plan, x, ldx, Wt, ldw, d_At_ptrs, d_Bt_ptrs, y, ldy, workspace, workspace_bytes, stream=None):
     _check(_fused_forward(plan.handle, _ptr(x), int(ldx), _ptr(Wt), int(ldw), _ptr(d_At_ptrs), _ptr(d_Bt_ptrs), _ptr(y), int(ldy),
                           _ptr(workspace), int(workspace_bytes), _stream(stream)), "lora_fused_forward")
+
+
+def bind_attention(*addresses):
+    """As that of _calls: the functions' addresses in the order attention_plan_upload, attention, cache_append, cache_read,
+    cache_attention, cache_evict"""
+    global _attention_upload, _attention, _append, _read, _cache_attention, _evict
+    _attention_upload, _attention, _append, _read, _cache_attention, _evict = (
+        prototype(address) for prototype, address in zip(_ATTENTION_PROTOTYPES, addresses))
+
+
+def lora_attention_plan_upload(plan, stream=None):
+    _check(_attention_upload(plan.handle, _stream(stream)), "lora_attention_plan_upload")
+
+
+def lora_attention(plan, q, ldq, k, ldk, v, ldv, o, ldo, scale, stream=None):
+    _check(_attention(plan.handle, _ptr(q), int(ldq), _ptr(k), int(ldk), _ptr(v), int(ldv), _ptr(o), int(ldo), float(scale), _stream(stream)),
+           "lora_attention")
+
+
+def lora_cache_append(cache, dtype, num_tokens, max_new, d_indptr, k, ldk, v, ldv, stream=None):
+    _check(_append(cache.handle, int(dtype), int(num_tokens), int(max_new), _ptr(d_indptr), _ptr(k), int(ldk), _ptr(v), int(ldv), _stream(stream)),
+           "lora_cache_append")
+
+
+def lora_cache_read(cache, dtype, num_tokens, max_new, d_indptr, k, ldk, v, ldv, stream=None):
+    _check(_read(cache.handle, int(dtype), int(num_tokens), int(max_new), _ptr(d_indptr), _ptr(k), int(ldk), _ptr(v), int(ldv), _stream(stream)),
+           "lora_cache_read")
+
+
+def lora_cache_attention(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, o, ldo, scale, decay, workspace, workspace_bytes, stream=None):
+    _check(_cache_attention(cache.handle, int(dtype), int(num_heads), int(num_tokens), int(max_new), _ptr(d_indptr), _ptr(q), int(ldq), _ptr(o), int(ldo),
+                            float(scale), float(decay), _ptr(workspace), int(workspace_bytes), _stream(stream)), "lora_cache_attention")
+
+
+def lora_cache_evict(cache, target, budget, recent, d_kept, stream=None):
+    _check(_evict(cache.handle, target.handle, int(budget), int(recent), _ptr(d_kept), _stream(stream)), "lora_cache_evict")

@@ -57,6 +57,55 @@ std::mutex g_cache_mutex;
 std::vector<cached_buf> g_cache;       // released plan tables, reused by later plans
 constexpr size_t kCacheMax = 16;
 
+}  // namespace
+
+lora_status lora_take_tables(int dev, size_t bytes, size_t* cls, void** dbuf, void** hbuf)
+{
+    // size classes (powers of two from 4 KiB) so that released buffers fit later plans
+    *cls = 4096;
+    while (*cls < bytes) *cls <<= 1;
+    {
+        std::lock_guard<std::mutex> lock(g_cache_mutex);
+        for (size_t i = 0; i < g_cache.size(); ++i) {
+            if (g_cache[i].device == dev && g_cache[i].bytes == *cls) {
+                *dbuf = g_cache[i].dev;
+                *hbuf = g_cache[i].host;
+                g_cache.erase(g_cache.begin() + i);
+                return LORA_OK;
+            }
+        }
+    }
+    if (hipMalloc(dbuf, *cls) != hipSuccess) { (void)hipGetLastError(); return LORA_ERR_NOMEM; }
+    if (hipHostMalloc(hbuf, *cls, hipHostMallocDefault) != hipSuccess) {
+        (void)hipGetLastError();
+        (void)hipFree(*dbuf);
+        return LORA_ERR_NOMEM;
+    }
+    return LORA_OK;
+}
+
+void lora_give_tables(int device, size_t cls, void* dbuf, void* hbuf)
+{
+    int cur = -1;
+    (void)hipGetDevice(&cur);
+    if (cur != device) (void)hipSetDevice(device);
+    bool kept = false;
+    {
+        std::lock_guard<std::mutex> lock(g_cache_mutex);
+        if (g_cache.size() < kCacheMax) {
+            g_cache.push_back(cached_buf{device, cls, dbuf, hbuf});
+            kept = true;
+        }
+    }
+    if (!kept) {
+        (void)hipFree(dbuf);
+        (void)hipHostFree(hbuf);
+    }
+    if (cur != device && cur >= 0) (void)hipSetDevice(cur);
+}
+
+namespace {
+
 size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
@@ -115,30 +164,11 @@ lora_status ensure_uploaded(lora_plan* p, hipStream_t stream)
     (void)static_scratch(&static_base);
 
     const table_layout L = layout_of(p);
-    // size classes (powers of two from 4 KiB) so that released buffers fit later plans
-    size_t cls = 4096;
-    while (cls < L.total) cls <<= 1;
+    size_t cls = 0;
     void* dbuf = nullptr;
     void* hbuf = nullptr;
-    {
-        std::lock_guard<std::mutex> lock(g_cache_mutex);
-        for (size_t i = 0; i < g_cache.size(); ++i) {
-            if (g_cache[i].device == dev && g_cache[i].bytes == cls) {
-                dbuf = g_cache[i].dev;
-                hbuf = g_cache[i].host;
-                g_cache.erase(g_cache.begin() + i);
-                break;
-            }
-        }
-    }
-    if (!dbuf) {
-        if (hipMalloc(&dbuf, cls) != hipSuccess) { (void)hipGetLastError(); return LORA_ERR_NOMEM; }
-        if (hipHostMalloc(&hbuf, cls, hipHostMallocDefault) != hipSuccess) {
-            (void)hipGetLastError();
-            (void)hipFree(dbuf);
-            return LORA_ERR_NOMEM;
-        }
-    }
+    const lora_status taken = lora_take_tables(dev, L.total, &cls, &dbuf, &hbuf);
+    if (taken != LORA_OK) return taken;
     char* h = static_cast<char*>(hbuf);
     auto put = [&](size_t off, const void* src, size_t bytes) { if (bytes) std::memcpy(h + off, src, bytes); };
     put(L.perm, p->perm.data(), p->perm.size() * sizeof(int32_t));
@@ -236,22 +266,7 @@ bool share_memory(const lora_plan* p, const void* x, int64_t ldx, const void* y,
 // small cache for later plans.
 static void release_device_tables(lora_plan* p)
 {
-    int cur = -1;
-    (void)hipGetDevice(&cur);
-    if (cur != p->device) (void)hipSetDevice(p->device);
-    bool kept = false;
-    {
-        std::lock_guard<std::mutex> lock(g_cache_mutex);
-        if (g_cache.size() < kCacheMax) {
-            g_cache.push_back(cached_buf{p->device, p->d_bytes, p->d_buf, p->h_stage});
-            kept = true;
-        }
-    }
-    if (!kept) {
-        (void)hipFree(p->d_buf);
-        (void)hipHostFree(p->h_stage);
-    }
-    if (cur != p->device && cur >= 0) (void)hipSetDevice(cur);
+    lora_give_tables(p->device, p->d_bytes, p->d_buf, p->h_stage);
     p->d_buf = nullptr;
     p->h_stage = nullptr;
 }

@@ -1,0 +1,44 @@
+// Plans of prompt attention and the division of the cache's attention: host code, no HIP (attention_plan.cpp).
+#pragma once
+#include <vector>
+
+#include "../../include/lora_abi.h"
+
+// Some queries of one sequence, at most LORA_ATTENTION_ROWS
+struct attention_tile {
+    int32_t q_row0;      // first row of q and o
+    int32_t rows;
+    int32_t kv_row0;     // first row of k and v of the sequence
+    int32_t num_kv;      // keys of the sequence
+    int32_t ahead;       // query i of the tile sees the keys [0, clamp(ahead + i + 1, 0, num_kv)); not causal: num_kv all along
+    int32_t max_kv;      // keys that the last query sees
+    int32_t reserved0, reserved1;
+};
+
+#define LORA_ATTENTION_ROWS 128
+#define LORA_ATTENTION_MAX_ROWS (1 << 30)      /* of a batch: row numbers and sums of two stay below 2^31 */
+
+struct lora_attention_plan {
+    int32_t num_heads = 0, num_kv_heads = 0, head_dim = 0, dtype = 0;
+    int32_t num_queries = 0, num_keys = 0;
+    std::vector<attention_tile> tiles;      // most keys first
+
+    int device = -1;
+    size_t d_bytes = 0;
+    void* d_buf = nullptr;
+    void* h_stage = nullptr;
+};
+
+// set by the device side, so that the host code of plans links without it
+extern void (*lora_attention_plan_device_release)(lora_attention_plan*);
+
+// head_dim as the cache and the kernels hold it
+inline int32_t padded_head_dim(int32_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
+
+// how lora_cache_attention divides its work, from what the host knows; the workspace's parts follow from it
+struct cache_division {
+    int32_t row_tiles, splits, split_tokens;
+    size_t stats, partial, scores, total;      // bytes before each part, in all
+    int64_t score_stride;
+};
+cache_division divide_cache_attention(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new, bool weights);

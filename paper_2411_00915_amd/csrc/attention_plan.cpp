@@ -1,0 +1,94 @@
+// Host side of attention: the tiles of a batch of prompts, and how the cache's attention divides its work.  No HIP calls in
+// this file: everything here runs, and is tested, without a GPU.
+#include <algorithm>
+#include <new>
+
+#include "attention_internal.h"
+
+void (*lora_attention_plan_device_release)(lora_attention_plan*) = nullptr;
+
+namespace {
+bool offsets_ok(const int32_t* p, int32_t n)
+{
+    if (p[0] != 0) return false;
+    for (int32_t i = 0; i < n; ++i)
+        if (p[i + 1] < p[i]) return false;
+    return true;
+}
+}  // namespace
+
+extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, lora_attention_plan** out)
+{
+    if (out) *out = nullptr;
+    if (!d || !out || d->num_seqs < 0 || !d->q_indptr) return LORA_ERR_INVALID_ARG;
+    if (d->num_heads < 1 || d->num_kv_heads < 1 || d->num_heads % d->num_kv_heads != 0) return LORA_ERR_INVALID_ARG;
+    if (d->head_dim < 1 || d->head_dim > LORA_MAX_HEAD_DIM) return LORA_ERR_INVALID_ARG;
+    if ((d->dtype != LORA_F32 && d->dtype != LORA_BF16) || (d->causal != 0 && d->causal != 1)) return LORA_ERR_INVALID_ARG;
+    const int32_t* kv = d->kv_indptr ? d->kv_indptr : d->q_indptr;
+    if (!offsets_ok(d->q_indptr, d->num_seqs) || !offsets_ok(kv, d->num_seqs)) return LORA_ERR_INVALID_ARG;
+    if (d->q_indptr[d->num_seqs] > LORA_ATTENTION_MAX_ROWS || kv[d->num_seqs] > LORA_ATTENTION_MAX_ROWS) return LORA_ERR_UNSUPPORTED;
+    lora_attention_plan* p = nullptr;
+    try {
+        p = new lora_attention_plan;
+        p->num_heads = d->num_heads;
+        p->num_kv_heads = d->num_kv_heads;
+        p->head_dim = d->head_dim;
+        p->dtype = d->dtype;
+        p->num_queries = d->q_indptr[d->num_seqs];
+        p->num_keys = kv[d->num_seqs];
+        for (int32_t s = 0; s < d->num_seqs; ++s) {
+            const int32_t nq = d->q_indptr[s + 1] - d->q_indptr[s], nk = kv[s + 1] - kv[s];
+            for (int32_t r = 0; r < nq; r += LORA_ATTENTION_ROWS) {
+                attention_tile t{};
+                t.q_row0 = d->q_indptr[s] + r;
+                t.rows = std::min(LORA_ATTENTION_ROWS, nq - r);
+                t.kv_row0 = kv[s];
+                t.num_kv = nk;
+                t.ahead = d->causal ? nk - nq + r : nk;
+                t.max_kv = (int32_t)std::max<int64_t>(0, std::min<int64_t>(nk, (int64_t)t.ahead + t.rows));
+                p->tiles.push_back(t);
+            }
+        }
+        std::stable_sort(p->tiles.begin(), p->tiles.end(), [](const attention_tile& a, const attention_tile& b) { return a.max_kv > b.max_kv; });
+    } catch (const std::bad_alloc&) {
+        delete p;
+        return LORA_ERR_NOMEM;
+    }
+    *out = p;
+    return LORA_OK;
+}
+
+extern "C" void lora_attention_plan_destroy(lora_attention_plan* p)
+{
+    if (!p) return;
+    if (p->d_buf && lora_attention_plan_device_release) lora_attention_plan_device_release(p);
+    delete p;
+}
+
+extern "C" size_t lora_cache_page_bytes(int32_t page_tokens, int32_t head_dim)
+{
+    if (page_tokens < 32 || page_tokens > 1024 || page_tokens % 32 != 0 || head_dim < 1 || head_dim > LORA_MAX_HEAD_DIM) return 0;
+    return (size_t)page_tokens * (size_t)(padded_head_dim(head_dim) + 8);
+}
+
+cache_division divide_cache_attention(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new, bool weights)
+{
+    const int64_t rows = (int64_t)num_heads / c->num_kv_heads * max_new;          // of a kv head and a sequence
+    cache_division v{};
+    v.row_tiles = (int32_t)((rows + 31) / 32);
+    const int64_t wgs = (int64_t)c->num_seqs * c->num_kv_heads * v.row_tiles;
+    constexpr int64_t target = 768;
+    const int64_t most = (c->max_length + 255) / 256;
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(most, (target + wgs - 1) / std::max<int64_t>(wgs, 1)));
+    v.split_tokens = (int32_t)std::max<int64_t>(128, ((c->max_length + splits - 1) / splits + 127) / 128 * 128);
+    v.splits = (int32_t)std::max<int64_t>(1, ((int64_t)c->max_length + v.split_tokens - 1) / v.split_tokens);
+    const size_t out_rows = (size_t)num_tokens * num_heads;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off = (off + bytes + 255) / 256 * 256; return o; };
+    v.stats = take(v.splits > 1 || weights ? out_rows * v.splits * 8 : 0);
+    v.partial = take(v.splits > 1 ? out_rows * v.splits * c->head_dim * 4 : 0);
+    v.score_stride = ((int64_t)c->max_length + 31) / 32 * 32;
+    v.scores = take(weights ? out_rows * (size_t)v.score_stride * 4 : 0);
+    v.total = off;
+    return v;
+}

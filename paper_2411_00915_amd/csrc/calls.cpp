@@ -26,6 +26,15 @@ struct library {
     decltype(&lora_merge) merge;
 } lib;
 
+struct attention_library {
+    decltype(&lora_attention_plan_upload) plan_upload;
+    decltype(&lora_attention) attention;
+    decltype(&lora_cache_append) append;
+    decltype(&lora_cache_read) read;
+    decltype(&lora_cache_attention) cache_attention;
+    decltype(&lora_cache_evict) evict;
+} attention_lib;
+
 PyObject* check = nullptr;                 // check(status, name) raises
 PyObject* first_stream = nullptr;          // torch.cuda.current_stream() by itself: initialises torch's side
 PyObject *get_device = nullptr, *get_stream = nullptr;
@@ -71,14 +80,15 @@ bool real(PyObject* o, float* out)
     return true;
 }
 
-bool handle(PyObject* plan, lora_plan** out)
+template <typename Plan>
+bool handle(PyObject* plan, Plan** out)
 {
     PyObject* h = PyObject_GetAttr(plan, s_h);
     if (!h) return false;
     void* p = nullptr;
     const bool ok = address(h, &p);
     Py_DECREF(h);
-    *out = static_cast<lora_plan*>(p);
+    *out = static_cast<Plan*>(p);
     return ok;
 }
 
@@ -165,10 +175,11 @@ PyObject* result(lora_status status, const char* function)
     for (PyObject*& o : a) o = nullptr;                                                                                        \
     if (!arguments(__func__, names, count, REQUIRED, args, nargs, kwnames, a)) return nullptr;
 #define SIGNATURE(NAME) PyObject* NAME(PyObject*, PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames)
-#define CALL(EXPRESSION)                                                                                                        \
+#define CALL(EXPRESSION) CALL_OF(lib, EXPRESSION)
+#define CALL_OF(LIBRARY, EXPRESSION)                                                                                            \
     lora_status status;                                                                                                        \
     Py_BEGIN_ALLOW_THREADS                                                                                                     \
-    status = lib.EXPRESSION;                                                                                                   \
+    status = LIBRARY.EXPRESSION;                                                                                                   \
     Py_END_ALLOW_THREADS                                                                                                       \
     return result(status, __func__);
 
@@ -271,6 +282,94 @@ SIGNATURE(lora_fused_forward)
     CALL(fused_forward(plan, x, ldx, Wt, ldw, table(At), table(Bt), y, ldy, workspace, (size_t)bytes, stream))
 }
 
+SIGNATURE(lora_attention_plan_upload)
+{
+    ARGS(1, "plan", "stream")
+    lora_attention_plan* plan;
+    void* stream;
+    if (!handle(a[0], &plan) || !stream_of(a[1], &stream)) return nullptr;
+    CALL_OF(attention_lib, plan_upload(plan, stream))
+}
+
+SIGNATURE(lora_attention)
+{
+    ARGS(10, "plan", "q", "ldq", "k", "ldk", "v", "ldv", "o", "ldo", "scale", "stream")
+    lora_attention_plan* plan;
+    void *q, *k, *v, *o, *stream;
+    int64_t ldq, ldk, ldv, ldo;
+    float scale;
+    if (!handle(a[0], &plan) || !address(a[1], &q) || !integer(a[2], &ldq) || !address(a[3], &k) || !integer(a[4], &ldk) || !address(a[5], &v) ||
+        !integer(a[6], &ldv) || !address(a[7], &o) || !integer(a[8], &ldo) || !real(a[9], &scale) || !stream_of(a[10], &stream))
+        return nullptr;
+    CALL_OF(attention_lib, attention(plan, q, ldq, k, ldk, v, ldv, o, ldo, scale, stream))
+}
+
+SIGNATURE(lora_cache_append)
+{
+    ARGS(9, "cache", "dtype", "num_tokens", "max_new", "d_indptr", "k", "ldk", "v", "ldv", "stream")
+    const lora_cache* cache;
+    int64_t dtype, num_tokens, max_new, ldk, ldv;
+    void *indptr, *k, *v, *stream;
+    if (!handle(a[0], &cache) || !integer(a[1], &dtype) || !integer(a[2], &num_tokens) || !integer(a[3], &max_new) || !address(a[4], &indptr) ||
+        !address(a[5], &k) || !integer(a[6], &ldk) || !address(a[7], &v) || !integer(a[8], &ldv) || !stream_of(a[9], &stream))
+        return nullptr;
+    CALL_OF(attention_lib, append(cache, (int32_t)dtype, (int32_t)num_tokens, (int32_t)max_new, static_cast<const int32_t*>(indptr), k, ldk, v, ldv, stream))
+}
+
+SIGNATURE(lora_cache_read)
+{
+    ARGS(9, "cache", "dtype", "num_tokens", "max_new", "d_indptr", "k", "ldk", "v", "ldv", "stream")
+    const lora_cache* cache;
+    int64_t dtype, num_tokens, max_new, ldk, ldv;
+    void *indptr, *k, *v, *stream;
+    if (!handle(a[0], &cache) || !integer(a[1], &dtype) || !integer(a[2], &num_tokens) || !integer(a[3], &max_new) || !address(a[4], &indptr) ||
+        !address(a[5], &k) || !integer(a[6], &ldk) || !address(a[7], &v) || !integer(a[8], &ldv) || !stream_of(a[9], &stream))
+        return nullptr;
+    CALL_OF(attention_lib, read(cache, (int32_t)dtype, (int32_t)num_tokens, (int32_t)max_new, static_cast<const int32_t*>(indptr), k, ldk, v, ldv, stream))
+}
+
+SIGNATURE(lora_cache_attention)
+{
+    ARGS(14, "cache", "dtype", "num_heads", "num_tokens", "max_new", "d_indptr", "q", "ldq", "o", "ldo", "scale", "decay", "workspace", "workspace_bytes",
+         "stream")
+    const lora_cache* cache;
+    int64_t dtype, num_heads, num_tokens, max_new, ldq, ldo, bytes;
+    float scale, decay;
+    void *indptr, *q, *o, *workspace, *stream;
+    if (!handle(a[0], &cache) || !integer(a[1], &dtype) || !integer(a[2], &num_heads) || !integer(a[3], &num_tokens) || !integer(a[4], &max_new) ||
+        !address(a[5], &indptr) || !address(a[6], &q) || !integer(a[7], &ldq) || !address(a[8], &o) || !integer(a[9], &ldo) || !real(a[10], &scale) ||
+        !real(a[11], &decay) || !address(a[12], &workspace) || !integer(a[13], &bytes) || !stream_of(a[14], &stream))
+        return nullptr;
+    CALL_OF(attention_lib, cache_attention(cache, (int32_t)dtype, (int32_t)num_heads, (int32_t)num_tokens, (int32_t)max_new,
+                                           static_cast<const int32_t*>(indptr), q, ldq, o, ldo, scale, decay, workspace, (size_t)bytes, stream))
+}
+
+SIGNATURE(lora_cache_evict)
+{
+    ARGS(5, "cache", "target", "budget", "recent", "d_kept", "stream")
+    const lora_cache *cache, *target;
+    int64_t budget, recent;
+    void *kept, *stream;
+    if (!handle(a[0], &cache) || !handle(a[1], &target) || !integer(a[2], &budget) || !integer(a[3], &recent) || !address(a[4], &kept) ||
+        !stream_of(a[5], &stream))
+        return nullptr;
+    CALL_OF(attention_lib, evict(cache, target, (int32_t)budget, (int32_t)recent, static_cast<int32_t*>(kept), stream))
+}
+
+// bind_attention(addresses of the library's functions in the order of `attention_library`)
+PyObject* bind_attention(PyObject*, PyObject* args)
+{
+    unsigned long long p[6];
+    if (!PyArg_ParseTuple(args, "KKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5])) return nullptr;
+    attention_lib = attention_library{reinterpret_cast<decltype(attention_library::plan_upload)>(p[0]),
+                                      reinterpret_cast<decltype(attention_library::attention)>(p[1]),
+                                      reinterpret_cast<decltype(attention_library::append)>(p[2]),
+                                      reinterpret_cast<decltype(attention_library::read)>(p[3]),
+                                      reinterpret_cast<decltype(attention_library::cache_attention)>(p[4]),
+                                      reinterpret_cast<decltype(attention_library::evict)>(p[5])};
+    Py_RETURN_NONE;
+}
+
 // bind(check, first_stream, addresses of the library's functions in the order of `library`)
 PyObject* bind(PyObject*, PyObject* args)
 {
@@ -293,6 +392,7 @@ PyObject* bind(PyObject*, PyObject* args)
     {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(NAME)), METH_FASTCALL | METH_KEYWORDS, #NAME SIGNATURE_ "\n--\n\n"}
 PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, nullptr},
+    {"bind_attention", bind_attention, METH_VARARGS, nullptr},
     METHOD(lora_plan_upload, "(plan, stream=None)"),
     METHOD(lora_shrink, "(plan, x, ldx, d_At_ptrs, v, stream=None)"),
     METHOD(lora_expand, "(plan, v, d_Bt_ptrs, y, ldy, beta=1.0, stream=None)"),
@@ -301,6 +401,13 @@ PyMethodDef methods[] = {
     METHOD(lora_base_gemm, "(num_tokens, k, n, dtype, x, ldx, Wt, ldw, y, ldy, stream=None)"),
     METHOD(lora_merge, "(num_layers, n, k, rank, scale, dtype, d_Wt_ptrs, ldw, d_At_ptrs, d_Bt_ptrs, variant=0, stream=None)"),
     METHOD(lora_fused_forward, "(plan, x, ldx, Wt, ldw, d_At_ptrs, d_Bt_ptrs, y, ldy, workspace, workspace_bytes, stream=None)"),
+    METHOD(lora_attention_plan_upload, "(plan, stream=None)"),
+    METHOD(lora_attention, "(plan, q, ldq, k, ldk, v, ldv, o, ldo, scale, stream=None)"),
+    METHOD(lora_cache_append, "(cache, dtype, num_tokens, max_new, d_indptr, k, ldk, v, ldv, stream=None)"),
+    METHOD(lora_cache_read, "(cache, dtype, num_tokens, max_new, d_indptr, k, ldk, v, ldv, stream=None)"),
+    METHOD(lora_cache_attention,
+           "(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, o, ldo, scale, decay, workspace, workspace_bytes, stream=None)"),
+    METHOD(lora_cache_evict, "(cache, target, budget, recent, d_kept, stream=None)"),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

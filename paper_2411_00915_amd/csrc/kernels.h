@@ -41,6 +41,10 @@ struct lora_dev_tables {
     void* layer_sync;              // hand-off counters of launch_layer_small; null: the plan has none
 };
 
+// the pool of plans' device tables with their pinned staging buffers (abi.hip); cls: the size that was given out
+lora_status lora_take_tables(int dev, size_t bytes, size_t* cls, void** dbuf, void** hbuf);
+void lora_give_tables(int device, size_t cls, void* dbuf, void* hbuf);
+
 // general VALU family (any dtype, any alignment)
 hipError_t launch_shrink_general(const lora_plan* p, const lora_dev_tables& d, const void* x, int64_t ldx,
                                  const void* const* At, float* v, hipStream_t stream);

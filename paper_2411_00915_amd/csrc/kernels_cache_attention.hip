@@ -1,0 +1,488 @@
+// Attention of new tokens over a cache of 4-bit keys and values.
+//
+// With a token's value = code * step + zero (keys and values alike, one step and one zero per token and head),
+//     q . k_t     = step_t (q . code_t) + zero_t sum(q)
+//     sum p_t v_t = sum (p_t step_t) code_t + sum p_t zero_t
+// so the matrix cores work on the codes and the scales act on scores and softmax weights, never on elements.  A code becomes
+// bf16 by two instructions a pair: (word shifted & 0x00780078) | 0x41804180 is 16 + code twice.  The sums are those of code - 7.5,
+// about which the codes lie evenly, and zero + 7.5 step stands in for zero: the score's sum starts at -23.5 sum(q), and
+// 23.5 sum(p step), as the matrix cores see it (one more product with ones), is taken off behind the second sum.  So the rounding
+// of p step to bf16 meets codes of no common offset (with it: 4.5e-3 of the result instead of 2.3e-3, the output's own rounding,
+// 1.7e-3, included).  fp32 queries and weights go in three bf16 terms (24 bits), and codes are converted without the 16.
+//
+// A wavefront takes 32 tokens of a head at a time, keys as rows of S^T = K Q^T (two products of 16 tokens), so that a lane ends
+// with 8 tokens of one query row: exactly what the second product O^T = V^T P^T wants as its second operand.  No token crosses a
+// lane; maxima do, over the 4 lanes of a row.  The pages are laid out so that every load is 16 bytes a lane and an operand as
+// it is.  The four wavefronts of a workgroup take turns at the blocks of 32 and meet in LDS at the end; long contexts are
+// split over workgroups as well, which a second launch joins.
+#include <hip/hip_runtime.h>
+
+#include "cache_format.h"
+#include "launch.h"
+#include "mfma_tile.h"
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// 8 codes (low nibble first) as the operand pairs (i, i + 4)
+template <bool EXACT>
+__device__ __forceinline__ op16 key_operand(uint32_t w)
+{
+    op16 o;
+    if constexpr (EXACT) {
+        uint32_t u[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = __float_as_uint((float)(w >> (4 * i) & 15u)), hi = __float_as_uint((float)(w >> (4 * i + 16) & 15u));
+            u[i] = lo >> 16 | (hi & 0xffff0000u);
+        }
+        o.u = uint4{u[0], u[1], u[2], u[3]};
+    } else
+        o.u = uint4{(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u,
+                    (w >> 9 & 0x00780078u) | 0x41804180u};
+    return o;
+}
+
+// nibble n (0 or 1) of the bytes in bits 0..7 and 16..23
+template <bool EXACT>
+__device__ __forceinline__ uint32_t code_pair(uint32_t w, int n)
+{
+    if constexpr (EXACT) {
+        const uint32_t lo = __float_as_uint((float)(w >> (4 * n) & 15u)), hi = __float_as_uint((float)(w >> (4 * n + 16) & 15u));
+        return lo >> 16 | (hi & 0xffff0000u);
+    }
+    return ((n == 0 ? w << 3 : w >> 1) & 0x00780078u) | 0x41804180u;
+}
+
+// a lane's share of a block of 32 tokens
+template <int DP>
+struct block_loads {
+    uint32_t k[2][DP / 32];      // the two products' rows: 16 bytes at DP 128
+    uint32_t v[DP / 16];         // 8 tokens x DP/16 codes
+    uint32_t kw[8], vw[8];       // words of its 8 tokens
+};
+
+__device__ __forceinline__ void get16(const unsigned char* p, uint32_t* w)
+{
+    const uint4 u = ld16(reinterpret_cast<const bf16_t*>(p));
+    w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+}
+
+// `at`: the block's first place in its page
+template <int DP>
+__device__ __forceinline__ void load_block(block_loads<DP>& b, const unsigned char* page, int page_tokens, int at, int r, int g)
+{
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const unsigned char* p = page + (at + 8 * (r >> 2) + (r & 3) + 4 * x) * (DP / 2) + g * (DP / 8);
+        if constexpr (DP == 64) {
+            const uint2 u = *reinterpret_cast<const uint2*>(p);
+            b.k[x][0] = u.x; b.k[x][1] = u.y;
+        } else
+#pragma unroll
+            for (int i = 0; i < DP / 128; ++i) get16(p + 16 * i, b.k[x] + 4 * i);
+    }
+    const unsigned char* v = page + page_tokens * (DP / 2) + (at >> 5) * (DP * 16) + (g * 16 + r) * (DP / 4);
+#pragma unroll
+    for (int i = 0; i < DP / 64; ++i) get16(v + 16 * i, b.v + 4 * i);
+    const unsigned char* w = page + page_tokens * DP + (at + 8 * g) * 4;
+    get16(w, b.kw);
+    get16(w + 16, b.kw + 4);
+    get16(w + page_tokens * 4, b.vw);
+    get16(w + page_tokens * 4 + 16, b.vw + 4);
+}
+
+// operand of the values: row r of the product is dim (DP/16) r + n, its 8 tokens in the registers' order
+template <int DP, bool EXACT>
+__device__ __forceinline__ op16 value_operand(const uint32_t* v, int n)
+{
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {                              // tokens 2i and 2i + 1
+        if constexpr (DP == 64) {                              // (two tokens to a word, 4 codes each)
+            const uint32_t w = v[i] >> (8 * (n >> 1)) & 0x00ff00ffu;
+            u[i] = code_pair<EXACT>(w, n & 1);
+        } else {
+            constexpr int W = DP / 128;                        // words a token
+            const uint32_t a = v[2 * i * W + (n >> 3)], b = v[(2 * i + 1) * W + (n >> 3)];
+            const int byte = (n & 7) >> 1;
+            const uint32_t w = __builtin_amdgcn_perm(b, a, 0x0c040c00u + byte * 0x00010001u);
+            u[i] = code_pair<EXACT>(w, n & 1);
+        }
+    }
+    op16 o;
+    o.u = uint4{u[0], u[1], u[2], u[3]};
+    return o;
+}
+
+// x[0..7] in TERMS bf16 terms
+template <int TERMS>
+__device__ __forceinline__ void terms_of(const float* x, op16* t)
+{
+    float rest[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rest[i] = x[i];
+#pragma unroll
+    for (int n = 0; n < TERMS; ++n) {
+        uint32_t h[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            h[i] = f32_to_bf16(rest[i]);
+            rest[i] -= bf16_to_f32((bf16_t)h[i]);
+        }
+        t[n].u = uint4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+    }
+}
+
+template <typename T, int DP, int CT, bool KEEP>
+__global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_args a)
+{
+    constexpr bool EXACT = sizeof(T) == 4;
+    constexpr int TERMS = EXACT ? 3 : 1, NS = DP / 32, NB = DP / 16;
+    constexpr float OFFSET = EXACT ? 7.5f : 23.5f;         // of what the matrix cores see, from code - 7.5
+    __shared__ __align__(16) float red[4][16][DP + 4];
+    __shared__ float red_m[4][16], red_l[4][16];
+    const cache_args& c = a.c;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
+    int id = blockIdx.x;
+    const int head = id % c.kv_heads;
+    id /= c.kv_heads;
+    const int rt = id % a.row_tiles;
+    id /= a.row_tiles;
+    const int split = id % a.splits, seq = id / a.splits;
+    const cache_rows rows = rows_of(c, seq);
+    const int R = min(rows.count, c.max_new) * a.group, row0 = rt * (16 * CT);      // query rows: token major, then the group's heads
+    if (row0 >= R) return;
+    const int length = length_of(c, seq), D = c.head_dim;
+    // what a query row sees: slots below seen(row)
+    auto seen = [&](int row) { return max(0, length - rows.count + row / a.group + 1); };
+    const int least = seen(row0), most = seen(min(R, row0 + 16 * CT) - 1);
+    const int t0 = split * a.split_tokens, t1 = min(most, t0 + a.split_tokens);
+
+    op16 q[CT][NS][TERMS];
+    float qsum[CT], start[CT];
+    int limit[CT];
+    const float c2 = a.scale * kLog2e;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        const int row = row0 + 16 * ct + r;
+        const bool valid = row < R;
+        const T* const p = static_cast<const T*>(a.q) + (int64_t)(rows.first + (valid ? row / a.group : 0)) * a.ldq +
+                           (int64_t)(head * a.group + (valid ? row % a.group : 0)) * D;
+        limit[ct] = valid ? seen(row) : 0;
+        float sum = 0.f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            float x[8];
+            const int d0 = (DP / 4) * g + 8 * s;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int d = d0 + (i >> 1) + 4 * (i & 1);     // (key_operand's order)
+                x[i] = valid && d < D ? elem<T>::load(p + d) : 0.f;
+                sum += x[i];
+            }
+            terms_of<TERMS>(x, q[ct][s]);
+        }
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        qsum[ct] = sum * c2;
+        start[ct] = -OFFSET * sum;
+    }
+
+    floatx4 acc[CT][NB], ones[CT];
+    float m[CT], ref[CT], l[CT], z[CT];                        // l, z: of this lane's tokens only
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        m[ct] = -INFINITY;
+        ref[ct] = l[ct] = z[ct] = 0.f;
+        ones[ct] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[ct][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    op16 one;
+    one.u = uint4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+
+    const int blocks_a_page = c.page_tokens >> 5, last = (t1 + 31) >> 5;
+    auto page_at = [&](int b) -> const unsigned char* {        // null: not there
+        const int64_t p = page_of(c, seq, b / blocks_a_page);
+        return p < 0 ? nullptr : c.pages + (p * c.kv_heads + head) * c.page_bytes;
+    };
+    auto compute = [&](const block_loads<DP>& in, int b) {
+        float x[CT][8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                          // tokens 8g + 4h + i
+            floatx4 s[CT];
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) s[ct] = floatx4{start[ct], start[ct], start[ct], start[ct]};
+#pragma unroll
+            for (int n = 0; n < NS; ++n) {
+                const op16 k = key_operand<EXACT>(in.k[h][n]);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int t = 0; t < TERMS; ++t) s[ct] = mfma(k, q[ct][n][t], s[ct]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t w = in.kw[4 * h + i];
+                const float step = __uint_as_float(w << 16), middle = __uint_as_float(w & 0xffff0000u) + 7.5f * step;
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) x[ct][4 * h + i] = step * c2 * s[ct][i] + middle * qsum[ct];
+            }
+        }
+        const int tok = 32 * b + 8 * g;
+        const bool masked = 32 * b + 32 > least;               // some row does not see all of the block
+        float step[8], middle[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            step[i] = __uint_as_float(in.vw[i] << 16);
+            middle[i] = __uint_as_float(in.vw[i] & 0xffff0000u) + 7.5f * step[i];
+        }
+        if (masked)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+                    if (tok + i >= limit[ct]) x[ct][i] = -INFINITY;
+            }
+        if constexpr (KEEP)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const int row = row0 + 16 * ct + r;
+                if (row >= R) continue;
+                float* const p = a.scores + ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + tok;
+                *reinterpret_cast<float4*>(p) = float4{x[ct][0], x[ct][1], x[ct][2], x[ct][3]};
+                *reinterpret_cast<float4*>(p + 4) = float4{x[ct][4], x[ct][5], x[ct][6], x[ct][7]};
+            }
+        // the running maximum, raised only where a score is 2^8 above it (weights then stay below 2^8)
+        float mx[CT];
+        bool raise = false;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            mx[ct] = x[ct][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) mx[ct] = fmaxf(mx[ct], x[ct][i]);
+            mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 16, 64));
+            mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 32, 64));
+            raise |= mx[ct] > m[ct] + 8.f;
+        }
+        if (__ballot(raise)) {
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const float mn = fmaxf(m[ct], mx[ct]), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
+                m[ct] = mn;
+                ref[ct] = mn == -INFINITY ? 0.f : mn;
+                l[ct] *= alpha;
+                z[ct] *= alpha;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    ones[ct][i] *= alpha;
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) acc[ct][n][i] *= alpha;
+                }
+            }
+        }
+        op16 p[CT][TERMS];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool there = !masked || tok + i < limit[ct];
+                const float e = __builtin_amdgcn_exp2f(x[ct][i] - ref[ct]);
+                l[ct] += e;
+                w[i] = there ? e * step[i] : 0.f;              // (what is not seen may hold anything)
+                z[ct] += there ? e * middle[i] : 0.f;
+            }
+            terms_of<TERMS>(w, p[ct]);
+#pragma unroll
+            for (int t = 0; t < TERMS; ++t) ones[ct] = mfma(one, p[ct][t], ones[ct]);
+        }
+#pragma unroll
+        for (int n = 0; n < NB; ++n) {
+            const op16 v = value_operand<DP, EXACT>(in.v, n);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int t = 0; t < TERMS; ++t) acc[ct][n] = mfma(v, p[ct][t], acc[ct][n]);
+        }
+    };
+
+    for (int b = (t0 >> 5) + wave; b < last; b += 4) {
+        const unsigned char* const page = page_at(b);
+        if (!page) {
+            if constexpr (KEEP)                                // (a slot that is not there is not seen)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                    const int row = row0 + 16 * ct + r;
+                    if (row >= R) continue;
+                    float* const p = a.scores + ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride;
+                    for (int i = 0; i < 8; ++i) p[32 * b + 8 * g + i] = -INFINITY;
+                }
+            continue;
+        }
+        block_loads<DP> in;
+        load_block<DP>(in, page, c.page_tokens, (b % blocks_a_page) * 32, r, g);
+        compute(in, b);
+    }
+
+    // the wavefronts' sums meet, column tile by column tile
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+        l[ct] += __shfl_xor(l[ct], 16, 64);
+        l[ct] += __shfl_xor(l[ct], 32, 64);
+        z[ct] += __shfl_xor(z[ct], 16, 64);
+        z[ct] += __shfl_xor(z[ct], 32, 64);
+        __syncthreads();
+        if (g == 0) red_m[wave][r] = m[ct];
+        __syncthreads();
+        float top = fmaxf(fmaxf(red_m[0][r], red_m[1][r]), fmaxf(red_m[2][r], red_m[3][r]));
+        const float f = m[ct] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[ct] - top);
+        const float add = z[ct] - OFFSET * ones[ct][0];
+        // a wavefront that saw nothing has summed nothing
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < NB; n += 4)
+                *reinterpret_cast<float4*>(&red[wave][r][NB * (4 * g + i) + n]) =
+                    float4{f * (acc[ct][n][i] + add), f * (acc[ct][n + 1][i] + add), f * (acc[ct][n + 2][i] + add), f * (acc[ct][n + 3][i] + add)};
+        if (g == 0) red_l[wave][r] = f * l[ct];
+        __syncthreads();
+        const int col = tid >> 4, row = row0 + 16 * ct + col;
+        if (row < R) {
+            const int64_t out_row = (int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group;
+            const float sum = (red_l[0][col] + red_l[1][col]) + (red_l[2][col] + red_l[3][col]);
+            if (a.stats && (tid & 15) == 0)
+                a.stats[out_row * a.splits + split] = float2{fmaxf(fmaxf(red_m[0][col], red_m[1][col]), fmaxf(red_m[2][col], red_m[3][col])), sum};
+            const float inv = a.partial ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
+            T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + row / a.group) * a.ldo + (int64_t)(head * a.group + row % a.group) * D;
+            for (int d = tid & 15; d < D; d += 16) {
+                const float o = ((red[0][col][d] + red[1][col][d]) + (red[2][col][d] + red[3][col][d])) * inv;
+                if (a.partial) a.partial[(out_row * a.splits + split) * D + d] = o;
+                else elem<T>::store(out + d, o);
+            }
+        }
+    }
+}
+
+// The splits of a query row joined: a wavefront a row
+template <typename T>
+__global__ __launch_bounds__(256) void cache_join_kernel(cache_attention_args a)
+{
+    const cache_args& c = a.c;
+    const int lane = threadIdx.x & 63, D = c.head_dim;
+    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (row >= (int64_t)c.num_seqs * c.max_new * a.num_heads) return;
+    const int head = (int)(row % a.num_heads);
+    const int64_t at = row / a.num_heads;
+    const int seq = (int)(at / c.max_new), i = (int)(at % c.max_new);
+    const cache_rows rows = rows_of(c, seq);
+    if (i >= rows.count) return;
+    const int64_t out_row = (int64_t)(rows.first + i) * a.num_heads + head;
+    const float2* const st = a.stats + out_row * a.splits;
+    float top = -INFINITY;
+    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, st[s].x);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 e = st[s];
+        if (e.y == 0.f) continue;                              // (nothing seen; NaN goes on)
+        const float f = __builtin_amdgcn_exp2f(e.x - top);
+        sum += f * e.y;
+        const float* const p = a.partial + (out_row * a.splits + s) * D;
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+            if (lane + 64 * n < D) o[n] += f * p[lane + 64 * n];
+    }
+    T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + i) * a.ldo + (int64_t)head * D;
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+        if (lane + 64 * n < D) elem<T>::store(out + lane + 64 * n, sum == 0.f ? 0.f : o[n] / sum);
+}
+
+// Accumulated weights: a thread a slot of one sequence and kv head, over all query rows, whose scores the attention left behind
+__global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args a, int chunks)
+{
+    __shared__ float lse[256];                                 // of 256 rows at a time: maximum + log2(sum), inf where nothing is seen
+    const cache_args& c = a.c;
+    const int tid = threadIdx.x;
+    int id = blockIdx.x;
+    const int chunk = id % chunks;
+    id /= chunks;
+    const int head = id % c.kv_heads, seq = id / c.kv_heads;
+    const cache_rows rows = rows_of(c, seq);
+    const int length = length_of(c, seq), R = min(rows.count, c.max_new) * a.group;
+    if (R == 0 || chunk * 256 >= length) return;
+    const int slot = chunk * 256 + tid;
+    float sum = 0.f;
+    for (int r0 = 0; r0 < R; r0 += 256) {
+        __syncthreads();
+        if (r0 + tid < R) {
+            const int row = r0 + tid;
+            const float2* const st = a.stats + ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.splits;
+            float top = -INFINITY, l = 0.f;
+            for (int s = 0; s < a.splits; ++s) top = fmaxf(top, st[s].x);
+            for (int s = 0; s < a.splits; ++s)
+                if (st[s].y != 0.f) l += __builtin_amdgcn_exp2f(st[s].x - top) * st[s].y;
+            lse[tid] = l == 0.f ? INFINITY : top + log2f(l);
+        }
+        __syncthreads();
+        const int n = min(256, R - r0);
+        for (int j = 0; j < n; ++j) {
+            const int row = r0 + j;
+            if (slot >= length - rows.count + row / a.group + 1) continue;
+            const float x = a.scores[((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + slot];
+            sum += __builtin_amdgcn_exp2f(x - lse[j]);
+        }
+    }
+    if (slot >= length) return;
+    const int page = slot / c.page_tokens;
+    const int64_t p = page_of(c, seq, page);
+    if (p < 0) return;
+    float* const w = c.weight + (p * c.kv_heads + head) * c.page_tokens + slot - page * c.page_tokens;
+    *w = a.decay == 0.f ? sum : a.decay * *w + sum;
+}
+
+template <typename T, int DP>
+void launch_main(const cache_attention_args& a, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)((int64_t)a.c.num_seqs * a.c.kv_heads * a.splits * a.row_tiles));
+    const bool wide = (int64_t)a.group * a.c.max_new > 16;
+    if (a.scores) {
+        if (wide) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, 2, true>), grid, dim3(256), 0, stream, a);
+        else LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, 1, true>), grid, dim3(256), 0, stream, a);
+    } else {
+        if (wide) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, 2, false>), grid, dim3(256), 0, stream, a);
+        else LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, 1, false>), grid, dim3(256), 0, stream, a);
+    }
+}
+
+template <typename T>
+hipError_t launch_all(const cache_attention_args& a, hipStream_t stream)
+{
+    switch (padded_head_dim(a.c.head_dim)) {
+        case 64: launch_main<T, 64>(a, stream); break;
+        case 128: launch_main<T, 128>(a, stream); break;
+        default: launch_main<T, 256>(a, stream);
+    }
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && a.splits > 1) {
+        const int64_t rows = (int64_t)a.c.num_seqs * a.c.max_new * a.num_heads;
+        LORA_LAUNCH(LORA_K_CACHE_JOIN, (cache_join_kernel<T>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, a);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess && a.scores) {
+        const int chunks = (a.c.max_length + 255) / 256;
+        LORA_LAUNCH(LORA_K_CACHE_WEIGHT, cache_weight_kernel, dim3((uint32_t)(a.c.num_seqs * a.c.kv_heads * chunks)), dim3(256), 0, stream, a, chunks);
+        e = hipGetLastError();
+    }
+    return e;
+}
+}  // namespace
+
+hipError_t launch_cache_attention(const cache_attention_args& a, int32_t dtype, hipStream_t stream)
+{
+    return dtype == LORA_F32 ? launch_all<float>(a, stream) : launch_all<bf16_t>(a, stream);
+}

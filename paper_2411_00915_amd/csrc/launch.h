@@ -32,6 +32,14 @@ enum lora_kernel_id {
     LORA_K_SHRINK_ROWS,
     LORA_K_EXPAND_ROWS,
     LORA_K_DELTA_F32,
+    LORA_K_ATTENTION_GENERAL,
+    LORA_K_CACHE_APPEND,
+    LORA_K_CACHE_READ,
+    LORA_K_CACHE_ATTENTION,
+    LORA_K_CACHE_JOIN,
+    LORA_K_CACHE_WEIGHT,
+    LORA_K_CACHE_SELECT,
+    LORA_K_CACHE_MOVE,
     LORA_K_PROBE_EMPTY,
     LORA_K_PROBE_READ,
     LORA_K_PROBE_MFMA,
