@@ -112,7 +112,7 @@ extern "C" lora_status lora_attention(lora_attention_plan* p, const void* q, int
     if (st != LORA_OK) return st;
     const attention_args a{static_cast<const attention_tile*>(p->d_buf), (int32_t)p->tiles.size(), p->num_heads, p->num_heads / p->num_kv_heads,
                            p->head_dim, q, k, v, o, ldq, ldk, ldv, ldo, scale};
-    return status_of(launch_attention_general(a, p->dtype, stream));
+    return status_of(attention_tiled_supported(a, p->dtype) ? launch_attention_tiled(a, p->dtype, stream) : launch_attention_general(a, p->dtype, stream));
 }
 
 extern "C" lora_status lora_cache_append(const lora_cache* c, int32_t dtype, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr, const void* k,

@@ -15,6 +15,9 @@ struct attention_args {
 };
 
 hipError_t launch_attention_general(const attention_args& a, int32_t dtype, hipStream_t stream);
+// 16-byte aligned rows and heads
+bool attention_tiled_supported(const attention_args& a, int32_t dtype);
+hipError_t launch_attention_tiled(const attention_args& a, int32_t dtype, hipStream_t stream);
 
 // What the kernels of the cache take: the descriptor's fields by value
 struct cache_args {

@@ -4,6 +4,7 @@
 #include "device_util.h"
 #include "kernels_attention.h"
 #include "launch.h"
+#include "mfma_tile.h"
 
 // ---------------------------------------------------------------------------
 // Any layout, dtype and head_dim: a wavefront per query and head.  Keys in steps of 64, one a lane for the scores; then lanes
@@ -63,5 +64,363 @@ hipError_t launch_attention_general(const attention_args& a, int32_t dtype, hipS
         LORA_LAUNCH(LORA_K_ATTENTION_GENERAL, (attention_general_kernel<float>), grid, dim3(256), 0, stream, a);
     else
         LORA_LAUNCH(LORA_K_ATTENTION_GENERAL, (attention_general_kernel<bf16_t>), grid, dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Aligned prompts, on the matrix cores.  A workgroup takes up to 128 queries of one head, 32 a wavefront; keys and values come
+// in tiles of BK tokens, straight to LDS, one tile ahead of the products.
+//
+//     S^T = K Q^T     keys are the rows of the product, so that a lane ends with 16 (of 32) keys of one query, and maximum and
+//                     sum of the softmax meet in two lanes only
+//     O^T = V^T P^T   the same registers, rounded to bf16, are the second operand as they are; V is read across (transposing
+//                     LDS reads), tokens in the order that the first product left them in
+//
+// bf16: 32 x 32 x 16 products; fp32: 32 x 32 x 2 of exact products.  The softmax runs to base 2 (its factor goes with the
+// scale, in 32 bits) against a maximum that is raised only where a score is 2^8 above it.
+namespace {
+
+typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
+typedef __attribute__((__vector_size__(4 * sizeof(short)))) short shortx4;
+
+// What of rows x width bytes lies from `base` on, for loads of 16 bytes a lane straight to LDS; reads behind `bytes` give zeros
+struct tile_source {
+    u32x4 rsrc;
+    __device__ __forceinline__ void set(const char* base, int64_t bytes)
+    {
+        const uint64_t b = reinterpret_cast<uint64_t>(base);
+        rsrc[0] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+        rsrc[1] = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32) & 0xffff);
+        rsrc[2] = (uint32_t)__builtin_amdgcn_readfirstlane((int)min(max(bytes, (int64_t)0), (int64_t)0x7fffffff));
+        rsrc[3] = 0x00020000u;
+    }
+    __device__ __forceinline__ void load(uint32_t offset, uint32_t lds) const
+    {
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset), "s"(rsrc), "s"(lds) : "memory");
+#endif
+    }
+};
+
+// places of 16-byte chunks in a row of LDS, so that the lanes of a read meet different banks
+template <typename T, int DP>
+__device__ __forceinline__ int key_place(int c, int row)
+{
+    constexpr int CH = DP * (int)sizeof(T) / 16;
+    if constexpr (CH == 12) return (c + (row >> 2 & 3)) % 12;
+    else if constexpr (CH == 8) return c ^ (row >> 1 & 7);
+    else return c ^ (row & 15);
+}
+template <typename T, int DP>
+__device__ __forceinline__ int key_chunk(int place, int row)      // the other way round
+{
+    if constexpr (DP * (int)sizeof(T) / 16 == 12) return (place + 12 - (row >> 2 & 3)) % 12;
+    else return key_place<T, DP>(place, row);
+}
+template <typename T, int DP>
+__device__ __forceinline__ int value_place(int c, int row)        // its own inverse
+{
+    constexpr int CH = DP * (int)sizeof(T) / 16;
+    if constexpr (sizeof(T) == 4) return c ^ (row >> 2 & 1) << 3;
+    else if constexpr (CH == 12) return c;
+    else if constexpr (CH == 8) return c ^ (row >> 1 & 1) << 2;
+    else return c ^ (row & 3) << 2;
+}
+
+// two bf16, infinities and NaN as 0
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t u)
+{
+    return ((u & 0x7f80u) == 0x7f80u ? 0u : u & 0xffffu) | ((u & 0x7f800000u) == 0x7f800000u ? 0u : u & 0xffff0000u);
+}
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return f32_to_bf16(a) | (uint32_t)f32_to_bf16(b) << 16; }
+
+template <typename T, int DP, int BK>
+__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel(attention_args a)
+{
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int ROW = DP * (int)sizeof(T), CH = ROW / 16;         // bytes and chunks of a token
+    constexpr int LOADS = BK * CH / 256;                           // of a wavefront, for one tile of keys
+    constexpr int NB = DP / 32, SB = BK / 32;
+    constexpr int QR = F32 ? DP / 2 : DP / 16;                      // fp32: a register per two dims; bf16: 8 dims a lane and product
+    __shared__ __align__(1024) char lds[2][2][BK * ROW];            // buffer, keys / values
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
+    // heads in runs on the XCDs (workgroups go round them), what is left of them dealt out
+    const int H = a.num_heads, whole = H / 8, id = blockIdx.x, xcd = id & 7, slot = id >> 3;
+    int head, tile;
+    if (slot < whole * a.num_tiles) {
+        head = xcd * whole + slot / a.num_tiles;
+        tile = slot % a.num_tiles;
+    } else {
+        const int rest = (slot - whole * a.num_tiles) * 8 + xcd, left = H - 8 * whole;
+        if (left == 0 || rest >= left * a.num_tiles) return;
+        head = 8 * whole + rest % left;
+        tile = rest / left;
+    }
+    const attention_tile t = a.tiles[tile];
+    const int D = a.head_dim;
+    const char* const kb = static_cast<const char*>(a.k) + ((int64_t)t.kv_row0 * a.ldk + (int64_t)(head / a.group) * D) * (int)sizeof(T);
+    const char* const vb = static_cast<const char*>(a.v) + ((int64_t)t.kv_row0 * a.ldv + (int64_t)(head / a.group) * D) * (int)sizeof(T);
+    const int64_t kpitch = a.ldk * (int)sizeof(T), vpitch = a.ldv * (int)sizeof(T);
+    const int tiles = (t.max_kv + BK - 1) / BK;
+
+    // this lane's chunks of a tile: what is past head_dim is past every row, and comes as zeros
+    uint32_t k_off[LOADS], v_off[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int p = (wave * LOADS + i) * 64 + lane, row = p / CH, place = p % CH;
+        const int kc = key_chunk<T, DP>(place, row), vc = value_place<T, DP>(place, row);
+        k_off[i] = kc * (16 / (int)sizeof(T)) < D ? (uint32_t)(row * kpitch + kc * 16) : 0x80000000u;
+        v_off[i] = vc * (16 / (int)sizeof(T)) < D ? (uint32_t)(row * vpitch + vc * 16) : 0x80000000u;
+    }
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(lds)) + wave * (LOADS * 1024);
+    auto fetch = [&](int n) {
+        const int64_t left = (int64_t)t.num_kv - (int64_t)n * BK;          // rows; the last ends with its head
+        tile_source s;
+        s.set(kb + (int64_t)n * BK * kpitch, (left - 1) * kpitch + (int64_t)D * (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) s.load(k_off[i], lds0 + (n & 1) * (2 * BK * ROW) + i * 1024);
+        s.set(vb + (int64_t)n * BK * vpitch, (left - 1) * vpitch + (int64_t)D * (int)sizeof(T));
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) s.load(v_off[i], lds0 + (n & 1) * (2 * BK * ROW) + BK * ROW + i * 1024);
+    };
+    if (tiles > 0) fetch(0);
+
+    // queries; a negative scale turns their sign
+    const int row = wave * 32 + col;
+    const bool valid = row < t.rows;
+    const T* const qp = static_cast<const T*>(a.q) + (int64_t)(t.q_row0 + (valid ? row : 0)) * a.ldq + (int64_t)head * D;
+    float qf[F32 ? QR : 1];
+    op16 qb[F32 ? 1 : QR];
+    if constexpr (F32) {
+#pragma unroll
+        for (int c = 0; c < QR / 4; ++c) {
+            const int d = 8 * c + 4 * half;
+            const float4 x = valid && d < D ? *reinterpret_cast<const float4*>(qp + d) : float4{0.f, 0.f, 0.f, 0.f};
+            qf[4 * c] = x.x; qf[4 * c + 1] = x.y; qf[4 * c + 2] = x.z; qf[4 * c + 3] = x.w;
+        }
+        if (a.scale < 0.f)
+#pragma unroll
+            for (int i = 0; i < QR; ++i) qf[i] = -qf[i];
+    } else {
+        const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+        for (int s = 0; s < QR; ++s) {
+            const int d = 16 * s + 8 * half;
+            uint4 u = valid && d < D ? ld16(reinterpret_cast<const bf16_t*>(qp) + d) : uint4{0, 0, 0, 0};
+            qb[s].u = uint4{u.x ^ sign, u.y ^ sign, u.z ^ sign, u.w ^ sign};
+        }
+    }
+    const float c2 = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1.17549435e-38f);
+    const int limit = valid ? max(0, min(t.num_kv, t.ahead + row + 1)) : 0;
+    // of the wavefront's queries, what the first and the last see
+    const int least = max(0, min(t.num_kv, t.ahead + wave * 32 + 1));
+    const int most = wave * 32 < t.rows ? max(0, min(t.num_kv, t.ahead + min(t.rows, wave * 32 + 32))) : 0;
+
+    floatx16 acc[NB];
+#pragma unroll
+    for (int n = 0; n < NB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
+    float m = -INFINITY, ref = 0.f, l = 0.f;
+
+    for (int n = 0; n < tiles; ++n) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();                                       // the tile is there, and nobody reads the other buffer any more
+        if (n + 1 < tiles) fetch(n + 1);
+        if (n * BK >= most) continue;
+        const char* const keys = lds[n & 1][0];
+        const char* const values = lds[n & 1][1];
+        floatx16 x[SB];
+#pragma unroll
+        for (int b = 0; b < SB; ++b) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[b][i] = 0.f;
+            const int r = 32 * b + col;
+            if constexpr (F32) {
+#pragma unroll
+                for (int c = 0; c < QR / 4; ++c) {
+                    const float4 k = *reinterpret_cast<const float4*>(keys + r * ROW + key_place<T, DP>(2 * c + half, r) * 16);
+                    x[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.x, qf[4 * c], x[b], 0, 0, 0);
+                    x[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.y, qf[4 * c + 1], x[b], 0, 0, 0);
+                    x[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.z, qf[4 * c + 2], x[b], 0, 0, 0);
+                    x[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k.w, qf[4 * c + 3], x[b], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < QR; ++s) {
+                    op16 k;
+                    k.u = *reinterpret_cast<const uint4*>(keys + r * ROW + key_place<T, DP>(2 * s + half, r) * 16);
+                    x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k.v, qb[s].v, x[b], 0, 0, 0);
+                }
+            }
+        }
+        const bool masked = (n + 1) * BK > least;
+        if (masked)
+#pragma unroll
+            for (int b = 0; b < SB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (n * BK + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3) >= limit) x[b][i] = -INFINITY;
+        float mx = x[0][0];
+#pragma unroll
+        for (int b = 0; b < SB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[b][i]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
+        if (__ballot(mx > m + 8.f)) {
+            const float top = fmaxf(m, mx), alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+            m = top;
+            ref = top == -INFINITY ? 0.f : top;
+            l *= alpha;
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[d][i] *= alpha;
+        }
+#pragma unroll
+        for (int b = 0; b < SB; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[b][i] = __builtin_amdgcn_exp2f(x[b][i] * c2 - ref);
+                l += x[b][i];
+            }
+        // values: fp32 one dim a lane, bf16 four tokens of a dim by a transposing read (of 16 lanes, lane i points at 4 dims of
+        // token i/4 and gets dim i of the four tokens)
+        auto value_f32 = [&](int token, int d) { return *reinterpret_cast<const float*>(values + token * ROW + value_place<T, DP>(d >> 2, token) * 16 + (d & 3) * 4); };
+        auto value_bf16 = [&](int b, int s, int d, int lane) {  // tokens 32 b + 16 s + 4 half + (0..3) and 8 on
+            union { shortx4 h[2]; op16 o; } u;
+#if defined(__HIP_DEVICE_COMPILE__)
+            const int c = 4 * d + 2 * (lane >> 4 & 1) + (lane >> 1 & 1);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int token = 32 * b + 16 * s + 8 * e + 4 * (lane >> 5) + (lane >> 2 & 3);
+                u.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) shortx4*)(values + token * ROW + value_place<T, DP>(c, token) * 16 + (lane & 1) * 8));
+            }
+#endif
+            return u.o;
+        };
+        bool wild = false;
+        if (masked) {                                          // a weight of 0 does not hide infinities and NaN from the product
+            if constexpr (F32) {
+#pragma unroll 1
+                for (int i = half; i < BK; i += 2)
+#pragma unroll
+                    for (int d = 0; d < NB; ++d) wild |= !(fabsf(value_f32(i, 32 * d + col)) < INFINITY);
+            } else {
+                uint32_t any = 0;
+#pragma unroll 2
+                for (int i = 0; i < BK * CH / 64; ++i) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(values + (i * 64 + lane) * 16);
+                    any |= ((u.x & 0x7fff7fffu) + 0x00800080u) | ((u.y & 0x7fff7fffu) + 0x00800080u) | ((u.z & 0x7fff7fffu) + 0x00800080u) |
+                           ((u.w & 0x7fff7fffu) + 0x00800080u);
+                }
+                wild = (any & 0x80008000u) != 0;
+            }
+            wild = __ballot(wild) != 0;
+        }
+        if constexpr (F32) {
+#pragma unroll
+            for (int b = 0; b < SB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+#pragma unroll
+                    for (int d = 0; d < NB; ++d) {
+                        float v = value_f32(32 * b + 8 * (i >> 2) + 4 * half + (i & 3), 32 * d + col);
+                        if (wild) v = fabsf(v) < INFINITY ? v : 0.f;
+                        acc[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, x[b][i], acc[d], 0, 0, 0);
+                    }
+        } else {
+            op16 p[SB][2];
+#pragma unroll
+            for (int b = 0; b < SB; ++b)
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+                    p[b][s].u = uint4{pack_bf16(x[b][8 * s], x[b][8 * s + 1]), pack_bf16(x[b][8 * s + 2], x[b][8 * s + 3]),
+                                      pack_bf16(x[b][8 * s + 4], x[b][8 * s + 5]), pack_bf16(x[b][8 * s + 6], x[b][8 * s + 7])};
+            if (!wild)
+#pragma unroll
+                for (int b = 0; b < SB; ++b)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int d = 0; d < NB; ++d) acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_bf16(b, s, d, lane).v, p[b][s].v, acc[d], 0, 0, 0);
+            else {
+                int here = lane;                               // (opaque, so that no address of this rare path is kept for it)
+                asm volatile("" : "+v"(here));
+#pragma unroll
+                for (int b = 0; b < SB; ++b)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int d = 0; d < NB; ++d) {
+                            op16 v = value_bf16(b, s, d, here);
+                            v.u = uint4{finite_or_zero(v.u.x), finite_or_zero(v.u.y), finite_or_zero(v.u.z), finite_or_zero(v.u.w)};
+                            acc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.v, p[b][s].v, acc[d], 0, 0, 0);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+            }
+        }
+        if (wild) {
+            // the products above are over the finite values; what the others make of a dim of a query is found token by token
+            int there = half;
+            asm volatile("" : "+v"(there));
+#pragma unroll 1
+            for (int j = 0; j < BK; ++j) {
+                const bool sees = n * BK + j < limit;
+#pragma unroll
+                for (int d = 0; d < NB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int at = 32 * d + 8 * (i >> 2) + 4 * there + (i & 3);
+                        const float v = elem<T>::load(reinterpret_cast<const T*>(values + j * ROW + value_place<T, DP>(at * (int)sizeof(T) / 16, j) * 16) +
+                                                      at % (16 / (int)sizeof(T)));
+                        acc[d][i] += sees && !(fabsf(v) < INFINITY) ? v : 0.f;
+                        asm volatile("" : "+v"(there));
+                    }
+            }
+        }
+    }
+
+    l += __shfl_xor(l, 32, 64);
+    if (!valid) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T* const out = static_cast<T*>(a.o) + (int64_t)(t.q_row0 + row) * a.ldo + (int64_t)head * D;
+#pragma unroll
+    for (int d = 0; d < NB; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int at = 32 * d + 2 * i + 4 * half;
+            if (at >= D) continue;                             // (D is a multiple of 4)
+            const float y[4] = {acc[d][i] * inv, acc[d][i + 1] * inv, acc[d][i + 2] * inv, acc[d][i + 3] * inv};
+            if constexpr (F32) *reinterpret_cast<float4*>(out + at) = float4{y[0], y[1], y[2], y[3]};
+            else *reinterpret_cast<uint2*>(out + at) = uint2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        }
+}
+}  // namespace
+
+bool attention_tiled_supported(const attention_args& a, int32_t dtype)
+{
+    const int64_t es = dtype == LORA_F32 ? 4 : 2, most = (int64_t)1 << 24;      // (a tile's rows have to lie within 2 GB)
+    const uintptr_t all = reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(a.o) |
+                          (uintptr_t)((a.ldq | a.ldk | a.ldv | a.ldo | a.head_dim) * es);
+    return (all & 15) == 0 && a.ldk * es < 2 * most && a.ldv * es < 2 * most;
+}
+
+hipError_t launch_attention_tiled(const attention_args& a, int32_t dtype, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)(((int64_t)a.num_tiles * a.num_heads + 7) / 8 * 8));
+#define TILED(T, DP, BK) LORA_LAUNCH(LORA_K_ATTENTION_TILED, (attention_tiled_kernel<T, DP, BK>), grid, dim3(256), 0, stream, a)
+    if (dtype == LORA_F32) {
+        if (a.head_dim <= 64) TILED(float, 64, 32);
+        else if (a.head_dim <= 128) TILED(float, 128, 32);
+        else TILED(float, 256, 32);
+    } else {
+        if (a.head_dim <= 64) TILED(bf16_t, 64, 64);
+        else if (a.head_dim <= 96) TILED(bf16_t, 96, 64);
+        else if (a.head_dim <= 128) TILED(bf16_t, 128, 64);
+        else TILED(bf16_t, 256, 32);
+    }
     return hipGetLastError();
 }
