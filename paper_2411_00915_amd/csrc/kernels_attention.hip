@@ -184,7 +184,6 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) s.load(v_off[i], lds0 + (n & 1) * (2 * BK * ROW) + BK * ROW + i * 1024);
     };
-    if (tiles > 0) fetch(0);
 
     // queries; a negative scale turns their sign
     const int row = wave * 32 + col;
@@ -218,12 +217,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     const int most = wave * 32 < t.rows ? max(0, min(t.num_kv, t.ahead + min(t.rows, wave * 32 + 32))) : 0;
 
     floatx16 acc[NB];
+    float l = 0.f;
+    // A weight of 0 does not hide infinities and NaN of a value from the product.  Where the result holds any, the workgroup goes
+    // through its tiles once more and takes them out of the products where some query does not see the token.
+    auto pass = [&](const bool careful) {
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
-    float m = -INFINITY, ref = 0.f, l = 0.f;
-
+    float m = -INFINITY, ref = 0.f;
+    l = 0.f;
+    if (tiles > 0) fetch(0);
     for (int n = 0; n < tiles; ++n) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();                                       // the tile is there, and nobody reads the other buffer any more
@@ -301,25 +305,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 #endif
             return u.o;
         };
-        bool wild = false;
-        if (masked) {                                          // a weight of 0 does not hide infinities and NaN from the product
-            if constexpr (F32) {
-#pragma unroll 1
-                for (int i = half; i < BK; i += 2)
-#pragma unroll
-                    for (int d = 0; d < NB; ++d) wild |= !(fabsf(value_f32(i, 32 * d + col)) < INFINITY);
-            } else {
-                uint32_t any = 0;
-#pragma unroll 2
-                for (int i = 0; i < BK * CH / 64; ++i) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(values + (i * 64 + lane) * 16);
-                    any |= ((u.x & 0x7fff7fffu) + 0x00800080u) | ((u.y & 0x7fff7fffu) + 0x00800080u) | ((u.z & 0x7fff7fffu) + 0x00800080u) |
-                           ((u.w & 0x7fff7fffu) + 0x00800080u);
-                }
-                wild = (any & 0x80008000u) != 0;
-            }
-            wild = __ballot(wild) != 0;
-        }
+        const bool wild = careful && masked;
         if constexpr (F32) {
 #pragma unroll
             for (int b = 0; b < SB; ++b)
@@ -384,6 +370,17 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     }
 
     l += __shfl_xor(l, 32, 64);
+    };
+#pragma unroll 1
+    for (int careful = 0; careful < 2; ++careful) {
+        pass(careful != 0);
+        float sum = l;                                         // (not finite where one of them is not, or they are past its range)
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum += fabsf(acc[d][i]);
+        if (!__syncthreads_or(!(sum < INFINITY))) break;
+    }
     if (!valid) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* const out = static_cast<T*>(a.o) + (int64_t)(t.q_row0 + row) * a.ldo + (int64_t)head * D;
