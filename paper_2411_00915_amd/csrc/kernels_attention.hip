@@ -1,6 +1,8 @@
 // Attention of a batch of prompts.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "device_util.h"
 #include "kernels_attention.h"
 #include "launch.h"
@@ -133,7 +135,23 @@ __device__ __forceinline__ uint32_t finite_or_zero(uint32_t u)
     return ((u & 0x7f80u) == 0x7f80u ? 0u : u & 0xffffu) | ((u & 0x7f800000u) == 0x7f800000u ? 0u : u & 0xffff0000u);
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return f32_to_bf16(a) | (uint32_t)f32_to_bf16(b) << 16; }
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    typedef __attribute__((__vector_size__(2 * sizeof(float)))) float floatx2;
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{a, b}), bf16x2));      // (one conversion for both)
+}
+
+// the greater of the two lanes of a query
+__device__ __forceinline__ float max_of_halves(float x)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+#else
+    return x;
+#endif
+}
 
 template <typename T, int DP, int BK>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel(attention_args a)
@@ -220,7 +238,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     float l = 0.f;
     // A weight of 0 does not hide infinities and NaN of a value from the product.  Where the result holds any, the workgroup goes
     // through its tiles once more and takes them out of the products where some query does not see the token.
-    auto pass = [&](const bool careful) {
+    auto pass = [&](auto careful_) {
+    constexpr bool careful = decltype(careful_)::value;
 #pragma unroll
     for (int n = 0; n < NB; ++n)
 #pragma unroll
@@ -260,18 +279,21 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
             }
         }
         const bool masked = (n + 1) * BK > least;
-        if (masked)
+        if (masked) {
+            int first = limit - n * BK - 4 * half;
+            asm volatile("" : "+v"(first));                    // (a branch, not selects in every tile)
 #pragma unroll
             for (int b = 0; b < SB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (n * BK + 32 * b + 8 * (i >> 2) + 4 * half + (i & 3) >= limit) x[b][i] = -INFINITY;
+                    if (32 * b + 8 * (i >> 2) + (i & 3) >= first) x[b][i] = -INFINITY;
+        }
         float mx = x[0][0];
 #pragma unroll
         for (int b = 0; b < SB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[b][i]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
+        mx = max_of_halves(mx) * c2;
         if (__ballot(mx > m + 8.f)) {
             const float top = fmaxf(m, mx), alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
             m = top;
@@ -371,16 +393,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 
     l += __shfl_xor(l, 32, 64);
     };
-#pragma unroll 1
-    for (int careful = 0; careful < 2; ++careful) {
-        pass(careful != 0);
-        float sum = l;                                         // (not finite where one of them is not, or they are past its range)
+    pass(std::false_type{});
+    float sum = l;                                             // (not finite where one of them is not, or they are past its range)
 #pragma unroll
-        for (int d = 0; d < NB; ++d)
+    for (int d = 0; d < NB; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum += fabsf(acc[d][i]);
-        if (!__syncthreads_or(!(sum < INFINITY))) break;
-    }
+        for (int i = 0; i < 16; ++i) sum += fabsf(acc[d][i]);
+    if (__syncthreads_or(!(sum < INFINITY))) pass(std::true_type{});
     if (!valid) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* const out = static_cast<T*>(a.o) + (int64_t)(t.q_row0 + row) * a.ldo + (int64_t)head * D;
