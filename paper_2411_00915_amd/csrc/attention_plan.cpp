@@ -15,6 +15,35 @@ bool offsets_ok(const int32_t* p, int32_t n)
         if (p[i + 1] < p[i]) return false;
     return true;
 }
+
+// The workgroups' work.  Workgroups go round the 8 XCDs, so every eighth item is one XCD's: it gets whole heads, one behind the
+// other, so that the workgroups that run beside each other there read the same keys and values; heads that are left over
+// go to the XCD that has the least to do.  Tiles of a head: most keys first.
+void order_items(lora_attention_plan* p)
+{
+    constexpr int X = 8;
+    std::vector<attention_item> list[X];
+    int64_t cost[X] = {};
+    auto add = [&](int x, int32_t tile, int32_t head) {
+        list[x].push_back(attention_item{tile, head});
+        cost[x] += (int64_t)p->tiles[tile].max_kv + 64;
+    };
+    const int32_t H = p->num_heads, group = H / p->num_kv_heads, T = (int32_t)p->tiles.size();
+    // runs of heads that belong together stay together: of 4, 2 or 1 (as many as a tile may take)
+    const int32_t unit = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1, units = H / unit, whole = units / X;
+    for (int32_t u = 0; u < whole * X; ++u)
+        for (int32_t t = 0; t < T; ++t)
+            for (int32_t h = 0; h < unit; h += p->tiles[t].heads) add(u / whole, t, u * unit + h);
+    for (int32_t t = 0; t < T; ++t)
+        for (int32_t u = whole * X; u < units; ++u)
+            for (int32_t h = 0; h < unit; h += p->tiles[t].heads)
+                add((int)(std::min_element(cost, cost + X) - cost), t, u * unit + h);
+    size_t longest = 0;
+    for (const auto& l : list) longest = std::max(longest, l.size());
+    p->items.assign(longest * X, attention_item{-1, 0});
+    for (int x = 0; x < X; ++x)
+        for (size_t i = 0; i < list[x].size(); ++i) p->items[i * X + x] = list[x][i];
+}
 }  // namespace
 
 extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, lora_attention_plan** out)
@@ -36,6 +65,7 @@ extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, 
         p->dtype = d->dtype;
         p->num_queries = d->q_indptr[d->num_seqs];
         p->num_keys = kv[d->num_seqs];
+        const int32_t group = d->num_heads / d->num_kv_heads;
         for (int32_t s = 0; s < d->num_seqs; ++s) {
             const int32_t nq = d->q_indptr[s + 1] - d->q_indptr[s], nk = kv[s + 1] - kv[s];
             for (int32_t r = 0; r < nq; r += LORA_ATTENTION_ROWS) {
@@ -45,11 +75,17 @@ extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, 
                 t.kv_row0 = kv[s];
                 t.num_kv = nk;
                 t.ahead = d->causal ? nk - nq + r : nk;
+                t.heads = group % 4 == 0 && t.rows <= LORA_ATTENTION_ROWS / 4 ? 4 : group % 2 == 0 && t.rows <= LORA_ATTENTION_ROWS / 2 ? 2 : 1;
                 t.max_kv = (int32_t)std::max<int64_t>(0, std::min<int64_t>(nk, (int64_t)t.ahead + t.rows));
                 p->tiles.push_back(t);
             }
         }
         std::stable_sort(p->tiles.begin(), p->tiles.end(), [](const attention_tile& a, const attention_tile& b) { return a.max_kv > b.max_kv; });
+        if ((int64_t)p->tiles.size() * p->num_heads > LORA_ATTENTION_MAX_ITEMS) {
+            delete p;
+            return LORA_ERR_UNSUPPORTED;
+        }
+        order_items(p);
     } catch (const std::bad_alloc&) {
         delete p;
         return LORA_ERR_NOMEM;

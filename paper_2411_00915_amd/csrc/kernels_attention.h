@@ -7,7 +7,8 @@
 
 struct attention_args {
     const attention_tile* tiles;
-    int32_t num_tiles, num_heads, group, head_dim;      // group: query heads of a kv head
+    const attention_item* items;
+    int32_t num_tiles, num_items, num_heads, group, head_dim;      // group: query heads of a kv head
     const void *q, *k, *v;
     void* o;
     int64_t ldq, ldk, ldv, ldo;

@@ -163,22 +163,13 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     constexpr int QR = F32 ? DP / 2 : DP / 16;                      // fp32: a register per two dims; bf16: 8 dims a lane and product
     __shared__ __align__(1024) char lds[2][2][BK * ROW];            // buffer, keys / values
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
-    // heads in runs on the XCDs (workgroups go round them), what is left of them dealt out
-    const int H = a.num_heads, whole = H / 8, id = blockIdx.x, xcd = id & 7, slot = id >> 3;
-    int head, tile;
-    if (slot < whole * a.num_tiles) {
-        head = xcd * whole + slot / a.num_tiles;
-        tile = slot % a.num_tiles;
-    } else {
-        const int rest = (slot - whole * a.num_tiles) * 8 + xcd, left = H - 8 * whole;
-        if (left == 0 || rest >= left * a.num_tiles) return;
-        head = 8 * whole + rest % left;
-        tile = rest / left;
-    }
-    const attention_tile t = a.tiles[tile];
+    const attention_item item = a.items[blockIdx.x];
+    if (item.tile < 0) return;
+    const attention_tile t = a.tiles[item.tile];
+    const int waves = 4 / t.heads, head = item.head + wave / waves, row0 = wave % waves * 32;      // this wavefront's head, and its first query
     const int D = a.head_dim;
-    const char* const kb = static_cast<const char*>(a.k) + ((int64_t)t.kv_row0 * a.ldk + (int64_t)(head / a.group) * D) * (int)sizeof(T);
-    const char* const vb = static_cast<const char*>(a.v) + ((int64_t)t.kv_row0 * a.ldv + (int64_t)(head / a.group) * D) * (int)sizeof(T);
+    const char* const kb = static_cast<const char*>(a.k) + ((int64_t)t.kv_row0 * a.ldk + (int64_t)(item.head / a.group) * D) * (int)sizeof(T);
+    const char* const vb = static_cast<const char*>(a.v) + ((int64_t)t.kv_row0 * a.ldv + (int64_t)(item.head / a.group) * D) * (int)sizeof(T);
     const int64_t kpitch = a.ldk * (int)sizeof(T), vpitch = a.ldv * (int)sizeof(T);
     const int tiles = (t.max_kv + BK - 1) / BK;
 
@@ -204,7 +195,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     };
 
     // queries; a negative scale turns their sign
-    const int row = wave * 32 + col;
+    const int row = row0 + col;
     const bool valid = row < t.rows;
     const T* const qp = static_cast<const T*>(a.q) + (int64_t)(t.q_row0 + (valid ? row : 0)) * a.ldq + (int64_t)head * D;
     float qf[F32 ? QR : 1];
@@ -231,8 +222,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     const float c2 = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1.17549435e-38f);
     const int limit = valid ? max(0, min(t.num_kv, t.ahead + row + 1)) : 0;
     // of the wavefront's queries, what the first and the last see
-    const int least = max(0, min(t.num_kv, t.ahead + wave * 32 + 1));
-    const int most = wave * 32 < t.rows ? max(0, min(t.num_kv, t.ahead + min(t.rows, wave * 32 + 32))) : 0;
+    const int least = max(0, min(t.num_kv, t.ahead + row0 + 1));
+    const int most = row0 < t.rows ? max(0, min(t.num_kv, t.ahead + min(t.rows, row0 + 32))) : 0;
 
     floatx16 acc[NB];
     float l = 0.f;
@@ -426,7 +417,7 @@ bool attention_tiled_supported(const attention_args& a, int32_t dtype)
 
 hipError_t launch_attention_tiled(const attention_args& a, int32_t dtype, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)(((int64_t)a.num_tiles * a.num_heads + 7) / 8 * 8));
+    const dim3 grid((uint32_t)a.num_items);
 #define TILED(T, DP, BK) LORA_LAUNCH(LORA_K_ATTENTION_TILED, (attention_tiled_kernel<T, DP, BK>), grid, dim3(256), 0, stream, a)
     if (dtype == LORA_F32) {
         if (a.head_dim <= 64) TILED(float, 64, 32);
