@@ -31,7 +31,7 @@ lora_status ensure_uploaded(lora_attention_plan* p, hipStream_t stream)
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess) return LORA_ERR_DEVICE;
     if (p->d_buf) return p->device == dev ? LORA_OK : LORA_ERR_INVALID_ARG;      // a plan lives on one device
-    const size_t tiles = p->tiles.size() * sizeof(attention_tile), items = p->items.size() * sizeof(attention_item), bytes = std::max<size_t>(tiles + items, 64);
+    const size_t tiles = p->tiles.size() * sizeof(attention_tile), items = p->items.size() * sizeof(attention_tile), bytes = std::max<size_t>(tiles + items, 64);
     size_t cls = 0;
     void *dbuf = nullptr, *hbuf = nullptr;
     const lora_status st = lora_take_tables(dev, bytes, &cls, &dbuf, &hbuf);
@@ -111,7 +111,7 @@ extern "C" lora_status lora_attention(lora_attention_plan* p, const void* q, int
     const lora_status st = ensure_uploaded(p, stream);
     if (st != LORA_OK) return st;
     const attention_tile* const tiles = static_cast<const attention_tile*>(p->d_buf);
-    const attention_args a{tiles, reinterpret_cast<const attention_item*>(tiles + p->tiles.size()), (int32_t)p->tiles.size(), (int32_t)p->items.size(), p->num_heads, p->num_heads / p->num_kv_heads,
+    const attention_args a{tiles, tiles + p->tiles.size(), (int32_t)p->tiles.size(), (int32_t)p->items.size(), p->num_heads, p->num_heads / p->num_kv_heads,
                            p->head_dim, q, k, v, o, ldq, ldk, ldv, ldo, scale};
     return status_of(attention_tiled_supported(a, p->dtype) ? launch_attention_tiled(a, p->dtype, stream) : launch_attention_general(a, p->dtype, stream));
 }

@@ -13,13 +13,7 @@ struct attention_tile {
     int32_t ahead;       // query i of the tile sees the keys [0, clamp(ahead + i + 1, 0, num_kv)); not causal: num_kv all along
     int32_t max_kv;      // keys that the last query sees
     int32_t heads;       // heads of one kv head that a workgroup takes together: 1, or 2 or 4 where the queries are few (tiled kernel)
-    int32_t reserved;
-};
-
-// Work of a workgroup of the tiled kernel: a tile, and the first of its heads
-struct attention_item {
-    int32_t tile;        // -1: none
-    int32_t head;
+    int32_t head;        // in a workgroup's item: the first of its heads
 };
 
 #define LORA_ATTENTION_ROWS 128
@@ -30,7 +24,7 @@ struct lora_attention_plan {
     int32_t num_heads = 0, num_kv_heads = 0, head_dim = 0, dtype = 0;
     int32_t num_queries = 0, num_keys = 0;
     std::vector<attention_tile> tiles;      // most keys first
-    std::vector<attention_item> items;      // in the order of the workgroups
+    std::vector<attention_tile> items;      // tiles with their heads, in the order of the workgroups of the tiled kernel; heads 0: nothing
 
     int device = -1;
     size_t d_bytes = 0;

@@ -22,10 +22,11 @@ bool offsets_ok(const int32_t* p, int32_t n)
 void order_items(lora_attention_plan* p)
 {
     constexpr int X = 8;
-    std::vector<attention_item> list[X];
+    std::vector<attention_tile> list[X];
     int64_t cost[X] = {};
     auto add = [&](int x, int32_t tile, int32_t head) {
-        list[x].push_back(attention_item{tile, head});
+        list[x].push_back(p->tiles[tile]);
+        list[x].back().head = head;
         cost[x] += (int64_t)p->tiles[tile].max_kv + 64;
     };
     const int32_t H = p->num_heads, group = H / p->num_kv_heads, T = (int32_t)p->tiles.size();
@@ -40,7 +41,7 @@ void order_items(lora_attention_plan* p)
                 add((int)(std::min_element(cost, cost + X) - cost), t, u * unit + h);
     size_t longest = 0;
     for (const auto& l : list) longest = std::max(longest, l.size());
-    p->items.assign(longest * X, attention_item{-1, 0});
+    p->items.assign(longest * X, attention_tile{});
     for (int x = 0; x < X; ++x)
         for (size_t i = 0; i < list[x].size(); ++i) p->items[i * X + x] = list[x][i];
 }

@@ -7,7 +7,7 @@
 
 struct attention_args {
     const attention_tile* tiles;
-    const attention_item* items;
+    const attention_tile* items;
     int32_t num_tiles, num_items, num_heads, group, head_dim;      // group: query heads of a kv head
     const void *q, *k, *v;
     void* o;

@@ -163,13 +163,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     constexpr int QR = F32 ? DP / 2 : DP / 16;                      // fp32: a register per two dims; bf16: 8 dims a lane and product
     __shared__ __align__(1024) char lds[2][2][BK * ROW];            // buffer, keys / values
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
-    const attention_item item = a.items[blockIdx.x];
-    if (item.tile < 0) return;
-    const attention_tile t = a.tiles[item.tile];
-    const int waves = 4 / t.heads, head = item.head + wave / waves, row0 = wave % waves * 32;      // this wavefront's head, and its first query
+    const attention_tile t = a.items[blockIdx.x];
+    if (t.heads == 0) return;
+    const int waves = 4 / t.heads, head = t.head + wave / waves, row0 = wave % waves * 32;      // this wavefront's head, and its first query
     const int D = a.head_dim;
-    const char* const kb = static_cast<const char*>(a.k) + ((int64_t)t.kv_row0 * a.ldk + (int64_t)(item.head / a.group) * D) * (int)sizeof(T);
-    const char* const vb = static_cast<const char*>(a.v) + ((int64_t)t.kv_row0 * a.ldv + (int64_t)(item.head / a.group) * D) * (int)sizeof(T);
+    const char* const kb = static_cast<const char*>(a.k) + ((int64_t)t.kv_row0 * a.ldk + (int64_t)(t.head / a.group) * D) * (int)sizeof(T);
+    const char* const vb = static_cast<const char*>(a.v) + ((int64_t)t.kv_row0 * a.ldv + (int64_t)(t.head / a.group) * D) * (int)sizeof(T);
     const int64_t kpitch = a.ldk * (int)sizeof(T), vpitch = a.ldv * (int)sizeof(T);
     const int tiles = (t.max_kv + BK - 1) / BK;
 
@@ -193,6 +192,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) s.load(v_off[i], lds0 + (n & 1) * (2 * BK * ROW) + BK * ROW + i * 1024);
     };
+
+    if (tiles > 0) fetch(0);
 
     // queries; a negative scale turns their sign
     const int row = row0 + col;
@@ -237,7 +238,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
         for (int i = 0; i < 16; ++i) acc[n][i] = 0.f;
     float m = -INFINITY, ref = 0.f;
     l = 0.f;
-    if (tiles > 0) fetch(0);
+    if (careful && tiles > 0) fetch(0);
     for (int n = 0; n < tiles; ++n) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();                                       // the tile is there, and nobody reads the other buffer any more
@@ -391,18 +392,29 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum += fabsf(acc[d][i]);
     if (__syncthreads_or(!(sum < INFINITY))) pass(std::true_type{});
-    if (!valid) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* const out = static_cast<T*>(a.o) + (int64_t)(t.q_row0 + row) * a.ldo + (int64_t)head * D;
+    T* const out = static_cast<T*>(a.o) + (int64_t)(t.q_row0 + (valid ? row : 0)) * a.ldo + (int64_t)head * D;
 #pragma unroll
     for (int d = 0; d < NB; ++d)
+        if constexpr (F32) {
 #pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-            const int at = 32 * d + 2 * i + 4 * half;
-            if (at >= D) continue;                             // (D is a multiple of 4)
-            const float y[4] = {acc[d][i] * inv, acc[d][i + 1] * inv, acc[d][i + 2] * inv, acc[d][i + 3] * inv};
-            if constexpr (F32) *reinterpret_cast<float4*>(out + at) = float4{y[0], y[1], y[2], y[3]};
-            else *reinterpret_cast<uint2*>(out + at) = uint2{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+            for (int i = 0; i < 16; i += 4) {
+                const int at = 32 * d + 2 * i + 4 * half;
+                if (valid && at < D) *reinterpret_cast<float4*>(out + at) = float4{acc[d][i] * inv, acc[d][i + 1] * inv, acc[d][i + 2] * inv, acc[d][i + 3] * inv};
+            }
+        } else {
+#if defined(__HIP_DEVICE_COMPILE__)
+            // 4 dims of a query in each half of the wavefront: two such pairs change places to stores of 8 dims a lane
+#pragma unroll
+            for (int i = 0; i < 16; i += 8) {
+                uint32_t u[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] = pack_bf16(acc[d][i + 2 * e] * inv, acc[d][i + 2 * e + 1] * inv);
+                const auto x = __builtin_amdgcn_permlane32_swap(u[0], u[2], false, false), y = __builtin_amdgcn_permlane32_swap(u[1], u[3], false, false);
+                const int at = 32 * d + 2 * i + 8 * half;
+                if (valid && at < D) *reinterpret_cast<uint4*>(out + at) = uint4{x[0], y[0], x[1], y[1]};
+            }
+#endif
         }
 }
 }  // namespace
