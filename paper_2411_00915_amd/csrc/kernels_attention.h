@@ -41,9 +41,9 @@ struct cache_attention_args {
     int32_t num_heads, group;
     float scale, decay;          // decay < 0: weights are left alone
     int32_t row_tiles, splits, split_tokens;
-    float2* stats;               // [num_tokens * num_heads][splits] maximum (base 2) and sum
+    float2* stats;               // [num_tokens * num_heads][splits] maximum and sum
     float* partial;              // [num_tokens * num_heads][splits][head_dim], where splits > 1
-    float* scores;               // [num_tokens * num_heads][score_stride] (base 2), where weights are wanted
+    float* scores;               // [num_tokens * num_heads][score_stride], where weights are wanted
     int64_t score_stride;
 };
 

@@ -135,13 +135,6 @@ __device__ __forceinline__ uint32_t finite_or_zero(uint32_t u)
     return ((u & 0x7f80u) == 0x7f80u ? 0u : u & 0xffffu) | ((u & 0x7f800000u) == 0x7f800000u ? 0u : u & 0xffff0000u);
 }
 
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
-{
-    typedef __attribute__((__vector_size__(2 * sizeof(float)))) float floatx2;
-    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
-    return __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{a, b}), bf16x2));      // (one conversion for both)
-}
-
 // the greater of the two lanes of a query
 __device__ __forceinline__ float max_of_halves(float x)
 {
@@ -228,8 +221,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 
     floatx16 acc[NB];
     float l = 0.f;
-    // A weight of 0 does not hide infinities and NaN of a value from the product.  Where the result holds any, the workgroup goes
-    // through its tiles once more and takes them out of the products where some query does not see the token.
+    // A weight of 0 does not hide infinities and NaN of a value from the product, and scores near the end of 32 bits are past it
+    // when scaled to base 2.  Where the result holds infinities or NaN, or a query that sees keys has no weight, the workgroup
+    // goes through its tiles once more: such values are taken out of the products where some query does not see the token,
+    // and scores are scaled behind the subtraction of their maximum.
     auto pass = [&](auto careful_) {
     constexpr bool careful = decltype(careful_)::value;
 #pragma unroll
@@ -285,9 +280,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
         for (int b = 0; b < SB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[b][i]);
-        mx = max_of_halves(mx) * c2;
-        if (__ballot(mx > m + 8.f)) {
-            const float top = fmaxf(m, mx), alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - top);
+        mx = max_of_halves(mx) * (careful ? 1.f : c2);
+        if (__ballot(careful ? (mx - m) * c2 > 8.f : mx > m + 8.f)) {
+            const float top = fmaxf(m, mx), alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * (careful ? c2 : 1.f));
             m = top;
             ref = top == -INFINITY ? 0.f : top;
             l *= alpha;
@@ -300,7 +295,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
         for (int b = 0; b < SB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[b][i] = __builtin_amdgcn_exp2f(x[b][i] * c2 - ref);
+                x[b][i] = __builtin_amdgcn_exp2f(careful ? (x[b][i] - ref) * c2 : x[b][i] * c2 - ref);
                 l += x[b][i];
             }
         // values: fp32 one dim a lane, bf16 four tokens of a dim by a transposing read (of 16 lanes, lane i points at 4 dims of
@@ -391,7 +386,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     for (int d = 0; d < NB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum += fabsf(acc[d][i]);
-    if (__syncthreads_or(!(sum < INFINITY))) pass(std::true_type{});
+    if (__syncthreads_or(!(sum < INFINITY) || (l == 0.f && limit > 0))) pass(std::true_type{});
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* const out = static_cast<T*>(a.o) + (int64_t)(t.q_row0 + (valid ? row : 0)) * a.ldo + (int64_t)head * D;
 #pragma unroll

@@ -17,17 +17,33 @@
 // split over workgroups as well, which a second launch joins.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "cache_format.h"
 #include "launch.h"
 #include "mfma_tile.h"
 
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
+// scaled to base 2 behind the subtraction: scores up to the end of 32 bits stay in range
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+
+// the two constants of a conversion: one instruction takes at most one scalar register, so the mask lives in a vector register
+struct code_bits {
+    uint32_t mask, sixteen;
+    __device__ __forceinline__ code_bits()
+    {
+        mask = 0x00780078u;
+        sixteen = 0x41804180u;
+        asm volatile("" : "+v"(mask));
+        asm volatile("" : "+s"(sixteen));
+    }
+    __device__ __forceinline__ uint32_t operator()(uint32_t w) const { return (w & mask) | sixteen; }
+};
 
 // 8 codes (low nibble first) as the operand pairs (i, i + 4)
 template <bool EXACT>
-__device__ __forceinline__ op16 key_operand(uint32_t w)
+__device__ __forceinline__ op16 key_operand(uint32_t w, const code_bits& bits)
 {
     op16 o;
     if constexpr (EXACT) {
@@ -39,20 +55,19 @@ __device__ __forceinline__ op16 key_operand(uint32_t w)
         }
         o.u = uint4{u[0], u[1], u[2], u[3]};
     } else
-        o.u = uint4{(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u,
-                    (w >> 9 & 0x00780078u) | 0x41804180u};
+        o.u = uint4{bits(w << 3), bits(w >> 1), bits(w >> 5), bits(w >> 9)};
     return o;
 }
 
 // nibble n (0 or 1) of the bytes in bits 0..7 and 16..23
 template <bool EXACT>
-__device__ __forceinline__ uint32_t code_pair(uint32_t w, int n)
+__device__ __forceinline__ uint32_t code_pair(uint32_t w, int n, const code_bits& bits)
 {
     if constexpr (EXACT) {
         const uint32_t lo = __float_as_uint((float)(w >> (4 * n) & 15u)), hi = __float_as_uint((float)(w >> (4 * n + 16) & 15u));
         return lo >> 16 | (hi & 0xffff0000u);
     }
-    return ((n == 0 ? w << 3 : w >> 1) & 0x00780078u) | 0x41804180u;
+    return bits(n == 0 ? w << 3 : w >> 1);
 }
 
 // a lane's share of a block of 32 tokens
@@ -71,7 +86,7 @@ __device__ __forceinline__ void get16(const unsigned char* p, uint32_t* w)
 
 // `at`: the block's first place in its page
 template <int DP>
-__device__ __forceinline__ void load_block(block_loads<DP>& b, const unsigned char* page, int page_tokens, int at, int r, int g)
+__device__ __forceinline__ void load_keys(block_loads<DP>& b, const unsigned char* page, int page_tokens, int at, int r, int g)
 {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -83,32 +98,36 @@ __device__ __forceinline__ void load_block(block_loads<DP>& b, const unsigned ch
 #pragma unroll
             for (int i = 0; i < DP / 128; ++i) get16(p + 16 * i, b.k[x] + 4 * i);
     }
-    const unsigned char* v = page + page_tokens * (DP / 2) + (at >> 5) * (DP * 16) + (g * 16 + r) * (DP / 4);
-#pragma unroll
-    for (int i = 0; i < DP / 64; ++i) get16(v + 16 * i, b.v + 4 * i);
     const unsigned char* w = page + page_tokens * DP + (at + 8 * g) * 4;
     get16(w, b.kw);
     get16(w + 16, b.kw + 4);
-    get16(w + page_tokens * 4, b.vw);
-    get16(w + page_tokens * 4 + 16, b.vw + 4);
+}
+template <int DP>
+__device__ __forceinline__ void load_values(block_loads<DP>& b, const unsigned char* page, int page_tokens, int at, int r, int g)
+{
+    const unsigned char* v = page + page_tokens * (DP / 2) + (at >> 5) * (DP * 16) + (g * 16 + r) * (DP / 4);
+#pragma unroll
+    for (int i = 0; i < DP / 64; ++i) get16(v + 16 * i, b.v + 4 * i);
+    const unsigned char* w = page + page_tokens * (DP + 4) + (at + 8 * g) * 4;
+    get16(w, b.vw);
+    get16(w + 16, b.vw + 4);
 }
 
 // operand of the values: row r of the product is dim (DP/16) r + n, its 8 tokens in the registers' order
 template <int DP, bool EXACT>
-__device__ __forceinline__ op16 value_operand(const uint32_t* v, int n)
+__device__ __forceinline__ op16 value_operand(const uint32_t* v, int n, const code_bits& bits)
 {
     uint32_t u[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {                              // tokens 2i and 2i + 1
         if constexpr (DP == 64) {                              // (two tokens to a word, 4 codes each)
-            const uint32_t w = v[i] >> (8 * (n >> 1)) & 0x00ff00ffu;
-            u[i] = code_pair<EXACT>(w, n & 1);
+            u[i] = EXACT ? code_pair<EXACT>(v[i] >> (4 * n), 0, bits) : bits(n == 0 ? v[i] << 3 : v[i] >> (4 * n - 3));
         } else {
             constexpr int W = DP / 128;                        // words a token
             const uint32_t a = v[2 * i * W + (n >> 3)], b = v[(2 * i + 1) * W + (n >> 3)];
             const int byte = (n & 7) >> 1;
             const uint32_t w = __builtin_amdgcn_perm(b, a, 0x0c040c00u + byte * 0x00010001u);
-            u[i] = code_pair<EXACT>(w, n & 1);
+            u[i] = code_pair<EXACT>(w, n & 1, bits);
         }
     }
     op16 o;
@@ -120,6 +139,10 @@ __device__ __forceinline__ op16 value_operand(const uint32_t* v, int n)
 template <int TERMS>
 __device__ __forceinline__ void terms_of(const float* x, op16* t)
 {
+    if constexpr (TERMS == 1) {
+        t[0].u = uint4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
+        return;
+    }
     float rest[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) rest[i] = x[i];
@@ -135,8 +158,20 @@ __device__ __forceinline__ void terms_of(const float* x, op16* t)
     }
 }
 
+// the greatest of the four lanes of a query row
+__device__ __forceinline__ float max_of_rows(float x)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+#endif
+    return x;
+}
+
 template <typename T, int DP, int CT, bool KEEP>
-__global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_args a)
+__global__ __launch_bounds__(256, sizeof(T) == 2 && CT == 1 && DP <= 128 ? DP == 64 ? 4 : 3 : DP <= 128 ? 2 : 1) void cache_attention_kernel(cache_attention_args a)
 {
     constexpr bool EXACT = sizeof(T) == 4;
     constexpr int TERMS = EXACT ? 3 : 1, NS = DP / 32, NB = DP / 16;
@@ -163,7 +198,7 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_ar
     op16 q[CT][NS][TERMS];
     float qsum[CT], start[CT];
     int limit[CT];
-    const float c2 = a.scale * kLog2e;
+    const float scale = a.scale;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         const int row = row0 + 16 * ct + r;
@@ -186,7 +221,7 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_ar
         }
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
-        qsum[ct] = sum * c2;
+        qsum[ct] = sum * scale;
         start[ct] = -OFFSET * sum;
     }
 
@@ -204,11 +239,25 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_ar
     one.u = uint4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
 
     const int blocks_a_page = c.page_tokens >> 5, last = (t1 + 31) >> 5;
+    typedef const __attribute__((address_space(4))) int32_t* constants;         // (nothing writes the table while the kernel runs)
+    const constants table = (constants)(uintptr_t)(c.page_table + (int64_t)seq * c.table_stride);
     auto page_at = [&](int b) -> const unsigned char* {        // null: not there
-        const int64_t p = page_of(c, seq, b / blocks_a_page);
-        return p < 0 ? nullptr : c.pages + (p * c.kv_heads + head) * c.page_bytes;
+        const int64_t p = table[b / blocks_a_page];
+        return p < 0 || p >= c.num_pages ? nullptr : c.pages + (p * c.kv_heads + head) * c.page_bytes;
     };
-    auto compute = [&](const block_loads<DP>& in, int b) {
+    const code_bits bits;
+    auto keep_scores = [&](int ct, int tok, const float* x) {
+        const int row = row0 + 16 * ct + r;
+        if (row >= R) return;
+        float* const p = a.scores + ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + tok;
+        *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]};
+        *reinterpret_cast<float4*>(p + 4) = float4{x[4], x[5], x[6], x[7]};
+    };
+    // One block.  Keys and values of the wavefront's next block are asked for as soon as this one's are in operands: `ahead` is
+    // that block's page, `at` its place in it (null: none).
+    block_loads<DP> in;
+    auto compute = [&](int b, const unsigned char* ahead, int at, auto masked_) {
+        constexpr bool masked = decltype(masked_)::value;      // some row does not see all of the block
         float x[CT][8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {                          // tokens 8g + 4h + i
@@ -217,7 +266,7 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_ar
             for (int ct = 0; ct < CT; ++ct) s[ct] = floatx4{start[ct], start[ct], start[ct], start[ct]};
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
-                const op16 k = key_operand<EXACT>(in.k[h][n]);
+                const op16 k = key_operand<EXACT>(in.k[h][n], bits);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
@@ -228,34 +277,21 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_ar
                 const uint32_t w = in.kw[4 * h + i];
                 const float step = __uint_as_float(w << 16), middle = __uint_as_float(w & 0xffff0000u) + 7.5f * step;
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) x[ct][4 * h + i] = step * c2 * s[ct][i] + middle * qsum[ct];
+                for (int ct = 0; ct < CT; ++ct) x[ct][4 * h + i] = step * scale * s[ct][i] + middle * qsum[ct];
             }
         }
+        if (ahead) load_keys<DP>(in, ahead, c.page_tokens, at, r, g);
         const int tok = 32 * b + 8 * g;
-        const bool masked = 32 * b + 32 > least;               // some row does not see all of the block
-        float step[8], middle[8];
+        if constexpr (masked)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            step[i] = __uint_as_float(in.vw[i] << 16);
-            middle[i] = __uint_as_float(in.vw[i] & 0xffff0000u) + 7.5f * step[i];
-        }
-        if (masked)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
                     if (tok + i >= limit[ct]) x[ct][i] = -INFINITY;
-            }
         if constexpr (KEEP)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) {
-                const int row = row0 + 16 * ct + r;
-                if (row >= R) continue;
-                float* const p = a.scores + ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + tok;
-                *reinterpret_cast<float4*>(p) = float4{x[ct][0], x[ct][1], x[ct][2], x[ct][3]};
-                *reinterpret_cast<float4*>(p + 4) = float4{x[ct][4], x[ct][5], x[ct][6], x[ct][7]};
-            }
-        // the running maximum, raised only where a score is 2^8 above it (weights then stay below 2^8)
+            for (int ct = 0; ct < CT; ++ct) keep_scores(ct, tok, x[ct]);
+        // the running maximum, raised only where a score is 5.5 above it (weights then stay below 2^8)
         float mx[CT];
         bool raise = false;
 #pragma unroll
@@ -263,14 +299,13 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_ar
             mx[ct] = x[ct][0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) mx[ct] = fmaxf(mx[ct], x[ct][i]);
-            mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 16, 64));
-            mx[ct] = fmaxf(mx[ct], __shfl_xor(mx[ct], 32, 64));
-            raise |= mx[ct] > m[ct] + 8.f;
+            mx[ct] = max_of_rows(mx[ct]);
+            raise |= mx[ct] > m[ct] + 5.5f;
         }
         if (__ballot(raise)) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
-                const float mn = fmaxf(m[ct], mx[ct]), alpha = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[ct] - mn);
+                const float mn = fmaxf(m[ct], mx[ct]), alpha = mn == -INFINITY ? 1.f : exp_of(m[ct] - mn);
                 m[ct] = mn;
                 ref[ct] = mn == -INFINITY ? 0.f : mn;
                 l[ct] *= alpha;
@@ -284,47 +319,73 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_ar
             }
         }
         op16 p[CT][TERMS];
+        float w[CT][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float step = __uint_as_float(in.vw[i] << 16), middle = __uint_as_float(in.vw[i] & 0xffff0000u) + 7.5f * step;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) {
+                const bool there = !masked || tok + i < limit[ct];
+                const float e = exp_of(x[ct][i] - ref[ct]);
+                l[ct] += e;
+                w[ct][i] = there ? e * step : 0.f;             // (what is not seen may hold anything)
+                z[ct] += there ? e * middle : 0.f;
+            }
+        }
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-            float w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const bool there = !masked || tok + i < limit[ct];
-                const float e = __builtin_amdgcn_exp2f(x[ct][i] - ref[ct]);
-                l[ct] += e;
-                w[i] = there ? e * step[i] : 0.f;              // (what is not seen may hold anything)
-                z[ct] += there ? e * middle[i] : 0.f;
-            }
-            terms_of<TERMS>(w, p[ct]);
+            terms_of<TERMS>(w[ct], p[ct]);
 #pragma unroll
             for (int t = 0; t < TERMS; ++t) ones[ct] = mfma(one, p[ct][t], ones[ct]);
         }
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-            const op16 v = value_operand<DP, EXACT>(in.v, n);
+            const op16 v = value_operand<DP, EXACT>(in.v, n, bits);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t) acc[ct][n] = mfma(v, p[ct][t], acc[ct][n]);
         }
+        if (ahead) load_values<DP>(in, ahead, c.page_tokens, at, r, g);
     };
-
-    for (int b = (t0 >> 5) + wave; b < last; b += 4) {
-        const unsigned char* const page = page_at(b);
-        if (!page) {
-            if constexpr (KEEP)                                // (a slot that is not there is not seen)
+    auto absent = [&](int b) {
+        if constexpr (KEEP) {                                  // (a slot that is not there is not seen)
+            const float none[8] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) {
-                    const int row = row0 + 16 * ct + r;
-                    if (row >= R) continue;
-                    float* const p = a.scores + ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride;
-                    for (int i = 0; i < 8; ++i) p[32 * b + 8 * g + i] = -INFINITY;
-                }
-            continue;
+            for (int ct = 0; ct < CT; ++ct) keep_scores(ct, 32 * b + 8 * g, none);
         }
-        block_loads<DP> in;
-        load_block<DP>(in, page, c.page_tokens, (b % blocks_a_page) * 32, r, g);
-        compute(in, b);
+    };
+    // the wavefront's first block from b on whose page is there: its page and place, or null and b >= last
+    int b = (t0 >> 5) + wave, at = 0;
+    auto find = [&]() -> const unsigned char* {
+        for (; b < last; b += 4) {
+            const unsigned char* const p = page_at(b);
+            if (p) {
+                at = b % blocks_a_page * 32;
+                return p;
+            }
+            absent(b);
+        }
+        return nullptr;
+    };
+    const unsigned char* page = find();
+    if (page) {
+        load_keys<DP>(in, page, c.page_tokens, at, r, g);
+        load_values<DP>(in, page, c.page_tokens, at, r, g);
+    }
+    const int full = min(last, least >> 5);                    // blocks that every row sees
+    while (b < full) {
+        const int now = b;
+        b += 4;
+        page = find();
+        compute(now, page, at, std::false_type{});
+    }
+#pragma unroll 1
+    while (b < last) {
+        const int now = b;
+        b += 4;
+        page = find();
+        compute(now, page, at, std::true_type{});
     }
 
     // the wavefronts' sums meet, column tile by column tile
@@ -338,7 +399,7 @@ __global__ __launch_bounds__(256) void cache_attention_kernel(cache_attention_ar
         if (g == 0) red_m[wave][r] = m[ct];
         __syncthreads();
         float top = fmaxf(fmaxf(red_m[0][r], red_m[1][r]), fmaxf(red_m[2][r], red_m[3][r]));
-        const float f = m[ct] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref[ct] - top);
+        const float f = m[ct] == -INFINITY ? 0.f : exp_of(ref[ct] - top);
         const float add = z[ct] - OFFSET * ones[ct][0];
         // a wavefront that saw nothing has summed nothing
 #pragma unroll
@@ -389,7 +450,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attention_args a)
     for (int s = 0; s < a.splits; ++s) {
         const float2 e = st[s];
         if (e.y == 0.f) continue;                              // (nothing seen; NaN goes on)
-        const float f = __builtin_amdgcn_exp2f(e.x - top);
+        const float f = exp_of(e.x - top);
         sum += f * e.y;
         const float* const p = a.partial + (out_row * a.splits + s) * D;
 #pragma unroll
@@ -405,7 +466,7 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attention_args a)
 // Accumulated weights: a thread a slot of one sequence and kv head, over all query rows, whose scores the attention left behind
 __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args a, int chunks)
 {
-    __shared__ float lse[256];                                 // of 256 rows at a time: maximum + log2(sum), inf where nothing is seen
+    __shared__ float lse[256];                                 // of 256 rows at a time: maximum + log(sum), inf where nothing is seen
     const cache_args& c = a.c;
     const int tid = threadIdx.x;
     int id = blockIdx.x;
@@ -425,8 +486,8 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args 
             float top = -INFINITY, l = 0.f;
             for (int s = 0; s < a.splits; ++s) top = fmaxf(top, st[s].x);
             for (int s = 0; s < a.splits; ++s)
-                if (st[s].y != 0.f) l += __builtin_amdgcn_exp2f(st[s].x - top) * st[s].y;
-            lse[tid] = l == 0.f ? INFINITY : top + log2f(l);
+                if (st[s].y != 0.f) l += exp_of(st[s].x - top) * st[s].y;
+            lse[tid] = l == 0.f ? INFINITY : top + logf(l);
         }
         __syncthreads();
         const int n = min(256, R - r0);
@@ -434,7 +495,7 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args 
             const int row = r0 + j;
             if (slot >= length - rows.count + row / a.group + 1) continue;
             const float x = a.scores[((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + slot];
-            sum += __builtin_amdgcn_exp2f(x - lse[j]);
+            sum += exp_of(x - lse[j]);
         }
     }
     if (slot >= length) return;

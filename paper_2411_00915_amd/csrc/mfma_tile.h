@@ -52,6 +52,14 @@ __device__ __forceinline__ floatx4 mfma(const op16& a, const op16& b, floatx4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
 }
 
+// two values rounded to bf16 by one conversion, the first in the low half
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
+{
+    typedef __attribute__((__vector_size__(2 * sizeof(float)))) float floatx2;
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((floatx2{a, b}), bf16x2));      // (one conversion for both)
+}
+
 static __device__ __align__(256) uint32_t lora_zero_block[64];       // what masked-out loads read (never written)
 __device__ __forceinline__ void split_bf16(const float* f, op16& hi, op16& lo)
 {
