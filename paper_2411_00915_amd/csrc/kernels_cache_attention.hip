@@ -70,47 +70,53 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t w, int n, const code_bits
     return bits(n == 0 ? w << 3 : w >> 1);
 }
 
-// a lane's share of a block of 32 tokens
+// A block of 32 tokens in LDS: what each lane wants of it as keys, in rows of 16 bytes a lane (DP 64: as the page has them), then
+// as values, then the words of its keys and of its values
 template <int DP>
-struct block_loads {
-    uint32_t k[2][DP / 32];      // the two products' rows: 16 bytes at DP 128
-    uint32_t v[DP / 16];         // 8 tokens x DP/16 codes
-    uint32_t kw[8], vw[8];       // words of its 8 tokens
+struct block_lds {
+    static constexpr int LOADS = DP / 64;                      // of 1 KB, keys and values each
+    static constexpr int VALUES = LOADS * 1024, WORDS = 2 * VALUES, BYTES = WORDS + 256, COUNT = 2 * LOADS + 1;
 };
 
-__device__ __forceinline__ void get16(const unsigned char* p, uint32_t* w)
+__device__ __forceinline__ void get16(const char* p, uint32_t* w)
 {
-    const uint4 u = ld16(reinterpret_cast<const bf16_t*>(p));
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
     w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
 }
 
+__device__ __forceinline__ void load4_to_lds(const char* base, uint32_t off, uint32_t lds_base)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" ::"v"(off), "s"(base), "s"(lds_base) : "memory");
+}
+
+// this lane's offsets in a page, from the block's own
+template <int DP>
+struct block_offsets {
+    uint32_t key[block_lds<DP>::LOADS], value, word;
+    __device__ __forceinline__ block_offsets(int page_tokens, int lane)
+    {
+        const int r = lane & 15, g = lane >> 4;
+#pragma unroll
+        for (int i = 0; i < block_lds<DP>::LOADS; ++i)         // DP 128: a product's rows each; 256: their halves
+            key[i] = DP == 64 ? 16 * lane : (8 * (r >> 2) + (r & 3) + 4 * (i / (DP / 128))) * (DP / 2) + g * (DP / 8) + i % (DP / 128) * 16;
+        value = DP == 64 ? 16 * lane : (g * 16 + r) * (DP / 4);
+        word = 4 * (lane < 32 ? lane : page_tokens + lane - 32);
+    }
+};
+
 // `at`: the block's first place in its page
 template <int DP>
-__device__ __forceinline__ void load_keys(block_loads<DP>& b, const unsigned char* page, int page_tokens, int at, int r, int g)
+__device__ __forceinline__ void fetch_block(const unsigned char* page, int page_tokens, int at, const block_offsets<DP>& off, uint32_t lds)
 {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const char* const p = reinterpret_cast<const char*>(page);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-        const unsigned char* p = page + (at + 8 * (r >> 2) + (r & 3) + 4 * x) * (DP / 2) + g * (DP / 8);
-        if constexpr (DP == 64) {
-            const uint2 u = *reinterpret_cast<const uint2*>(p);
-            b.k[x][0] = u.x; b.k[x][1] = u.y;
-        } else
+    for (int i = 0; i < block_lds<DP>::LOADS; ++i) load16_to_lds(p + at * (DP / 2), off.key[i], lds + i * 1024);
 #pragma unroll
-            for (int i = 0; i < DP / 128; ++i) get16(p + 16 * i, b.k[x] + 4 * i);
-    }
-    const unsigned char* w = page + page_tokens * DP + (at + 8 * g) * 4;
-    get16(w, b.kw);
-    get16(w + 16, b.kw + 4);
-}
-template <int DP>
-__device__ __forceinline__ void load_values(block_loads<DP>& b, const unsigned char* page, int page_tokens, int at, int r, int g)
-{
-    const unsigned char* v = page + page_tokens * (DP / 2) + (at >> 5) * (DP * 16) + (g * 16 + r) * (DP / 4);
-#pragma unroll
-    for (int i = 0; i < DP / 64; ++i) get16(v + 16 * i, b.v + 4 * i);
-    const unsigned char* w = page + page_tokens * (DP + 4) + (at + 8 * g) * 4;
-    get16(w, b.vw);
-    get16(w + 16, b.vw + 4);
+    for (int i = 0; i < block_lds<DP>::LOADS; ++i)
+        load16_to_lds(p + page_tokens * (DP / 2) + (at >> 5) * (DP * 16) + 16 * i, off.value, lds + block_lds<DP>::VALUES + i * 1024);
+    load4_to_lds(p + page_tokens * DP + at * 4, off.word, lds + block_lds<DP>::WORDS);
+#endif
 }
 
 // operand of the values: row r of the product is dim (DP/16) r + n, its 8 tokens in the registers' order
@@ -171,12 +177,14 @@ __device__ __forceinline__ float max_of_rows(float x)
 }
 
 template <typename T, int DP, int CT, bool KEEP>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && CT == 1 && DP <= 128 ? DP == 64 ? 4 : 3 : DP <= 128 ? 2 : 1) void cache_attention_kernel(cache_attention_args a)
+__global__ __launch_bounds__(256, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 : 2) void cache_attention_kernel(cache_attention_args a)
 {
     constexpr bool EXACT = sizeof(T) == 4;
     constexpr int TERMS = EXACT ? 3 : 1, NS = DP / 32, NB = DP / 16;
     constexpr float OFFSET = EXACT ? 7.5f : 23.5f;         // of what the matrix cores see, from code - 7.5
-    __shared__ __align__(16) float red[4][16][DP + 4];
+    constexpr int RING = DP == 64 ? 3 : 2, RING_BYTES = 4 * RING * block_lds<DP>::BYTES, RED_BYTES = 4 * 16 * (DP + 4) * 4;
+    __shared__ __align__(16) char lds[RING_BYTES > RED_BYTES ? RING_BYTES : RED_BYTES];
+    float (*const red)[16][DP + 4] = reinterpret_cast<float (*)[16][DP + 4]>(lds);           // (when the rings are done with)
     __shared__ float red_m[4][16], red_l[4][16];
     const cache_args& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
@@ -253,34 +261,41 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && CT == 1 && DP <= 128 ? DP ==
         *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]};
         *reinterpret_cast<float4*>(p + 4) = float4{x[4], x[5], x[6], x[7]};
     };
-    // One block.  Keys and values of the wavefront's next block are asked for as soon as this one's are in operands: `ahead` is
-    // that block's page, `at` its place in it (null: none).
-    block_loads<DP> in;
-    auto compute = [&](int b, const unsigned char* ahead, int at, auto masked_) {
+    auto compute = [&](int b, const char* block, auto masked_) {
         constexpr bool masked = decltype(masked_)::value;      // some row does not see all of the block
+        typedef block_lds<DP> L;
         float x[CT][8];
+        uint32_t kw[8];
+        get16(block + L::WORDS + 32 * g, kw);
+        get16(block + L::WORDS + 32 * g + 16, kw + 4);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {                          // tokens 8g + 4h + i
+            uint32_t k[DP / 32];
+            if constexpr (DP == 64) {
+                const uint2 u = *reinterpret_cast<const uint2*>(block + (8 * (r >> 2) + (r & 3) + 4 * h) * 32 + 8 * g);
+                k[0] = u.x; k[1] = u.y;
+            } else
+#pragma unroll
+                for (int i = 0; i < DP / 128; ++i) get16(block + (h * (DP / 128) + i) * 1024 + 16 * lane, k + 4 * i);
             floatx4 s[CT];
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) s[ct] = floatx4{start[ct], start[ct], start[ct], start[ct]};
 #pragma unroll
             for (int n = 0; n < NS; ++n) {
-                const op16 k = key_operand<EXACT>(in.k[h][n], bits);
+                const op16 ko = key_operand<EXACT>(k[n], bits);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                    for (int t = 0; t < TERMS; ++t) s[ct] = mfma(k, q[ct][n][t], s[ct]);
+                    for (int t = 0; t < TERMS; ++t) s[ct] = mfma(ko, q[ct][n][t], s[ct]);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const uint32_t w = in.kw[4 * h + i];
+                const uint32_t w = kw[4 * h + i];
                 const float step = __uint_as_float(w << 16), middle = __uint_as_float(w & 0xffff0000u) + 7.5f * step;
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) x[ct][4 * h + i] = step * scale * s[ct][i] + middle * qsum[ct];
             }
         }
-        if (ahead) load_keys<DP>(in, ahead, c.page_tokens, at, r, g);
         const int tok = 32 * b + 8 * g;
         if constexpr (masked)
 #pragma unroll
@@ -320,9 +335,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && CT == 1 && DP <= 128 ? DP ==
         }
         op16 p[CT][TERMS];
         float w[CT][8];
+        uint32_t vw[8];
+        get16(block + L::WORDS + 128 + 32 * g, vw);
+        get16(block + L::WORDS + 128 + 32 * g + 16, vw + 4);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float step = __uint_as_float(in.vw[i] << 16), middle = __uint_as_float(in.vw[i] & 0xffff0000u) + 7.5f * step;
+            const float step = __uint_as_float(vw[i] << 16), middle = __uint_as_float(vw[i] & 0xffff0000u) + 7.5f * step;
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 const bool there = !masked || tok + i < limit[ct];
@@ -338,15 +356,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && CT == 1 && DP <= 128 ? DP ==
 #pragma unroll
             for (int t = 0; t < TERMS; ++t) ones[ct] = mfma(one, p[ct][t], ones[ct]);
         }
+        uint32_t v[DP / 16];                                   // 8 tokens x DP/16 codes
+#pragma unroll
+        for (int i = 0; i < DP / 64; ++i) get16(block + L::VALUES + i * 1024 + 16 * lane, v + 4 * i);
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
-            const op16 v = value_operand<DP, EXACT>(in.v, n, bits);
+            const op16 vo = value_operand<DP, EXACT>(v, n, bits);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int t = 0; t < TERMS; ++t) acc[ct][n] = mfma(v, p[ct][t], acc[ct][n]);
+                for (int t = 0; t < TERMS; ++t) acc[ct][n] = mfma(vo, p[ct][t], acc[ct][n]);
         }
-        if (ahead) load_values<DP>(in, ahead, c.page_tokens, at, r, g);
     };
     auto absent = [&](int b) {
         if constexpr (KEEP) {                                  // (a slot that is not there is not seen)
@@ -368,25 +388,35 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && CT == 1 && DP <= 128 ? DP ==
         }
         return nullptr;
     };
-    const unsigned char* page = find();
-    if (page) {
-        load_keys<DP>(in, page, c.page_tokens, at, r, g);
-        load_values<DP>(in, page, c.page_tokens, at, r, g);
-    }
+    // A ring of RING blocks a wavefront: RING - 1 on their way while one is computed with.  Nobody else touches it, so there is no
+    // barrier; loads return in order, so when no more are out than the later blocks', this one's have landed.
+    const block_offsets<DP> off(c.page_tokens, lane);
+    char* const ring = lds + wave * (RING * block_lds<DP>::BYTES);
+    const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_address(ring));
     const int full = min(last, least >> 5);                    // blocks that every row sees
-    while (b < full) {
-        const int now = b;
+    int queue[RING], slot = 0;                                 // blocks in their order; >= last: none
+    auto ask = [&](int place) {                                // the next block into a place of the ring
+        const unsigned char* const page = find();
+        const int found = b;
+        if (page) fetch_block<DP>(page, c.page_tokens, at, off, ring_at + place * block_lds<DP>::BYTES);
         b += 4;
-        page = find();
-        compute(now, page, at, std::false_type{});
-    }
+        return found;
+    };
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) queue[i] = ask(i);
+    auto turn = [&](auto masked) {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the block before this one is read: its place is free)
+        queue[RING - 1] = ask(slot == 0 ? RING - 1 : slot - 1);
+        if (queue[RING - 1] < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * block_lds<DP>::COUNT) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        compute(queue[0], ring + slot * block_lds<DP>::BYTES, masked);
+#pragma unroll
+        for (int i = 0; i < RING - 1; ++i) queue[i] = queue[i + 1];
+        slot = slot == RING - 1 ? 0 : slot + 1;
+    };
+    while (queue[0] < full) turn(std::false_type{});
 #pragma unroll 1
-    while (b < last) {
-        const int now = b;
-        b += 4;
-        page = find();
-        compute(now, page, at, std::true_type{});
-    }
+    while (queue[0] < last) turn(std::true_type{});
 
     // the wavefronts' sums meet, column tile by column tile
 #pragma unroll
