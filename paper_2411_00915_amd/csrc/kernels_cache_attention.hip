@@ -457,40 +457,49 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 :
     }
 }
 
-// The splits of a query row joined: a wavefront a row
+// The splits of a query row joined: a workgroup a row, its wavefronts take turns at the splits, four at a time.  Leaves the
+// logarithm of the row's sum (with its maximum) in place of its first split's statistics, for the weights.
 template <typename T>
 __global__ __launch_bounds__(256) void cache_join_kernel(cache_attention_args a)
 {
+    __shared__ float red[4][LORA_MAX_HEAD_DIM], red_sum[4], red_top[4];
     const cache_args& c = a.c;
-    const int lane = threadIdx.x & 63, D = c.head_dim;
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (row >= (int64_t)c.num_seqs * c.max_new * a.num_heads) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, D = c.head_dim;
+    const int64_t row = blockIdx.x;
     const int head = (int)(row % a.num_heads);
     const int64_t at = row / a.num_heads;
     const int seq = (int)(at / c.max_new), i = (int)(at % c.max_new);
     const cache_rows rows = rows_of(c, seq);
     if (i >= rows.count) return;
     const int64_t out_row = (int64_t)(rows.first + i) * a.num_heads + head;
-    const float2* const st = a.stats + out_row * a.splits;
+    float2* const st = a.stats + out_row * a.splits;
     float top = -INFINITY;
-    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, st[s].x);
+    for (int s = tid; s < a.splits; s += 256) top = fmaxf(top, st[s].x);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    if (lane == 0) red_top[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red_top[0], red_top[1]), fmaxf(red_top[2], red_top[3]));
     float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
+#pragma unroll 4
+    for (int s = wave; s < a.splits; s += 4) {
         const float2 e = st[s];
-        if (e.y == 0.f) continue;                              // (nothing seen; NaN goes on)
-        const float f = exp_of(e.x - top);
-        sum += f * e.y;
         const float* const p = a.partial + (out_row * a.splits + s) * D;
+        const float f = e.y == 0.f ? 0.f : exp_of(e.x - top);  // (nothing seen: its maximum is -inf, perhaps all are; NaN goes on)
+        sum += f * e.y;
 #pragma unroll
         for (int n = 0; n < 4; ++n)
             if (lane + 64 * n < D) o[n] += f * p[lane + 64 * n];
     }
-    T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + i) * a.ldo + (int64_t)head * D;
+    if (lane == 0) red_sum[wave] = sum;
 #pragma unroll
     for (int n = 0; n < 4; ++n)
-        if (lane + 64 * n < D) elem<T>::store(out + lane + 64 * n, sum == 0.f ? 0.f : o[n] / sum);
+        if (lane + 64 * n < D) red[wave][lane + 64 * n] = o[n];
+    __syncthreads();
+    sum = (red_sum[0] + red_sum[1]) + (red_sum[2] + red_sum[3]);
+    T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + i) * a.ldo + (int64_t)head * D;
+    if (tid < D) elem<T>::store(out + tid, sum == 0.f ? 0.f : ((red[0][tid] + red[1][tid]) + (red[2][tid] + red[3][tid])) / sum);
+    if (tid == 0) st[0] = float2{sum == 0.f ? INFINITY : top + logf(sum), sum};
 }
 
 // Accumulated weights: a thread a slot of one sequence and kv head, over all query rows, whose scores the attention left behind
@@ -512,20 +521,18 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args 
         __syncthreads();
         if (r0 + tid < R) {
             const int row = r0 + tid;
-            const float2* const st = a.stats + ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.splits;
-            float top = -INFINITY, l = 0.f;
-            for (int s = 0; s < a.splits; ++s) top = fmaxf(top, st[s].x);
-            for (int s = 0; s < a.splits; ++s)
-                if (st[s].y != 0.f) l += exp_of(st[s].x - top) * st[s].y;
-            lse[tid] = l == 0.f ? INFINITY : top + logf(l);
+            const float2 st = a.stats[((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.splits];
+            lse[tid] = a.splits > 1 ? st.x : st.y == 0.f ? INFINITY : st.x + logf(st.y);
         }
         __syncthreads();
         const int n = min(256, R - r0);
+#pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const int row = r0 + j;
-            if (slot >= length - rows.count + row / a.group + 1) continue;
-            const float x = a.scores[((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + slot];
-            sum += exp_of(x - lse[j]);
+            // (behind what the row sees nothing has been written)
+            const bool sees = slot < length - rows.count + row / a.group + 1;
+            const int64_t at = ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + slot;
+            sum += sees ? exp_of(a.scores[at] - lse[j]) : 0.f;
         }
     }
     if (slot >= length) return;
@@ -561,7 +568,7 @@ hipError_t launch_all(const cache_attention_args& a, hipStream_t stream)
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
         const int64_t rows = (int64_t)a.c.num_seqs * a.c.max_new * a.num_heads;
-        LORA_LAUNCH(LORA_K_CACHE_JOIN, (cache_join_kernel<T>), dim3((uint32_t)((rows + 3) / 4)), dim3(256), 0, stream, a);
+        LORA_LAUNCH(LORA_K_CACHE_JOIN, (cache_join_kernel<T>), dim3((uint32_t)rows), dim3(256), 0, stream, a);
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.scores) {
