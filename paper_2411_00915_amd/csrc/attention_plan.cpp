@@ -114,9 +114,10 @@ cache_division divide_cache_attention(const lora_cache* c, int32_t num_heads, in
     cache_division v{};
     v.row_tiles = (int32_t)((rows + 31) / 32);
     const int64_t wgs = (int64_t)c->num_seqs * c->num_kv_heads * v.row_tiles;
-    constexpr int64_t target = 768;
-    const int64_t most = (c->max_length + 255) / 256;
-    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(most, (target + wgs - 1) / std::max<int64_t>(wgs, 1)));
+    // Long contexts are split where there are fewer workgroups than compute units: into two rounds of them (a workgroup a compute
+    // unit does not hide its loads), of 512 tokens (four blocks a wavefront) or more.
+    const int64_t most = (c->max_length + 511) / 512;
+    const int64_t splits = wgs >= 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>(most, (512 + wgs - 1) / std::max<int64_t>(wgs, 1)));
     v.split_tokens = (int32_t)std::max<int64_t>(128, ((c->max_length + splits - 1) / splits + 127) / 128 * 128);
     v.splits = (int32_t)std::max<int64_t>(1, ((int64_t)c->max_length + v.split_tokens - 1) / v.split_tokens);
     const size_t out_rows = (size_t)num_tokens * num_heads;

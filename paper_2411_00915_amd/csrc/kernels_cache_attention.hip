@@ -457,12 +457,14 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 :
     }
 }
 
-// The splits of a query row joined: a workgroup a row, its wavefronts take turns at the splits, four at a time.  Leaves the
+// The splits of a query row joined: a workgroup a row, its wavefronts take turns at the splits.  Leaves the
 // logarithm of the row's sum (with its maximum) in place of its first split's statistics, for the weights.
+constexpr int kJoinThreads = 512;
 template <typename T>
-__global__ __launch_bounds__(256) void cache_join_kernel(cache_attention_args a)
+__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(cache_attention_args a)
 {
-    __shared__ float red[4][LORA_MAX_HEAD_DIM], red_sum[4], red_top[4];
+    constexpr int WAVES = kJoinThreads / 64;
+    __shared__ float red[WAVES][LORA_MAX_HEAD_DIM], red_sum[WAVES], red_top[WAVES];
     const cache_args& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, D = c.head_dim;
     const int64_t row = blockIdx.x;
@@ -474,15 +476,17 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attention_args a)
     const int64_t out_row = (int64_t)(rows.first + i) * a.num_heads + head;
     float2* const st = a.stats + out_row * a.splits;
     float top = -INFINITY;
-    for (int s = tid; s < a.splits; s += 256) top = fmaxf(top, st[s].x);
+    for (int s = tid; s < a.splits; s += kJoinThreads) top = fmaxf(top, st[s].x);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
     if (lane == 0) red_top[wave] = top;
     __syncthreads();
-    top = fmaxf(fmaxf(red_top[0], red_top[1]), fmaxf(red_top[2], red_top[3]));
+    top = red_top[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, red_top[w]);
     float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = wave; s < a.splits; s += 4) {
+    for (int s = wave; s < a.splits; s += WAVES) {
         const float2 e = st[s];
         const float* const p = a.partial + (out_row * a.splits + s) * D;
         const float f = e.y == 0.f ? 0.f : exp_of(e.x - top);  // (nothing seen: its maximum is -inf, perhaps all are; NaN goes on)
@@ -496,13 +500,20 @@ __global__ __launch_bounds__(256) void cache_join_kernel(cache_attention_args a)
     for (int n = 0; n < 4; ++n)
         if (lane + 64 * n < D) red[wave][lane + 64 * n] = o[n];
     __syncthreads();
-    sum = (red_sum[0] + red_sum[1]) + (red_sum[2] + red_sum[3]);
+    sum = 0.f;
+    float all = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        sum += red_sum[w];
+        if (tid < D) all += red[w][tid];
+    }
     T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + i) * a.ldo + (int64_t)head * D;
-    if (tid < D) elem<T>::store(out + tid, sum == 0.f ? 0.f : ((red[0][tid] + red[1][tid]) + (red[2][tid] + red[3][tid])) / sum);
+    if (tid < D) elem<T>::store(out + tid, sum == 0.f ? 0.f : all / sum);
     if (tid == 0) st[0] = float2{sum == 0.f ? INFINITY : top + logf(sum), sum};
 }
 
-// Accumulated weights: a thread a slot of one sequence and kv head, over all query rows, whose scores the attention left behind
+// Accumulated weights: a thread four slots of one sequence and kv head, over all query rows, whose scores the attention left behind
+constexpr int kWeightSlots = 1024;
 __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args a, int chunks)
 {
     __shared__ float lse[256];                                 // of 256 rows at a time: maximum + log(sum), inf where nothing is seen
@@ -514,9 +525,9 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args 
     const int head = id % c.kv_heads, seq = id / c.kv_heads;
     const cache_rows rows = rows_of(c, seq);
     const int length = length_of(c, seq), R = min(rows.count, c.max_new) * a.group;
-    if (R == 0 || chunk * 256 >= length) return;
-    const int slot = chunk * 256 + tid;
-    float sum = 0.f;
+    if (R == 0 || chunk * kWeightSlots >= length) return;
+    const int slot = chunk * kWeightSlots + 4 * tid;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
     for (int r0 = 0; r0 < R; r0 += 256) {
         __syncthreads();
         if (r0 + tid < R) {
@@ -526,21 +537,24 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args 
         }
         __syncthreads();
         const int n = min(256, R - r0);
+        if (slot >= length) continue;
 #pragma unroll 4
         for (int j = 0; j < n; ++j) {
-            const int row = r0 + j;
-            // (behind what the row sees nothing has been written)
-            const bool sees = slot < length - rows.count + row / a.group + 1;
+            const int row = r0 + j, sees = length - rows.count + row / a.group + 1 - slot;       // of the four, the first so many
             const int64_t at = ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + slot;
-            sum += sees ? exp_of(a.scores[at] - lse[j]) : 0.f;
+            const float4 x = *reinterpret_cast<const float4*>(a.scores + at);                    // (not written where it sees nothing)
+            sum[0] += sees > 0 ? exp_of(x.x - lse[j]) : 0.f;
+            sum[1] += sees > 1 ? exp_of(x.y - lse[j]) : 0.f;
+            sum[2] += sees > 2 ? exp_of(x.z - lse[j]) : 0.f;
+            sum[3] += sees > 3 ? exp_of(x.w - lse[j]) : 0.f;
         }
     }
     if (slot >= length) return;
-    const int page = slot / c.page_tokens;
+    const int page = slot / c.page_tokens;                     // (of all four: pages are multiples of 32)
     const int64_t p = page_of(c, seq, page);
     if (p < 0) return;
     float* const w = c.weight + (p * c.kv_heads + head) * c.page_tokens + slot - page * c.page_tokens;
-    *w = a.decay == 0.f ? sum : a.decay * *w + sum;
+    for (int e = 0; e < min(4, length - slot); ++e) w[e] = a.decay == 0.f ? sum[e] : a.decay * w[e] + sum[e];
 }
 
 template <typename T, int DP>
@@ -568,11 +582,11 @@ hipError_t launch_all(const cache_attention_args& a, hipStream_t stream)
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && a.splits > 1) {
         const int64_t rows = (int64_t)a.c.num_seqs * a.c.max_new * a.num_heads;
-        LORA_LAUNCH(LORA_K_CACHE_JOIN, (cache_join_kernel<T>), dim3((uint32_t)rows), dim3(256), 0, stream, a);
+        LORA_LAUNCH(LORA_K_CACHE_JOIN, (cache_join_kernel<T>), dim3((uint32_t)rows), dim3(kJoinThreads), 0, stream, a);
         e = hipGetLastError();
     }
     if (e == hipSuccess && a.scores) {
-        const int chunks = (a.c.max_length + 255) / 256;
+        const int chunks = (a.c.max_length + kWeightSlots - 1) / kWeightSlots;
         LORA_LAUNCH(LORA_K_CACHE_WEIGHT, cache_weight_kernel, dim3((uint32_t)(a.c.num_seqs * a.c.kv_heads * chunks)), dim3(256), 0, stream, a, chunks);
         e = hipGetLastError();
     }
