@@ -124,6 +124,7 @@ extern "C" lora_status lora_cache_append(const lora_cache* c, int32_t dtype, int
     if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
     const int64_t row = (int64_t)c->num_kv_heads * c->head_dim;
     if (!k || !v || ldk < row || ldv < row || misaligned(k, elem_bytes(dtype)) || misaligned(v, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
+    if ((int64_t)num_tokens / 32 + 1 > INT32_MAX / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
     return status_of(launch_cache_append(args_of(c, num_tokens, max_new, d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -135,6 +136,7 @@ extern "C" lora_status lora_cache_read(const lora_cache* c, int32_t dtype, int32
     if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
     const int64_t row = (int64_t)c->num_kv_heads * c->head_dim;
     if (!k || !v || ldk < row || ldv < row || misaligned(k, elem_bytes(dtype)) || misaligned(v, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
+    if ((int64_t)num_tokens / 32 + 1 > INT32_MAX / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
     return status_of(launch_cache_read(args_of(c, num_tokens, max_new, d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
 }
 

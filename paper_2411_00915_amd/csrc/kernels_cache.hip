@@ -1,33 +1,82 @@
 // The cache in 4 bits: tokens into it, their values out of it, and eviction.  (Attention over it: kernels_cache_attention.hip.)
 #include <hip/hip_runtime.h>
 
+#include <climits>
+
 #include "cache_format.h"
 #include "launch.h"
 
 // ---------------------------------------------------------------------------
-// Append.  16 lanes hold a token's keys (then values) of one head, lane r the dims (DP/16) r ...: a lane's codes are whole words
-// of the format in both parts, so nothing is exchanged but the least and the greatest element.  Memory bound: 4 D bytes of bf16
-// in, D + 8 out.
+// Tokens go in and out in tiles of 32 packed rows of one head.  16 lanes hold a token's keys and values, lane r the dims (DP/16) r
+// ...: a lane's codes are whole words of the format in both parts, so nothing is exchanged but the least and the greatest
+// element.  A token's keys are one run of bytes in its page; its values are 16 pieces that lie beside those of the seven
+// tokens around it, so they pass through LDS and go 8 tokens at a time (4 bytes apart a lane, 32 bytes together).
 namespace {
 
-// sequence of packed row t, or -1: the last with indptr[s] <= t that has it
-__device__ __forceinline__ int sequence_of(const cache_args& c, int t)
+constexpr int kTile = 32;
+
+// where the tokens of a tile are: the head's page (from the pool's start; -1: nowhere) and the place in it
+struct tile_places {
+    int64_t page[kTile];
+    int at[kTile];
+    int known[kTile];      // the row is one of the call's tokens
+};
+
+// the last s with indptr[s] <= t, by all lanes of a wavefront together; t is the same in all of them
+__device__ __forceinline__ int search_indptr(const cache_args& c, int t, int lane)
 {
-    if (!c.indptr) return t < c.num_seqs ? t : -1;
-    int lo = 0, hi = c.num_seqs;                               // indptr[lo] <= t < indptr[hi], if the offsets are in order
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (c.indptr[mid] <= t) lo = mid; else hi = mid;
+    int lo = 0, n = c.num_seqs;
+    while (n > 1) {
+        const int step = (n + 63) >> 6, i = lane * step;
+        const int count = __popcll(__ballot(i < n && c.indptr[lo + min(i, n - 1)] <= t));
+        const int skip = max(count - 1, 0) * step;
+        lo += skip;
+        n = min(step, n - skip);
     }
-    return t >= c.indptr[lo] && t < c.indptr[lo + 1] ? lo : -1;
+    return lo;
 }
 
-// slot of packed row t of sequence s; -1 where there is none
-__device__ __forceinline__ int slot_of(const cache_args& c, int s, int t)
+// Places of rows t0 ... in a wavefront (lanes 0 .. 31 a row each)
+__device__ __forceinline__ void find_places(const cache_args& c, int t0, int head, int lane, tile_places& p)
 {
-    const cache_rows rows = rows_of(c, s);
-    const int i = t - rows.first;
-    return i >= 0 && i < min(rows.count, c.max_new) ? length_of(c, s) - rows.count + i : -1;
+    const int t = t0 + lane;
+    const bool mine = lane < kTile && t < c.num_tokens;
+    int s = -1;
+    if (!c.indptr) s = mine && t < c.num_seqs ? t : -1;
+    else {
+        // the first row's sequence, then the ends of 64 sequences at a time, of which each row counts those it is behind
+        int base = search_indptr(c, t0, lane);
+        if (mine) s = base;
+        for (;; base += 64) {
+            const int end = base + 1 + lane < c.num_seqs ? c.indptr[base + 1 + lane] : INT_MAX;
+            int behind = 0;
+#pragma unroll
+            for (int step = 32; step > 0; step >>= 1)          // ends are in order
+                if (__shfl(end, behind + step - 1, 64) <= t) behind += step;
+            behind += __shfl(end, 63, 64) <= t && behind == 63 ? 1 : 0;
+            const bool on = mine && s == base && behind == 64;
+            if (mine && s == base) s = base + behind;
+            if (!__ballot(on)) break;
+        }
+    }
+    if (lane >= kTile) return;
+    int64_t page = -1;
+    int at = 0, known = 0;
+    if (s >= 0 && s < c.num_seqs) {
+        const cache_rows rows = rows_of(c, s);
+        const int i = t - rows.first;
+        known = i >= 0 && i < min(rows.count, c.max_new);
+        const int slot = known ? length_of(c, s) - rows.count + i : -1;
+        if (slot >= 0) {
+            const int number = slot / c.page_tokens;
+            at = slot - number * c.page_tokens;
+            page = page_of(c, s, number);
+            if (page >= 0) page = page * c.kv_heads + head;
+        }
+    }
+    p.page[lane] = page;
+    p.at[lane] = at;
+    p.known[lane] = known;
 }
 
 template <typename T, int E>
@@ -117,64 +166,92 @@ __device__ __forceinline__ uint32_t quantise(const float* x, int count, uint32_t
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void cache_append_kernel(cache_args c, const T* k, int64_t ldk, const T* v, int64_t ldv, bool aligned)
 {
-    constexpr int E = DP / 16;
-    const int64_t item = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int r = threadIdx.x & 15;
-    if (item >= (int64_t)c.num_tokens * c.kv_heads) return;    // (whole groups of 16 lanes)
-    const int t = (int)(item / c.kv_heads), head = (int)(item - (int64_t)t * c.kv_heads);
-    const int s = sequence_of(c, t);
-    const int slot = s < 0 ? -1 : slot_of(c, s, t);
-    if (slot < 0) return;
-    const int page = slot / c.page_tokens, at = slot - page * c.page_tokens;
-    const int64_t id = page_of(c, s, page);
-    if (id < 0) return;
+    constexpr int E = DP / 16, W = (E + 7) / 8;                // elements and words of a lane
+    __shared__ tile_places places;
+    __shared__ uint32_t values[kTile][16 * W + 1];
+    const int tid = threadIdx.x, r = tid & 15, head = blockIdx.x % c.kv_heads, t0 = blockIdx.x / c.kv_heads * kTile;
     const int d0 = r * E, count = min(E, c.head_dim - d0);
-    float x[2][E];
-    load_elems<T, E>(k + (int64_t)t * ldk + head * c.head_dim + d0, count, aligned, x[0]);
-    load_elems<T, E>(v + (int64_t)t * ldv + head * c.head_dim + d0, count, aligned, x[1]);
-    unsigned char* const base = c.pages + (id * c.kv_heads + head) * c.page_bytes;
+    float x[2][2][E];                                          // tokens tid / 16 and 16 on, keys and values
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        uint32_t codes[(E + 7) / 8];
-        const uint32_t word = quantise<E>(x[part], count, codes);
-        store_codes<DP>(base + (part ? value_offset<DP>(c.page_tokens, at, r) : key_offset<DP>(at, r)), codes);
-        if (r == 0) *reinterpret_cast<uint32_t*>(base + word_offset<DP>(c.page_tokens, at, part)) = word;
+    for (int h = 0; h < 2; ++h) {
+        const int t = min(t0 + (tid >> 4) + 16 * h, c.num_tokens - 1);
+        load_elems<T, E>(k + (int64_t)t * ldk + head * c.head_dim + d0, count, aligned, x[h][0]);
+        load_elems<T, E>(v + (int64_t)t * ldv + head * c.head_dim + d0, count, aligned, x[h][1]);
     }
-    if (r == 0 && c.weight) c.weight[(id * c.kv_heads + head) * c.page_tokens + at] = 0.f;
+    if (tid < 64) find_places(c, t0, head, tid, places);
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = (tid >> 4) + 16 * h;
+        uint32_t codes[2][W], words[2];
+#pragma unroll
+        for (int part = 0; part < 2; ++part) words[part] = quantise<E>(x[h][part], count, codes[part]);
+#pragma unroll
+        for (int w = 0; w < W; ++w) values[i][W * r + w] = codes[1][w];
+        const int64_t page = places.page[i];
+        if (page < 0) continue;
+        unsigned char* const base = c.pages + page * c.page_bytes;
+        store_codes<DP>(base + key_offset<DP>(places.at[i], r), codes[0]);
+        if (r < 2) *reinterpret_cast<uint32_t*>(base + word_offset<DP>(c.page_tokens, places.at[i], r)) = r ? words[1] : words[0];
+        if (r == 2 && c.weight) c.weight[page * c.page_tokens + places.at[i]] = 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int i = tid & 31, q = (tid >> 5) + 8 * n;
+        if (places.page[i] >= 0)
+            store_codes<DP>(c.pages + places.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, places.at[i], q), &values[i][W * q]);
+    }
 }
 
 template <typename T, int DP>
 __global__ __launch_bounds__(256) void cache_read_kernel(cache_args c, T* k, int64_t ldk, T* v, int64_t ldv, bool aligned)
 {
-    constexpr int E = DP / 16;
-    const int64_t item = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int r = threadIdx.x & 15;
-    if (item >= (int64_t)c.num_tokens * c.kv_heads) return;
-    const int t = (int)(item / c.kv_heads), head = (int)(item - (int64_t)t * c.kv_heads);
-    const int s = sequence_of(c, t);
-    if (s < 0) return;
-    const cache_rows rows = rows_of(c, s);
-    if (t - rows.first >= min(rows.count, c.max_new)) return;
-    const int slot = slot_of(c, s, t);
-    const int page = slot < 0 ? 0 : slot / c.page_tokens, at = slot - page * c.page_tokens;
-    const int64_t id = slot < 0 ? -1 : page_of(c, s, page);
+    constexpr int E = DP / 16, W = (E + 7) / 8;
+    __shared__ tile_places places;
+    __shared__ uint32_t values[kTile][16 * W + 1];
+    const int tid = threadIdx.x, r = tid & 15, head = blockIdx.x % c.kv_heads, t0 = blockIdx.x / c.kv_heads * kTile;
     const int d0 = r * E, count = min(E, c.head_dim - d0);
-    const unsigned char* const base = c.pages + (max(id, (int64_t)0) * c.kv_heads + head) * c.page_bytes;
+    if (tid < 64) find_places(c, t0, head, tid, places);
+    __syncthreads();
+    uint32_t codes[2][2][W], words[2][2];                      // a page that is not there: zeros
 #pragma unroll
-    for (int part = 0; part < 2; ++part) {
-        float x[E];
+    for (int n = 0; n < 2; ++n) {
+        const int i = tid & 31, q = (tid >> 5) + 8 * n;
+        uint32_t u[W] = {};
+        if (places.page[i] >= 0) load_codes<DP>(c.pages + places.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, places.at[i], q), u);
 #pragma unroll
-        for (int i = 0; i < E; ++i) x[i] = 0.f;
-        if (id >= 0) {
-            uint32_t codes[(E + 7) / 8];
-            load_codes<DP>(base + (part ? value_offset<DP>(c.page_tokens, at, r) : key_offset<DP>(at, r)), codes);
-            const uint32_t word = *reinterpret_cast<const uint32_t*>(base + word_offset<DP>(c.page_tokens, at, part));
-            const float step = __uint_as_float(word << 16), zero = __uint_as_float(word & 0xffff0000u);
+        for (int w = 0; w < W; ++w) values[i][W * q + w] = u[w];
+    }
 #pragma unroll
-            for (int i = 0; i < E; ++i) x[i] = (float)(codes[i / 8] >> (4 * (i % 8)) & 15u) * step + zero;
+    for (int h = 0; h < 2; ++h) {
+        const int i = (tid >> 4) + 16 * h;
+        const int64_t page = places.page[i];
+        words[h][0] = words[h][1] = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) codes[h][0][w] = 0;
+        if (page < 0) continue;
+        const unsigned char* const base = c.pages + page * c.page_bytes;
+        load_codes<DP>(base + key_offset<DP>(places.at[i], r), codes[h][0]);
+#pragma unroll
+        for (int part = 0; part < 2; ++part) words[h][part] = *reinterpret_cast<const uint32_t*>(base + word_offset<DP>(c.page_tokens, places.at[i], part));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = (tid >> 4) + 16 * h;
+        if (!places.known[i]) continue;
+#pragma unroll
+        for (int w = 0; w < W; ++w) codes[h][1][w] = values[i][W * r + w];
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const float step = __uint_as_float(words[h][part] << 16), zero = __uint_as_float(words[h][part] & 0xffff0000u);
+            float x[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[e] = (float)(codes[h][part][e / 8] >> (4 * (e % 8)) & 15u) * step + zero;
+            T* const out = (part ? v + (int64_t)(t0 + i) * ldv : k + (int64_t)(t0 + i) * ldk) + head * c.head_dim + d0;
+            store_elems<T, E>(out, count, aligned, x);
         }
-        if (part) store_elems<T, E>(v + (int64_t)t * ldv + head * c.head_dim + d0, count, aligned, x);
-        else store_elems<T, E>(k + (int64_t)t * ldk + head * c.head_dim + d0, count, aligned, x);
     }
 }
 
@@ -187,7 +264,9 @@ bool rows_aligned(const void* k, int64_t ldk, const void* v, int64_t ldv, int32_
 // ---------------------------------------------------------------------------
 // Eviction, first step: a workgroup per sequence and head finds what is kept.  The weights as whole numbers in their order, NaN
 // above all; the budget-th largest of them by four passes over their bytes (a histogram of 256 bins each), then the slots in
-// order: above it, all; equal to it, the first few.
+// order: above it, all; equal to it, the first few.  The numbers stay in LDS where they fit (KEYS of them; else they are read
+// again in every pass).  Many weights share their first byte, the exponent's: a wavefront adds the four bins that its first lanes
+// name in one go each.
 __device__ __forceinline__ uint32_t order_of(float w)
 {
     if (w != w) return 0xffffffffu;
@@ -202,12 +281,12 @@ __device__ __forceinline__ uint32_t key_at(const cache_args& c, int s, int head,
     return id < 0 ? order_of(0.f) : order_of(c.weight[(id * c.kv_heads + head) * c.page_tokens + slot - page * c.page_tokens]);
 }
 
-constexpr int kSelectThreads = 1024;
-
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+template <int KEYS>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args c, int32_t* target_length, int budget, int recent, int32_t* kept)
 {
-    __shared__ int bins[256];
-    __shared__ int counts[2][kSelectThreads / 64];
+    __shared__ uint32_t keys[KEYS > 0 ? KEYS : 1];
+    __shared__ int bins[256], counts[2][kSelectWaves];
     __shared__ uint32_t found[2];                              // prefix so far, how many are still wanted of it
     const int s = blockIdx.x / c.kv_heads, head = blockIdx.x % c.kv_heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int length = length_of(c, s);
@@ -218,81 +297,132 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
         return;
     }
     const int old = length - recent, wanted = budget - recent; // (wanted < old)
-    uint32_t threshold = 0xffffffffu;
-    int ties = 0;                                              // of the slots at the threshold, the first so many
-    if (wanted > 0) {
-        if (tid == 0) { found[0] = 0; found[1] = (uint32_t)wanted; }
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < 256; i += kSelectThreads) bins[i] = 0;
-            __syncthreads();
-            const uint32_t prefix = found[0], still = found[1];
-            for (int i = tid; i < old; i += kSelectThreads) {
-                const uint32_t key = key_at(c, s, head, i);
-                if (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8)) atomicAdd(&bins[key >> shift & 255u], 1);
+    for (int i = tid; i < recent; i += kSelectThreads) out[wanted + i] = old + i;
+    if (wanted == 0) return;
+    if constexpr (KEYS > 0)                                    // (the launch sees to it that old <= KEYS)
+#pragma unroll 8
+        for (int i = tid; i < old; i += kSelectThreads) keys[i] = key_at(c, s, head, i);
+    auto key_of = [&](int i) -> uint32_t {
+        if constexpr (KEYS > 0) return keys[i];
+        else return key_at(c, s, head, i);
+    };
+    if (tid == 0) { found[0] = 0; found[1] = (uint32_t)wanted; }
+    const int steps = (old + kSelectThreads - 1) / kSelectThreads;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) bins[tid] = 0;
+        __syncthreads();
+        const uint32_t prefix = found[0], still = found[1];
+        for (int n = 0; n < steps; ++n) {
+            const int i = n * kSelectThreads + tid;
+            const uint32_t key = i < old ? key_of(i) : 0u;
+            bool on = i < old && (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8));
+            const uint32_t bin = key >> shift & 255u;
+#pragma unroll
+            for (int round = 0; round < 4; ++round) {
+                const uint64_t left = __ballot(on);
+                if (!left) break;
+                const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)bin, __ffsll((unsigned long long)left) - 1);
+                const uint64_t same = __ballot(on && bin == first);
+                if (lane == 0) atomicAdd(&bins[first], __popcll(same));
+                on = on && bin != first;
             }
-            __syncthreads();
-            if (tid == 0) {
-                uint32_t left = still;
-                int b = 255;
-                while (b > 0 && (uint32_t)bins[b] < left) left -= (uint32_t)bins[b--];
-                found[0] = prefix | (uint32_t)b << shift;
+            if (on) atomicAdd(&bins[bin], 1);
+        }
+        __syncthreads();
+        if (wave == 0) {                                       // from the highest bin down, four bins a lane
+            int mine[4], sum = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += mine[e] = bins[255 - 4 * lane - e];
+            int up = sum;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const int x = __shfl_up(up, off, 64);
+                if (lane >= off) up += x;
+            }
+            if (lane == __ffsll((unsigned long long)__ballot((uint32_t)up >= still)) - 1) {
+                uint32_t left = still - (uint32_t)(up - sum);
+                int e = 0;
+                while (e < 3 && (uint32_t)mine[e] < left) left -= (uint32_t)mine[e++];
+                found[0] = prefix | (uint32_t)(255 - 4 * lane - e) << shift;
                 found[1] = left;
             }
-            __syncthreads();
         }
-        threshold = found[0];
-        ties = (int)found[1];
-    }
-    int above = 0, equal = 0;                                  // of all slots before the step's
-    for (int i0 = 0; i0 < old && wanted > 0; i0 += kSelectThreads) {
-        const int i = i0 + tid;
-        const uint32_t key = i < old ? key_at(c, s, head, i) : 0u;
-        const bool is_above = i < old && key > threshold, is_equal = i < old && key == threshold;
-        const uint64_t ma = __ballot(is_above), me = __ballot(is_equal), below = ((uint64_t)1 << lane) - 1;
-        __syncthreads();                                       // (the counts of the step before are read)
-        if (lane == 0) { counts[0][wave] = __popcll(ma); counts[1][wave] = __popcll(me); }
         __syncthreads();
-        int a = above + __popcll(ma & below), e = equal + __popcll(me & below);
-        for (int w = 0; w < kSelectThreads / 64; ++w) {
-            if (w < wave) { a += counts[0][w]; e += counts[1][w]; }
-            above += counts[0][w];
-            equal += counts[1][w];
-        }
-        if (is_above || (is_equal && e < ties)) out[a + min(e, ties)] = i;
     }
-    for (int i = tid; i < recent; i += kSelectThreads) out[wanted + i] = old + i;
+    const uint32_t threshold = found[0];
+    const int ties = (int)found[1];                            // of the slots at the threshold, the first so many
+    // A run of slots to a wavefront: it counts, then writes behind what the wavefronts before it have counted.
+    const int run = (old + kSelectThreads - 1) / kSelectThreads * 64, begin = wave * run, end = min(old, begin + run);
+    int above = 0, equal = 0;
+    for (int i0 = begin; i0 < end; i0 += 64) {
+        const uint32_t key = i0 + lane < end ? key_of(i0 + lane) : 0u;
+        above += __popcll(__ballot(i0 + lane < end && key > threshold));
+        equal += __popcll(__ballot(i0 + lane < end && key == threshold));
+    }
+    if (lane == 0) { counts[0][wave] = above; counts[1][wave] = equal; }
+    __syncthreads();
+    above = equal = 0;
+    for (int w = 0; w < wave; ++w) { above += counts[0][w]; equal += counts[1][w]; }
+    const uint64_t below = ((uint64_t)1 << lane) - 1;
+    for (int i0 = begin; i0 < end; i0 += 64) {
+        const int i = i0 + lane;
+        const uint32_t key = i < end ? key_of(i) : 0u;
+        const bool is_above = i < end && key > threshold, is_equal = i < end && key == threshold;
+        const uint64_t ma = __ballot(is_above), me = __ballot(is_equal);
+        const int a = above + __popcll(ma & below), e = equal + __popcll(me & below);
+        if (is_above || (is_equal && e < ties)) out[a + min(e, ties)] = i;
+        above += __popcll(ma);
+        equal += __popcll(me);
+    }
 }
 
-// Second step: the kept tokens' codes, words and weights, 16 lanes a token of a head.
+// Second step: the kept tokens' codes, words and weights, a workgroup 32 of them of a head.
 template <int DP>
-__global__ __launch_bounds__(256) void cache_move_kernel(cache_args c, cache_args to, int budget, const int32_t* kept)
+__global__ __launch_bounds__(256) void cache_move_kernel(cache_args c, cache_args to, int budget, int tiles, const int32_t* kept)
 {
-    constexpr int E = DP / 16;
-    const int64_t item = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-    const int r = threadIdx.x & 15;
-    if (item >= (int64_t)c.num_seqs * c.kv_heads * budget) return;
-    const int64_t group = item / budget;
-    const int j = (int)(item - group * budget), s = (int)(group / c.kv_heads), head = (int)(group - (int64_t)s * c.kv_heads);
-    const int slot = kept[item];
-    if (slot < 0 || slot >= c.max_length) return;
-    const int page = slot / c.page_tokens, at = slot - page * c.page_tokens, new_page = j / to.page_tokens, new_at = j - new_page * to.page_tokens;
-    const int64_t id = page_of(c, s, page), new_id = page_of(to, s, new_page);
-    if (new_id < 0) return;
-    unsigned char* const dst = to.pages + (new_id * c.kv_heads + head) * c.page_bytes;
-    const unsigned char* const src = c.pages + (max(id, (int64_t)0) * c.kv_heads + head) * c.page_bytes;
-    uint32_t k[(E + 7) / 8] = {}, v[(E + 7) / 8] = {};         // (a page that is not there reads as zeros)
-    if (id >= 0) {
-        load_codes<DP>(src + key_offset<DP>(at, r), k);
-        load_codes<DP>(src + value_offset<DP>(c.page_tokens, at, r), v);
+    constexpr int E = DP / 16, W = (E + 7) / 8;
+    __shared__ tile_places from, where;
+    const int tid = threadIdx.x, r = tid & 15;
+    const int64_t group = blockIdx.x / tiles;                  // sequence and head
+    const int j0 = (int)(blockIdx.x - group * tiles) * kTile, s = (int)(group / c.kv_heads), head = (int)(group - (int64_t)s * c.kv_heads);
+    if (tid < kTile) {
+        const int j = j0 + tid, slot = j < budget ? kept[group * budget + j] : -1;
+        int64_t src = -1, dst = -1;
+        int at = 0;
+        if (slot >= 0 && slot < c.max_length) {
+            const int number = slot / c.page_tokens, there = j / c.page_tokens;
+            at = slot - number * c.page_tokens;
+            src = page_of(c, s, number);
+            dst = page_of(to, s, there);
+            where.at[tid] = j - there * c.page_tokens;
+        }
+        from.page[tid] = src < 0 ? -1 : src * c.kv_heads + head;
+        from.at[tid] = at;
+        where.page[tid] = dst < 0 ? -1 : dst * c.kv_heads + head;
     }
-    store_codes<DP>(dst + key_offset<DP>(new_at, r), k);
-    store_codes<DP>(dst + value_offset<DP>(c.page_tokens, new_at, r), v);
-    if (r < 2)
-        *reinterpret_cast<uint32_t*>(dst + word_offset<DP>(c.page_tokens, new_at, r)) =
-            id < 0 ? 0u : *reinterpret_cast<const uint32_t*>(src + word_offset<DP>(c.page_tokens, at, r));
-    if (r == 2)
-        to.weight[(new_id * c.kv_heads + head) * c.page_tokens + new_at] =
-            id < 0 ? 0.f : c.weight[(id * c.kv_heads + head) * c.page_tokens + at];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int i = tid & 31, q = (tid >> 5) + 8 * n;
+        uint32_t u[W] = {};                                    // (a page that is not there reads as zeros)
+        if (from.page[i] >= 0) load_codes<DP>(c.pages + from.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, from.at[i], q), u);
+        if (where.page[i] >= 0) store_codes<DP>(to.pages + where.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, where.at[i], q), u);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int i = (tid >> 4) + 16 * h;
+        if (where.page[i] < 0) continue;
+        const bool there = from.page[i] >= 0;
+        const unsigned char* const src = c.pages + max(from.page[i], (int64_t)0) * c.page_bytes;
+        unsigned char* const dst = to.pages + where.page[i] * c.page_bytes;
+        uint32_t u[W] = {};
+        if (there) load_codes<DP>(src + key_offset<DP>(from.at[i], r), u);
+        store_codes<DP>(dst + key_offset<DP>(where.at[i], r), u);
+        if (r < 2)
+            *reinterpret_cast<uint32_t*>(dst + word_offset<DP>(c.page_tokens, where.at[i], r)) =
+                there ? *reinterpret_cast<const uint32_t*>(src + word_offset<DP>(c.page_tokens, from.at[i], r)) : 0u;
+        if (r == 2) to.weight[where.page[i] * c.page_tokens + where.at[i]] = there ? c.weight[from.page[i] * c.page_tokens + from.at[i]] : 0.f;
+    }
 }
 
 #define BY_HEAD_DIM(KERNEL, ...)                                                              \
@@ -301,12 +431,12 @@ __global__ __launch_bounds__(256) void cache_move_kernel(cache_args c, cache_arg
         case 128: KERNEL(128, __VA_ARGS__); break;                                            \
         default: KERNEL(256, __VA_ARGS__);                                                    \
     }
-dim3 groups_of_16(int64_t items) { return dim3((uint32_t)((items + 15) / 16)); }
+int32_t tiles_of(int32_t tokens) { return (tokens + kTile - 1) / kTile; }
 }  // namespace
 
 hipError_t launch_cache_append(const cache_args& c, int32_t dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, hipStream_t stream)
 {
-    const dim3 grid = groups_of_16((int64_t)c.num_tokens * c.kv_heads);
+    const dim3 grid((uint32_t)(tiles_of(c.num_tokens) * c.kv_heads));
     const bool aligned = rows_aligned(k, ldk, v, ldv, c.head_dim, dtype);
 #define APPEND(DP, T) LORA_LAUNCH(LORA_K_CACHE_APPEND, (cache_append_kernel<T, DP>), grid, dim3(256), 0, stream, c, static_cast<const T*>(k), ldk, static_cast<const T*>(v), ldv, aligned)
     if (dtype == LORA_F32) { BY_HEAD_DIM(APPEND, float) }
@@ -316,7 +446,7 @@ hipError_t launch_cache_append(const cache_args& c, int32_t dtype, const void* k
 
 hipError_t launch_cache_read(const cache_args& c, int32_t dtype, void* k, int64_t ldk, void* v, int64_t ldv, hipStream_t stream)
 {
-    const dim3 grid = groups_of_16((int64_t)c.num_tokens * c.kv_heads);
+    const dim3 grid((uint32_t)(tiles_of(c.num_tokens) * c.kv_heads));
     const bool aligned = rows_aligned(k, ldk, v, ldv, c.head_dim, dtype);
 #define READ(DP, T) LORA_LAUNCH(LORA_K_CACHE_READ, (cache_read_kernel<T, DP>), grid, dim3(256), 0, stream, c, static_cast<T*>(k), ldk, static_cast<T*>(v), ldv, aligned)
     if (dtype == LORA_F32) { BY_HEAD_DIM(READ, float) }
@@ -327,12 +457,18 @@ hipError_t launch_cache_read(const cache_args& c, int32_t dtype, void* k, int64_
 hipError_t launch_cache_evict(const cache_args& c, const cache_args& to, int32_t* target_length, int32_t budget, int32_t recent, int32_t* kept,
                               hipStream_t stream)
 {
-    LORA_LAUNCH(LORA_K_CACHE_SELECT, cache_select_kernel, dim3((uint32_t)(c.num_seqs * c.kv_heads)), dim3(kSelectThreads), 0, stream, c, target_length, budget,
-                recent, kept);
+    // (in LDS: 4096 weights a workgroup and two workgroups a compute unit, or 32768 and one)
+    const dim3 grid1((uint32_t)(c.num_seqs * c.kv_heads));
+    const int32_t old = c.max_length - recent;
+#define SELECT(KEYS) LORA_LAUNCH(LORA_K_CACHE_SELECT, (cache_select_kernel<KEYS>), grid1, dim3(kSelectThreads), 0, stream, c, target_length, budget, recent, kept)
+    if (old <= 4096) SELECT(4096);
+    else if (old <= 32768) SELECT(32768);
+    else SELECT(0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || budget == 0) return e;
-    const dim3 grid = groups_of_16((int64_t)c.num_seqs * c.kv_heads * budget);
-#define MOVE(DP, UNUSED) LORA_LAUNCH(LORA_K_CACHE_MOVE, (cache_move_kernel<DP>), grid, dim3(256), 0, stream, c, to, budget, kept)
+    const int32_t tiles = tiles_of(budget);
+    const dim3 grid((uint32_t)(c.num_seqs * c.kv_heads * tiles));
+#define MOVE(DP, UNUSED) LORA_LAUNCH(LORA_K_CACHE_MOVE, (cache_move_kernel<DP>), grid, dim3(256), 0, stream, c, to, budget, tiles, kept)
     BY_HEAD_DIM(MOVE, )
     return hipGetLastError();
 }
