@@ -17,6 +17,12 @@ __device__ __forceinline__ cache_rows rows_of(const cache_args& c, int s)
 
 __device__ __forceinline__ int length_of(const cache_args& c, int s) { return min(max(c.length[s], 0), c.max_length); }
 
+// the page that a slot is in (pages are mostly powers of two)
+__device__ __forceinline__ int page_number(const cache_args& c, int slot)
+{
+    return (c.page_tokens & (c.page_tokens - 1)) == 0 ? slot >> __builtin_ctz(c.page_tokens) : slot / c.page_tokens;
+}
+
 // page number `page` of sequence s in the pool, or -1.  page < table_stride: slots are below max_length
 __device__ __forceinline__ int64_t page_of(const cache_args& c, int s, int page)
 {

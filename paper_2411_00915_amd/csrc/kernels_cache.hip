@@ -36,39 +36,47 @@ __device__ __forceinline__ int search_indptr(const cache_args& c, int t, int lan
     return lo;
 }
 
-// Places of rows t0 ... in a wavefront (lanes 0 .. 31 a row each)
+// Places of rows t0 ... by a wavefront (lanes 0 .. 31 a row each).  The trips to memory are what it takes: one for a window of
+// 63 sequences' offsets and lengths (two more to find the window where there are many), one for the pages.
 __device__ __forceinline__ void find_places(const cache_args& c, int t0, int head, int lane, tile_places& p)
 {
-    const int t = t0 + lane;
+    const int t = t0 + lane, S = c.num_seqs;
     const bool mine = lane < kTile && t < c.num_tokens;
-    int s = -1;
-    if (!c.indptr) s = mine && t < c.num_seqs ? t : -1;
-    else {
-        // the first row's sequence, then the ends of 64 sequences at a time, of which each row counts those it is behind
-        int base = search_indptr(c, t0, lane);
-        if (mine) s = base;
-        for (;; base += 64) {
-            const int end = base + 1 + lane < c.num_seqs ? c.indptr[base + 1 + lane] : INT_MAX;
-            int behind = 0;
+    int s = -1, first = t, next = t + 1, length = 0;
+    if (!c.indptr) {
+        if (mine && t < S) {
+            s = t;
+            length = c.length[t];
+        }
+    } else {
+        bool pending = mine;
+        for (int base = S < 64 ? 0 : search_indptr(c, t0, lane);; base += 63) {
+            const int starts = base + lane <= S ? c.indptr[base + lane] : INT_MAX, held = c.length[min(base + lane, S - 1)];
+            int j = 0;                                         // starts are in order: of lanes 1 .. 63, how many are not behind t
 #pragma unroll
-            for (int step = 32; step > 0; step >>= 1)          // ends are in order
-                if (__shfl(end, behind + step - 1, 64) <= t) behind += step;
-            behind += __shfl(end, 63, 64) <= t && behind == 63 ? 1 : 0;
-            const bool on = mine && s == base && behind == 64;
-            if (mine && s == base) s = base + behind;
-            if (!__ballot(on)) break;
+            for (int step = 32; step > 0; step >>= 1)
+                if (__shfl(starts, min(j + step, 63), 64) <= t) j += step;
+            const int a = __shfl(starts, j, 64), b = __shfl(starts, min(j + 1, 63), 64), n = __shfl(held, j, 64);
+            if (pending && j < 63) {
+                s = base + j;
+                first = a;
+                next = b;
+                length = n;
+                pending = false;
+            }
+            if (!__ballot(pending) || base + 63 > S) break;
         }
     }
     if (lane >= kTile) return;
     int64_t page = -1;
     int at = 0, known = 0;
-    if (s >= 0 && s < c.num_seqs) {
-        const cache_rows rows = rows_of(c, s);
-        const int i = t - rows.first;
-        known = i >= 0 && i < min(rows.count, c.max_new);
-        const int slot = known ? length_of(c, s) - rows.count + i : -1;
+    if (s >= 0 && s < S) {
+        first = min(max(first, 0), c.num_tokens);              // (as rows_of and length_of)
+        const int count = min(max(next, first), c.num_tokens) - first, i = t - first;
+        known = i >= 0 && i < min(count, c.max_new);
+        const int slot = known ? min(max(length, 0), c.max_length) - count + i : -1;
         if (slot >= 0) {
-            const int number = slot / c.page_tokens;
+            const int number = page_number(c, slot);
             at = slot - number * c.page_tokens;
             page = page_of(c, s, number);
             if (page >= 0) page = page * c.kv_heads + head;
@@ -128,39 +136,41 @@ __device__ __forceinline__ void store_elems(T* p, int count, bool aligned, const
 template <int E>
 __device__ __forceinline__ uint32_t quantise(const float* x, int count, uint32_t* codes)
 {
-    float lo = INFINITY, hi = -INFINITY;
-    bool bad = false;
+    float lo = INFINITY, hi = -INFINITY, wild = 0.f;           // wild: NaN where an element is not finite
 #pragma unroll
     for (int i = 0; i < E; ++i)
         if (i < count) {
             lo = fminf(lo, x[i]);
             hi = fmaxf(hi, x[i]);
-            bad |= !(fabsf(x[i]) < INFINITY);
+            wild = __builtin_fmaf(x[i], 0.f, wild);
         }
-    int any = bad;
 #pragma unroll
     for (int off = 8; off > 0; off >>= 1) {
         lo = fminf(lo, __shfl_xor(lo, off, 16));
         hi = fmaxf(hi, __shfl_xor(hi, off, 16));
-        any |= __shfl_xor(any, off, 16);
+        wild += __shfl_xor(wild, off, 16);
     }
     uint32_t z = __float_as_uint(lo);                          // rounded down to bf16
     z = (z & 0xffff0000u) + ((z >> 31) && (z & 0xffffu) ? 0x10000u : 0u);
     const float zero = __uint_as_float(z), range = hi - zero;
     float step = bf16_to_f32(f32_to_bf16(range * (1.f / 15.f)));
     if (step < 0x1p-100f) step = 0.f;
-    any |= !(fabsf(zero) < INFINITY) || !(range < INFINITY);
+    const bool bad = wild != 0.f || !(fabsf(zero) < INFINITY) || !(range < INFINITY);
+    // (x - zero) / step, rounded as a division is: with the reciprocal rounded to nearest, one step of Newton's on the quotient
+    // gives the nearest one (Markstein); step is a bf16 of 2^-100 and more, so nothing on the way is lost below the normal numbers
+    const float inverse = 1.f / step;
+    const bool none = step == 0.f || bad;
 #pragma unroll
     for (int w = 0; w < (E + 7) / 8; ++w) {
         uint32_t u = 0;
 #pragma unroll
         for (int i = 0; i < (E < 8 ? E : 8); ++i) {
-            const float c = fminf(fmaxf(rintf((x[8 * w + i] - zero) / step), 0.f), 15.f);
-            u |= (8 * w + i < count && step > 0.f && !any ? (uint32_t)c : 0u) << (4 * i);
+            const float d = x[8 * w + i] - zero, q0 = d * inverse, q = __builtin_fmaf(__builtin_fmaf(-q0, step, d), inverse, q0);
+            u |= (8 * w + i < count ? (uint32_t)__builtin_amdgcn_fmed3f(rintf(q), 0.f, 15.f) : 0u) << (4 * i);
         }
-        codes[w] = u;
+        codes[w] = none ? 0u : u;
     }
-    return any ? 0x7fc07fc0u : (z | __float_as_uint(step) >> 16);
+    return bad ? 0x7fc07fc0u : (z | __float_as_uint(step) >> 16);
 }
 
 template <typename T, int DP>
@@ -264,9 +274,9 @@ bool rows_aligned(const void* k, int64_t ldk, const void* v, int64_t ldv, int32_
 // ---------------------------------------------------------------------------
 // Eviction, first step: a workgroup per sequence and head finds what is kept.  The weights as whole numbers in their order, NaN
 // above all; the budget-th largest of them by four passes over their bytes (a histogram of 256 bins each), then the slots in
-// order: above it, all; equal to it, the first few.  The numbers stay in LDS where they fit (KEYS of them; else they are read
-// again in every pass).  Many weights share their first byte, the exponent's: a wavefront adds the four bins that its first lanes
-// name in one go each.
+// order: above it, all; equal to it, the first few.  A thread keeps its numbers in registers, STEPS of them (0: they are read
+// again in every pass).  Many weights share their first byte, the exponent's: a wavefront adds the four bins that its first
+// lanes name in one go each.
 __device__ __forceinline__ uint32_t order_of(float w)
 {
     if (w != w) return 0xffffffffu;
@@ -276,17 +286,17 @@ __device__ __forceinline__ uint32_t order_of(float w)
 
 __device__ __forceinline__ uint32_t key_at(const cache_args& c, int s, int head, int slot)
 {
-    const int page = slot / c.page_tokens;
+    const int page = page_number(c, slot);
     const int64_t id = page_of(c, s, page);
     return id < 0 ? order_of(0.f) : order_of(c.weight[(id * c.kv_heads + head) * c.page_tokens + slot - page * c.page_tokens]);
 }
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
-template <int KEYS>
+template <int STEPS>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args c, int32_t* target_length, int budget, int recent, int32_t* kept)
 {
-    __shared__ uint32_t keys[KEYS > 0 ? KEYS : 1];
-    __shared__ int bins[256], counts[2][kSelectWaves];
+    constexpr int COUNTS = (STEPS > 0 ? STEPS : 1) * kSelectWaves;
+    __shared__ int bins[256], counts[2][COUNTS];
     __shared__ uint32_t found[2];                              // prefix so far, how many are still wanted of it
     const int s = blockIdx.x / c.kv_heads, head = blockIdx.x % c.kv_heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int length = length_of(c, s);
@@ -299,35 +309,40 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
     const int old = length - recent, wanted = budget - recent; // (wanted < old)
     for (int i = tid; i < recent; i += kSelectThreads) out[wanted + i] = old + i;
     if (wanted == 0) return;
-    if constexpr (KEYS > 0)                                    // (the launch sees to it that old <= KEYS)
-#pragma unroll 8
-        for (int i = tid; i < old; i += kSelectThreads) keys[i] = key_at(c, s, head, i);
-    auto key_of = [&](int i) -> uint32_t {
-        if constexpr (KEYS > 0) return keys[i];
-        else return key_at(c, s, head, i);
+    uint32_t keys[STEPS > 0 ? STEPS : 1];                      // slots tid, tid + 1024 ...  (the launch sees to it that they are enough)
+    if constexpr (STEPS > 0)
+#pragma unroll
+        for (int n = 0; n < STEPS; ++n) keys[n] = n * kSelectThreads + tid < old ? key_at(c, s, head, n * kSelectThreads + tid) : 0u;
+    const int steps = (old + kSelectThreads - 1) / kSelectThreads;
+    // f(step, slot, key), slots of a step in the order of the threads
+    auto each = [&](auto f) {
+        if constexpr (STEPS > 0) {
+#pragma unroll
+            for (int n = 0; n < STEPS; ++n)
+                if (n < steps) f(n, n * kSelectThreads + tid, keys[n]);
+        } else
+            for (int n = 0; n < steps; ++n) f(n, n * kSelectThreads + tid, n * kSelectThreads + tid < old ? key_at(c, s, head, n * kSelectThreads + tid) : 0u);
     };
     if (tid == 0) { found[0] = 0; found[1] = (uint32_t)wanted; }
-    const int steps = (old + kSelectThreads - 1) / kSelectThreads;
+#pragma unroll 1
     for (int shift = 24; shift >= 0; shift -= 8) {
         if (tid < 256) bins[tid] = 0;
         __syncthreads();
         const uint32_t prefix = found[0], still = found[1];
-        for (int n = 0; n < steps; ++n) {
-            const int i = n * kSelectThreads + tid;
-            const uint32_t key = i < old ? key_of(i) : 0u;
+        each([&](int, int i, uint32_t key) {
             bool on = i < old && (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8));
             const uint32_t bin = key >> shift & 255u;
-#pragma unroll
-            for (int round = 0; round < 4; ++round) {
+#pragma unroll 1
+            for (int round = shift == 24 ? 4 : 1; round > 0; --round) {
                 const uint64_t left = __ballot(on);
-                if (!left) break;
+                if (!left) return;
                 const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)bin, __ffsll((unsigned long long)left) - 1);
                 const uint64_t same = __ballot(on && bin == first);
                 if (lane == 0) atomicAdd(&bins[first], __popcll(same));
                 on = on && bin != first;
             }
             if (on) atomicAdd(&bins[bin], 1);
-        }
+        });
         __syncthreads();
         if (wave == 0) {                                       // from the highest bin down, four bins a lane
             int mine[4], sum = 0;
@@ -351,28 +366,49 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
     }
     const uint32_t threshold = found[0];
     const int ties = (int)found[1];                            // of the slots at the threshold, the first so many
-    // A run of slots to a wavefront: it counts, then writes behind what the wavefronts before it have counted.
-    const int run = (old + kSelectThreads - 1) / kSelectThreads * 64, begin = wave * run, end = min(old, begin + run);
-    int above = 0, equal = 0;
-    for (int i0 = begin; i0 < end; i0 += 64) {
-        const uint32_t key = i0 + lane < end ? key_of(i0 + lane) : 0u;
-        above += __popcll(__ballot(i0 + lane < end && key > threshold));
-        equal += __popcll(__ballot(i0 + lane < end && key == threshold));
-    }
-    if (lane == 0) { counts[0][wave] = above; counts[1][wave] = equal; }
-    __syncthreads();
-    above = equal = 0;
-    for (int w = 0; w < wave; ++w) { above += counts[0][w]; equal += counts[1][w]; }
     const uint64_t below = ((uint64_t)1 << lane) - 1;
-    for (int i0 = begin; i0 < end; i0 += 64) {
-        const int i = i0 + lane;
-        const uint32_t key = i < end ? key_of(i) : 0u;
-        const bool is_above = i < end && key > threshold, is_equal = i < end && key == threshold;
-        const uint64_t ma = __ballot(is_above), me = __ballot(is_equal);
-        const int a = above + __popcll(ma & below), e = equal + __popcll(me & below);
+    auto put = [&](int i, uint32_t key, int above, int equal) { // above, equal: how many such come before this wavefront's
+        const bool is_above = i < old && key > threshold, is_equal = i < old && key == threshold;
+        const int a = above + __popcll(__ballot(is_above) & below), e = equal + __popcll(__ballot(is_equal) & below);
         if (is_above || (is_equal && e < ties)) out[a + min(e, ties)] = i;
-        above += __popcll(ma);
-        equal += __popcll(me);
+    };
+    auto count = [&](int n, int i, uint32_t key) {
+        const int a = __popcll(__ballot(i < old && key > threshold)), e = __popcll(__ballot(i < old && key == threshold));
+        if (lane == 0) { counts[0][n * kSelectWaves + wave] = a; counts[1][n * kSelectWaves + wave] = e; }
+    };
+    if constexpr (STEPS > 0) {
+        each(count);
+        __syncthreads();
+        if (wave < 2) {                                        // sums over what comes before, in the order of the slots
+            int before = 0;
+            for (int i0 = 0; i0 < steps * kSelectWaves; i0 += 64) {
+                const int mine = i0 + lane < steps * kSelectWaves ? counts[wave][i0 + lane] : 0;
+                int up = mine;
+#pragma unroll
+                for (int off = 1; off < 64; off <<= 1) {
+                    const int x = __shfl_up(up, off, 64);
+                    if (lane >= off) up += x;
+                }
+                if (i0 + lane < steps * kSelectWaves) counts[wave][i0 + lane] = before + up - mine;
+                before += __shfl(up, 63, 64);
+            }
+        }
+        __syncthreads();
+        each([&](int n, int i, uint32_t key) { put(i, key, counts[0][n * kSelectWaves + wave], counts[1][n * kSelectWaves + wave]); });
+    } else {
+        int above = 0, equal = 0;
+        each([&](int, int i, uint32_t key) {
+            __syncthreads();                                   // (the counts of the step before are read)
+            count(0, i, key);
+            __syncthreads();
+            int a = 0, e = 0;
+            for (int w = 0; w < kSelectWaves; ++w) {
+                if (w == wave) { a = above; e = equal; }
+                above += counts[0][w];
+                equal += counts[1][w];
+            }
+            put(i, key, a, e);
+        });
     }
 }
 
@@ -390,7 +426,7 @@ __global__ __launch_bounds__(256) void cache_move_kernel(cache_args c, cache_arg
         int64_t src = -1, dst = -1;
         int at = 0;
         if (slot >= 0 && slot < c.max_length) {
-            const int number = slot / c.page_tokens, there = j / c.page_tokens;
+            const int number = page_number(c, slot), there = page_number(c, j);
             at = slot - number * c.page_tokens;
             src = page_of(c, s, number);
             dst = page_of(to, s, there);
@@ -401,27 +437,29 @@ __global__ __launch_bounds__(256) void cache_move_kernel(cache_args c, cache_arg
         where.page[tid] = dst < 0 ? -1 : dst * c.kv_heads + head;
     }
     __syncthreads();
+    uint32_t v[2][W], k[2][W], words[2];                       // (a page that is not there reads as zeros)
+    float weight[2];
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-        const int i = tid & 31, q = (tid >> 5) + 8 * n;
-        uint32_t u[W] = {};                                    // (a page that is not there reads as zeros)
-        if (from.page[i] >= 0) load_codes<DP>(c.pages + from.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, from.at[i], q), u);
-        if (where.page[i] >= 0) store_codes<DP>(to.pages + where.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, where.at[i], q), u);
+    for (int h = 0; h < 2; ++h) {
+        const int i = tid & 31, q = (tid >> 5) + 8 * h, j = (tid >> 4) + 16 * h;
+        const bool there = from.page[j] >= 0;
+        const unsigned char* const src = c.pages + max(from.page[j], (int64_t)0) * c.page_bytes;
+#pragma unroll
+        for (int w = 0; w < W; ++w) v[h][w] = k[h][w] = 0;
+        if (from.page[i] >= 0) load_codes<DP>(c.pages + from.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, from.at[i], q), v[h]);
+        if (there) load_codes<DP>(src + key_offset<DP>(from.at[j], r), k[h]);
+        words[h] = there && r < 2 ? *reinterpret_cast<const uint32_t*>(src + word_offset<DP>(c.page_tokens, from.at[j], r & 1)) : 0u;
+        weight[h] = there && r == 2 ? c.weight[from.page[j] * c.page_tokens + from.at[j]] : 0.f;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int i = (tid >> 4) + 16 * h;
-        if (where.page[i] < 0) continue;
-        const bool there = from.page[i] >= 0;
-        const unsigned char* const src = c.pages + max(from.page[i], (int64_t)0) * c.page_bytes;
-        unsigned char* const dst = to.pages + where.page[i] * c.page_bytes;
-        uint32_t u[W] = {};
-        if (there) load_codes<DP>(src + key_offset<DP>(from.at[i], r), u);
-        store_codes<DP>(dst + key_offset<DP>(where.at[i], r), u);
-        if (r < 2)
-            *reinterpret_cast<uint32_t*>(dst + word_offset<DP>(c.page_tokens, where.at[i], r)) =
-                there ? *reinterpret_cast<const uint32_t*>(src + word_offset<DP>(c.page_tokens, from.at[i], r)) : 0u;
-        if (r == 2) to.weight[where.page[i] * c.page_tokens + where.at[i]] = there ? c.weight[from.page[i] * c.page_tokens + from.at[i]] : 0.f;
+        const int i = tid & 31, q = (tid >> 5) + 8 * h, j = (tid >> 4) + 16 * h;
+        if (where.page[i] >= 0) store_codes<DP>(to.pages + where.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, where.at[i], q), v[h]);
+        if (where.page[j] < 0) continue;
+        unsigned char* const dst = to.pages + where.page[j] * c.page_bytes;
+        store_codes<DP>(dst + key_offset<DP>(where.at[j], r), k[h]);
+        if (r < 2) *reinterpret_cast<uint32_t*>(dst + word_offset<DP>(c.page_tokens, where.at[j], r)) = words[h];
+        if (r == 2) to.weight[where.page[j] * c.page_tokens + where.at[j]] = weight[h];
     }
 }
 
@@ -457,12 +495,11 @@ hipError_t launch_cache_read(const cache_args& c, int32_t dtype, void* k, int64_
 hipError_t launch_cache_evict(const cache_args& c, const cache_args& to, int32_t* target_length, int32_t budget, int32_t recent, int32_t* kept,
                               hipStream_t stream)
 {
-    // (in LDS: 4096 weights a workgroup and two workgroups a compute unit, or 32768 and one)
     const dim3 grid1((uint32_t)(c.num_seqs * c.kv_heads));
     const int32_t old = c.max_length - recent;
-#define SELECT(KEYS) LORA_LAUNCH(LORA_K_CACHE_SELECT, (cache_select_kernel<KEYS>), grid1, dim3(kSelectThreads), 0, stream, c, target_length, budget, recent, kept)
-    if (old <= 4096) SELECT(4096);
-    else if (old <= 32768) SELECT(32768);
+#define SELECT(STEPS) LORA_LAUNCH(LORA_K_CACHE_SELECT, (cache_select_kernel<STEPS>), grid1, dim3(kSelectThreads), 0, stream, c, target_length, budget, recent, kept)
+    if (old <= 4 * kSelectThreads) SELECT(4);
+    else if (old <= 32 * kSelectThreads) SELECT(32);
     else SELECT(0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || budget == 0) return e;
