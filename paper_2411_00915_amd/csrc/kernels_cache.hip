@@ -273,10 +273,10 @@ bool rows_aligned(const void* k, int64_t ldk, const void* v, int64_t ldv, int32_
 
 // ---------------------------------------------------------------------------
 // Eviction, first step: a workgroup per sequence and head finds what is kept.  The weights as whole numbers in their order, NaN
-// above all; the budget-th largest of them by four passes over their bytes (a histogram of 256 bins each), then the slots in
+// above all; the budget-th largest of them by three passes over their bits (histograms of 11, 11 and 10), then the slots in
 // order: above it, all; equal to it, the first few.  A thread keeps its numbers in registers, STEPS of them (0: they are read
-// again in every pass).  Many weights share their first byte, the exponent's: a wavefront adds the four bins that its first
-// lanes name in one go each.
+// again in every pass).  Many weights share their first bits, the exponent's: a wavefront adds those of its first lane's bin in
+// one go.
 __device__ __forceinline__ uint32_t order_of(float w)
 {
     if (w != w) return 0xffffffffu;
@@ -296,7 +296,7 @@ template <int STEPS>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args c, int32_t* target_length, int budget, int recent, int32_t* kept)
 {
     constexpr int COUNTS = (STEPS > 0 ? STEPS : 1) * kSelectWaves;
-    __shared__ int bins[256], counts[2][COUNTS];
+    __shared__ int bins[2 * kSelectThreads], totals[kSelectWaves], counts[2][COUNTS];
     __shared__ uint32_t found[2];                              // prefix so far, how many are still wanted of it
     const int s = blockIdx.x / c.kv_heads, head = blockIdx.x % c.kv_heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int length = length_of(c, s);
@@ -325,42 +325,42 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
     };
     if (tid == 0) { found[0] = 0; found[1] = (uint32_t)wanted; }
 #pragma unroll 1
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (tid < 256) bins[tid] = 0;
+    for (int shift = 21; shift >= 0; shift = shift == 21 ? 10 : shift - 10) {
+        const uint32_t digit = shift == 0 ? 1023u : 2047u;     // 11, 11 and 10 bits
+        bins[tid] = bins[tid + kSelectThreads] = 0;
         __syncthreads();
-        const uint32_t prefix = found[0], still = found[1];
+        const uint32_t prefix = found[0], still = found[1], above_digit = shift == 21 ? 0u : ~0u << (shift == 10 ? 21 : 10);
         each([&](int, int i, uint32_t key) {
-            bool on = i < old && (shift == 24 || key >> (shift + 8) == prefix >> (shift + 8));
-            const uint32_t bin = key >> shift & 255u;
-#pragma unroll 1
-            for (int round = shift == 24 ? 4 : 1; round > 0; --round) {
-                const uint64_t left = __ballot(on);
-                if (!left) return;
-                const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)bin, __ffsll((unsigned long long)left) - 1);
-                const uint64_t same = __ballot(on && bin == first);
+            bool on = i < old && ((key ^ prefix) & above_digit) == 0;
+            const uint64_t any = __ballot(on);
+            if (!any) return;
+            const uint32_t at = key >> shift & digit;
+            if (shift == 21) {
+                const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)at, __ffsll((unsigned long long)any) - 1);
+                const uint64_t same = __ballot(on && at == first);
                 if (lane == 0) atomicAdd(&bins[first], __popcll(same));
-                on = on && bin != first;
+                on = on && at != first;
             }
-            if (on) atomicAdd(&bins[bin], 1);
+            if (on) atomicAdd(&bins[at], 1);
         });
         __syncthreads();
-        if (wave == 0) {                                       // from the highest bin down, four bins a lane
-            int mine[4], sum = 0;
+        // from the highest bin down, two a thread: the one at which what is wanted is reached
+        const int b = 2047 - 2 * tid, high = bins[b], sum = high + bins[b - 1];
+        int up = sum;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum += mine[e] = bins[255 - 4 * lane - e];
-            int up = sum;
+        for (int off = 1; off < 64; off <<= 1) {
+            const int x = __shfl_up(up, off, 64);
+            if (lane >= off) up += x;
+        }
+        if (lane == 63) totals[wave] = up;
+        __syncthreads();
 #pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const int x = __shfl_up(up, off, 64);
-                if (lane >= off) up += x;
-            }
-            if (lane == __ffsll((unsigned long long)__ballot((uint32_t)up >= still)) - 1) {
-                uint32_t left = still - (uint32_t)(up - sum);
-                int e = 0;
-                while (e < 3 && (uint32_t)mine[e] < left) left -= (uint32_t)mine[e++];
-                found[0] = prefix | (uint32_t)(255 - 4 * lane - e) << shift;
-                found[1] = left;
-            }
+        for (int w = 0; w < kSelectWaves; ++w) up += w < wave ? totals[w] : 0;
+        if ((uint32_t)up >= still && (uint32_t)(up - sum) < still) {
+            const uint32_t left = still - (uint32_t)(up - sum);
+            const bool upper = (uint32_t)high >= left;
+            found[0] = prefix | (uint32_t)(upper ? b : b - 1) << shift;
+            found[1] = upper ? left : left - (uint32_t)high;
         }
         __syncthreads();
     }
