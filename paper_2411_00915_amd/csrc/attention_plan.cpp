@@ -102,6 +102,13 @@ extern "C" void lora_attention_plan_destroy(lora_attention_plan* p)
     delete p;
 }
 
+// Not part of the ABI: the workgroups' work of the tiled kernel, eight int32 an item (attention_tile), for the plan's tests
+extern "C" int32_t lora_attention_plan_items(const lora_attention_plan* p, const int32_t** items)
+{
+    *items = reinterpret_cast<const int32_t*>(p->items.data());
+    return (int32_t)p->items.size();
+}
+
 extern "C" size_t lora_cache_page_bytes(int32_t page_tokens, int32_t head_dim)
 {
     if (page_tokens < 32 || page_tokens > 1024 || page_tokens % 32 != 0 || head_dim < 1 || head_dim > LORA_MAX_HEAD_DIM) return 0;

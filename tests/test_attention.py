@@ -167,6 +167,35 @@ def test_prompts_between_other_columns(dtype, pad, shift, D):
 
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,Hkv", [(16, 2), (16, 8), (12, 12), (40, 8), (9, 3), (20, 10), (28, 4)])
+def test_prompts_of_many_heads(dtype, H, Hkv):
+    """Heads of one kv head in a workgroup of their own or together, runs of them on the XCDs and what is left over"""
+    nq, nk = [33, 7, 150, 64], [60, 7, 150, 64]
+    check_prompt(*prompt_case(np.random.default_rng(H), nq, nk, H, Hkv, 64, dtype), nq, nk, dtype, True, 0.125)
+
+
+@gpu
+def test_prompts_whose_rows_lie_beyond_4_gb():
+    nk, D, ld = [20000, 40], 64, 120008
+    rng = np.random.default_rng(21)
+    nq = [2, 40]
+    q, k, v = prompt_case(rng, nq, nk, 2, 1, D, BF16)
+    kd, vd = (torch.empty(sum(nk) * ld, dtype=torch.bfloat16, device=DEV).view(sum(nk), ld) for _ in range(2))
+    assert kd.numel() * 2 > 1 << 32
+    kd[:, :D], vd[:, :D] = to_device(k, BF16).view(-1, D), to_device(v, BF16).view(-1, D)
+    qd, od = to_device(q, BF16), torch.zeros(q.shape, dtype=torch.bfloat16, device=DEV)
+    plan = B.lora_attention_plan(offsets(nq), offsets(nk), 2, 1, D, BF16)
+    B.lora_attention(plan, qd, 2 * D, kd, ld, vd, ld, od, 2 * D, 0.125)
+    torch.cuda.synchronize()
+    got = od.float().cpu().numpy()
+    for a, b, n, m in ((slice(0, 2), slice(0, 20000), 2, 20000), (slice(2, 42), slice(20000, 20040), 40, 40)):
+        o, tol, amount, _ = reference(q[a], k[b], v[b], 0.125, lambda i: i + m - n + 1)
+        check(got[a], o, tol, amount, BF16)
+    plan.destroy()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
 def test_prompts_with_other_scales(dtype, scale):
     nq, nk = [90, 20], [100, 20]
@@ -504,6 +533,90 @@ def test_single_tokens_need_no_offsets_and_any_layout_will_do(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("decay", [-1.0, 0.0])
+def test_more_rows_than_a_tile_and_than_the_weights_take_at_a_time(decay):
+    rng = np.random.default_rng(14)
+    lengths, new, D = [150, 75], [70, 75], 64
+    pool = Pool(lengths, 1, D, 32)
+    vals = tokens(rng, lengths, 1, D, BF16)
+    pool.fill(vals, BF16)
+    q = rounded(rng.standard_normal((145, 4, D)), BF16)
+    got = run_cache(pool, q, new, BF16, 0.125, decay)
+    check_cache(pool, vals, q, new, lengths, BF16, 0.125, got, None if decay < 0 else (0.0, 0.0))
+
+
+@gpu
+def test_a_cache_beyond_4_gb():
+    """Pages at the far end of a large pool, tables of int32 page numbers into it"""
+    page, Hkv, D, H = 1024, 16, 128, 16
+    size = B.lora_cache_page_bytes(page, D)
+    count = (5 << 30) // (size * Hkv)
+    pages = torch.empty((count, Hkv, size), dtype=torch.uint8, device=DEV)
+    assert pages.numel() > 1 << 32
+    lengths = [1500, 20]
+    table = torch.tensor([[count - 1, 0], [count - 2, 1]], dtype=torch.int32, device=DEV)
+    length = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    weight = torch.zeros((count, Hkv, page), device=DEV)
+    cache = B.lora_cache(pages, table, length, page, Hkv, D, 2000, weight)
+    rng = np.random.default_rng(3)
+    vals = tokens(rng, lengths, Hkv, D, BF16)
+    kd, vd = (to_device(np.concatenate([x[i] for x in vals]), BF16) for i in (0, 1))
+    ptr = torch.tensor(offsets(lengths), device=DEV)
+    B.lora_cache_append(cache, BF16, sum(lengths), 1500, ptr, kd, Hkv * D, vd, Hkv * D)
+    ko, vo = torch.zeros_like(kd), torch.zeros_like(vd)
+    B.lora_cache_read(cache, BF16, sum(lengths), 1500, ptr, ko, Hkv * D, vo, Hkv * D)
+    q = to_device(rng.standard_normal((2, H, D)), BF16)
+    o = torch.zeros_like(q)
+    room = B.lora_cache_workspace(cache, H, 2, 1, True)
+    ws = torch.empty(max(room, 256), dtype=torch.uint8, device=DEV)
+    B.lora_cache_attention(cache, BF16, H, 2, 1, None, q, H * D, o, H * D, D ** -0.5, 0.0, ws, room)
+    torch.cuda.synchronize()
+    first = 0
+    for s, n in enumerate(lengths):
+        for part, got in ((0, ko), (1, vo)):
+            assert np.array_equal(got[first:first + n].float().cpu().numpy().reshape(n, Hkv, D), rounded(held(vals[s][part]), BF16))
+        first += n
+        p = np.zeros((n, Hkv))
+        for h in range(H):
+            x = held(vals[s][0])[:, h].astype(np.float64) @ q[s, h].double().cpu().numpy() * D ** -0.5
+            e = np.exp(x - x.max())
+            p[:, h] = e / e.sum()
+            want = p[:, h] @ held(vals[s][1])[:, h]
+            assert np.linalg.norm(o[s, h].double().cpu().numpy() - want) <= 2.0 ** -6 * np.linalg.norm(want)
+        got = np.concatenate([weight[int(table[s, i])].cpu().numpy().T[:max(0, min(page, n - i * page))] for i in range(2)])
+        assert np.abs(got - p).max() <= 1e-4
+
+
+@gpu
+def test_bounds_that_the_call_gives_hold_whatever_the_device_says():
+    """Lengths past max_length are cut, tokens past max_new and rows past num_tokens left out"""
+    rng = np.random.default_rng(15)
+    D, Hkv, H = 64, 2, 4
+    pool = Pool([100, 60], Hkv, D, 32, max_length=90)
+    vals = tokens(rng, [90, 60], Hkv, D, BF16)
+    pool.length.copy_(torch.tensor([1000, 60], dtype=torch.int32))          # (90 of the first)
+    pool.fill(vals, BF16)
+    ptr = torch.tensor([0, 6, 9], dtype=torch.int32, device=DEV)
+    q = to_device(rng.standard_normal((9, H, D)), BF16)
+    out = torch.full_like(q, 7.0)
+    room = B.lora_cache_workspace(pool.cache, H, 8, 4, False)
+    ws = torch.empty(max(room, 256), dtype=torch.uint8, device=DEV)
+    B.lora_cache_attention(pool.cache, BF16, H, 8, 4, ptr, q, H * D, out, H * D, 0.125, -1.0, ws, room)
+    torch.cuda.synchronize()
+    got = out.float().cpu().numpy()
+    assert (got[4:6] == 7).all() and (got[8:] == 7).all()
+    qf = q.float().cpu().numpy()
+    for s, rows, last in ((0, range(0, 4), 90 - 6), (1, range(6, 8), 60 - 2)):              # (of the second, two rows are in the call)
+        for i, row in enumerate(rows):
+            for h in range(H):
+                k, v = (held(x)[:last + i + 1, h // 2].astype(np.float64) for x in vals[s])
+                x = k @ qf[row, h] * 0.125
+                e = np.exp(x - x.max())
+                want = (e / e.sum()) @ v
+                assert np.linalg.norm(got[row, h] - want) <= 2.0 ** -6 * np.linalg.norm(want), (s, i, h)
+
+
+@gpu
 def test_pages_that_are_not_there_are_not_seen():
     rng = np.random.default_rng(6)
     lengths, D = [200, 130, 40], 64
@@ -623,6 +736,36 @@ def test_eviction(D, page, budget, recent):
 
 
 @gpu
+@pytest.mark.parametrize("length,budget,recent", [(4096, 1000, 0), (4500, 4097, 3), (5000, 700, 100), (32768, 9000, 0), (40000, 1234, 34), (40000, 39990, 1)])
+def test_eviction_of_long_caches(length, budget, recent):
+    rng = np.random.default_rng(length + budget)
+    Hkv, D, page = 2, 64, 128
+    pool = Pool([length, 17], Hkv, D, page)
+    w = np.exp(3 * rng.standard_normal((length, Hkv))).astype(np.float32)
+    w[rng.random(w.shape) < 0.3] = 0                        # exactly none
+    w[:, 1] = np.round(w[:, 1])                             # ties everywhere
+    flat = pool.weight.cpu().numpy()
+    i = np.arange(length)
+    flat[pool.table[0, i // page], :, i % page] = w
+    pool.weight.copy_(torch.from_numpy(flat))
+    target = Pool([budget, budget], Hkv, D, page, seed=3)
+    kept = torch.full((2, Hkv, budget), -9, dtype=torch.int32, device=DEV)
+    B.lora_cache_evict(pool.cache, target.cache, budget, recent, kept)
+    torch.cuda.synchronize()
+    for h in range(Hkv):
+        want = kept_slots(w[:, h], length, budget, recent)
+        assert kept[0, h].tolist() == want
+        assert kept[1, h].tolist() == (list(range(17)) + [-1] * budget)[:budget]
+        a, b = pool.table[0, np.array(want) // page], np.array(want) % page
+        c, d = target.table[0, np.arange(budget) // page], np.arange(budget) % page
+        assert np.array_equal(target.weight.cpu().numpy()[c, h, d], w[want, h])
+        (sk, sv), (skw, svw) = unpacked(pool.pages, page, D)
+        (tk, tv), (tkw, tvw) = unpacked(target.pages, page, D)
+        assert np.array_equal(tk[c, h, d], sk[a, h, b]) and np.array_equal(tv[c, h, d], sv[a, h, b])
+        assert np.array_equal(tkw[c, h, d], skw[a, h, b]) and np.array_equal(tvw[c, h, d], svw[a, h, b])
+
+
+@gpu
 def test_a_cache_lives_through_prompt_decode_and_eviction():
     """Attention over what eviction left equals attention over the kept tokens, new ones appended behind them"""
     rng = np.random.default_rng(12)
@@ -651,6 +794,80 @@ def test_a_cache_lives_through_prompt_decode_and_eviction():
     q = rounded(rng.standard_normal((5, H, D)), BF16)
     got = run_cache(target, q, [3, 2], BF16, 0.125)
     check_cache(target, vals, q, [3, 2], [203, 92], BF16, 0.125, got)
+
+
+# ---- plans and calls (no GPU) --------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("H,Hkv", [(1, 1), (4, 4), (8, 1), (32, 8), (40, 40), (28, 4), (9, 3), (12, 2), (64, 8)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_a_plans_items_cover_every_query_of_every_head_once(H, Hkv, causal):
+    rng = np.random.default_rng(H)
+    for nq, nk in LENGTHS + [(rng.integers(0, 700, 40).tolist(), rng.integers(0, 900, 40).tolist()), ([], []), ([0, 0], [5, 0])]:
+        plan = B.lora_attention_plan(offsets(nq), offsets(nk), H, Hkv, 64, BF16, causal)
+        items = B.lora_attention_plan_items(plan)
+        seen = np.zeros((sum(nq), H), int)
+        qo, ko = offsets(nq), offsets(nk)
+        assert len(items) % 8 == 0
+        for row, rows, key, keys, ahead, most, heads, head in items:
+            if heads == 0:
+                continue
+            s = int(np.searchsorted(qo, row, side="right")) - 1
+            assert qo[s] <= row and row + rows <= qo[s + 1] and (key, keys) == (ko[s], nk[s]) and 1 <= rows <= 128
+            first = row - qo[s]
+            sees = [max(0, min(nk[s], nk[s] - nq[s] + first + i + 1)) if causal else nk[s] for i in range(rows)]
+            assert [max(0, min(keys, ahead + i + 1)) for i in range(rows)] == sees and most == sees[-1]
+            assert heads in (1, 2, 4) and head // (H // Hkv) == (head + heads - 1) // (H // Hkv) and heads * rows <= 128
+            seen[row:row + rows, head:head + heads] += 1
+        assert (seen == 1).all()
+        # the XCDs' shares (every eighth item): none has more than its part and the heaviest unit of heads
+        load = [sum(int(i[5]) + 64 for i in items[x::8] if i[6]) for x in range(8)]
+        unit = max((int(i[5]) + 64 for i in items if i[6]), default=0) * 4 * max(1, -(-len(items) // max(H, 1)))
+        assert max(load) - min(load) <= unit
+        plan.destroy()
+
+
+def test_plans_are_the_same_for_the_same_batch():
+    a, b = (B.lora_attention_plan(offsets([5, 300, 70]), None, 12, 4, 80, F32) for _ in range(2))
+    assert np.array_equal(B.lora_attention_plan_items(a), B.lora_attention_plan_items(b))
+
+
+P, I32, I64, F, Z = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
+ABI = {"lora_attention_plan_upload": [P, P], "lora_attention": [P, P, I64, P, I64, P, I64, P, I64, F, P],
+       "lora_cache_append": [P, I32, I32, I32, P, P, I64, P, I64, P], "lora_cache_read": [P, I32, I32, I32, P, P, I64, P, I64, P],
+       "lora_cache_attention": [P, I32, I32, I32, I32, P, P, I64, P, I64, F, F, P, Z, P], "lora_cache_evict": [P, P, I32, I32, P, P]}
+
+
+@pytest.mark.parametrize("calls", ["_calls", "calls_ctypes"])
+@pytest.mark.parametrize("name", list(ABI))
+def test_arguments_reach_the_abi(calls, name):
+    """By position and by name, in place; what is missing or too much is refused"""
+    import importlib
+    import inspect
+    import types
+    module = importlib.import_module("paper_2411_00915_amd." + calls)
+    seen, status = [], [0]
+    keep = [ctypes.CFUNCTYPE(ctypes.c_int, *arguments)(lambda *a, n=n: (seen.append((n, list(a))), status[0])[1]) for n, arguments in ABI.items()]
+    if calls == "calls_ctypes":
+        module.bind(B._check, B._first_stream, *[B._address(keep[0])] * 8)
+    module.bind_attention(*(B._address(f) for f in keep))
+    try:
+        function = getattr(module, name)
+        parameters = inspect.signature(function).parameters
+        assert list(parameters) == list(inspect.signature(getattr(B, name)).parameters)
+        values = {p: types.SimpleNamespace(handle=0x1000 + i) if p in ("plan", "cache", "target") else 0.25 if p in ("scale", "decay") else 64 + i
+                  for i, p in enumerate(parameters)}
+        expected = [0x1000 + i if p in ("plan", "cache", "target") else v for i, (p, v) in enumerate(values.items())]
+        function(*values.values())
+        function(**dict(reversed(values.items())))
+        assert seen == [(name, expected)] * 2
+        for wrong in (list(values.values())[:-2], [*values.values(), 0]):
+            with pytest.raises(TypeError):
+                function(*wrong)
+        status[0] = B.LORA_ERR_WORKSPACE
+        with pytest.raises(B.LoraError, match=f"{name}: workspace"):
+            function(**values)
+    finally:
+        if calls == "_calls":
+            module.bind_attention(*(B._address(getattr(B._lib, n)) for n in ABI))
 
 
 # ---- refusals (no GPU) ---------------------------------------------------------------------------------------------------
@@ -713,7 +930,7 @@ def fake(**f):
     d = dict(pages=1 << 20, weight=1 << 21, page_table=1 << 22, length=1 << 23, num_pages=8, num_seqs=2, table_stride=4, max_length=200, page_tokens=64,
              num_kv_heads=2, head_dim=64)
     d.update(f)
-    return B.Cache(B.CacheDesc(*(d[n] for n, _ in B.CacheDesc._fields_)), None)
+    return B.Cache(B.CacheDesc(*(d[n] for n, _ in B.CacheDesc._fields_)))
 
 
 WRONG_CACHES = [dict(pages=None), dict(pages=(1 << 20) + 8), dict(page_table=None), dict(length=None), dict(num_pages=-1), dict(num_seqs=-1),
