@@ -123,6 +123,8 @@ _lib.lora_attention_plan_create.restype = ctypes.c_int
 _lib.lora_attention_plan_create.argtypes = [ctypes.POINTER(AttentionDesc), ctypes.POINTER(_vp)]
 _lib.lora_attention_plan_destroy.restype = None
 _lib.lora_attention_plan_destroy.argtypes = [_vp]
+_lib.lora_attention_plan_items.restype = ctypes.c_int32
+_lib.lora_attention_plan_items.argtypes = [_vp, ctypes.POINTER(_i32p)]
 _lib.lora_cache_page_bytes.restype = ctypes.c_size_t
 _lib.lora_cache_page_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32]
 _lib.lora_cache_workspace.restype = ctypes.c_int
@@ -445,6 +447,14 @@ def lora_attention_plan_create_raw(desc: Optional[AttentionDesc]):
     return st, out.value
 
 
+def lora_attention_plan_items(plan: AttentionPlan) -> np.ndarray:
+    """The plan's work by workgroup, [items, 8]: first query row, queries, first key row, keys of the sequence, keys that the query before
+    the first sees, keys that the last sees, heads (0: nothing to do), first head"""
+    p = _i32p()
+    n = _lib.lora_attention_plan_items(plan.handle, ctypes.byref(p))
+    return np.ctypeslib.as_array(p, shape=(n * 8,)).copy().reshape(n, 8) if n else np.zeros((0, 8), np.int32)
+
+
 def lora_cache_page_bytes(page_tokens: int, head_dim: int) -> int:
     return int(_lib.lora_cache_page_bytes(int(page_tokens), int(head_dim)))
 
@@ -452,10 +462,10 @@ def lora_cache_page_bytes(page_tokens: int, head_dim: int) -> int:
 class Cache:
     """A lora_cache descriptor and the device tensors that it names (kept alive by it)."""
 
-    def __init__(self, desc: CacheDesc, keepalive):
+    def __init__(self, desc: CacheDesc, pages=None, weight=None, page_table=None, length=None):
         self.desc = desc
         self.handle = ctypes.addressof(desc)
-        self._keep = keepalive
+        self.pages, self.weight, self.page_table, self.length = pages, weight, page_table, length
 
 
 def lora_cache(pages, page_table, length, page_tokens, num_kv_heads, head_dim, max_length, weight=None) -> Cache:
@@ -476,7 +486,7 @@ def lora_cache(pages, page_table, length, page_tokens, num_kv_heads, head_dim, m
         raise ValueError("weight: one for every slot of every page and head")
     desc = CacheDesc(_ptr(pages), _ptr(weight), _ptr(page_table), _ptr(length), num_pages, int(length.shape[0]), int(page_table.shape[1]),
                      int(max_length), int(page_tokens), int(num_kv_heads), int(head_dim))
-    return Cache(desc, (pages, weight, page_table, length))
+    return Cache(desc, pages, weight, page_table, length)
 
 
 def lora_cache_workspace(cache: Cache, num_heads, num_tokens, max_new, weights=False) -> int:
