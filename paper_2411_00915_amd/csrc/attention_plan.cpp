@@ -81,7 +81,7 @@ extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, 
                 p->tiles.push_back(t);
             }
         }
-        std::stable_sort(p->tiles.begin(), p->tiles.end(), [](const attention_tile& a, const attention_tile& b) { return a.max_kv > b.max_kv; });
+        std::stable_sort(p->tiles.begin(), p->tiles.end(), [](const attention_tile& a, const attention_tile& b) { return a.max_kv != b.max_kv ? a.max_kv > b.max_kv : a.rows < b.rows; });
         if ((int64_t)p->tiles.size() * p->num_heads > LORA_ATTENTION_MAX_ITEMS) {
             delete p;
             return LORA_ERR_UNSUPPORTED;
