@@ -182,6 +182,7 @@ extern "C" lora_status lora_cache_attention(const lora_cache* c, int32_t dtype, 
     a.row_tiles = v.row_tiles;
     a.splits = v.splits;
     a.split_tokens = v.split_tokens;
+    a.waves = v.waves;
     a.stats = v.splits > 1 || weights ? reinterpret_cast<float2*>(w + v.stats) : nullptr;
     a.partial = v.splits > 1 ? reinterpret_cast<float*>(w + v.partial) : nullptr;
     a.scores = weights ? reinterpret_cast<float*>(w + v.scores) : nullptr;

@@ -40,7 +40,7 @@ inline int32_t padded_head_dim(int32_t d) { return d <= 64 ? 64 : d <= 128 ? 128
 
 // how lora_cache_attention divides its work, from what the host knows; the workspace's parts follow from it
 struct cache_division {
-    int32_t row_tiles, splits, split_tokens;
+    int32_t row_tiles, splits, split_tokens, waves;      // waves: wavefronts of a workgroup
     size_t stats, partial, scores, total;      // bytes before each part, in all
     int64_t score_stride;
 };

@@ -129,6 +129,10 @@ cache_division divide_cache_attention(const lora_cache* c, int32_t num_heads, in
         return std::min<int64_t>((total + wgs - 1) / std::max<int64_t>(wgs, 1), (c->max_length + tokens - 1) / tokens);
     };
     const int64_t splits = std::max<int64_t>(1, std::max(wgs < 256 ? pieces(512, wgs < 128 ? 256 : 512) : 1, pieces(1024, 2048)));
+    // In one piece, and fewer than two workgroups a compute unit: eight wavefronts each (one tile of rows, heads of up to 128; 8
+    // requests of 700 tokens, 32 heads: 14.4 us with four, 12.2 with eight; with pieces to join it is the other way round, 12.6
+    // and 13.7 for one request of 2000).
+    v.waves = splits == 1 && wgs < 512 && rows <= 16 && padded_head_dim(c->head_dim) <= 128 ? 8 : 4;
     v.split_tokens = (int32_t)std::max<int64_t>(128, ((c->max_length + splits - 1) / splits + 127) / 128 * 128);
     v.splits = (int32_t)std::max<int64_t>(1, ((int64_t)c->max_length + v.split_tokens - 1) / v.split_tokens);
     const size_t out_rows = (size_t)num_tokens * num_heads;

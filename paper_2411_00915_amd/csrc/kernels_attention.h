@@ -40,7 +40,7 @@ struct cache_attention_args {
     int64_t ldq, ldo;
     int32_t num_heads, group;
     float scale, decay;          // decay < 0: weights are left alone
-    int32_t row_tiles, splits, split_tokens;
+    int32_t row_tiles, splits, split_tokens, waves;
     float2* stats;               // [num_tokens * num_heads][splits] maximum and sum
     float* partial;              // [num_tokens * num_heads][splits][head_dim], where splits > 1
     float* scores;               // [num_tokens * num_heads][score_stride], where weights are wanted

@@ -176,16 +176,16 @@ __device__ __forceinline__ float max_of_rows(float x)
     return x;
 }
 
-template <typename T, int DP, int CT, bool KEEP>
-__global__ __launch_bounds__(256, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 : 2) void cache_attention_kernel(cache_attention_args a)
+template <typename T, int DP, int CT, bool KEEP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 : 2) void cache_attention_kernel(cache_attention_args a)
 {
     constexpr bool EXACT = sizeof(T) == 4;
     constexpr int TERMS = EXACT ? 3 : 1, NS = DP / 32, NB = DP / 16;
     constexpr float OFFSET = EXACT ? 7.5f : 23.5f;         // of what the matrix cores see, from code - 7.5
-    constexpr int RING = DP == 64 ? 3 : 2, RING_BYTES = 4 * RING * block_lds<DP>::BYTES, RED_BYTES = 4 * 16 * (DP + 4) * 4;
+    constexpr int RING = DP == 64 ? 3 : 2, RING_BYTES = WAVES * RING * block_lds<DP>::BYTES, RED_BYTES = WAVES * 16 * (DP + 4) * 4;
     __shared__ __align__(16) char lds[RING_BYTES > RED_BYTES ? RING_BYTES : RED_BYTES];
     float (*const red)[16][DP + 4] = reinterpret_cast<float (*)[16][DP + 4]>(lds);           // (when the rings are done with)
-    __shared__ float red_m[4][16], red_l[4][16];
+    __shared__ float red_m[WAVES][16], red_l[WAVES][16];
     const cache_args& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     int id = blockIdx.x;
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 :
     // the wavefront's first block from b on whose page is there: its page and place, or null and b >= last
     int b = (t0 >> 5) + wave, at = 0;
     auto find = [&]() -> const unsigned char* {
-        for (; b < last; b += 4) {
+        for (; b < last; b += WAVES) {
             const unsigned char* const p = page_at(b);
             if (p) {
                 at = b % blocks_a_page * 32;
@@ -399,7 +399,7 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 :
         const unsigned char* const page = find();
         const int found = b;
         if (page) fetch_block<DP>(page, c.page_tokens, at, off, ring_at + place * block_lds<DP>::BYTES);
-        b += 4;
+        b += WAVES;
         return found;
     };
 #pragma unroll
@@ -428,7 +428,9 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 :
         __syncthreads();
         if (g == 0) red_m[wave][r] = m[ct];
         __syncthreads();
-        float top = fmaxf(fmaxf(red_m[0][r], red_m[1][r]), fmaxf(red_m[2][r], red_m[3][r]));
+        float top = red_m[0][r];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) top = fmaxf(top, red_m[w][r]);
         const float f = m[ct] == -INFINITY ? 0.f : exp_of(ref[ct] - top);
         const float add = z[ct] - OFFSET * ones[ct][0];
         // a wavefront that saw nothing has summed nothing
@@ -440,16 +442,24 @@ __global__ __launch_bounds__(256, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 :
                     float4{f * (acc[ct][n][i] + add), f * (acc[ct][n + 1][i] + add), f * (acc[ct][n + 2][i] + add), f * (acc[ct][n + 3][i] + add)};
         if (g == 0) red_l[wave][r] = f * l[ct];
         __syncthreads();
-        const int col = tid >> 4, row = row0 + 16 * ct + col;
+        constexpr int LANES = 4 * WAVES;                       // threads a query row
+        const int col = tid / LANES, row = row0 + 16 * ct + col;
         if (row < R) {
             const int64_t out_row = (int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group;
-            const float sum = (red_l[0][col] + red_l[1][col]) + (red_l[2][col] + red_l[3][col]);
-            if (a.stats && (tid & 15) == 0)
-                a.stats[out_row * a.splits + split] = float2{fmaxf(fmaxf(red_m[0][col], red_m[1][col]), fmaxf(red_m[2][col], red_m[3][col])), sum};
+            float sum = 0.f, most_of = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                sum += red_l[w][col];
+                most_of = fmaxf(most_of, red_m[w][col]);
+            }
+            if (a.stats && tid % LANES == 0) a.stats[out_row * a.splits + split] = float2{most_of, sum};
             const float inv = a.partial ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
             T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + row / a.group) * a.ldo + (int64_t)(head * a.group + row % a.group) * D;
-            for (int d = tid & 15; d < D; d += 16) {
-                const float o = ((red[0][col][d] + red[1][col][d]) + (red[2][col][d] + red[3][col][d])) * inv;
+            for (int d = tid % LANES; d < D; d += LANES) {
+                float o = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) o += red[w][col][d];
+                o *= inv;
                 if (a.partial) a.partial[(out_row * a.splits + split) * D + d] = o;
                 else elem<T>::store(out + d, o);
             }
@@ -557,18 +567,21 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args 
     for (int e = 0; e < min(4, length - slot); ++e) w[e] = a.decay == 0.f ? sum[e] : a.decay * w[e] + sum[e];
 }
 
+template <typename T, int DP, int CT, int WAVES>
+void launch_shape(const cache_attention_args& a, hipStream_t stream)
+{
+    const dim3 grid((uint32_t)((int64_t)a.c.num_seqs * a.c.kv_heads * a.splits * a.row_tiles)), block(64 * WAVES);
+    if (a.scores) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, true, WAVES>), grid, block, 0, stream, a);
+    else LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, false, WAVES>), grid, block, 0, stream, a);
+}
+
 template <typename T, int DP>
 void launch_main(const cache_attention_args& a, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)((int64_t)a.c.num_seqs * a.c.kv_heads * a.splits * a.row_tiles));
-    const bool wide = (int64_t)a.group * a.c.max_new > 16;
-    if (a.scores) {
-        if (wide) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, 2, true>), grid, dim3(256), 0, stream, a);
-        else LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, 1, true>), grid, dim3(256), 0, stream, a);
-    } else {
-        if (wide) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, 2, false>), grid, dim3(256), 0, stream, a);
-        else LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, 1, false>), grid, dim3(256), 0, stream, a);
-    }
+    if ((int64_t)a.group * a.c.max_new > 16) return launch_shape<T, DP, 2, 4>(a, stream);
+    if constexpr (DP <= 128)
+        if (a.waves == 8) return launch_shape<T, DP, 1, 8>(a, stream);
+    launch_shape<T, DP, 1, 4>(a, stream);
 }
 
 template <typename T>
