@@ -71,6 +71,17 @@ lora_status check_tokens(const lora_cache* c, int32_t dtype, int32_t num_tokens,
     return check_cache(c);
 }
 
+// of lora_cache_attention: rows, workgroups and the workspace's parts that the kernels' 32- and 64-bit numbers hold
+lora_status check_rows(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new)
+{
+    if (num_heads < 1 || num_heads % c->num_kv_heads != 0) return LORA_ERR_INVALID_ARG;
+    const int64_t rows = (int64_t)num_tokens * num_heads;
+    if (rows > INT32_MAX || (int64_t)c->num_seqs * max_new > INT32_MAX / num_heads) return LORA_ERR_UNSUPPORTED;
+    if ((int64_t)c->num_seqs * c->num_kv_heads > INT32_MAX / (c->max_length / 256 + 1)) return LORA_ERR_UNSUPPORTED;
+    if (rows > ((int64_t)1 << 40) / std::max<int64_t>(c->max_length, 1)) return LORA_ERR_UNSUPPORTED;
+    return LORA_OK;
+}
+
 cache_args args_of(const lora_cache* c, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr)
 {
     cache_args a{};
@@ -125,7 +136,7 @@ extern "C" lora_status lora_cache_append(const lora_cache* c, int32_t dtype, int
     const int64_t row = (int64_t)c->num_kv_heads * c->head_dim;
     if (!k || !v || ldk < row || ldv < row || misaligned(k, elem_bytes(dtype)) || misaligned(v, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
     if ((int64_t)num_tokens / 32 + 1 > INT32_MAX / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
-    return status_of(launch_cache_append(args_of(c, num_tokens, max_new, d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
+    return status_of(launch_cache_append(args_of(c, num_tokens, std::min(max_new, num_tokens), d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
 }
 
 extern "C" lora_status lora_cache_read(const lora_cache* c, int32_t dtype, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr, void* k, int64_t ldk,
@@ -137,16 +148,18 @@ extern "C" lora_status lora_cache_read(const lora_cache* c, int32_t dtype, int32
     const int64_t row = (int64_t)c->num_kv_heads * c->head_dim;
     if (!k || !v || ldk < row || ldv < row || misaligned(k, elem_bytes(dtype)) || misaligned(v, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
     if ((int64_t)num_tokens / 32 + 1 > INT32_MAX / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
-    return status_of(launch_cache_read(args_of(c, num_tokens, max_new, d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
+    return status_of(launch_cache_read(args_of(c, num_tokens, std::min(max_new, num_tokens), d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
 }
 
 extern "C" lora_status lora_cache_workspace(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new, int32_t weights, size_t* bytes)
 {
     if (!bytes) return LORA_ERR_INVALID_ARG;
     *bytes = 0;
-    const lora_status st = check_tokens(c, LORA_BF16, num_tokens, max_new, nullptr);
+    lora_status st = check_tokens(c, LORA_BF16, num_tokens, max_new, nullptr);
     if (st != LORA_OK) return st;
-    if (num_heads < 1 || num_heads % c->num_kv_heads != 0) return LORA_ERR_INVALID_ARG;
+    max_new = std::min(max_new, num_tokens);                   // (no sequence has more)
+    st = check_rows(c, num_heads, num_tokens, max_new);
+    if (st != LORA_OK) return st;
     if (num_tokens > 0 && max_new > 0 && c->num_seqs > 0) *bytes = divide_cache_attention(c, num_heads, num_tokens, max_new, weights != 0).total;
     return LORA_OK;
 }
@@ -155,9 +168,12 @@ extern "C" lora_status lora_cache_attention(const lora_cache* c, int32_t dtype, 
                                             const int32_t* d_indptr, const void* q, int64_t ldq, void* o, int64_t ldo, float scale, float decay,
                                             void* workspace, size_t workspace_bytes, void* hip_stream)
 {
-    const lora_status st = check_tokens(c, dtype, num_tokens, max_new, d_indptr);
+    lora_status st = check_tokens(c, dtype, num_tokens, max_new, d_indptr);
     if (st != LORA_OK) return st;
-    if (num_heads < 1 || num_heads % c->num_kv_heads != 0 || !std::isfinite(scale) || !(decay <= 1.f)) return LORA_ERR_INVALID_ARG;
+    if (!std::isfinite(scale) || !(decay <= 1.f)) return LORA_ERR_INVALID_ARG;
+    max_new = std::min(max_new, num_tokens);
+    st = check_rows(c, num_heads, num_tokens, max_new);
+    if (st != LORA_OK) return st;
     const bool weights = decay >= 0.f;
     if (weights && c->num_seqs > 0 && !c->weight) return LORA_ERR_INVALID_ARG;
     if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
@@ -165,9 +181,7 @@ extern "C" lora_status lora_cache_attention(const lora_cache* c, int32_t dtype, 
     if (!q || !o || ldq < row || ldo < row || misaligned(q, elem_bytes(dtype)) || misaligned(o, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
     const cache_division v = divide_cache_attention(c, num_heads, num_tokens, max_new, weights);
     if (v.total > 0 && (!workspace || workspace_bytes < v.total || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
-    if ((int64_t)c->num_seqs * c->num_kv_heads * v.splits > INT32_MAX / std::max(1, v.row_tiles) || (int64_t)num_tokens * num_heads > INT32_MAX ||
-        (int64_t)c->num_seqs * max_new > INT32_MAX / num_heads || (int64_t)c->num_seqs * c->num_kv_heads > INT32_MAX / (c->max_length / 256 + 1))
-        return LORA_ERR_UNSUPPORTED;
+    if ((int64_t)c->num_seqs * c->num_kv_heads * v.splits > INT32_MAX / std::max(1, v.row_tiles)) return LORA_ERR_UNSUPPORTED;
     char* const w = static_cast<char*>(workspace);
     cache_attention_args a{};
     a.c = args_of(c, num_tokens, max_new, d_indptr);

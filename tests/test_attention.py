@@ -978,6 +978,12 @@ def test_the_caches_calls_refuse_what_is_wrong():
     assert B._lib.lora_cache_workspace(fake().handle, 4, 2, 1, 0, None) == B.LORA_ERR_INVALID_ARG
     assert B.lora_cache_workspace(fake(), 4, 0, 1) == 0
 
+    for f in (dict(n=2 ** 29, H=8), dict(n=2 ** 20, most=2 ** 31 - 1, H=4)):                # rows past 32 bits, of all and of all sequences
+        refused("attention", fake(num_seqs=2 ** 12), status=B.LORA_ERR_UNSUPPORTED, **f)
+    with pytest.raises(B.LoraError):                        # a workspace of a few TB
+        B.lora_cache_workspace(fake(max_length=2 ** 30, table_stride=2 ** 24), 1024, 2 ** 10, 1, True)
+    assert B.lora_cache_workspace(fake(), 4, 2, 2 ** 31 - 1, True) == B.lora_cache_workspace(fake(), 4, 2, 2, True)
+
     def evict_refused(source, target, budget=100, recent=10, kept=4096, status=B.LORA_ERR_INVALID_ARG):
         with pytest.raises(B.LoraError, match="lora_cache_evict") as e:
             B.lora_cache_evict(source, target, budget, recent, kept, stream=0)
