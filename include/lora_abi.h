@@ -408,7 +408,7 @@ typedef struct {
 /* Pure host code: tiles of the queries, longest first.  One plan serves all layers of the batch.
  * LORA_ERR_INVALID_ARG: null desc / out / q_indptr, offsets that do not start at 0 or decrease, heads < 1, num_heads no
  * multiple of num_kv_heads, head_dim outside 1 .. LORA_MAX_HEAD_DIM, unknown dtype, causal other than 0 or 1.
- * LORA_ERR_UNSUPPORTED: more than 2^30 rows, or than 2^27 heads of tiles of 128 queries. */
+ * LORA_ERR_UNSUPPORTED: more than 2^30 rows, or more workgroups (heads of tiles of 128 queries) than a launch holds, 2^24. */
 lora_status lora_attention_plan_create(const lora_attention_desc* desc, lora_attention_plan** out);
 void        lora_attention_plan_destroy(lora_attention_plan* plan);
 lora_status lora_attention_plan_upload(lora_attention_plan* plan, void* hip_stream);

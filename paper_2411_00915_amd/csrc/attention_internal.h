@@ -17,7 +17,7 @@ struct attention_tile {
 };
 
 #define LORA_ATTENTION_ROWS 128
-#define LORA_ATTENTION_MAX_ITEMS (1 << 27)
+#define LORA_ATTENTION_MAX_WORKGROUPS ((1 << 24) - 1)   /* a launch holds fewer than 2^32 threads; these have 256 */
 #define LORA_ATTENTION_MAX_ROWS (1 << 30)      /* of a batch: row numbers and sums of two stay below 2^31 */
 
 struct lora_attention_plan {

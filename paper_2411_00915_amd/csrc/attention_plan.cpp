@@ -18,8 +18,8 @@ bool offsets_ok(const int32_t* p, int32_t n)
 
 // The workgroups' work.  Workgroups go round the 8 XCDs, so every eighth item is one XCD's: it gets whole heads, one behind the
 // other, so that the workgroups that run beside each other there read the same keys and values; heads that are left over
-// go to the XCD that has the least to do.  Tiles of a head: most keys first.
-void order_items(lora_attention_plan* p)
+// go to the XCD that has the least to do.  Tiles of a head: most keys first.  False: more workgroups than a launch holds.
+bool order_items(lora_attention_plan* p)
 {
     constexpr int X = 8;
     std::vector<attention_tile> list[X];
@@ -41,9 +41,11 @@ void order_items(lora_attention_plan* p)
                 add((int)(std::min_element(cost, cost + X) - cost), t, u * unit + h);
     size_t longest = 0;
     for (const auto& l : list) longest = std::max(longest, l.size());
+    if (longest > LORA_ATTENTION_MAX_WORKGROUPS / X) return false;
     p->items.assign(longest * X, attention_tile{});
     for (int x = 0; x < X; ++x)
         for (size_t i = 0; i < list[x].size(); ++i) p->items[i * X + x] = list[x][i];
+    return true;
 }
 }  // namespace
 
@@ -82,11 +84,10 @@ extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, 
             }
         }
         std::stable_sort(p->tiles.begin(), p->tiles.end(), [](const attention_tile& a, const attention_tile& b) { return a.max_kv != b.max_kv ? a.max_kv > b.max_kv : a.rows < b.rows; });
-        if ((int64_t)p->tiles.size() * p->num_heads > LORA_ATTENTION_MAX_ITEMS) {
+        if ((int64_t)p->tiles.size() * p->num_heads > LORA_ATTENTION_MAX_WORKGROUPS || !order_items(p)) {
             delete p;
             return LORA_ERR_UNSUPPORTED;
         }
-        order_items(p);
     } catch (const std::bad_alloc&) {
         delete p;
         return LORA_ERR_NOMEM;

@@ -1002,6 +1002,26 @@ def test_the_caches_calls_refuse_what_is_wrong():
     evict_refused(B.Plan(None, None), fake(**other))
 
 
+def test_launches_of_too_many_threads_are_refused():
+    """2^24 workgroups of 256 threads are more than a launch holds"""
+    seqs = np.arange(2 ** 14 + 1, dtype=np.int32)
+    for heads, fits in ((8, True), (1024, False)):
+        desc = B.AttentionDesc(2 ** 14, seqs.ctypes.data_as(B._i32p), None, heads, heads, 64, BF16, 1)
+        st, handle = B.lora_attention_plan_create_raw(desc)
+        assert st == (B.LORA_OK if fits else B.LORA_ERR_UNSUPPORTED)
+        if handle:
+            B.AttentionPlan(handle).destroy()
+    many = fake(num_kv_heads=2 ** 20, num_seqs=2 ** 4)
+    for call in (lambda: B.lora_cache_append(many, BF16, 1024, 64, 4096, 4096, 2 ** 26, 8192, 2 ** 26, stream=0),
+                 lambda: B.lora_cache_read(many, BF16, 1024, 64, 4096, 4096, 2 ** 26, 8192, 2 ** 26, stream=0),
+                 lambda: B.lora_cache_attention(many, BF16, 2 ** 20, 16, 1, None, 4096, 2 ** 26, 8192, 2 ** 26, 1.0, -1.0, 1 << 24, 1 << 40, stream=0),
+                 lambda: B.lora_cache_workspace(many, 2 ** 20, 16, 1),
+                 lambda: B.lora_cache_evict(many, fake(num_kv_heads=2 ** 20, num_seqs=2 ** 4, length=1 << 25), 100, 10, 4096, stream=0)):
+        with pytest.raises(B.LoraError) as e:
+            call()
+        assert e.value.status == B.LORA_ERR_UNSUPPORTED
+
+
 def test_bytes_of_a_page():
     assert [B.lora_cache_page_bytes(64, d) for d in (1, 64, 65, 128, 129, 256)] == [64 * 72, 64 * 72, 64 * 136, 64 * 136, 64 * 264, 64 * 264]
     assert [B.lora_cache_page_bytes(*a) for a in ((0, 64), (31, 64), (33, 64), (1056, 64), (64, 0), (64, 257), (-32, 64))] == [0] * 7
