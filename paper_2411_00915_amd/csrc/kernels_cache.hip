@@ -173,39 +173,47 @@ __device__ __forceinline__ uint32_t quantise(const float* x, int count, uint32_t
     return bad ? 0x7fc07fc0u : (z | __float_as_uint(step) >> 16);
 }
 
+// A fifth wavefront finds the places while four make the codes
+constexpr int kAppendThreads = 320;
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void cache_append_kernel(cache_args c, const T* k, int64_t ldk, const T* v, int64_t ldv, bool aligned)
+__global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(cache_args c, const T* k, int64_t ldk, const T* v, int64_t ldv, bool aligned)
 {
     constexpr int E = DP / 16, W = (E + 7) / 8;                // elements and words of a lane
     __shared__ tile_places places;
     __shared__ uint32_t values[kTile][16 * W + 1];
     const int tid = threadIdx.x, r = tid & 15, head = blockIdx.x % c.kv_heads, t0 = blockIdx.x / c.kv_heads * kTile;
     const int d0 = r * E, count = min(E, c.head_dim - d0);
-    float x[2][2][E];                                          // tokens tid / 16 and 16 on, keys and values
+    uint32_t codes[2][W], words[2][2];                         // of the keys; of tokens tid / 16 and 16 on
+    if (tid >= 256) find_places(c, t0, head, tid - 256, places);
+    else {
+        float x[2][2][E];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int t = min(t0 + (tid >> 4) + 16 * h, c.num_tokens - 1);
-        load_elems<T, E>(k + (int64_t)t * ldk + head * c.head_dim + d0, count, aligned, x[h][0]);
-        load_elems<T, E>(v + (int64_t)t * ldv + head * c.head_dim + d0, count, aligned, x[h][1]);
+        for (int h = 0; h < 2; ++h) {
+            const int t = min(t0 + (tid >> 4) + 16 * h, c.num_tokens - 1);
+            load_elems<T, E>(k + (int64_t)t * ldk + head * c.head_dim + d0, count, aligned, x[h][0]);
+            load_elems<T, E>(v + (int64_t)t * ldv + head * c.head_dim + d0, count, aligned, x[h][1]);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t u[W];
+            words[h][0] = quantise<E>(x[h][0], count, codes[h]);
+            words[h][1] = quantise<E>(x[h][1], count, u);
+#pragma unroll
+            for (int w = 0; w < W; ++w) values[(tid >> 4) + 16 * h][W * r + w] = u[w];
+        }
     }
-    if (tid < 64) find_places(c, t0, head, tid, places);
     __syncthreads();
+    if (tid >= 256) return;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int i = (tid >> 4) + 16 * h;
-        uint32_t codes[2][W], words[2];
-#pragma unroll
-        for (int part = 0; part < 2; ++part) words[part] = quantise<E>(x[h][part], count, codes[part]);
-#pragma unroll
-        for (int w = 0; w < W; ++w) values[i][W * r + w] = codes[1][w];
         const int64_t page = places.page[i];
         if (page < 0) continue;
         unsigned char* const base = c.pages + page * c.page_bytes;
-        store_codes<DP>(base + key_offset<DP>(places.at[i], r), codes[0]);
-        if (r < 2) *reinterpret_cast<uint32_t*>(base + word_offset<DP>(c.page_tokens, places.at[i], r)) = r ? words[1] : words[0];
+        store_codes<DP>(base + key_offset<DP>(places.at[i], r), codes[h]);
+        if (r < 2) *reinterpret_cast<uint32_t*>(base + word_offset<DP>(c.page_tokens, places.at[i], r)) = r ? words[h][1] : words[h][0];
         if (r == 2 && c.weight) c.weight[page * c.page_tokens + places.at[i]] = 0.f;
     }
-    __syncthreads();
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
         const int i = tid & 31, q = (tid >> 5) + 8 * n;
@@ -476,7 +484,7 @@ hipError_t launch_cache_append(const cache_args& c, int32_t dtype, const void* k
 {
     const dim3 grid((uint32_t)(tiles_of(c.num_tokens) * c.kv_heads));
     const bool aligned = rows_aligned(k, ldk, v, ldv, c.head_dim, dtype);
-#define APPEND(DP, T) LORA_LAUNCH(LORA_K_CACHE_APPEND, (cache_append_kernel<T, DP>), grid, dim3(256), 0, stream, c, static_cast<const T*>(k), ldk, static_cast<const T*>(v), ldv, aligned)
+#define APPEND(DP, T) LORA_LAUNCH(LORA_K_CACHE_APPEND, (cache_append_kernel<T, DP>), grid, dim3(kAppendThreads), 0, stream, c, static_cast<const T*>(k), ldk, static_cast<const T*>(v), ldv, aligned)
     if (dtype == LORA_F32) { BY_HEAD_DIM(APPEND, float) }
     else { BY_HEAD_DIM(APPEND, bf16_t) }
     return hipGetLastError();
