@@ -77,7 +77,8 @@ lora_status check_rows(const lora_cache* c, int32_t num_heads, int32_t num_token
     if (num_heads < 1 || num_heads % c->num_kv_heads != 0) return LORA_ERR_INVALID_ARG;
     const int64_t rows = (int64_t)num_tokens * num_heads;
     if (rows > INT32_MAX || (int64_t)c->num_seqs * max_new > INT32_MAX / num_heads) return LORA_ERR_UNSUPPORTED;
-    if ((int64_t)c->num_seqs * c->num_kv_heads > LORA_ATTENTION_MAX_WORKGROUPS / (c->max_length / 1024 + 1)) return LORA_ERR_UNSUPPORTED;
+    // (the launch behind the attention's: up to a workgroup of 512 threads for 2048 slots, beside those of the rows to be joined)
+    if ((int64_t)c->num_seqs * c->num_kv_heads > LORA_ATTENTION_MAX_WORKGROUPS / 4 / (c->max_length / 2048 + 1)) return LORA_ERR_UNSUPPORTED;
     if (rows > ((int64_t)1 << 40) / std::max<int64_t>(c->max_length, 1)) return LORA_ERR_UNSUPPORTED;
     return LORA_OK;
 }

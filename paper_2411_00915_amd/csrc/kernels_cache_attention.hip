@@ -467,36 +467,36 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     }
 }
 
-// The splits of a query row joined: a workgroup a row, its wavefronts take turns at the splits.  Leaves the
-// logarithm of the row's sum (with its maximum) in place of its first split's statistics, for the weights.
-constexpr int kJoinThreads = 512;
+// What is left when all splits are done, in one launch: the first `rows` workgroups join the splits of a query row each, the others
+// add up accumulated weights.
+constexpr int kFinishThreads = 512, kFinishWaves = kFinishThreads / 64, kWeightSlots = 4 * kFinishThreads;
+
+// a row's splits: the wavefronts take turns at them
 template <typename T>
-__global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(cache_attention_args a)
+__device__ __forceinline__ void join_row(const cache_attention_args& a, int64_t row)
 {
-    constexpr int WAVES = kJoinThreads / 64;
-    __shared__ float red[WAVES][LORA_MAX_HEAD_DIM], red_sum[WAVES], red_top[WAVES];
+    __shared__ float red[kFinishWaves][LORA_MAX_HEAD_DIM], red_sum[kFinishWaves], red_top[kFinishWaves];
     const cache_args& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, D = c.head_dim;
-    const int64_t row = blockIdx.x;
     const int head = (int)(row % a.num_heads);
     const int64_t at = row / a.num_heads;
     const int seq = (int)(at / c.max_new), i = (int)(at % c.max_new);
     const cache_rows rows = rows_of(c, seq);
     if (i >= rows.count) return;
     const int64_t out_row = (int64_t)(rows.first + i) * a.num_heads + head;
-    float2* const st = a.stats + out_row * a.splits;
+    const float2* const st = a.stats + out_row * a.splits;
     float top = -INFINITY;
-    for (int s = tid; s < a.splits; s += kJoinThreads) top = fmaxf(top, st[s].x);
+    for (int s = tid; s < a.splits; s += kFinishThreads) top = fmaxf(top, st[s].x);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
     if (lane == 0) red_top[wave] = top;
     __syncthreads();
     top = red_top[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, red_top[w]);
+    for (int w = 1; w < kFinishWaves; ++w) top = fmaxf(top, red_top[w]);
     float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = wave; s < a.splits; s += WAVES) {
+    for (int s = wave; s < a.splits; s += kFinishWaves) {
         const float2 e = st[s];
         const float* const p = a.partial + (out_row * a.splits + s) * D;
         const float f = e.y == 0.f ? 0.f : exp_of(e.x - top);  // (nothing seen: its maximum is -inf, perhaps all are; NaN goes on)
@@ -513,46 +513,50 @@ __global__ __launch_bounds__(kJoinThreads) void cache_join_kernel(cache_attentio
     sum = 0.f;
     float all = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+    for (int w = 0; w < kFinishWaves; ++w) {
         sum += red_sum[w];
         if (tid < D) all += red[w][tid];
     }
     T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + i) * a.ldo + (int64_t)head * D;
     if (tid < D) elem<T>::store(out + tid, sum == 0.f ? 0.f : all / sum);
-    if (tid == 0) st[0] = float2{sum == 0.f ? INFINITY : top + logf(sum), sum};
 }
 
 // Accumulated weights: a thread four slots of one sequence and kv head, over all query rows, whose scores the attention left behind
-constexpr int kWeightSlots = 1024;
-__global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args a, int chunks)
+__device__ __forceinline__ void add_weights(const cache_attention_args& a, int id, int chunks)
 {
-    __shared__ float lse[256];                                 // of 256 rows at a time: maximum + log(sum), inf where nothing is seen
+    constexpr int MOST = 256;
+    __shared__ float lse[MOST];                                // of that many rows at a time: maximum + log(sum), inf where nothing is seen
     const cache_args& c = a.c;
-    const int tid = threadIdx.x;
-    int id = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int chunk = id % chunks;
     id /= chunks;
     const int head = id % c.kv_heads, seq = id / c.kv_heads;
     const cache_rows rows = rows_of(c, seq);
     const int length = length_of(c, seq), R = min(rows.count, c.max_new) * a.group;
-    if (R == 0 || chunk * kWeightSlots >= length) return;
+    if (R == 0 || (int64_t)chunk * kWeightSlots >= length) return;
+    auto row_at = [&](int row) { return (int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group; };
+    const int share = a.splits >= 64 ? 6 : 32 - __builtin_clz(max(a.splits, 1) * 2 - 1) - 1, lanes = 1 << share;      // 2^share lanes a row
     const int slot = chunk * kWeightSlots + 4 * tid;
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int r0 = 0; r0 < R; r0 += 256) {
+    for (int r0 = 0; r0 < R; r0 += MOST) {
+        const int n = min(MOST, R - r0);
         __syncthreads();
-        if (r0 + tid < R) {
-            const int row = r0 + tid;
-            const float2 st = a.stats[((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.splits];
-            lse[tid] = a.splits > 1 ? st.x : st.y == 0.f ? INFINITY : st.x + logf(st.y);
+        for (int j0 = wave << (6 - share); j0 < n; j0 += kFinishWaves << (6 - share)) {
+            const int j = j0 + (lane >> share);
+            const float2* const st = a.stats + row_at(r0 + min(j, n - 1)) * a.splits;
+            float top = -INFINITY, all = 0.f;
+            for (int s = lane & (lanes - 1); s < a.splits; s += lanes) top = fmaxf(top, st[s].x);
+            for (int off = lanes >> 1; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+            for (int s = lane & (lanes - 1); s < a.splits; s += lanes) all += st[s].y == 0.f ? 0.f : st[s].y * exp_of(st[s].x - top);
+            for (int off = lanes >> 1; off > 0; off >>= 1) all += __shfl_xor(all, off, 64);
+            if (j < n && (lane & (lanes - 1)) == 0) lse[j] = all == 0.f ? INFINITY : top + logf(all);
         }
         __syncthreads();
-        const int n = min(256, R - r0);
         if (slot >= length) continue;
 #pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const int row = r0 + j, sees = length - rows.count + row / a.group + 1 - slot;       // of the four, the first so many
-            const int64_t at = ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + slot;
-            const float4 x = *reinterpret_cast<const float4*>(a.scores + at);                    // (not written where it sees nothing)
+            const float4 x = *reinterpret_cast<const float4*>(a.scores + row_at(row) * a.score_stride + slot);       // (not written where it sees nothing)
             sum[0] += sees > 0 ? exp_of(x.x - lse[j]) : 0.f;
             sum[1] += sees > 1 ? exp_of(x.y - lse[j]) : 0.f;
             sum[2] += sees > 2 ? exp_of(x.z - lse[j]) : 0.f;
@@ -565,6 +569,14 @@ __global__ __launch_bounds__(256) void cache_weight_kernel(cache_attention_args 
     if (p < 0) return;
     float* const w = c.weight + (p * c.kv_heads + head) * c.page_tokens + slot - page * c.page_tokens;
     for (int e = 0; e < min(4, length - slot); ++e) w[e] = a.decay == 0.f ? sum[e] : a.decay * w[e] + sum[e];
+}
+
+template <typename T>
+__global__ __launch_bounds__(kFinishThreads) void cache_finish_kernel(cache_attention_args a, int rows, int chunks)
+{
+    const int id = blockIdx.x;
+    if (id < rows) join_row<T>(a, id);
+    else add_weights(a, id - rows, chunks);
 }
 
 template <typename T, int DP, int CT, int WAVES>
@@ -593,14 +605,11 @@ hipError_t launch_all(const cache_attention_args& a, hipStream_t stream)
         default: launch_main<T, 256>(a, stream);
     }
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && a.splits > 1) {
-        const int64_t rows = (int64_t)a.c.num_seqs * a.c.max_new * a.num_heads;
-        LORA_LAUNCH(LORA_K_CACHE_JOIN, (cache_join_kernel<T>), dim3((uint32_t)rows), dim3(kJoinThreads), 0, stream, a);
-        e = hipGetLastError();
-    }
-    if (e == hipSuccess && a.scores) {
-        const int chunks = (a.c.max_length + kWeightSlots - 1) / kWeightSlots;
-        LORA_LAUNCH(LORA_K_CACHE_WEIGHT, cache_weight_kernel, dim3((uint32_t)(a.c.num_seqs * a.c.kv_heads * chunks)), dim3(256), 0, stream, a, chunks);
+    const int64_t rows = a.splits > 1 ? (int64_t)a.c.num_seqs * a.c.max_new * a.num_heads : 0;
+    const int chunks = a.scores ? (a.c.max_length + kWeightSlots - 1) / kWeightSlots : 0;
+    const int64_t last = rows + (int64_t)a.c.num_seqs * a.c.kv_heads * chunks;
+    if (e == hipSuccess && last > 0) {
+        LORA_LAUNCH(LORA_K_CACHE_FINISH, (cache_finish_kernel<T>), dim3((uint32_t)last), dim3(kFinishThreads), 0, stream, a, (int)rows, chunks);
         e = hipGetLastError();
     }
     return e;

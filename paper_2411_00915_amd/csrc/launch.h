@@ -37,8 +37,7 @@ enum lora_kernel_id {
     LORA_K_CACHE_APPEND,
     LORA_K_CACHE_READ,
     LORA_K_CACHE_ATTENTION,
-    LORA_K_CACHE_JOIN,
-    LORA_K_CACHE_WEIGHT,
+    LORA_K_CACHE_FINISH,
     LORA_K_CACHE_SELECT,
     LORA_K_CACHE_MOVE,
     LORA_K_PROBE_EMPTY,
