@@ -282,9 +282,9 @@ bool rows_aligned(const void* k, int64_t ldk, const void* v, int64_t ldv, int32_
 // ---------------------------------------------------------------------------
 // Eviction, first step: a workgroup per sequence and head finds what is kept.  The weights as whole numbers in their order, NaN
 // above all; the budget-th largest of them by three passes over their bits (histograms of 11, 11 and 10), then the slots in
-// order: above it, all; equal to it, the first few.  A thread keeps its numbers in registers, STEPS of them (0: they are read
-// again in every pass).  Many weights share their first bits, the exponent's: a wavefront adds those of its first lane's bin in
-// one go.
+// order: above it, all; equal to it, the first few.  A thread has four slots in a row at a time (one address, one load), 4 STEPS
+// in all, whose numbers stay in registers (STEPS 0: they are read again in every pass).  Many weights share their first bits,
+// the exponent's: a wavefront adds those of its first lane's bin in one go.
 __device__ __forceinline__ uint32_t order_of(float w)
 {
     if (w != w) return 0xffffffffu;
@@ -292,14 +292,30 @@ __device__ __forceinline__ uint32_t order_of(float w)
     return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-__device__ __forceinline__ uint32_t key_at(const cache_args& c, int s, int head, int slot)
+// of the slots slot .. slot + 3 (in one page: below `end`, slot is a multiple of 4); 0, which no weight gives, from `end` on
+__device__ __forceinline__ void keys_at(const cache_args& c, int s, int head, int slot, int end, uint32_t* keys)
 {
-    const int page = page_number(c, slot);
-    const int64_t id = page_of(c, s, page);
-    return id < 0 ? order_of(0.f) : order_of(c.weight[(id * c.kv_heads + head) * c.page_tokens + slot - page * c.page_tokens]);
+    struct __attribute__((packed, aligned(4))) four { float w[4]; } x = {};
+    if (slot < end) {
+        const int page = page_number(c, slot);
+        const int64_t id = page_of(c, s, page);
+        if (id >= 0) x = *reinterpret_cast<const four*>(c.weight + (id * c.kv_heads + head) * c.page_tokens + slot - page * c.page_tokens);
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) keys[e] = e < end - slot ? order_of(x.w[e]) : 0u;
 }
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+// how many lanes before this one are in the mask, on top of n
+__device__ __forceinline__ int lanes_before(uint64_t mask, int n)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, (uint32_t)n));
+#else
+    return n;
+#endif
+}
+
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kSelectStep = 4 * kSelectThreads;
 template <int STEPS>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args c, int32_t* target_length, int budget, int recent, int32_t* kept)
 {
@@ -317,19 +333,22 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
     const int old = length - recent, wanted = budget - recent; // (wanted < old)
     for (int i = tid; i < recent; i += kSelectThreads) out[wanted + i] = old + i;
     if (wanted == 0) return;
-    uint32_t keys[STEPS > 0 ? STEPS : 1];                      // slots tid, tid + 1024 ...  (the launch sees to it that they are enough)
+    uint32_t held[STEPS > 0 ? STEPS : 1][4];                   // (the launch sees to it that STEPS are enough)
     if constexpr (STEPS > 0)
 #pragma unroll
-        for (int n = 0; n < STEPS; ++n) keys[n] = n * kSelectThreads + tid < old ? key_at(c, s, head, n * kSelectThreads + tid) : 0u;
-    const int steps = (old + kSelectThreads - 1) / kSelectThreads;
-    // f(step, slot, key), slots of a step in the order of the threads
+        for (int n = 0; n < STEPS; ++n) keys_at(c, s, head, n * kSelectStep + 4 * tid, old, held[n]);
+    const int steps = (int)(((int64_t)old + kSelectStep - 1) / kSelectStep);
+    // f(step, keys), slots of a step in the order of the threads
     auto each = [&](auto f) {
         if constexpr (STEPS > 0) {
 #pragma unroll
             for (int n = 0; n < STEPS; ++n)
-                if (n < steps) f(n, n * kSelectThreads + tid, keys[n]);
+                if (n < steps) f(n, held[n]);
         } else
-            for (int n = 0; n < steps; ++n) f(n, n * kSelectThreads + tid, n * kSelectThreads + tid < old ? key_at(c, s, head, n * kSelectThreads + tid) : 0u);
+            for (int n = 0; n < steps; ++n) {
+                keys_at(c, s, head, (int)min((int64_t)n * kSelectStep + 4 * tid, (int64_t)old), old, held[0]);
+                f(n, held[0]);
+            }
     };
     if (tid == 0) { found[0] = 0; found[1] = (uint32_t)wanted; }
 #pragma unroll 1
@@ -337,20 +356,24 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
         const uint32_t digit = shift == 0 ? 1023u : 2047u;     // 11, 11 and 10 bits
         bins[tid] = bins[tid + kSelectThreads] = 0;
         __syncthreads();
-        const uint32_t prefix = found[0], still = found[1], above_digit = shift == 21 ? 0u : ~0u << (shift == 10 ? 21 : 10);
-        each([&](int, int i, uint32_t key) {
-            bool on = i < old && ((key ^ prefix) & above_digit) == 0;
-            const uint64_t any = __ballot(on);
-            if (!any) return;
-            const uint32_t at = key >> shift & digit;
-            if (shift == 21) {
-                const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)at, __ffsll((unsigned long long)any) - 1);
-                const uint64_t same = __ballot(on && at == first);
-                if (lane == 0) atomicAdd(&bins[first], __popcll(same));
-                on = on && at != first;
-            }
-            if (on) atomicAdd(&bins[at], 1);
-        });
+        const uint32_t prefix = found[0], still = found[1];
+        if (shift == 21)                                       // (keys of 0 are the only ones in bin 0, and what is wanted is above it)
+            each([&](int, const uint32_t* keys) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t at = keys[e] >> 21, first = (uint32_t)__builtin_amdgcn_readfirstlane((int)at);
+                    const int same = __popcll(__ballot(at == first));
+                    if (lane == 0 || at != first) atomicAdd(&bins[at], lane == 0 ? same : 1);
+                }
+            });
+        else {
+            const int fixed = shift == 10 ? 21 : 10;
+            each([&](int, const uint32_t* keys) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (keys[e] >> fixed == prefix >> fixed) atomicAdd(&bins[keys[e] >> shift & digit], 1);
+            });
+        }
         __syncthreads();
         // from the highest bin down, two a thread: the one at which what is wanted is reached
         const int b = 2047 - 2 * tid, high = bins[b], sum = high + bins[b - 1];
@@ -372,17 +395,31 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
         }
         __syncthreads();
     }
-    const uint32_t threshold = found[0];
+    const uint32_t threshold = found[0];                       // (not 0: keys of 0 are neither above it nor equal)
     const int ties = (int)found[1];                            // of the slots at the threshold, the first so many
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    auto put = [&](int i, uint32_t key, int above, int equal) { // above, equal: how many such come before this wavefront's
-        const bool is_above = i < old && key > threshold, is_equal = i < old && key == threshold;
-        const int a = above + __popcll(__ballot(is_above) & below), e = equal + __popcll(__ballot(is_equal) & below);
-        if (is_above || (is_equal && e < ties)) out[a + min(e, ties)] = i;
+    auto put = [&](int n, const uint32_t* keys, int above, int equal) {      // above, equal: how many such come before this wavefront's
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            above = lanes_before(__ballot(keys[e] > threshold), above);
+            equal = lanes_before(__ballot(keys[e] == threshold), equal);
+        }
+        const int slot = (int)((uint32_t)n * kSelectStep + 4u * tid);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool is_above = keys[e] > threshold, is_equal = keys[e] == threshold;
+            if (is_above || (is_equal && equal < ties)) out[above + min(equal, ties)] = slot + e;
+            above += is_above;
+            equal += is_equal;
+        }
     };
-    auto count = [&](int n, int i, uint32_t key) {
-        const int a = __popcll(__ballot(i < old && key > threshold)), e = __popcll(__ballot(i < old && key == threshold));
-        if (lane == 0) { counts[0][n * kSelectWaves + wave] = a; counts[1][n * kSelectWaves + wave] = e; }
+    auto count = [&](int n, const uint32_t* keys) {
+        int a = 0, q = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            a += __popcll(__ballot(keys[e] > threshold));
+            q += __popcll(__ballot(keys[e] == threshold));
+        }
+        if (lane == 0) { counts[0][n * kSelectWaves + wave] = a; counts[1][n * kSelectWaves + wave] = q; }
     };
     if constexpr (STEPS > 0) {
         each(count);
@@ -402,12 +439,12 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
             }
         }
         __syncthreads();
-        each([&](int n, int i, uint32_t key) { put(i, key, counts[0][n * kSelectWaves + wave], counts[1][n * kSelectWaves + wave]); });
+        each([&](int n, const uint32_t* keys) { put(n, keys, counts[0][n * kSelectWaves + wave], counts[1][n * kSelectWaves + wave]); });
     } else {
         int above = 0, equal = 0;
-        each([&](int, int i, uint32_t key) {
+        each([&](int n, const uint32_t* keys) {
             __syncthreads();                                   // (the counts of the step before are read)
-            count(0, i, key);
+            count(0, keys);
             __syncthreads();
             int a = 0, e = 0;
             for (int w = 0; w < kSelectWaves; ++w) {
@@ -415,7 +452,7 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
                 above += counts[0][w];
                 equal += counts[1][w];
             }
-            put(i, key, a, e);
+            put(n, keys, a, e);
         });
     }
 }
@@ -506,8 +543,8 @@ hipError_t launch_cache_evict(const cache_args& c, const cache_args& to, int32_t
     const dim3 grid1((uint32_t)(c.num_seqs * c.kv_heads));
     const int32_t old = c.max_length - recent;
 #define SELECT(STEPS) LORA_LAUNCH(LORA_K_CACHE_SELECT, (cache_select_kernel<STEPS>), grid1, dim3(kSelectThreads), 0, stream, c, target_length, budget, recent, kept)
-    if (old <= 4 * kSelectThreads) SELECT(4);
-    else if (old <= 32 * kSelectThreads) SELECT(32);
+    if (old <= kSelectStep) SELECT(1);
+    else if (old <= 8 * kSelectStep) SELECT(8);
     else SELECT(0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || budget == 0) return e;
