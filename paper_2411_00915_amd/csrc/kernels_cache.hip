@@ -457,54 +457,59 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
     }
 }
 
-// Second step: the kept tokens' codes, words and weights, a workgroup 32 of them of a head.
+// Second step: the kept tokens' codes, words and weights, a workgroup kMoved of them of a head: three trips to memory (what is
+// kept, its pages, their contents).
+constexpr int kMoved = 64;
 template <int DP>
 __global__ __launch_bounds__(256) void cache_move_kernel(cache_args c, cache_args to, int budget, int tiles, const int32_t* kept)
 {
-    constexpr int E = DP / 16, W = (E + 7) / 8;
-    __shared__ tile_places from, where;
+    constexpr int E = DP / 16, W = (E + 7) / 8, N = kMoved / 16;
+    __shared__ int64_t from[kMoved], where[kMoved];            // the head's page (-1: nowhere)
+    __shared__ int from_at[kMoved], where_at[kMoved];
     const int tid = threadIdx.x, r = tid & 15;
     const int64_t group = blockIdx.x / tiles;                  // sequence and head
-    const int j0 = (int)(blockIdx.x - group * tiles) * kTile, s = (int)(group / c.kv_heads), head = (int)(group - (int64_t)s * c.kv_heads);
-    if (tid < kTile) {
+    const int j0 = (int)(blockIdx.x - group * tiles) * kMoved, s = (int)(group / c.kv_heads), head = (int)(group - (int64_t)s * c.kv_heads);
+    if (tid < kMoved) {
         const int j = j0 + tid, slot = j < budget ? kept[group * budget + j] : -1;
         int64_t src = -1, dst = -1;
-        int at = 0;
+        int at = 0, there = 0;
         if (slot >= 0 && slot < c.max_length) {
-            const int number = page_number(c, slot), there = page_number(c, j);
+            const int number = page_number(c, slot), page = page_number(c, j);
             at = slot - number * c.page_tokens;
+            there = j - page * c.page_tokens;
             src = page_of(c, s, number);
-            dst = page_of(to, s, there);
-            where.at[tid] = j - there * c.page_tokens;
+            dst = page_of(to, s, page);
         }
-        from.page[tid] = src < 0 ? -1 : src * c.kv_heads + head;
-        from.at[tid] = at;
-        where.page[tid] = dst < 0 ? -1 : dst * c.kv_heads + head;
+        from[tid] = src < 0 ? -1 : src * c.kv_heads + head;
+        from_at[tid] = at;
+        where[tid] = dst < 0 ? -1 : dst * c.kv_heads + head;
+        where_at[tid] = there;
     }
     __syncthreads();
-    uint32_t v[2][W], k[2][W], words[2];                       // (a page that is not there reads as zeros)
-    float weight[2];
+    uint32_t v[N][W], k[N][W], words[N];                       // (a page that is not there reads as zeros)
+    float weight[N];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int i = tid & 31, q = (tid >> 5) + 8 * h, j = (tid >> 4) + 16 * h;
-        const bool there = from.page[j] >= 0;
-        const unsigned char* const src = c.pages + max(from.page[j], (int64_t)0) * c.page_bytes;
+    for (int h = 0; h < N; ++h) {
+        const int at = tid + 256 * h, i = (at >> 7) * 8 + (at & 7), q = at >> 3 & 15, j = (tid >> 4) + 16 * h;      // values in the target's order
+        const int64_t page = from[j];
+        const unsigned char* const src = c.pages + max(page, (int64_t)0) * c.page_bytes;
 #pragma unroll
         for (int w = 0; w < W; ++w) v[h][w] = k[h][w] = 0;
-        if (from.page[i] >= 0) load_codes<DP>(c.pages + from.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, from.at[i], q), v[h]);
-        if (there) load_codes<DP>(src + key_offset<DP>(from.at[j], r), k[h]);
-        words[h] = there && r < 2 ? *reinterpret_cast<const uint32_t*>(src + word_offset<DP>(c.page_tokens, from.at[j], r & 1)) : 0u;
-        weight[h] = there && r == 2 ? c.weight[from.page[j] * c.page_tokens + from.at[j]] : 0.f;
+        if (from[i] >= 0) load_codes<DP>(c.pages + from[i] * c.page_bytes + value_offset<DP>(c.page_tokens, from_at[i], q), v[h]);
+        if (page >= 0) load_codes<DP>(src + key_offset<DP>(from_at[j], r), k[h]);
+        words[h] = page >= 0 && r < 2 ? *reinterpret_cast<const uint32_t*>(src + word_offset<DP>(c.page_tokens, from_at[j], r & 1)) : 0u;
+        weight[h] = page >= 0 && r == 2 ? c.weight[page * c.page_tokens + from_at[j]] : 0.f;
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int i = tid & 31, q = (tid >> 5) + 8 * h, j = (tid >> 4) + 16 * h;
-        if (where.page[i] >= 0) store_codes<DP>(to.pages + where.page[i] * c.page_bytes + value_offset<DP>(c.page_tokens, where.at[i], q), v[h]);
-        if (where.page[j] < 0) continue;
-        unsigned char* const dst = to.pages + where.page[j] * c.page_bytes;
-        store_codes<DP>(dst + key_offset<DP>(where.at[j], r), k[h]);
-        if (r < 2) *reinterpret_cast<uint32_t*>(dst + word_offset<DP>(c.page_tokens, where.at[j], r)) = words[h];
-        if (r == 2) to.weight[where.page[j] * c.page_tokens + where.at[j]] = weight[h];
+    for (int h = 0; h < N; ++h) {
+        const int at = tid + 256 * h, i = (at >> 7) * 8 + (at & 7), q = at >> 3 & 15, j = (tid >> 4) + 16 * h;      // values in the target's order
+        if (where[i] >= 0) store_codes<DP>(to.pages + where[i] * c.page_bytes + value_offset<DP>(c.page_tokens, where_at[i], q), v[h]);
+        const int64_t page = where[j];
+        if (page < 0) continue;
+        unsigned char* const dst = to.pages + page * c.page_bytes;
+        store_codes<DP>(dst + key_offset<DP>(where_at[j], r), k[h]);
+        if (r < 2) *reinterpret_cast<uint32_t*>(dst + word_offset<DP>(c.page_tokens, where_at[j], r)) = words[h];
+        if (r == 2) to.weight[page * c.page_tokens + where_at[j]] = weight[h];
     }
 }
 
@@ -548,7 +553,7 @@ hipError_t launch_cache_evict(const cache_args& c, const cache_args& to, int32_t
     else SELECT(0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || budget == 0) return e;
-    const int32_t tiles = tiles_of(budget);
+    const int32_t tiles = budget / kMoved + (budget % kMoved != 0);
     const dim3 grid((uint32_t)(c.num_seqs * c.kv_heads * tiles));
 #define MOVE(DP, UNUSED) LORA_LAUNCH(LORA_K_CACHE_MOVE, (cache_move_kernel<DP>), grid, dim3(256), 0, stream, c, to, budget, tiles, kept)
     BY_HEAD_DIM(MOVE, )
