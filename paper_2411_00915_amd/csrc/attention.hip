@@ -31,13 +31,12 @@ lora_status ensure_uploaded(lora_attention_plan* p, hipStream_t stream)
     int dev = -1;
     if (hipGetDevice(&dev) != hipSuccess) return LORA_ERR_DEVICE;
     if (p->d_buf) return p->device == dev ? LORA_OK : LORA_ERR_INVALID_ARG;      // a plan lives on one device
-    const size_t tiles = p->tiles.size() * sizeof(attention_tile), items = p->items.size() * sizeof(attention_tile), bytes = std::max<size_t>(tiles + items, 64);
+    const size_t items = p->items.size() * sizeof(attention_tile), bytes = std::max<size_t>(items, 64);
     size_t cls = 0;
     void *dbuf = nullptr, *hbuf = nullptr;
     const lora_status st = lora_take_tables(dev, bytes, &cls, &dbuf, &hbuf);
     if (st != LORA_OK) return st;
-    std::memcpy(hbuf, p->tiles.data(), tiles);
-    std::memcpy(static_cast<char*>(hbuf) + tiles, p->items.data(), items);
+    std::memcpy(hbuf, p->items.data(), items);
     if (hipMemcpyAsync(dbuf, hbuf, bytes, hipMemcpyHostToDevice, stream) != hipSuccess) {
         (void)hipGetLastError();
         lora_give_tables(dev, cls, dbuf, hbuf);
@@ -114,7 +113,7 @@ extern "C" lora_status lora_attention(lora_attention_plan* p, const void* q, int
                                       void* o, int64_t ldo, float scale, void* hip_stream)
 {
     if (!p || !std::isfinite(scale)) return LORA_ERR_INVALID_ARG;
-    if (p->tiles.empty()) return LORA_OK;
+    if (p->items.empty()) return LORA_OK;
     const int64_t q_row = (int64_t)p->num_heads * p->head_dim, kv_row = (int64_t)p->num_kv_heads * p->head_dim;
     const size_t e = elem_bytes(p->dtype);
     if (!q || !o || ldq < q_row || ldo < q_row || misaligned(q, e) || misaligned(o, e)) return LORA_ERR_INVALID_ARG;
@@ -122,10 +121,9 @@ extern "C" lora_status lora_attention(lora_attention_plan* p, const void* q, int
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const lora_status st = ensure_uploaded(p, stream);
     if (st != LORA_OK) return st;
-    const attention_tile* const tiles = static_cast<const attention_tile*>(p->d_buf);
-    const attention_args a{tiles, tiles + p->tiles.size(), (int32_t)p->tiles.size(), (int32_t)p->items.size(), p->num_heads, p->num_heads / p->num_kv_heads,
-                           p->head_dim, q, k, v, o, ldq, ldk, ldv, ldo, scale};
-    return status_of(attention_tiled_supported(a, p->dtype) ? launch_attention_tiled(a, p->dtype, stream) : launch_attention_general(a, p->dtype, stream));
+    const attention_args a{static_cast<const attention_tile*>(p->d_buf), (int32_t)p->items.size(), p->num_heads / p->num_kv_heads, p->head_dim,
+                           q, k, v, o, ldq, ldk, ldv, ldo, scale};
+    return status_of(launch_attention(a, p->dtype, stream));
 }
 
 extern "C" lora_status lora_cache_append(const lora_cache* c, int32_t dtype, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr, const void* k,

@@ -6,19 +6,15 @@
 #include "attention_internal.h"
 
 struct attention_args {
-    const attention_tile* tiles;
     const attention_tile* items;
-    int32_t num_tiles, num_items, num_heads, group, head_dim;      // group: query heads of a kv head
+    int32_t num_items, group, head_dim;      // group: query heads of a kv head
     const void *q, *k, *v;
     void* o;
     int64_t ldq, ldk, ldv, ldo;
     float scale;
 };
 
-hipError_t launch_attention_general(const attention_args& a, int32_t dtype, hipStream_t stream);
-// 16-byte aligned rows and heads
-bool attention_tiled_supported(const attention_args& a, int32_t dtype);
-hipError_t launch_attention_tiled(const attention_args& a, int32_t dtype, hipStream_t stream);
+hipError_t launch_attention(const attention_args& a, int32_t dtype, hipStream_t stream);
 
 // What the kernels of the cache take: the descriptor's fields by value
 struct cache_args {

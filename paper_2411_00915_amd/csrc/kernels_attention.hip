@@ -9,69 +9,8 @@
 #include "mfma_tile.h"
 
 // ---------------------------------------------------------------------------
-// Any layout, dtype and head_dim: a wavefront per query and head.  Keys in steps of 64, one a lane for the scores; then lanes
-// are dims, and the softmax weights go round by shuffles.  Keys that the query does not see are not read.
-namespace {
-template <typename T>
-__global__ __launch_bounds__(256) void attention_general_kernel(attention_args a)
-{
-    const int64_t id = blockIdx.x;
-    const attention_tile t = a.tiles[id / a.num_heads];
-    const int head = (int)(id % a.num_heads), lane = threadIdx.x & 63, D = a.head_dim;
-    const T* const kb = static_cast<const T*>(a.k) + (int64_t)t.kv_row0 * a.ldk + (int64_t)(head / a.group) * D;
-    const T* const vb = static_cast<const T*>(a.v) + (int64_t)t.kv_row0 * a.ldv + (int64_t)(head / a.group) * D;
-    for (int i = threadIdx.x >> 6; i < t.rows; i += 4) {
-        const T* const q = static_cast<const T*>(a.q) + (int64_t)(t.q_row0 + i) * a.ldq + (int64_t)head * D;
-        const int sees = max(0, min(t.num_kv, t.ahead + i + 1));
-        float o[4] = {0.f, 0.f, 0.f, 0.f}, m = -INFINITY, l = 0.f;
-        for (int j0 = 0; j0 < sees; j0 += 64) {
-            const int n = min(64, sees - j0);
-            float x = -INFINITY;
-            if (lane < n) {
-                const T* const k = kb + (int64_t)(j0 + lane) * a.ldk;
-                float s = 0.f;
-                for (int d = 0; d < D; ++d) s += elem<T>::load(q + d) * elem<T>::load(k + d);
-                x = s * a.scale;
-            }
-            float mx = x;
-#pragma unroll
-            for (int off = 32; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor(mx, off, 64));
-            mx = fmaxf(m, mx);
-            const float ref = mx == -INFINITY ? 0.f : mx, alpha = m == -INFINITY ? 0.f : expf(m - ref);
-            const float p = lane < n ? expf(x - ref) : 0.f;
-            m = mx;
-            l = l * alpha + wave_sum(p);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) o[c] *= alpha;
-            for (int j = 0; j < n; ++j) {
-                const float pj = __shfl(p, j, 64);
-                const T* const v = vb + (int64_t)(j0 + j) * a.ldv;
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (lane + 64 * c < D) o[c] += pj * elem<T>::load(v + lane + 64 * c);
-            }
-        }
-        T* const out = static_cast<T*>(a.o) + (int64_t)(t.q_row0 + i) * a.ldo + (int64_t)head * D;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (lane + 64 * c < D) elem<T>::store(out + lane + 64 * c, l == 0.f ? 0.f : o[c] / l);
-    }
-}
-}  // namespace
-
-hipError_t launch_attention_general(const attention_args& a, int32_t dtype, hipStream_t stream)
-{
-    const dim3 grid((uint32_t)((int64_t)a.num_tiles * a.num_heads));
-    if (dtype == LORA_F32)
-        LORA_LAUNCH(LORA_K_ATTENTION_GENERAL, (attention_general_kernel<float>), grid, dim3(256), 0, stream, a);
-    else
-        LORA_LAUNCH(LORA_K_ATTENTION_GENERAL, (attention_general_kernel<bf16_t>), grid, dim3(256), 0, stream, a);
-    return hipGetLastError();
-}
-
-// ---------------------------------------------------------------------------
-// Aligned prompts, on the matrix cores.  A workgroup takes up to 128 queries of one head, 32 a wavefront; keys and values come
-// in tiles of BK tokens, straight to LDS, one tile ahead of the products.
+// A workgroup takes up to 128 queries of one head, 32 a wavefront; keys and values come in tiles of BK tokens, one tile ahead of
+// the products: straight to LDS where rows and heads are ALIGNED to 16 bytes, else element by element through registers.
 //
 //     S^T = K Q^T     keys are the rows of the product, so that a lane ends with 16 (of 32) keys of one query, and maximum and
 //                     sum of the softmax meet in two lanes only
@@ -129,6 +68,26 @@ __device__ __forceinline__ int value_place(int c, int row)        // its own inv
     else return c ^ (row & 3) << 2;
 }
 
+// 16 bytes of elements, of which there are n
+template <typename T>
+__device__ __forceinline__ uint4 load_elements(const T* p, int n)
+{
+    constexpr int E = 16 / (int)sizeof(T);
+    uint32_t u[4] = {};
+    auto take = [&](int i) {
+        if constexpr (sizeof(T) == 4) u[i] = __float_as_uint(p[i]);
+        else u[i / 2] |= (uint32_t)p[i] << 16 * (i & 1);
+    };
+    if (n >= E)
+#pragma unroll
+        for (int i = 0; i < E; ++i) take(i);
+    else
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+            if (i < n) take(i);
+    return uint4{u[0], u[1], u[2], u[3]};
+}
+
 // two bf16, infinities and NaN as 0
 __device__ __forceinline__ uint32_t finite_or_zero(uint32_t u)
 {
@@ -146,7 +105,7 @@ __device__ __forceinline__ float max_of_halves(float x)
 #endif
 }
 
-template <typename T, int DP, int BK>
+template <typename T, int DP, int BK, bool ALIGNED>
 __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel(attention_args a)
 {
     constexpr bool F32 = sizeof(T) == 4;
@@ -176,6 +135,20 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     }
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(lds)) + wave * (LOADS * 1024);
     auto fetch = [&](int n) {
+        if constexpr (!ALIGNED) {
+#pragma unroll 2
+            for (int i = 0; i < LOADS; ++i) {
+                const int p = (wave * LOADS + i) * 64 + lane, row = p / CH, place = p % CH;
+                const int kd = key_chunk<T, DP>(place, row) * (16 / (int)sizeof(T)), vd = value_place<T, DP>(place, row) * (16 / (int)sizeof(T));
+                const bool there = n * BK + row < t.num_kv;
+                const int64_t token = (int64_t)n * BK + (there ? row : 0);
+                const uint4 k = load_elements(reinterpret_cast<const T*>(kb) + token * a.ldk + kd, there ? D - kd : 0);
+                const uint4 v = load_elements(reinterpret_cast<const T*>(vb) + token * a.ldv + vd, there ? D - vd : 0);
+                *reinterpret_cast<uint4*>(lds[n & 1][0] + p * 16) = k;
+                *reinterpret_cast<uint4*>(lds[n & 1][1] + p * 16) = v;
+            }
+            return;
+        }
         const int64_t left = (int64_t)t.num_kv - (int64_t)n * BK;          // rows; the last ends with its head
         tile_source s;
         s.set(kb + (int64_t)n * BK * kpitch, (left - 1) * kpitch + (int64_t)D * (int)sizeof(T));
@@ -198,8 +171,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 #pragma unroll
         for (int c = 0; c < QR / 4; ++c) {
             const int d = 8 * c + 4 * half;
-            const float4 x = valid && d < D ? *reinterpret_cast<const float4*>(qp + d) : float4{0.f, 0.f, 0.f, 0.f};
-            qf[4 * c] = x.x; qf[4 * c + 1] = x.y; qf[4 * c + 2] = x.z; qf[4 * c + 3] = x.w;
+            const uint4 x = !ALIGNED ? load_elements(qp + d, valid ? D - d : 0) : valid && d < D ? *reinterpret_cast<const uint4*>(qp + d) : uint4{0, 0, 0, 0};
+            qf[4 * c] = __uint_as_float(x.x); qf[4 * c + 1] = __uint_as_float(x.y); qf[4 * c + 2] = __uint_as_float(x.z); qf[4 * c + 3] = __uint_as_float(x.w);
         }
         if (a.scale < 0.f)
 #pragma unroll
@@ -209,7 +182,7 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 #pragma unroll
         for (int s = 0; s < QR; ++s) {
             const int d = 16 * s + 8 * half;
-            uint4 u = valid && d < D ? ld16(reinterpret_cast<const bf16_t*>(qp) + d) : uint4{0, 0, 0, 0};
+            const uint4 u = !ALIGNED ? load_elements(qp + d, valid ? D - d : 0) : valid && d < D ? ld16(reinterpret_cast<const bf16_t*>(qp) + d) : uint4{0, 0, 0, 0};
             qb[s].u = uint4{u.x ^ sign, u.y ^ sign, u.z ^ sign, u.w ^ sign};
         }
     }
@@ -395,7 +368,12 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
 #pragma unroll
             for (int i = 0; i < 16; i += 4) {
                 const int at = 32 * d + 2 * i + 4 * half;
-                if (valid && at < D) *reinterpret_cast<float4*>(out + at) = float4{acc[d][i] * inv, acc[d][i + 1] * inv, acc[d][i + 2] * inv, acc[d][i + 3] * inv};
+                if constexpr (!ALIGNED) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (valid && at + e < D) out[at + e] = acc[d][i + e] * inv;
+                } else if (valid && at < D)
+                    *reinterpret_cast<float4*>(out + at) = float4{acc[d][i] * inv, acc[d][i + 1] * inv, acc[d][i + 2] * inv, acc[d][i + 3] * inv};
             }
         } else {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -407,34 +385,38 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
                 for (int e = 0; e < 4; ++e) u[e] = pack_bf16(acc[d][i + 2 * e] * inv, acc[d][i + 2 * e + 1] * inv);
                 const auto x = __builtin_amdgcn_permlane32_swap(u[0], u[2], false, false), y = __builtin_amdgcn_permlane32_swap(u[1], u[3], false, false);
                 const int at = 32 * d + 2 * i + 8 * half;
-                if (valid && at < D) *reinterpret_cast<uint4*>(out + at) = uint4{x[0], y[0], x[1], y[1]};
+                if constexpr (!ALIGNED) {
+                    const uint32_t w[4] = {x[0], y[0], x[1], y[1]};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (valid && at + e < D) out[at + e] = (bf16_t)(w[e / 2] >> 16 * (e & 1));
+                } else if (valid && at < D)
+                    *reinterpret_cast<uint4*>(out + at) = uint4{x[0], y[0], x[1], y[1]};
             }
 #endif
         }
 }
 }  // namespace
 
-bool attention_tiled_supported(const attention_args& a, int32_t dtype)
+hipError_t launch_attention(const attention_args& a, int32_t dtype, hipStream_t stream)
 {
-    const int64_t es = dtype == LORA_F32 ? 4 : 2, most = (int64_t)1 << 24;      // (a tile's rows have to lie within 2 GB)
+    const int64_t es = dtype == LORA_F32 ? 4 : 2, most = (int64_t)1 << 25;      // (a tile's rows have to lie within 2 GB)
     const uintptr_t all = reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(a.o) |
                           (uintptr_t)((a.ldq | a.ldk | a.ldv | a.ldo | a.head_dim) * es);
-    return (all & 15) == 0 && a.ldk * es < 2 * most && a.ldv * es < 2 * most;
-}
-
-hipError_t launch_attention_tiled(const attention_args& a, int32_t dtype, hipStream_t stream)
-{
+    const bool aligned = (all & 15) == 0 && a.ldk * es < most && a.ldv * es < most;
     const dim3 grid((uint32_t)a.num_items);
-#define TILED(T, DP, BK) LORA_LAUNCH(LORA_K_ATTENTION_TILED, (attention_tiled_kernel<T, DP, BK>), grid, dim3(256), 0, stream, a)
+#define TILED(T, DP, BK)                                                                                                                    \
+    if (aligned) LORA_LAUNCH(LORA_K_ATTENTION_TILED, (attention_tiled_kernel<T, DP, BK, true>), grid, dim3(256), 0, stream, a);             \
+    else LORA_LAUNCH(LORA_K_ATTENTION_UNALIGNED, (attention_tiled_kernel<T, DP, BK, false>), grid, dim3(256), 0, stream, a)
     if (dtype == LORA_F32) {
-        if (a.head_dim <= 64) TILED(float, 64, 32);
-        else if (a.head_dim <= 128) TILED(float, 128, 32);
-        else TILED(float, 256, 32);
+        if (a.head_dim <= 64) { TILED(float, 64, 32); }
+        else if (a.head_dim <= 128) { TILED(float, 128, 32); }
+        else { TILED(float, 256, 32); }
     } else {
-        if (a.head_dim <= 64) TILED(bf16_t, 64, 64);
-        else if (a.head_dim <= 96) TILED(bf16_t, 96, 64);
-        else if (a.head_dim <= 128) TILED(bf16_t, 128, 64);
-        else TILED(bf16_t, 256, 32);
+        if (a.head_dim <= 64) { TILED(bf16_t, 64, 64); }
+        else if (a.head_dim <= 96) { TILED(bf16_t, 96, 64); }
+        else if (a.head_dim <= 128) { TILED(bf16_t, 128, 64); }
+        else { TILED(bf16_t, 256, 32); }
     }
     return hipGetLastError();
 }

@@ -32,8 +32,8 @@ enum lora_kernel_id {
     LORA_K_SHRINK_ROWS,
     LORA_K_EXPAND_ROWS,
     LORA_K_DELTA_F32,
-    LORA_K_ATTENTION_GENERAL,
     LORA_K_ATTENTION_TILED,
+    LORA_K_ATTENTION_UNALIGNED,
     LORA_K_CACHE_APPEND,
     LORA_K_CACHE_READ,
     LORA_K_CACHE_ATTENTION,
