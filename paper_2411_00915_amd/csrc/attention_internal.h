@@ -12,7 +12,7 @@ struct attention_tile {
     int32_t num_kv;      // keys of the sequence
     int32_t ahead;       // query i of the tile sees the keys [0, clamp(ahead + i + 1, 0, num_kv)); not causal: num_kv all along
     int32_t max_kv;      // keys that the last query sees
-    int32_t heads;       // heads of one kv head that a workgroup takes together: 1, or 2 or 4 where the queries are few (tiled kernel)
+    int32_t heads;       // heads of one kv head that a workgroup takes together: 1, or 2 or 4 where the queries are few (a tile: at most so many)
     int32_t head;        // in a workgroup's item: the first of its heads
 };
 

@@ -24,21 +24,31 @@ bool order_items(lora_attention_plan* p)
     constexpr int X = 8;
     std::vector<attention_tile> list[X];
     int64_t cost[X] = {};
-    auto add = [&](int x, int32_t tile, int32_t head) {
+    auto add = [&](int x, int32_t tile, int32_t head, int32_t heads) {
         list[x].push_back(p->tiles[tile]);
         list[x].back().head = head;
+        list[x].back().heads = heads;
         cost[x] += (int64_t)p->tiles[tile].max_kv + 64;
     };
     const int32_t H = p->num_heads, group = H / p->num_kv_heads, T = (int32_t)p->tiles.size();
-    // runs of heads that belong together stay together: of 4, 2 or 1 (as many as a tile may take)
-    const int32_t unit = group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1, units = H / unit, whole = units / X;
+    // Runs of heads that belong together stay together: of 4, 2 or 1, of which a tile takes as many as it may -- but one by one
+    // where that makes no more than two workgroups a compute unit (4 requests of 20 queries behind 1000 keys, 32 heads on 8: 17.0 us
+    // by four, 16.2 by one).  Where most tiles have few queries, and 4 does not divide the heads of a kv head, a run is all of
+    // them, taken by fours, twos and one (150 of 40 queries behind 1000 keys, 40 heads on 8: 324 us by one, 146 by four and one).
+    const bool many = (int64_t)T * H > 512;
+    const int64_t few = std::count_if(p->tiles.begin(), p->tiles.end(), [](const attention_tile& t) { return t.heads > 1; });
+    const int32_t unit = group % 4 == 0 ? 4 : many && 2 * few >= T ? group : group % 2 == 0 ? 2 : 1, units = H / unit, whole = units / X;
+    auto taken = [&](int32_t t, int32_t h) {                   // from head h of a run on
+        const int32_t left = unit - h;
+        return !many ? 1 : std::min(p->tiles[t].heads, left >= 4 ? 4 : left >= 2 ? 2 : 1);
+    };
     for (int32_t u = 0; u < whole * X; ++u)
         for (int32_t t = 0; t < T; ++t)
-            for (int32_t h = 0; h < unit; h += p->tiles[t].heads) add(u / whole, t, u * unit + h);
+            for (int32_t h = 0, n; h < unit; h += n) add(u / whole, t, u * unit + h, n = taken(t, h));
     for (int32_t t = 0; t < T; ++t)
         for (int32_t u = whole * X; u < units; ++u)
-            for (int32_t h = 0; h < unit; h += p->tiles[t].heads)
-                add((int)(std::min_element(cost, cost + X) - cost), t, u * unit + h);
+            for (int32_t h = 0, n; h < unit; h += n)
+                add((int)(std::min_element(cost, cost + X) - cost), t, u * unit + h, n = taken(t, h));
     size_t longest = 0;
     for (const auto& l : list) longest = std::max(longest, l.size());
     if (longest > LORA_ATTENTION_MAX_WORKGROUPS / X) return false;
@@ -78,7 +88,7 @@ extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, 
                 t.kv_row0 = kv[s];
                 t.num_kv = nk;
                 t.ahead = d->causal ? nk - nq + r : nk;
-                t.heads = group % 4 == 0 && t.rows <= LORA_ATTENTION_ROWS / 4 ? 4 : group % 2 == 0 && t.rows <= LORA_ATTENTION_ROWS / 2 ? 2 : 1;
+                t.heads = group == 1 ? 1 : t.rows <= LORA_ATTENTION_ROWS / 4 ? 4 : t.rows <= LORA_ATTENTION_ROWS / 2 ? 2 : 1;
                 t.max_kv = (int32_t)std::max<int64_t>(0, std::min<int64_t>(nk, (int64_t)t.ahead + t.rows));
                 p->tiles.push_back(t);
             }
