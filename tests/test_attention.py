@@ -175,6 +175,21 @@ def test_prompts_of_many_heads(dtype, H, Hkv):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,Hkv,pad", [(16, 4, 0), (40, 8, 0), (28, 4, 0), (12, 2, 0), (10, 5, 0), (9, 1, 0), (28, 4, 3)])
+def test_many_prompts_of_few_queries(dtype, H, Hkv, pad):
+    """Enough of them that a workgroup takes several heads of a tile: 4, 2 and 1 of groups of 4, 5, 7, 6, 2 and 9"""
+    rng = np.random.default_rng(H + Hkv)
+    nq = rng.integers(0, 34, 70).tolist() + [40, 64, 65]
+    nk = [max(0, n + int(rng.integers(-3, 60))) for n in nq]
+    plan = B.lora_attention_plan(offsets(nq), offsets(nk), H, Hkv, 64, dtype)
+    heads = B.lora_attention_plan_items(plan)[:, 6]
+    plan.destroy()
+    assert (heads == (2 if H // Hkv == 2 else 4)).any()
+    check_prompt(*prompt_case(rng, nq, nk, H, Hkv, 64, dtype), nq, nk, dtype, True, 0.125, pad=pad)
+
+
+@gpu
 def test_prompts_whose_rows_lie_beyond_4_gb():
     nk, D, ld = [20000, 40], 64, 120008
     rng = np.random.default_rng(21)
@@ -823,6 +838,21 @@ def test_a_plans_items_cover_every_query_of_every_head_once(H, Hkv, causal):
         unit = max((int(i[5]) + 64 for i in items if i[6]), default=0) * 4 * max(1, -(-len(items) // max(H, 1)))
         assert max(load) - min(load) <= unit
         plan.destroy()
+
+
+@pytest.mark.parametrize("group,runs", [(1, [1]), (2, [2]), (3, [2, 1]), (4, [4]), (5, [4, 1]), (6, [4, 2]), (7, [4, 2, 1]), (8, [4, 4]), (9, [4, 4, 1])])
+def test_heads_of_few_queries_go_together(group, runs):
+    plan = B.lora_attention_plan(np.arange(401) * 20, None, 2 * group, 2, 64, BF16)
+    items = B.lora_attention_plan_items(plan)
+    items = items[items[:, 6] > 0]
+    for kv in (0, 1):
+        first = items[(items[:, 0] == 0) & (items[:, 7] // group == kv)]
+        assert first[np.argsort(first[:, 7]), 6].tolist() == runs
+    plan.destroy()
+    plan = B.lora_attention_plan([0, 20], None, 2 * group, 2, 64, BF16)       # a chip that is not full: one by one
+    items = B.lora_attention_plan_items(plan)
+    assert set(items[items[:, 6] > 0, 6]) == {1}
+    plan.destroy()
 
 
 def test_plans_are_the_same_for_the_same_batch():
