@@ -18,7 +18,17 @@
 //                     LDS reads), tokens in the order that the first product left them in
 //
 // bf16: 32 x 32 x 16 products; fp32: 32 x 32 x 2 of exact products.  The softmax runs to base 2 (its factor goes with the
-// scale, in 32 bits) against a maximum that is raised only where a score is 2^8 above it.
+// scale, in 32 bits) against a maximum that is raised only where a weight would pass 2^8, and the weights' sum is that of the
+// weights before they are rounded.
+//
+// What bounds it, bf16: matrix cores and the softmax's vector instructions, which run beside each other only in part.  Two prompts
+// of 8192 tokens, 40 heads of 128: 1.32 ms, 1.04 PFLOP/s, matrix cores busy in 52 % of the cycles, vector units in 48 %, no bank
+// conflicts.  Four of 1024 tokens, 32 heads: 52 us, 0.66 PFLOP/s, with the last tiles' tail.  fp32: the matrix cores, a product of
+// which takes 64 cycles: 4096 tokens, 16 heads of 64, 152 us.  Rows that are not ALIGNED: 4096 tokens, 32 heads of 128, 125 us
+// against 63.
+// Why so: 32 queries are a product's width, and four wavefronts share what is in LDS; of 64 keys a tile there are half the barriers
+// and maxima (32: 1436 against 1315 us), and heads past 128 have room for 32.  Few queries leave wavefronts without work: the
+// plan gives those other heads of the same keys.
 namespace {
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
