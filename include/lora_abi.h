@@ -447,7 +447,7 @@ typedef struct {
     int64_t        num_pages;
     int32_t        num_seqs;
     int32_t        table_stride;
-    int32_t        max_length;     /* no sequence is longer; <= table_stride * page_tokens */
+    int32_t        max_length;     /* no sequence is longer; <= table_stride * page_tokens, at most 2^30 */
     int32_t        page_tokens;    /* multiple of 32, at most 1024 */
     int32_t        num_kv_heads;
     int32_t        head_dim;

@@ -58,7 +58,7 @@ lora_status check_cache(const lora_cache* c)
     if (c->num_seqs == 0) return LORA_OK;
     if (!c->pages || !c->page_table || !c->length) return LORA_ERR_INVALID_ARG;
     if (misaligned(c->pages, 16) || misaligned(c->weight, 4) || misaligned(c->page_table, 4) || misaligned(c->length, 4)) return LORA_ERR_INVALID_ARG;
-    if (c->num_pages >= (int64_t)1 << 31) return LORA_ERR_UNSUPPORTED;
+    if (c->num_pages >= (int64_t)1 << 31 || c->max_length > LORA_ATTENTION_MAX_ROWS) return LORA_ERR_UNSUPPORTED;
     return LORA_OK;
 }
 

@@ -1032,6 +1032,21 @@ def test_the_caches_calls_refuse_what_is_wrong():
     evict_refused(B.Plan(None, None), fake(**other))
 
 
+def test_caches_of_more_than_2_to_30_tokens_are_refused():
+    """(slots and the ends of splits are 32-bit numbers)"""
+    for length, status in ((2 ** 30 + 1, B.LORA_ERR_UNSUPPORTED), (2 ** 31 - 1, B.LORA_ERR_UNSUPPORTED)):
+        long = fake(max_length=length, table_stride=2 ** 25)
+        for call in (lambda: B.lora_cache_append(long, BF16, 2, 1, None, 4096, 128, 8192, 128, stream=0),
+                     lambda: B.lora_cache_read(long, BF16, 2, 1, None, 4096, 128, 8192, 128, stream=0),
+                     lambda: B.lora_cache_attention(long, BF16, 4, 2, 1, None, 4096, 256, 8192, 256, 1.0, -1.0, 1 << 24, 1 << 40, stream=0),
+                     lambda: B.lora_cache_workspace(long, 4, 2, 1),
+                     lambda: B.lora_cache_evict(long, fake(length=1 << 25), 100, 10, 4096, stream=0)):
+            with pytest.raises(B.LoraError) as e:
+                call()
+            assert e.value.status == status
+    assert B.lora_cache_workspace(fake(max_length=2 ** 30, table_stride=2 ** 24), 4, 2, 1) > 0
+
+
 def test_launches_of_too_many_threads_are_refused():
     """2^24 workgroups of 256 threads are more than a launch holds"""
     seqs = np.arange(2 ** 14 + 1, dtype=np.int32)
