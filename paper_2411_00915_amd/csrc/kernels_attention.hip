@@ -22,7 +22,7 @@
 // weights before they are rounded.
 //
 // What bounds it, bf16: matrix cores and the softmax's vector instructions, which run beside each other only in part.  Two prompts
-// of 8192 tokens, 40 heads of 128: 1.32 ms, 1.04 PFLOP/s, matrix cores busy in 52 % of the cycles, vector units in 48 %, no bank
+// of 8192 tokens, 40 heads of 128: 1.32 ms, 1.04 PFLOP/s, matrix cores busy in 53 % of the cycles, vector units in 48 %, no bank
 // conflicts.  Four of 1024 tokens, 32 heads: 52 us, 0.66 PFLOP/s, with the last tiles' tail.  fp32: the matrix cores, a product of
 // which takes 64 cycles: 4096 tokens, 16 heads of 64, 152 us.  Rows that are not ALIGNED: 4096 tokens, 32 heads of 128, 125 us
 // against 63.
