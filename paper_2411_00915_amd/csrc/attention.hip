@@ -121,7 +121,7 @@ extern "C" lora_status lora_attention(lora_attention_plan* p, const void* q, int
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const lora_status st = ensure_uploaded(p, stream);
     if (st != LORA_OK) return st;
-    const attention_args a{static_cast<const attention_tile*>(p->d_buf), (int32_t)p->items.size(), p->num_heads / p->num_kv_heads, p->head_dim,
+    const attention_args a{static_cast<const attention_tile*>(p->d_buf), (int32_t)p->items.size(), p->most_rows, p->num_heads / p->num_kv_heads, p->head_dim,
                            q, k, v, o, ldq, ldk, ldv, ldo, scale};
     return status_of(launch_attention(a, p->dtype, stream));
 }

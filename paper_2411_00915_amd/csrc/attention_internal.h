@@ -23,6 +23,7 @@ struct attention_tile {
 struct lora_attention_plan {
     int32_t num_heads = 0, num_kv_heads = 0, head_dim = 0, dtype = 0;
     int32_t num_queries = 0, num_keys = 0;
+    int32_t most_rows = LORA_ATTENTION_ROWS;      // of a tile, where wavefronts may share a tile's keys
     std::vector<attention_tile> tiles;      // most keys first
     std::vector<attention_tile> items;      // tiles with their heads, in the order of the workgroups of the tiled kernel; heads 0: nothing
 

@@ -36,6 +36,11 @@ bool order_items(lora_attention_plan* p)
     // by four, 16.2 by one).  Where most tiles have few queries, and 4 does not divide the heads of a kv head, a run is all of
     // them, taken by fours, twos and one (150 of 40 queries behind 1000 keys, 40 heads on 8: 324 us by one, 146 by four and one).
     const bool many = (int64_t)T * H > 512;
+    // No more workgroups than compute units, few queries each and many keys: the wavefronts of one share its keys (8 requests of 20
+    // queries behind 1000 keys, 32 heads on 8: 20.6 us without, 15.9 shared, fp32 133 and 79; 15 of them 22.7 and 26.8, as a
+    // compute unit then holds one workgroup; 70 keys: 6.8 and 7.7).
+    if (T > 0 && (int64_t)T * H <= 256 && p->tiles[0].max_kv > 256)
+        p->most_rows = std::max_element(p->tiles.begin(), p->tiles.end(), [](const attention_tile& a, const attention_tile& b) { return a.rows < b.rows; })->rows;
     const int64_t few = std::count_if(p->tiles.begin(), p->tiles.end(), [](const attention_tile& t) { return t.heads > 1; });
     const int32_t unit = group % 4 == 0 ? 4 : many && 2 * few >= T ? group : group % 2 == 0 ? 2 : 1, units = H / unit, whole = units / X;
     auto taken = [&](int32_t t, int32_t h) {                   // from head h of a run on

@@ -7,7 +7,7 @@
 
 struct attention_args {
     const attention_tile* items;
-    int32_t num_items, group, head_dim;      // group: query heads of a kv head
+    int32_t num_items, most_rows, group, head_dim;      // most_rows: see lora_attention_plan; group: query heads of a kv head
     const void *q, *k, *v;
     void* o;
     int64_t ldq, ldk, ldv, ldo;

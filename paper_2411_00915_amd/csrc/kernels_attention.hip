@@ -28,7 +28,8 @@
 // against 63.
 // Why so: 32 queries are a product's width, and four wavefronts share what is in LDS; of 64 keys a tile there are half the barriers
 // and maxima (32: 1436 against 1315 us), and heads past 128 have room for 32.  Few queries leave wavefronts without work: the
-// plan gives those other heads of the same keys.
+// plan gives those other heads of the same keys, or, where the chip is not full anyway, KS of them share the tile's keys and add up
+// in the end (32 heads of 128 on 8, 8 x 20 queries behind 1000 keys: 20.6 -> 15.9 us; of 256 dims 41 -> 43: not there).
 namespace {
 
 typedef __attribute__((__vector_size__(16 * sizeof(float)))) float floatx16;
@@ -115,19 +116,20 @@ __device__ __forceinline__ float max_of_halves(float x)
 #endif
 }
 
-template <typename T, int DP, int BK, bool ALIGNED>
-__global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel(attention_args a)
+template <typename T, int DP, int BK, bool ALIGNED, int KS>
+__global__ __launch_bounds__(256, DP <= 128 && KS == 1 ? 2 : 1) void attention_tiled_kernel(attention_args a)
 {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int ROW = DP * (int)sizeof(T), CH = ROW / 16;         // bytes and chunks of a token
     constexpr int LOADS = BK * CH / 256;                           // of a wavefront, for one tile of keys
-    constexpr int NB = DP / 32, SB = BK / 32;
+    constexpr int NB = DP / 32, SB = BK / 32 / KS, PART = SB * 32;      // KS wavefronts share a tile's keys, PART of them each
     constexpr int QR = F32 ? DP / 2 : DP / 16;                      // fp32: a register per two dims; bf16: 8 dims a lane and product
     __shared__ __align__(1024) char lds[2][2][BK * ROW];            // buffer, keys / values
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, half = lane >> 5;
     const attention_tile t = a.items[blockIdx.x];
     if (t.heads == 0) return;
-    const int waves = 4 / t.heads, head = t.head + wave / waves, row0 = wave % waves * 32;      // this wavefront's head, and its first query
+    const int part = KS == 1 ? 0 : wave % KS, team = wave / KS;
+    const int waves = 4 / KS / t.heads, head = t.head + team / waves, row0 = team % waves * 32;      // this wavefront's head, and its first query
     const int D = a.head_dim;
     const char* const kb = static_cast<const char*>(a.k) + ((int64_t)t.kv_row0 * a.ldk + (int64_t)(t.head / a.group) * D) * (int)sizeof(T);
     const char* const vb = static_cast<const char*>(a.v) + ((int64_t)t.kv_row0 * a.ldv + (int64_t)(t.head / a.group) * D) * (int)sizeof(T);
@@ -221,9 +223,10 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();                                       // the tile is there, and nobody reads the other buffer any more
         if (n + 1 < tiles) fetch(n + 1);
-        if (n * BK >= most) continue;
-        const char* const keys = lds[n & 1][0];
-        const char* const values = lds[n & 1][1];
+        const int token0 = n * BK + part * PART;
+        if (token0 >= most) continue;
+        const char* const keys = lds[n & 1][0] + part * (PART * ROW);
+        const char* const values = lds[n & 1][1] + part * (PART * ROW);
         floatx16 x[SB];
 #pragma unroll
         for (int b = 0; b < SB; ++b) {
@@ -248,9 +251,9 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
                 }
             }
         }
-        const bool masked = (n + 1) * BK > least;
+        const bool masked = token0 + PART > least;
         if (masked) {
-            int first = limit - n * BK - 4 * half;
+            int first = limit - token0 - 4 * half;
             asm volatile("" : "+v"(first));                    // (a branch, not selects in every tile)
 #pragma unroll
             for (int b = 0; b < SB; ++b)
@@ -345,8 +348,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
             int there = half;
             asm volatile("" : "+v"(there));
 #pragma unroll 1
-            for (int j = 0; j < BK; ++j) {
-                const bool sees = n * BK + j < limit;
+            for (int j = 0; j < PART; ++j) {
+                const bool sees = token0 + j < limit;
 #pragma unroll
                 for (int d = 0; d < NB; ++d)
 #pragma unroll
@@ -362,6 +365,40 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     }
 
     l += __shfl_xor(l, 32, 64);
+    if constexpr (KS > 1) {                                    // the first of the wavefronts gets the others' sums
+        static_assert(4 / KS * ((KS - 1) * NB * 16 + 2 * KS) * 256 <= sizeof(lds), "they pass through the tiles' space");
+        float* const space = reinterpret_cast<float*>(lds) + team * ((KS - 1) * NB * 16 + 2 * KS) * 64 + lane;
+        float* const stats = space + (KS - 1) * NB * 16 * 64;
+        __syncthreads();
+        stats[2 * part * 64] = m;
+        __syncthreads();
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < KS; ++w) top = fmaxf(top, stats[2 * w * 64]);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * (careful ? c2 : 1.f));
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] *= f;
+        if (part > 0) {
+            stats[(2 * part + 1) * 64] = l;
+#pragma unroll
+            for (int d = 0; d < NB; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) space[((part - 1) * NB * 16 + d * 16 + i) * 64] = acc[d][i];
+        }
+        __syncthreads();
+        if (part == 0)
+#pragma unroll
+            for (int w = 1; w < KS; ++w) {
+                l += stats[(2 * w + 1) * 64];
+#pragma unroll
+                for (int d = 0; d < NB; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[d][i] += space[((w - 1) * NB * 16 + d * 16 + i) * 64];
+            }
+    }
     };
     pass(std::false_type{});
     float sum = l;                                             // (not finite where one of them is not, or they are past its range)
@@ -369,7 +406,8 @@ __global__ __launch_bounds__(256, DP <= 128 ? 2 : 1) void attention_tiled_kernel
     for (int d = 0; d < NB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum += fabsf(acc[d][i]);
-    if (__syncthreads_or(!(sum < INFINITY) || (l == 0.f && limit > 0))) pass(std::true_type{});
+    if (__syncthreads_or(part == 0 && (!(sum < INFINITY) || (l == 0.f && limit > 0)))) pass(std::true_type{});
+    if (part > 0) return;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     T* const out = static_cast<T*>(a.o) + (int64_t)(t.q_row0 + (valid ? row : 0)) * a.ldo + (int64_t)head * D;
 #pragma unroll
@@ -416,8 +454,22 @@ hipError_t launch_attention(const attention_args& a, int32_t dtype, hipStream_t 
     const bool aligned = (all & 15) == 0 && a.ldk * es < most && a.ldv * es < most;
     const dim3 grid((uint32_t)a.num_items);
 #define TILED(T, DP, BK)                                                                                                                    \
-    if (aligned) LORA_LAUNCH(LORA_K_ATTENTION_TILED, (attention_tiled_kernel<T, DP, BK, true>), grid, dim3(256), 0, stream, a);             \
-    else LORA_LAUNCH(LORA_K_ATTENTION_UNALIGNED, (attention_tiled_kernel<T, DP, BK, false>), grid, dim3(256), 0, stream, a)
+    if (aligned) LORA_LAUNCH(LORA_K_ATTENTION_TILED, (attention_tiled_kernel<T, DP, BK, true, 1>), grid, dim3(256), 0, stream, a);          \
+    else LORA_LAUNCH(LORA_K_ATTENTION_UNALIGNED, (attention_tiled_kernel<T, DP, BK, false, 1>), grid, dim3(256), 0, stream, a)
+#define SHARED(T, DP, BK, KS) LORA_LAUNCH(LORA_K_ATTENTION_SHARED, (attention_tiled_kernel<T, DP, BK, true, KS>), grid, dim3(256), 0, stream, a)
+    // few queries on a chip that is not full: a workgroup's wavefronts share the keys, as many as 128 KB of LDS hold a tile for
+    if (aligned && a.most_rows <= 32 && a.head_dim <= (dtype == LORA_F32 ? 64 : 128)) {
+        if (dtype == LORA_F32) SHARED(float, 64, 128, 4);
+        else if (a.head_dim <= 64) SHARED(bf16_t, 64, 128, 4);
+        else if (a.head_dim <= 96) SHARED(bf16_t, 96, 128, 4);
+        else SHARED(bf16_t, 128, 128, 4);
+        return hipGetLastError();
+    }
+    if (aligned && a.most_rows <= 64 && a.head_dim <= 128) {
+        if (dtype == LORA_F32) SHARED(float, 128, 64, 2);
+        else SHARED(bf16_t, 128, 128, 2);
+        return hipGetLastError();
+    }
     if (dtype == LORA_F32) {
         if (a.head_dim <= 64) { TILED(float, 64, 32); }
         else if (a.head_dim <= 128) { TILED(float, 128, 32); }

@@ -34,6 +34,7 @@ enum lora_kernel_id {
     LORA_K_DELTA_F32,
     LORA_K_ATTENTION_TILED,
     LORA_K_ATTENTION_UNALIGNED,
+    LORA_K_ATTENTION_SHARED,
     LORA_K_CACHE_APPEND,
     LORA_K_CACHE_READ,
     LORA_K_CACHE_ATTENTION,

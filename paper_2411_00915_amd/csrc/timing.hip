@@ -21,7 +21,7 @@ const char* kNames[LORA_K_COUNT] = {"shrink_general_kernel", "expand_general_ker
                                     "gemm_ring_kernel", "gemm_ring_kernel<delta>", "clear_words_kernel",
                                     "gemm_small_kernel", "gemm_small_kernel<delta>", "layer_small_kernel", "gemm_mid_kernel",
                                     "gemm_mid_kernel<delta>", "shrink_rows_kernel", "expand_rows_kernel",
-                                    "delta_f32_kernel", "attention_tiled_kernel", "attention_tiled_kernel<unaligned>", "cache_append_kernel",
+                                    "delta_f32_kernel", "attention_tiled_kernel", "attention_tiled_kernel<unaligned>", "attention_tiled_kernel<shared>", "cache_append_kernel",
                                     "cache_read_kernel", "cache_attention_kernel", "cache_finish_kernel",
                                     "cache_select_kernel", "cache_move_kernel", "probe_empty_kernel", "probe_read_kernel", "probe_mfma_kernel"};
 long long* g_trace = nullptr;

@@ -258,6 +258,53 @@ def test_what_a_query_does_not_see_has_no_effect(dtype, bad, D, shift, where):
 
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("D,pad", [(64, 0), (40, 0), (80, 0), (128, 0), (136, 0), (256, 0), (128, 3)])
+@pytest.mark.parametrize("nq,nk", [([20, 1, 32, 0], [1000, 700, 33, 5]), ([64, 5, 33], [65, 700, 3]), ([3, 7], [129, 0])])
+def test_few_queries_behind_many_keys(dtype, causal, D, pad, nq, nk):
+    """On a chip that is not full the wavefronts of a workgroup share a tile's keys: four where there are up to 32 queries, two up to 64"""
+    check_prompt(*prompt_case(np.random.default_rng(D + len(nq)), nq, nk, 4, 2, D, dtype), nq, nk, dtype, causal, D ** -0.5, pad=pad)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
+@pytest.mark.parametrize("n", [30, 60])
+def test_what_few_queries_do_not_see_has_no_effect(dtype, bad, D, n):
+    """Infinities and NaN in values that the last queries see: theirs are not finite, the others' as they were"""
+    nq, nk = [n, 9], [300, 200]
+    q, k, v = prompt_case(np.random.default_rng(n), nq, nk, 2, 1, D, dtype)
+    clean = run_prompt(q, k, v, nq, nk, dtype, True, D ** -0.5)
+    vb = v.copy()
+    vb[290, 0, 1::5] = bad                                  # seen by the last 10 of the first sequence
+    vb[300 + 199, 0, ::7] = bad                             # and by the last of the second
+    got = run_prompt(q, k, vb, nq, nk, dtype, True, D ** -0.5)
+    seen = np.zeros(sum(nq), dtype=bool)
+    seen[n - 10:n] = seen[n + 8] = True
+    assert np.isfinite(got[~seen]).all()
+    assert np.abs(got[~seen] - clean[~seen]).max() <= (2.0 ** -7 if dtype == BF16 else 2.0 ** -19) * np.abs(clean).max()
+    assert not np.isfinite(got[n - 10:n, :, 1::5]).any() and not np.isfinite(got[n + 8, :, ::7]).any()
+    others = np.ones(D, dtype=bool)
+    others[1::5] = False
+    assert np.isfinite(got[n - 10:n][:, :, others]).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n", [8, 40])
+def test_few_queries_whose_scores_grow_or_fall_along_the_keys(dtype, n):
+    """The wavefronts' maxima differ by hundreds; one alone has all of the weight"""
+    nq, nk, D = [n], [500], 64
+    q, k, v = prompt_case(np.random.default_rng(n), nq, nk, 2, 2, D, dtype)
+    for slope in (1.0, -1.0):
+        q[:, :, 0] = 8.0
+        k[:, :, 0] = rounded(slope * np.arange(500)[:, None] / 2 * np.ones((1, 2)), dtype)
+        check_prompt(q, k, v, nq, nk, dtype, False, 0.125)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
 def test_masks_of_the_types_lowest_value_in_keys(dtype):
     """Scores of the type's lowest finite value are scores like others: alone they share the weight"""
     low = float(torch.finfo(TORCH[dtype]).min)
