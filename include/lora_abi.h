@@ -381,7 +381,7 @@ lora_status lora_merge(int32_t num_layers, int32_t n, int32_t k, int32_t rank, f
  * (LORA_BF16 or LORA_F32); head h of a token is at h * head_dim of its row, rows `ld` elements apart, so that q, k and v may be
  * columns of one projection's output.  Query head h uses the keys and values of head h / (num_heads / num_kv_heads).
  * head_dim is 1 .. LORA_MAX_HEAD_DIM.  Pointers have to be aligned to an element; the kernels are fastest with 16 bytes, and
- * leading dimensions and head_dim multiples of 8 (fp32: 4): prompts of anything else take one to three times as long.
+ * leading dimensions and head_dim multiples of 8 (fp32: 4): prompts of anything else take up to three times as long.
  * Outputs must not share memory with inputs.
  *
  * Scores, softmax and sums are held in 32 bits; in bf16 the softmax weights are rounded to bf16 for the product with the
