@@ -125,6 +125,8 @@ _lib.lora_attention_plan_destroy.restype = None
 _lib.lora_attention_plan_destroy.argtypes = [_vp]
 _lib.lora_attention_plan_items.restype = ctypes.c_int32
 _lib.lora_attention_plan_items.argtypes = [_vp, ctypes.POINTER(_i32p)]
+_lib.lora_attention_plan_instance.restype = None
+_lib.lora_attention_plan_instance.argtypes = [_vp, ctypes.c_int32, ctypes.c_int64, _i32p]
 _lib.lora_cache_page_bytes.restype = ctypes.c_size_t
 _lib.lora_cache_page_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32]
 _lib.lora_cache_workspace.restype = ctypes.c_int
@@ -453,6 +455,14 @@ def lora_attention_plan_items(plan: AttentionPlan) -> np.ndarray:
     p = _i32p()
     n = _lib.lora_attention_plan_items(plan.handle, ctypes.byref(p))
     return np.ctypeslib.as_array(p, shape=(n * 8,)).copy().reshape(n, 8) if n else np.zeros((0, 8), np.int32)
+
+
+def lora_attention_plan_instance(plan: AttentionPlan, aligned, pitch) -> tuple:
+    """The kernel that a call with this plan takes where its rows are (not) aligned to 16 bytes and those of keys and values at most
+    `pitch` bytes apart: dims it is made for, keys of a tile, wavefronts that share them, whether they go straight to LDS"""
+    n = (ctypes.c_int32 * 4)()
+    _lib.lora_attention_plan_instance(plan.handle, int(bool(aligned)), int(pitch), n)
+    return n[0], n[1], n[2], bool(n[3])
 
 
 def lora_cache_page_bytes(page_tokens: int, head_dim: int) -> int:

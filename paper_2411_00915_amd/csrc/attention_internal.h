@@ -33,6 +33,14 @@ struct lora_attention_plan {
     void* h_stage = nullptr;
 };
 
+// The instance of the prompts' kernel that a call takes: dims that it is made for, keys of a tile, wavefronts that share a tile's keys;
+// aligned: keys and values straight to LDS
+struct attention_instance {
+    int32_t dims, keys, sharing, aligned;
+};
+// aligned: rows and heads of the call are to 16 bytes; pitch: the greater of the bytes between rows of k and between rows of v
+attention_instance choose_attention(int32_t dtype, int32_t head_dim, int32_t most_rows, bool aligned, int64_t pitch);
+
 // set by the device side, so that the host code of plans links without it
 extern void (*lora_attention_plan_device_release)(lora_attention_plan*);
 

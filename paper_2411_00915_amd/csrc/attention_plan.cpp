@@ -64,6 +64,20 @@ bool order_items(lora_attention_plan* p)
 }
 }  // namespace
 
+// A tile's loads straight to LDS address its rows by 32-bit offsets below 2^31 (what is behind that reads as zeros, and the chunks
+// past head_dim are put there), so all rows of an aligned instance's tile have to lie within 2 GB; rows further apart than that go
+// through registers.
+attention_instance choose_attention(int32_t dtype, int32_t head_dim, int32_t most_rows, bool aligned, int64_t pitch)
+{
+    const bool f32 = dtype == LORA_F32;
+    auto fits = [&](int32_t keys) { return aligned && pitch < ((int64_t)1 << 31) / keys; };
+    // few queries on a chip that is not full: a workgroup's wavefronts share the keys, as many as 128 KB of LDS hold a tile for
+    if (most_rows <= 32 && head_dim <= (f32 ? 64 : 128) && fits(128)) return {head_dim <= 64 ? 64 : head_dim <= 96 ? 96 : 128, 128, 4, 1};
+    if (most_rows <= 64 && head_dim <= 128 && fits(f32 ? 64 : 128)) return {128, f32 ? 64 : 128, 2, 1};
+    const int32_t dims = !f32 && head_dim > 64 && head_dim <= 96 ? 96 : padded_head_dim(head_dim), keys = f32 || dims == 256 ? 32 : 64;
+    return {dims, keys, 1, fits(keys)};
+}
+
 extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, lora_attention_plan** out)
 {
     if (out) *out = nullptr;
@@ -123,6 +137,16 @@ extern "C" int32_t lora_attention_plan_items(const lora_attention_plan* p, const
 {
     *items = reinterpret_cast<const int32_t*>(p->items.data());
     return (int32_t)p->items.size();
+}
+
+// Not part of the ABI: the instance that a call with this plan takes (attention_instance), for tests
+extern "C" void lora_attention_plan_instance(const lora_attention_plan* p, int32_t aligned, int64_t pitch, int32_t* instance)
+{
+    const attention_instance n = choose_attention(p->dtype, p->head_dim, p->most_rows, aligned != 0, pitch);
+    instance[0] = n.dims;
+    instance[1] = n.keys;
+    instance[2] = n.sharing;
+    instance[3] = n.aligned;
 }
 
 extern "C" size_t lora_cache_page_bytes(int32_t page_tokens, int32_t head_dim)

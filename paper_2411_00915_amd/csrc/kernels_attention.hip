@@ -1,6 +1,7 @@
 // Attention of a batch of prompts.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "device_util.h"
@@ -448,37 +449,35 @@ __global__ __launch_bounds__(256, DP <= 128 && KS == 1 ? 2 : 1) void attention_t
 
 hipError_t launch_attention(const attention_args& a, int32_t dtype, hipStream_t stream)
 {
-    const int64_t es = dtype == LORA_F32 ? 4 : 2, most = (int64_t)1 << 25;      // (a tile's rows have to lie within 2 GB)
+    const int64_t es = dtype == LORA_F32 ? 4 : 2;
     const uintptr_t all = reinterpret_cast<uintptr_t>(a.q) | reinterpret_cast<uintptr_t>(a.k) | reinterpret_cast<uintptr_t>(a.v) | reinterpret_cast<uintptr_t>(a.o) |
                           (uintptr_t)((a.ldq | a.ldk | a.ldv | a.ldo | a.head_dim) * es);
-    const bool aligned = (all & 15) == 0 && a.ldk * es < most && a.ldv * es < most;
+    const attention_instance n = choose_attention(dtype, a.head_dim, a.most_rows, (all & 15) == 0, std::max(a.ldk, a.ldv) * es);
     const dim3 grid((uint32_t)a.num_items);
+#define INSTANCE(ID, T, DP, BK, ALIGNED, KS)                                                                                                \
+    if (n.dims == DP && n.keys == BK && n.sharing == KS && (bool)n.aligned == ALIGNED) {                                                    \
+        LORA_LAUNCH(ID, (attention_tiled_kernel<T, DP, BK, ALIGNED, KS>), grid, dim3(256), 0, stream, a);                                   \
+        return hipGetLastError();                                                                                                           \
+    }
 #define TILED(T, DP, BK)                                                                                                                    \
-    if (aligned) LORA_LAUNCH(LORA_K_ATTENTION_TILED, (attention_tiled_kernel<T, DP, BK, true, 1>), grid, dim3(256), 0, stream, a);          \
-    else LORA_LAUNCH(LORA_K_ATTENTION_UNALIGNED, (attention_tiled_kernel<T, DP, BK, false, 1>), grid, dim3(256), 0, stream, a)
-#define SHARED(T, DP, BK, KS) LORA_LAUNCH(LORA_K_ATTENTION_SHARED, (attention_tiled_kernel<T, DP, BK, true, KS>), grid, dim3(256), 0, stream, a)
-    // few queries on a chip that is not full: a workgroup's wavefronts share the keys, as many as 128 KB of LDS hold a tile for
-    if (aligned && a.most_rows <= 32 && a.head_dim <= (dtype == LORA_F32 ? 64 : 128)) {
-        if (dtype == LORA_F32) SHARED(float, 64, 128, 4);
-        else if (a.head_dim <= 64) SHARED(bf16_t, 64, 128, 4);
-        else if (a.head_dim <= 96) SHARED(bf16_t, 96, 128, 4);
-        else SHARED(bf16_t, 128, 128, 4);
-        return hipGetLastError();
-    }
-    if (aligned && a.most_rows <= 64 && a.head_dim <= 128) {
-        if (dtype == LORA_F32) SHARED(float, 128, 64, 2);
-        else SHARED(bf16_t, 128, 128, 2);
-        return hipGetLastError();
-    }
+    INSTANCE(LORA_K_ATTENTION_TILED, T, DP, BK, true, 1)                                                                                    \
+    INSTANCE(LORA_K_ATTENTION_UNALIGNED, T, DP, BK, false, 1)
+#define SHARED(T, DP, BK, KS) INSTANCE(LORA_K_ATTENTION_SHARED, T, DP, BK, true, KS)
     if (dtype == LORA_F32) {
-        if (a.head_dim <= 64) { TILED(float, 64, 32); }
-        else if (a.head_dim <= 128) { TILED(float, 128, 32); }
-        else { TILED(float, 256, 32); }
+        SHARED(float, 64, 128, 4)
+        SHARED(float, 128, 64, 2)
+        TILED(float, 64, 32)
+        TILED(float, 128, 32)
+        TILED(float, 256, 32)
     } else {
-        if (a.head_dim <= 64) { TILED(bf16_t, 64, 64); }
-        else if (a.head_dim <= 96) { TILED(bf16_t, 96, 64); }
-        else if (a.head_dim <= 128) { TILED(bf16_t, 128, 64); }
-        else { TILED(bf16_t, 256, 32); }
+        SHARED(bf16_t, 64, 128, 4)
+        SHARED(bf16_t, 96, 128, 4)
+        SHARED(bf16_t, 128, 128, 4)
+        SHARED(bf16_t, 128, 128, 2)
+        TILED(bf16_t, 64, 64)
+        TILED(bf16_t, 96, 64)
+        TILED(bf16_t, 128, 64)
+        TILED(bf16_t, 256, 32)
     }
-    return hipGetLastError();
+    return hipErrorInvalidValue;                               // (not reached: these are all that there are)
 }

@@ -210,6 +210,26 @@ def test_prompts_whose_rows_lie_beyond_4_gb():
 
 
 @gpu
+@pytest.mark.parametrize("dtype,D", [(BF16, 64), (BF16, 128), (F32, 64), (F32, 128)])
+@pytest.mark.parametrize("n", [8, 40])
+@pytest.mark.parametrize("mb", [17, 31])
+def test_few_queries_behind_keys_whose_rows_lie_far_apart(dtype, D, n, mb):
+    """A tile's rows beyond 2 GB from its first: what is addressed by 32 bits would come as zeros"""
+    m, e = 300, torch.finfo(TORCH[dtype]).bits // 8
+    ld = (mb << 20) // e
+    q, k, v = prompt_case(np.random.default_rng(mb), [n], [m], 2, 1, D, dtype)
+    rows = torch.empty(m * ld, dtype=TORCH[dtype], device=DEV).view(m, ld)            # k and v beside each other
+    rows[:, :D], rows[:, D:2 * D] = to_device(k, dtype).view(m, D), to_device(v, dtype).view(m, D)
+    qd, od = to_device(q, dtype), torch.zeros(q.shape, dtype=TORCH[dtype], device=DEV)
+    plan = B.lora_attention_plan([0, n], [0, m], 2, 1, D, dtype)
+    B.lora_attention(plan, qd, 2 * D, rows, ld, rows.data_ptr() + D * e, ld, od, 2 * D, 0.125)
+    torch.cuda.synchronize()
+    o, tol, amount, _ = reference(q, k, v, 0.125, lambda i: i + m - n + 1)
+    check(od.float().cpu().numpy(), o, tol, amount, dtype)
+    plan.destroy()
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("scale", [-0.2, 0.0, 3.0])
 def test_prompts_with_other_scales(dtype, scale):
@@ -899,6 +919,22 @@ def test_heads_of_few_queries_go_together(group, runs):
     plan = B.lora_attention_plan([0, 20], None, 2 * group, 2, 64, BF16)       # a chip that is not full: one by one
     items = B.lora_attention_plan_items(plan)
     assert set(items[items[:, 6] > 0, 6]) == {1}
+    plan.destroy()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [1, 64, 80, 96, 100, 128, 200, 256])
+@pytest.mark.parametrize("n,shared", [(8, 4), (40, 2), (128, 1)])
+def test_all_rows_of_a_tile_lie_where_its_loads_reach(dtype, D, n, shared):
+    """Loads straight to LDS reach 2^31 bytes; a tile whose rows lie further apart is made smaller or goes through registers"""
+    plan = B.lora_attention_plan([0, n], [0, 300 + n], 2, 1, D, dtype)
+    for pitch in (1024, 2 ** 24 - 16, 2 ** 24, 17 << 20, 31 << 20, 2 ** 25 - 16, 2 ** 25, 2 ** 26 - 16, 2 ** 26, 2 ** 33, 2 ** 40):
+        dims, keys, sharing, direct = B.lora_attention_plan_instance(plan, True, pitch)
+        assert dims >= D and (not direct or keys * pitch < 2 ** 31)
+        assert direct == (pitch < 2 ** 26 if keys == 32 else pitch < 2 ** 25)
+        assert sharing in (1, shared, 2 if dtype == F32 else shared)
+        assert B.lora_attention_plan_instance(plan, False, pitch)[2:] == (1, False)
+    assert B.lora_attention_plan_instance(plan, True, 1024)[2] == (1 if D > 128 else 2 if dtype == F32 and D > 64 and n <= 64 else shared)
     plan.destroy()
 
 
