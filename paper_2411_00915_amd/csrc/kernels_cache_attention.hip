@@ -532,7 +532,9 @@ __device__ __forceinline__ void join_row(const cache_attention_args& a, int64_t 
 __device__ __forceinline__ void add_weights(const cache_attention_args& a, int id, int chunks)
 {
     constexpr int MOST = 256;
-    __shared__ float lse[MOST];                                // of that many rows at a time: maximum + log(sum), inf where nothing is seen
+    // Of that many rows at a time: maximum and 1 / sum (0, 0 where nothing is seen).  Apart: in maximum + log(sum) a large maximum
+    // takes the sum's bits.
+    __shared__ float2 stat[MOST];
     const cache_args& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int chunk = id % chunks;
@@ -556,18 +558,19 @@ __device__ __forceinline__ void add_weights(const cache_attention_args& a, int i
             for (int off = lanes >> 1; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
             for (int s = lane & (lanes - 1); s < a.splits; s += lanes) all += st[s].y == 0.f ? 0.f : st[s].y * exp_of(st[s].x - top);
             for (int off = lanes >> 1; off > 0; off >>= 1) all += __shfl_xor(all, off, 64);
-            if (j < n && (lane & (lanes - 1)) == 0) lse[j] = all == 0.f ? INFINITY : top + logf(all);
+            if (j < n && (lane & (lanes - 1)) == 0) stat[j] = all == 0.f ? float2{0.f, 0.f} : float2{top, 1.f / all};
         }
         __syncthreads();
         if (slot >= length) continue;
 #pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const int row = r0 + j, sees = length - rows.count + row / a.group + 1 - slot;       // of the four, the first so many
+            const float2 e = stat[j];
             const float4 x = *reinterpret_cast<const float4*>(a.scores + row_at(row) * a.score_stride + slot);       // (not written where it sees nothing)
-            sum[0] += sees > 0 ? exp_of(x.x - lse[j]) : 0.f;
-            sum[1] += sees > 1 ? exp_of(x.y - lse[j]) : 0.f;
-            sum[2] += sees > 2 ? exp_of(x.z - lse[j]) : 0.f;
-            sum[3] += sees > 3 ? exp_of(x.w - lse[j]) : 0.f;
+            sum[0] += sees > 0 ? exp_of(x.x - e.x) * e.y : 0.f;
+            sum[1] += sees > 1 ? exp_of(x.y - e.x) * e.y : 0.f;
+            sum[2] += sees > 2 ? exp_of(x.z - e.x) * e.y : 0.f;
+            sum[3] += sees > 3 ? exp_of(x.w - e.x) * e.y : 0.f;
         }
     }
     if (slot >= length) return;

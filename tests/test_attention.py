@@ -628,6 +628,25 @@ def test_more_rows_than_a_tile_and_than_the_weights_take_at_a_time(decay):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("lengths", [[4, 100], [5000]])
+@pytest.mark.parametrize("score", [1e4, -1e6, 1e6, 1e8, -1e8])
+def test_equal_scores_of_any_size_share_the_weight(dtype, lengths, score):
+    """In one piece and in several.  Equal scores lie 0 from their maximum, so a row's sum is the count of its keys, exactly, and a
+    slot's weight is off by the rounding of 1 / count for each of its rows and of their sum: (rows + 2) 2^-23 of it at most."""
+    H, D, new = 8, 64, 2
+    pool = Pool(lengths, 1, D, 64)
+    vals = [[np.ones((n, 1, D), np.float32), rounded(np.random.default_rng(n).standard_normal((n, 1, D)), dtype)] for n in lengths]
+    pool.fill(vals, dtype)
+    q = rounded(np.full((new * len(lengths), H, D), score / D), dtype)
+    run_cache(pool, q, [new] * len(lengths), dtype, 1.0, 0.0)
+    for s, n in enumerate(lengths):
+        want = np.full((n, 1), H / n + H / (n - 1))
+        want[-1] = H / n                                    # (the first of the two tokens does not see the last slot)
+        assert np.all(np.abs(pool.slots(pool.weight, s, n) / want - 1) <= (new * H + 2) * 2.0 ** -23), s
+
+
+@gpu
 def test_a_cache_beyond_4_gb():
     """Pages at the far end of a large pool, tables of int32 page numbers into it"""
     page, Hkv, D, H = 1024, 16, 128, 16
