@@ -76,8 +76,8 @@ lora_status check_rows(const lora_cache* c, int32_t num_heads, int32_t num_token
     if (num_heads < 1 || num_heads % c->num_kv_heads != 0) return LORA_ERR_INVALID_ARG;
     const int64_t rows = (int64_t)num_tokens * num_heads;
     if (rows > INT32_MAX || (int64_t)c->num_seqs * max_new > INT32_MAX / num_heads) return LORA_ERR_UNSUPPORTED;
-    // (the launch behind the attention's: up to a workgroup of 512 threads for 2048 slots, beside those of the rows to be joined)
-    if ((int64_t)c->num_seqs * c->num_kv_heads > LORA_ATTENTION_MAX_WORKGROUPS / 4 / (c->max_length / 2048 + 1)) return LORA_ERR_UNSUPPORTED;
+    // (the launch behind the attention's: up to a workgroup for 2048 slots, beside those of the rows to be joined, which are fewer)
+    if ((int64_t)c->num_seqs * c->num_kv_heads > most_workgroups(2 * LORA_CACHE_FINISH_THREADS) / (c->max_length / 2048 + 1)) return LORA_ERR_UNSUPPORTED;
     if (rows > ((int64_t)1 << 40) / std::max<int64_t>(c->max_length, 1)) return LORA_ERR_UNSUPPORTED;
     return LORA_OK;
 }
@@ -134,7 +134,7 @@ extern "C" lora_status lora_cache_append(const lora_cache* c, int32_t dtype, int
     if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
     const int64_t row = (int64_t)c->num_kv_heads * c->head_dim;
     if (!k || !v || ldk < row || ldv < row || misaligned(k, elem_bytes(dtype)) || misaligned(v, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
-    if ((int64_t)num_tokens / 32 + 1 > LORA_ATTENTION_MAX_WORKGROUPS / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
+    if (tiles_of_tokens(num_tokens) > most_workgroups(LORA_CACHE_APPEND_THREADS) / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
     return status_of(launch_cache_append(args_of(c, num_tokens, std::min(max_new, num_tokens), d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -146,7 +146,7 @@ extern "C" lora_status lora_cache_read(const lora_cache* c, int32_t dtype, int32
     if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
     const int64_t row = (int64_t)c->num_kv_heads * c->head_dim;
     if (!k || !v || ldk < row || ldv < row || misaligned(k, elem_bytes(dtype)) || misaligned(v, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
-    if ((int64_t)num_tokens / 32 + 1 > LORA_ATTENTION_MAX_WORKGROUPS / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
+    if (tiles_of_tokens(num_tokens) > most_workgroups(LORA_CACHE_READ_THREADS) / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
     return status_of(launch_cache_read(args_of(c, num_tokens, std::min(max_new, num_tokens), d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -180,7 +180,7 @@ extern "C" lora_status lora_cache_attention(const lora_cache* c, int32_t dtype, 
     if (!q || !o || ldq < row || ldo < row || misaligned(q, elem_bytes(dtype)) || misaligned(o, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
     const cache_division v = divide_cache_attention(c, num_heads, num_tokens, max_new, weights);
     if (v.total > 0 && (!workspace || workspace_bytes < v.total || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
-    if ((int64_t)c->num_seqs * c->num_kv_heads * v.splits > LORA_ATTENTION_MAX_WORKGROUPS / std::max(1, v.row_tiles)) return LORA_ERR_UNSUPPORTED;
+    if ((int64_t)c->num_seqs * c->num_kv_heads * v.splits > most_workgroups(64 * v.waves) / std::max(1, v.row_tiles)) return LORA_ERR_UNSUPPORTED;
     char* const w = static_cast<char*>(workspace);
     cache_attention_args a{};
     a.c = args_of(c, num_tokens, max_new, d_indptr);
@@ -214,7 +214,8 @@ extern "C" lora_status lora_cache_evict(const lora_cache* source, const lora_cac
         return LORA_ERR_INVALID_ARG;
     if (source->num_seqs == 0) return LORA_OK;
     if (!source->weight || !target->weight || (budget > 0 && !kept) || misaligned(kept, 4) || source->length == target->length) return LORA_ERR_INVALID_ARG;
-    if ((int64_t)source->num_seqs * source->num_kv_heads > LORA_ATTENTION_MAX_WORKGROUPS / std::max(4, budget / 32 + 1)) return LORA_ERR_UNSUPPORTED;
+    const int64_t heads = (int64_t)source->num_seqs * source->num_kv_heads;
+    if (heads > most_workgroups(LORA_CACHE_SELECT_THREADS) || heads > most_workgroups(LORA_CACHE_MOVE_THREADS) / (budget / 32 + 1)) return LORA_ERR_UNSUPPORTED;
     return status_of(launch_cache_evict(args_of(source, 0, 0, nullptr), args_of(target, 0, 0, nullptr), target->length, budget, recent, kept,
                                         static_cast<hipStream_t>(hip_stream)));
 }

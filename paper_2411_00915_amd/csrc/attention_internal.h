@@ -17,8 +17,12 @@ struct attention_tile {
 };
 
 #define LORA_ATTENTION_ROWS 128
-#define LORA_ATTENTION_MAX_WORKGROUPS ((1 << 24) - 1)   /* a launch holds fewer than 2^32 threads; these have 256 */
 #define LORA_ATTENTION_MAX_ROWS (1 << 30)      /* of a batch: row numbers and sums of two stay below 2^31 */
+
+// Threads of a workgroup, and how many workgroups of them a launch holds: fewer than 2^32 threads in all
+enum { LORA_ATTENTION_THREADS = 256, LORA_CACHE_APPEND_THREADS = 320, LORA_CACHE_READ_THREADS = 256, LORA_CACHE_FINISH_THREADS = 512, LORA_CACHE_SELECT_THREADS = 1024,
+       LORA_CACHE_MOVE_THREADS = 256 };
+constexpr int64_t most_workgroups(int64_t threads) { return (((int64_t)1 << 32) - 1) / threads; }
 
 struct lora_attention_plan {
     int32_t num_heads = 0, num_kv_heads = 0, head_dim = 0, dtype = 0;

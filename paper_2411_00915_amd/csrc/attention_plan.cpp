@@ -56,7 +56,7 @@ bool order_items(lora_attention_plan* p)
                 add((int)(std::min_element(cost, cost + X) - cost), t, u * unit + h, n = taken(t, h));
     size_t longest = 0;
     for (const auto& l : list) longest = std::max(longest, l.size());
-    if (longest > LORA_ATTENTION_MAX_WORKGROUPS / X) return false;
+    if ((int64_t)longest > most_workgroups(LORA_ATTENTION_THREADS) / X) return false;
     p->items.assign(longest * X, attention_tile{});
     for (int x = 0; x < X; ++x)
         for (size_t i = 0; i < list[x].size(); ++i) p->items[i * X + x] = list[x][i];
@@ -113,7 +113,7 @@ extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, 
             }
         }
         std::stable_sort(p->tiles.begin(), p->tiles.end(), [](const attention_tile& a, const attention_tile& b) { return a.max_kv != b.max_kv ? a.max_kv > b.max_kv : a.rows < b.rows; });
-        if ((int64_t)p->tiles.size() * p->num_heads > LORA_ATTENTION_MAX_WORKGROUPS || !order_items(p)) {
+        if ((int64_t)p->tiles.size() * p->num_heads > most_workgroups(LORA_ATTENTION_THREADS) || !order_items(p)) {
             delete p;
             return LORA_ERR_UNSUPPORTED;
         }

@@ -43,6 +43,9 @@ struct cache_attention_args {
     int64_t score_stride;
 };
 
+// The cache's tokens go in and out in tiles of 32 packed rows, a workgroup one of a head
+inline int64_t tiles_of_tokens(int64_t tokens) { return (tokens + 31) / 32; }
+
 hipError_t launch_cache_append(const cache_args& c, int32_t dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, hipStream_t stream);
 hipError_t launch_cache_read(const cache_args& c, int32_t dtype, void* k, int64_t ldk, void* v, int64_t ldv, hipStream_t stream);
 hipError_t launch_cache_attention(const cache_attention_args& a, int32_t dtype, hipStream_t stream);

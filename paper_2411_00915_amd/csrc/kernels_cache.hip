@@ -15,7 +15,7 @@
 // in 57, 332 MB, 5.8), by the chain offsets -> length -> page -> store where there are few (16 tokens: 5.4 in, 3.7 out).
 namespace {
 
-constexpr int kTile = 32;
+constexpr int kTile = 32;                                   // (tiles_of_tokens)
 
 // where the tokens of a tile are: the head's page (from the pool's start; -1: nowhere) and the place in it
 struct tile_places {
@@ -176,7 +176,7 @@ __device__ __forceinline__ uint32_t quantise(const float* x, int count, uint32_t
 }
 
 // A fifth wavefront finds the places while four make the codes
-constexpr int kAppendThreads = 320;
+constexpr int kAppendThreads = LORA_CACHE_APPEND_THREADS;
 template <typename T, int DP>
 __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(cache_args c, const T* k, int64_t ldk, const T* v, int64_t ldv, bool aligned)
 {
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kAppendThreads) void cache_append_kernel(cache_args
 }
 
 template <typename T, int DP>
-__global__ __launch_bounds__(256) void cache_read_kernel(cache_args c, T* k, int64_t ldk, T* v, int64_t ldv, bool aligned)
+__global__ __launch_bounds__(LORA_CACHE_READ_THREADS) void cache_read_kernel(cache_args c, T* k, int64_t ldk, T* v, int64_t ldv, bool aligned)
 {
     constexpr int E = DP / 16, W = (E + 7) / 8;
     __shared__ tile_places places;
@@ -318,7 +318,7 @@ __device__ __forceinline__ int lanes_before(uint64_t mask, int n)
 #endif
 }
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kSelectStep = 4 * kSelectThreads;
+constexpr int kSelectThreads = LORA_CACHE_SELECT_THREADS, kSelectWaves = kSelectThreads / 64, kSelectStep = 4 * kSelectThreads;
 template <int STEPS>
 __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args c, int32_t* target_length, int budget, int recent, int32_t* kept)
 {
@@ -466,7 +466,7 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
 // tokens to 4096 70 instead of 66).
 constexpr int kMoved = 64;
 template <int DP>
-__global__ __launch_bounds__(256) void cache_move_kernel(cache_args c, cache_args to, int budget, int tiles, const int32_t* kept)
+__global__ __launch_bounds__(LORA_CACHE_MOVE_THREADS) void cache_move_kernel(cache_args c, cache_args to, int budget, int tiles, const int32_t* kept)
 {
     constexpr int E = DP / 16, W = (E + 7) / 8, N = kMoved / 16;
     __shared__ int64_t from[kMoved], where[kMoved];            // the head's page (-1: nowhere)
@@ -524,12 +524,11 @@ __global__ __launch_bounds__(256) void cache_move_kernel(cache_args c, cache_arg
         case 128: KERNEL(128, __VA_ARGS__); break;                                            \
         default: KERNEL(256, __VA_ARGS__);                                                    \
     }
-int32_t tiles_of(int32_t tokens) { return (tokens + kTile - 1) / kTile; }
 }  // namespace
 
 hipError_t launch_cache_append(const cache_args& c, int32_t dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)(tiles_of(c.num_tokens) * c.kv_heads));
+    const dim3 grid((uint32_t)(tiles_of_tokens(c.num_tokens) * c.kv_heads));
     const bool aligned = rows_aligned(k, ldk, v, ldv, c.head_dim, dtype);
 #define APPEND(DP, T) LORA_LAUNCH(LORA_K_CACHE_APPEND, (cache_append_kernel<T, DP>), grid, dim3(kAppendThreads), 0, stream, c, static_cast<const T*>(k), ldk, static_cast<const T*>(v), ldv, aligned)
     if (dtype == LORA_F32) { BY_HEAD_DIM(APPEND, float) }
@@ -539,9 +538,9 @@ hipError_t launch_cache_append(const cache_args& c, int32_t dtype, const void* k
 
 hipError_t launch_cache_read(const cache_args& c, int32_t dtype, void* k, int64_t ldk, void* v, int64_t ldv, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)(tiles_of(c.num_tokens) * c.kv_heads));
+    const dim3 grid((uint32_t)(tiles_of_tokens(c.num_tokens) * c.kv_heads));
     const bool aligned = rows_aligned(k, ldk, v, ldv, c.head_dim, dtype);
-#define READ(DP, T) LORA_LAUNCH(LORA_K_CACHE_READ, (cache_read_kernel<T, DP>), grid, dim3(256), 0, stream, c, static_cast<T*>(k), ldk, static_cast<T*>(v), ldv, aligned)
+#define READ(DP, T) LORA_LAUNCH(LORA_K_CACHE_READ, (cache_read_kernel<T, DP>), grid, dim3(LORA_CACHE_READ_THREADS), 0, stream, c, static_cast<T*>(k), ldk, static_cast<T*>(v), ldv, aligned)
     if (dtype == LORA_F32) { BY_HEAD_DIM(READ, float) }
     else { BY_HEAD_DIM(READ, bf16_t) }
     return hipGetLastError();
@@ -560,7 +559,7 @@ hipError_t launch_cache_evict(const cache_args& c, const cache_args& to, int32_t
     if (e != hipSuccess || budget == 0) return e;
     const int32_t tiles = budget / kMoved + (budget % kMoved != 0);
     const dim3 grid((uint32_t)(c.num_seqs * c.kv_heads * tiles));
-#define MOVE(DP, UNUSED) LORA_LAUNCH(LORA_K_CACHE_MOVE, (cache_move_kernel<DP>), grid, dim3(256), 0, stream, c, to, budget, tiles, kept)
+#define MOVE(DP, UNUSED) LORA_LAUNCH(LORA_K_CACHE_MOVE, (cache_move_kernel<DP>), grid, dim3(LORA_CACHE_MOVE_THREADS), 0, stream, c, to, budget, tiles, kept)
     BY_HEAD_DIM(MOVE, )
     return hipGetLastError();
 }

@@ -476,7 +476,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
 // What is left when all splits are done, in one launch: the first `rows` workgroups join the splits of a query row each, the others
 // add up accumulated weights, for which they join the statistics themselves (one token over 8 caches of 2000, 32 heads on 8: 21.6 us
 // in all with two launches, 18.9 with one).  Bound by the scores that it reads, 67 MB in 22 us for four tokens over 131072.
-constexpr int kFinishThreads = 512, kFinishWaves = kFinishThreads / 64, kWeightSlots = 4 * kFinishThreads;
+constexpr int kFinishThreads = LORA_CACHE_FINISH_THREADS, kFinishWaves = kFinishThreads / 64, kWeightSlots = 4 * kFinishThreads;
 
 // a row's splits: the wavefronts take turns at them
 template <typename T>

@@ -1169,6 +1169,22 @@ def test_launches_of_too_many_threads_are_refused():
         assert e.value.status == B.LORA_ERR_UNSUPPORTED
 
 
+def test_an_append_of_too_many_threads_is_refused():
+    """Its workgroups have 320 threads, not 256: the bound is 2^32 / 320 of them.  (What is refused here does not reach the device.)"""
+    most = (2 ** 32 - 1) // 320
+    call = lambda f, heads, n: f(fake(num_kv_heads=heads, head_dim=1, num_seqs=2), BF16, n, 64, 4096, 4096, heads, 8192, heads, stream=0)
+    for heads in (1, 128, 4096):
+        n = (most // heads + 1) * 32                        # one workgroup more than that, for every head
+        if n > 2 ** 30:
+            n = 2 ** 30 + 1
+        with pytest.raises(B.LoraError) as e:
+            call(B.lora_cache_append, heads, n)
+        assert e.value.status == B.LORA_ERR_UNSUPPORTED, heads
+        with pytest.raises(B.LoraError) as e:               # a tile's last token counts as the whole tile
+            call(B.lora_cache_append, heads, n - 31)
+        assert e.value.status == B.LORA_ERR_UNSUPPORTED, heads
+
+
 def test_bytes_of_a_page():
     assert [B.lora_cache_page_bytes(64, d) for d in (1, 64, 65, 128, 129, 256)] == [64 * 72, 64 * 72, 64 * 136, 64 * 136, 64 * 264, 64 * 264]
     assert [B.lora_cache_page_bytes(*a) for a in ((0, 64), (31, 64), (33, 64), (1056, 64), (64, 0), (64, 257), (-32, 64))] == [0] * 7
