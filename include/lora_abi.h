@@ -476,9 +476,11 @@ lora_status lora_cache_read(const lora_cache* cache, int32_t dtype, int32_t num_
  * 0 .. L - n + i (single tokens: all).  Output as lora_attention's, over the values that the cache holds.
  * decay in [0, 1]: accumulated weights of every sequence that has a token in the call are carried on,
  *     weight[slot] = decay * weight[slot] + sum over its tokens and the kv head's query heads of p / sum p
- * (0: what was there is not read); negative: weights are left alone.
+ * (0: what was there is not read); negative: weights are left alone.  Each sequence carries on the weights of its own pages by itself,
+ * so with decay >= 0 no page may hold slots of two sequences that have tokens in the call: of a prefix that they shared, one
+ * sequence's share would be lost.  With a negative decay, and for lora_cache_read, sequences may share pages.
  * workspace: lora_cache_workspace's bytes for these arguments (weights: 1 where decay >= 0; 0 bytes: none needed), 256-byte
- * aligned.  Nothing in it is kept from one call to the next.  Deterministic: no atomics.
+ * aligned.  Nothing in it is kept from one call to the next.  Deterministic under that rule: no atomics.
  */
 lora_status lora_cache_workspace(const lora_cache* cache, int32_t num_heads, int32_t num_tokens, int32_t max_new, int32_t weights,
                                  size_t* bytes);
@@ -492,7 +494,7 @@ lora_status lora_cache_attention(const lora_cache* cache, int32_t dtype, int32_t
  * weights (ties: the lower slot; NaN counts as largest).  Kept tokens keep their order; target->length[s] = min(length, budget).
  * kept: device, [num_seqs][num_kv_heads][budget] int32, the slots kept, -1 behind them.  target: same num_seqs, num_kv_heads,
  * head_dim and page_tokens, max_length >= budget, a length array of its own; weights of both (they move along); its tables' pages must not
- * be pages of source's tables.  source is left as it was (its pages may be shared with other caches).
+ * be pages of source's tables, nor a page of one sequence another's.  source is left as it was (its pages may be shared with other caches).
  */
 lora_status lora_cache_evict(const lora_cache* source, const lora_cache* target, int32_t budget, int32_t recent, int32_t* kept,
                              void* hip_stream);

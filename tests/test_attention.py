@@ -628,6 +628,27 @@ def test_more_rows_than_a_tile_and_than_the_weights_take_at_a_time(decay):
 
 
 @gpu
+def test_sequences_may_share_the_pages_of_a_prefix():
+    """... where no weights are kept: two sequences over the same first 64 tokens, each with its own behind them"""
+    rng = np.random.default_rng(31)
+    D, lengths, shared = 64, [90, 130], 64
+    pool = Pool(lengths, 2, D, 32)
+    vals = tokens(rng, lengths, 2, D, BF16)
+    for part in range(2):
+        vals[1][part][:shared] = vals[0][part][:shared]
+    pool.table[1, :2] = pool.table[0, :2]
+    pool.d_table.copy_(torch.from_numpy(pool.table))
+    for s, new in ((0, 90), (1, 130 - shared)):             # (the prefix is written once)
+        kd, vd = (to_device(x[-new:], BF16) for x in vals[s])
+        ptr = torch.tensor([0, 0 if s else new, new], dtype=torch.int32, device=DEV)
+        B.lora_cache_append(pool.cache, BF16, new, new, ptr, kd, 2 * D, vd, 2 * D)
+    q = rounded(rng.standard_normal((4, 4, D)), BF16)
+    got = run_cache(pool, q, [2, 2], BF16, 0.125)
+    check_cache(pool, vals, q, [2, 2], lengths, BF16, 0.125, got)
+    assert np.array_equal(run_cache(pool, q, [2, 2], BF16, 0.125), got)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("lengths", [[4, 100], [5000]])
 @pytest.mark.parametrize("score", [1e4, -1e6, 1e6, 1e8, -1e8])
