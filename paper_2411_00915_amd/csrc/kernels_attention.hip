@@ -207,10 +207,11 @@ __global__ __launch_bounds__(256, DP <= 128 && KS == 1 ? 2 : 1) void attention_t
 
     floatx16 acc[NB];
     float l = 0.f;
-    // A weight of 0 does not hide infinities and NaN of a value from the product, and scores near the end of 32 bits are past it
-    // when scaled to base 2.  Where the result holds infinities or NaN, or a query that sees keys has no weight, the workgroup
-    // goes through its tiles once more: such values are taken out of the products where some query does not see the token,
-    // and scores are scaled behind the subtraction of their maximum.
+    // A weight of 0 does not hide infinities and NaN of a value from the product, scores near the end of 32 bits are past it
+    // when scaled to base 2, and so are sums of values near it, with weights of up to 2^8.  Where the result holds infinities
+    // or NaN, or a query that sees keys has no weight, the workgroup goes through its tiles once more: such values are taken
+    // out of the products where some query does not see the token, scores are scaled behind the subtraction of their
+    // maximum, and all of a query's weights together are at most 1/2.
     auto pass = [&](auto careful_) {
     constexpr bool careful = decltype(careful_)::value;
 #pragma unroll
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256, DP <= 128 && KS == 1 ? 2 : 1) void attention_t
 #pragma unroll
             for (int i = 0; i < 16; ++i) mx = fmaxf(mx, x[b][i]);
         mx = max_of_halves(mx) * (careful ? 1.f : c2);
-        if (__ballot(careful ? (mx - m) * c2 > 8.f : mx > m + 8.f)) {
+        if (__ballot(mx > (careful ? m : m + 8.f))) {
             const float top = fmaxf(m, mx), alpha = top == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * (careful ? c2 : 1.f));
             m = top;
             ref = top == -INFINITY ? 0.f : top;
@@ -278,11 +279,17 @@ __global__ __launch_bounds__(256, DP <= 128 && KS == 1 ? 2 : 1) void attention_t
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[d][i] *= alpha;
         }
+        float share = 1.f;
+        if constexpr (careful) {                               // a power of 2 of at most 1 / (2 tiles BK), made anew so that no register is kept for it
+            int count = tiles;
+            asm volatile("" : "+s"(count));
+            share = __uint_as_float((uint32_t)(94 + __builtin_clz(count) - __builtin_ctz(BK)) << 23);
+        }
 #pragma unroll
         for (int b = 0; b < SB; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                x[b][i] = __builtin_amdgcn_exp2f(careful ? (x[b][i] - ref) * c2 : x[b][i] * c2 - ref);
+                x[b][i] = __builtin_amdgcn_exp2f(careful ? (x[b][i] - ref) * c2 : x[b][i] * c2 - ref) * share;
                 l += x[b][i];
             }
         // values: fp32 one dim a lane, bf16 four tokens of a dim by a transposing read (of 16 lanes, lane i points at 4 dims of

@@ -342,6 +342,23 @@ def test_masks_of_the_types_lowest_value_in_keys(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D,pad", [(64, 0), (80, 0), (128, 0), (256, 0), (128, 3)])
+@pytest.mark.parametrize("nq,nk", [([130, 5], [130, 40]), ([8, 20], [300, 700]), ([50], [600])])
+@pytest.mark.parametrize("slope", [0.0, 0.03, -0.03])
+def test_values_up_to_the_end_of_their_range(dtype, D, pad, nq, nk, slope):
+    """Their mean is in range; the sum of hundreds of them, and one of them times a weight above 1, are not.  slope: the maximum is
+    raised by little along the keys, so that weights stay relative to an earlier one"""
+    rng = np.random.default_rng(D + nq[0])
+    q, k, v = prompt_case(rng, nq, nk, 4, 2, D, dtype)
+    q[:, :, 0] = 8.0
+    k[:, :, 0] = rounded(slope * np.arange(sum(nk))[:, None] * np.ones((1, 2)), dtype)
+    big = 0.9 * float(torch.finfo(TORCH[dtype]).max)
+    v = rounded(big * rng.uniform(0.5, 1.0, v.shape) * np.where(rng.random(v.shape) < 0.2, -1, 1), dtype)
+    check_prompt(q, k, v, nq, nk, dtype, True, 0.125, pad=pad)
+
+
+@gpu
 def test_prompts_on_a_stream_of_their_own_in_a_graph_and_on_the_current_one():
     nq, D = [130, 40], 128
     q, k, v = (to_device(x, BF16) for x in prompt_case(np.random.default_rng(2), nq, nq, 4, 2, D, BF16))
