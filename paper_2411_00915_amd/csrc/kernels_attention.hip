@@ -199,7 +199,7 @@ __global__ __launch_bounds__(256, DP <= 128 && KS == 1 ? 2 : 1) void attention_t
             qb[s].u = uint4{u.x ^ sign, u.y ^ sign, u.z ^ sign, u.w ^ sign};
         }
     }
-    const float c2 = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1.17549435e-38f);
+    const float c2 = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1.40129846e-45f);      // (0 would make NaN of -inf, what is not seen)
     const int limit = valid ? max(0, min(t.num_kv, t.ahead + row + 1)) : 0;
     // of the wavefront's queries, what the first and the last see
     const int least = max(0, min(t.num_kv, t.ahead + row0 + 1));

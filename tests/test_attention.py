@@ -343,6 +343,20 @@ def test_masks_of_the_types_lowest_value_in_keys(dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale", [0.0, 2e-39, -2e-39, 1e-38])
+def test_scales_of_zero_and_below_the_normal_numbers(dtype, scale):
+    """Products of up to 1e38 meet them: scores of 0, and of up to 0.2 and 1"""
+    rng = np.random.default_rng(4)
+    nq, nk = [40], [100]
+    q, k, v = prompt_case(rng, nq, nk, 2, 2, 64, dtype)
+    q[:], k[:] = 0, 0
+    q[:, :, 3] = rounded(1e19, dtype)
+    k[:, :, 3] = rounded(1e19 * rng.uniform(-1, 1, (100, 2)), dtype)
+    check_prompt(q, k, v, nq, nk, dtype, True, float(np.float32(scale)))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("D,pad", [(64, 0), (80, 0), (128, 0), (256, 0), (128, 3)])
 @pytest.mark.parametrize("nq,nk", [([130, 5], [130, 40]), ([8, 20], [300, 700]), ([50], [600])])
 @pytest.mark.parametrize("slope", [0.0, 0.03, -0.03])
