@@ -385,8 +385,8 @@ lora_status lora_merge(int32_t num_layers, int32_t n, int32_t k, int32_t rank, f
  * Outputs must not share memory with inputs.
  *
  * Scores, softmax and sums are held in 32 bits; in bf16 the softmax weights are rounded to bf16 for the product with the
- * values, as the output is.  What a query does not see has no effect on it, also where it holds infinities or NaN; a query
- * that sees no key gets zeros.
+ * values, as the output is.  Values may be as large as their type holds: no sum over tokens takes their mean out of range.
+ * What a query does not see has no effect on it, also where it holds infinities or NaN; a query that sees no key gets zeros.
  */
 #define LORA_MAX_HEAD_DIM 256
 

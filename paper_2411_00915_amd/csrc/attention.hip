@@ -180,7 +180,8 @@ extern "C" lora_status lora_cache_attention(const lora_cache* c, int32_t dtype, 
     if (!q || !o || ldq < row || ldo < row || misaligned(q, elem_bytes(dtype)) || misaligned(o, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
     const cache_division v = divide_cache_attention(c, num_heads, num_tokens, max_new, weights);
     if (v.total > 0 && (!workspace || workspace_bytes < v.total || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
-    if ((int64_t)c->num_seqs * c->num_kv_heads * v.splits > most_workgroups(64 * v.waves) / std::max(1, v.row_tiles)) return LORA_ERR_UNSUPPORTED;
+    const int64_t rows = (int64_t)num_heads / c->num_kv_heads * max_new, tile = cache_tile_rows(dtype == LORA_F32, c->head_dim), row_tiles = (rows + tile - 1) / tile;
+    if ((int64_t)c->num_seqs * c->num_kv_heads * v.splits > most_workgroups(64 * v.waves) / std::max<int64_t>(1, row_tiles)) return LORA_ERR_UNSUPPORTED;
     char* const w = static_cast<char*>(workspace);
     cache_attention_args a{};
     a.c = args_of(c, num_tokens, max_new, d_indptr);
@@ -192,7 +193,7 @@ extern "C" lora_status lora_cache_attention(const lora_cache* c, int32_t dtype, 
     a.group = num_heads / c->num_kv_heads;
     a.scale = scale;
     a.decay = decay;
-    a.row_tiles = v.row_tiles;
+    a.row_tiles = (int32_t)row_tiles;
     a.splits = v.splits;
     a.split_tokens = v.split_tokens;
     a.waves = v.waves;

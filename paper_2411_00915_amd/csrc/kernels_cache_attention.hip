@@ -16,10 +16,10 @@
 // it is.  The wavefronts of a workgroup (four or eight) take turns at the blocks of 32 and meet in LDS at the end; long contexts
 // are split over workgroups as well, which a second launch joins.
 //
-// Bound by memory: 256 requests of 1024 tokens, 32 heads of 128, 247 us, 4.6 TB/s.  The codes come straight to LDS, a ring of
-// blocks for each wavefront: with registers as their target 343 us, as the compiler then has too few left to ask ahead (a ring of
-// three at 128 dims costs a workgroup a compute unit: 280).  Few requests are bound by the chain length -> page -> codes: 8 of 700
-// tokens 12.2 us.  Four tokens over 131072, 32 heads on 8, with accumulated weights: 46 us here, the scores written out for
+// Bound by memory: 256 requests of 1024 tokens, 32 heads of 128, 224 us, 5.0 TB/s.  The codes come straight to LDS, a ring of
+// blocks for each wavefront: with registers as their target 343 us against 247 at the time, as the compiler then has too few
+// left to ask ahead (a ring of three at 128 dims costs a workgroup a compute unit: 280).  Few requests are bound by the chain
+// length -> page -> codes: 8 of 700 tokens 11.0 us.  Four tokens over 131072, 32 heads on 8, with accumulated weights: 46 us here, the scores written out for
 // them (67 MB beside 147) included, 22 in the launch that reads them back.
 #include <hip/hip_runtime.h>
 
@@ -192,8 +192,8 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     __shared__ __align__(16) char lds[RING_BYTES > RED_BYTES ? RING_BYTES : RED_BYTES];
     float (*const red)[16][DP + 4] = reinterpret_cast<float (*)[16][DP + 4]>(lds);           // (when the rings are done with)
     __shared__ float red_m[WAVES][16], red_l[WAVES][16];
+    __shared__ int again;
     const cache_args& c = a.c;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
     int id = blockIdx.x;
     const int head = id % c.kv_heads;
     id /= c.kv_heads;
@@ -203,7 +203,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     const cache_rows rows = rows_of(c, seq);
     const int R = min(rows.count, c.max_new) * a.group, row0 = rt * (16 * CT);      // query rows: token major, then the group's heads
     if (row0 >= R) return;
-    const int length = length_of(c, seq), D = c.head_dim;
+    const int length = length_of(c, seq);
     // what a query row sees: slots below seen(row)
     auto seen = [&](int row) { return max(0, length - rows.count + row / a.group + 1); };
     const int least = seen(row0), most = seen(min(R, row0 + 16 * CT) - 1);
@@ -212,14 +212,26 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     op16 q[CT][NS][TERMS];
     float qsum[CT], start[CT];
     int limit[CT];
-    const float scale = a.scale;
+    // Once, but for numbers near the end of 32 bits, which the sums are past (weights go up to 2^8, codes to 31): where a query is so
+    // large, all are taken 2^-14 times; where the output is not finite, the blocks are gone through once more with all weights
+    // 2^-48 times (a mean does not depend on that).
+    float scale = a.scale, down = 1.f, lower = 0.f;
+    bool careful = false;
+    if (threadIdx.x == 0) again = 0;
+#pragma unroll 1
+    for (;;) {
+    bool huge = false;
+    int tid = threadIdx.x, D = c.head_dim, group = a.group;
+    asm volatile("" : "+v"(tid));                              // (opaque, so that nothing made of them is kept for another round)
+    asm volatile("" : "+s"(D), "+s"(group));
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
         const int row = row0 + 16 * ct + r;
         const bool valid = row < R;
-        const T* const p = static_cast<const T*>(a.q) + (int64_t)(rows.first + (valid ? row / a.group : 0)) * a.ldq +
-                           (int64_t)(head * a.group + (valid ? row % a.group : 0)) * D;
-        limit[ct] = valid ? seen(row) : 0;
+        const T* const p = static_cast<const T*>(a.q) + (int64_t)(rows.first + (valid ? row / group : 0)) * a.ldq +
+                           (int64_t)(head * group + (valid ? row % group : 0)) * D;
+        limit[ct] = valid ? max(0, length - rows.count + row / group + 1) : 0;
         float sum = 0.f;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
@@ -228,8 +240,14 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int d = d0 + (i >> 1) + 4 * (i & 1);     // (key_operand's order)
-                x[i] = valid && d < D ? elem<T>::load(p + d) : 0.f;
+                x[i] = elem<T>::load(p + min(d, D - 1)) * down;       // (no branch, so that all are on their way together)
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int d = d0 + (i >> 1) + 4 * (i & 1);
+                if (!valid || d >= D) x[i] = 0.f;
                 sum += x[i];
+                huge |= fabsf(x[i]) > 0x1p114f;
             }
             terms_of<TERMS>(x, q[ct][s]);
         }
@@ -239,6 +257,11 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
         start[ct] = -OFFSET * sum;
     }
 
+    if (__builtin_expect(down == 1.f && __ballot(huge) != 0, 0)) {
+        down = 0x1p-14f;
+        scale *= 0x1p14f;
+        continue;
+    }
     floatx4 acc[CT][NB], ones[CT];
     float m[CT], ref[CT], l[CT], z[CT];                        // l, z: of this lane's tokens only
 #pragma unroll
@@ -263,7 +286,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     auto keep_scores = [&](int ct, int tok, const float* x) {
         const int row = row0 + 16 * ct + r;
         if (row >= R) return;
-        float* const p = a.scores + ((int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group) * a.score_stride + tok;
+        float* const p = a.scores + ((int64_t)(rows.first + row / group) * a.num_heads + head * group + row % group) * a.score_stride + tok;
         *reinterpret_cast<float4*>(p) = float4{x[0], x[1], x[2], x[3]};
         *reinterpret_cast<float4*>(p + 4) = float4{x[4], x[5], x[6], x[7]};
     };
@@ -350,7 +373,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) {
                 const bool there = !masked || tok + i < limit[ct];
-                const float e = exp_of(x[ct][i] - ref[ct]);
+                const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[ct][i] - ref[ct], 1.44269504088896340736f, lower));
                 l[ct] += e;
                 w[ct][i] = there ? e * step : 0.f;             // (what is not seen may hold anything)
                 z[ct] += there ? e * middle : 0.f;
@@ -424,6 +447,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
 #pragma unroll 1
     while (queue[0] < last) turn(std::true_type{});
 
+    bool wild = false;
     // the wavefronts' sums meet, column tile by column tile
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -451,25 +475,33 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
         constexpr int LANES = 4 * WAVES;                       // threads a query row
         const int col = tid / LANES, row = row0 + 16 * ct + col;
         if (row < R) {
-            const int64_t out_row = (int64_t)(rows.first + row / a.group) * a.num_heads + head * a.group + row % a.group;
+            const int64_t out_row = (int64_t)(rows.first + row / group) * a.num_heads + head * group + row % group;
             float sum = 0.f, most_of = -INFINITY;
 #pragma unroll
             for (int w = 0; w < WAVES; ++w) {
                 sum += red_l[w][col];
                 most_of = fmaxf(most_of, red_m[w][col]);
             }
-            if (a.stats && tid % LANES == 0) a.stats[out_row * a.splits + split] = float2{most_of, sum};
-            const float inv = a.partial ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
-            T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + row / a.group) * a.ldo + (int64_t)(head * a.group + row % a.group) * D;
+            if (a.stats && tid % LANES == 0) a.stats[out_row * a.splits + split] = float2{most_of, careful ? sum * 0x1p48f : sum};
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + row / group) * a.ldo + (int64_t)(head * group + row % group) * D;
             for (int d = tid % LANES; d < D; d += LANES) {
                 float o = 0.f;
 #pragma unroll
                 for (int w = 0; w < WAVES; ++w) o += red[w][col][d];
                 o *= inv;
+                wild |= !(fabsf(o) < INFINITY);
                 if (a.partial) a.partial[(out_row * a.splits + split) * D + d] = o;
                 else elem<T>::store(out + d, o);
             }
         }
+    }
+    if (careful) return;
+    if (wild) again = 1;
+    __syncthreads();
+    if (!again) return;
+    careful = true;
+    lower = -48.f;
     }
 }
 
@@ -482,7 +514,7 @@ constexpr int kFinishThreads = LORA_CACHE_FINISH_THREADS, kFinishWaves = kFinish
 template <typename T>
 __device__ __forceinline__ void join_row(const cache_attention_args& a, int64_t row)
 {
-    __shared__ float red[kFinishWaves][LORA_MAX_HEAD_DIM], red_sum[kFinishWaves], red_top[kFinishWaves];
+    __shared__ float red[kFinishWaves][LORA_MAX_HEAD_DIM];
     const cache_args& c = a.c;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, D = c.head_dim;
     const int head = (int)(row % a.num_heads);
@@ -492,40 +524,33 @@ __device__ __forceinline__ void join_row(const cache_attention_args& a, int64_t 
     if (i >= rows.count) return;
     const int64_t out_row = (int64_t)(rows.first + i) * a.num_heads + head;
     const float2* const st = a.stats + out_row * a.splits;
-    float top = -INFINITY;
-    for (int s = tid; s < a.splits; s += kFinishThreads) top = fmaxf(top, st[s].x);
+    // a split's part of the row's sum, by every wavefront for itself; its output is a mean already, which no weight takes out of range
+    float top = -INFINITY, sum = 0.f;
+    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, st[s].x);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    if (lane == 0) red_top[wave] = top;
-    __syncthreads();
-    top = red_top[0];
-#pragma unroll
-    for (int w = 1; w < kFinishWaves; ++w) top = fmaxf(top, red_top[w]);
-    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    auto part = [&](float2 e) { return e.y == 0.f ? 0.f : exp_of(e.x - top) * e.y; };      // (nothing seen: its maximum is -inf, perhaps all are; NaN goes on)
+    for (int s = lane; s < a.splits; s += 64) sum += part(st[s]);
+    sum = wave_sum(sum);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    float o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int s = wave; s < a.splits; s += kFinishWaves) {
-        const float2 e = st[s];
         const float* const p = a.partial + (out_row * a.splits + s) * D;
-        const float f = e.y == 0.f ? 0.f : exp_of(e.x - top);  // (nothing seen: its maximum is -inf, perhaps all are; NaN goes on)
-        sum += f * e.y;
+        const float f = part(st[s]) * inv;
 #pragma unroll
         for (int n = 0; n < 4; ++n)
             if (lane + 64 * n < D) o[n] += f * p[lane + 64 * n];
     }
-    if (lane == 0) red_sum[wave] = sum;
 #pragma unroll
     for (int n = 0; n < 4; ++n)
         if (lane + 64 * n < D) red[wave][lane + 64 * n] = o[n];
     __syncthreads();
-    sum = 0.f;
+    if (tid >= D) return;
     float all = 0.f;
 #pragma unroll
-    for (int w = 0; w < kFinishWaves; ++w) {
-        sum += red_sum[w];
-        if (tid < D) all += red[w][tid];
-    }
-    T* const out = static_cast<T*>(a.o) + (int64_t)(rows.first + i) * a.ldo + (int64_t)head * D;
-    if (tid < D) elem<T>::store(out + tid, sum == 0.f ? 0.f : all / sum);
+    for (int w = 0; w < kFinishWaves; ++w) all += red[w][tid];
+    elem<T>::store(static_cast<T*>(a.o) + (int64_t)(rows.first + i) * a.ldo + (int64_t)head * D + tid, all);
 }
 
 // Accumulated weights: a thread four slots of one sequence and kv head, over all query rows, whose scores the attention left behind
@@ -600,7 +625,8 @@ void launch_shape(const cache_attention_args& a, hipStream_t stream)
 template <typename T, int DP>
 void launch_main(const cache_attention_args& a, hipStream_t stream)
 {
-    if ((int64_t)a.group * a.c.max_new > 16) return launch_shape<T, DP, 2, 4>(a, stream);
+    if constexpr (cache_tile_rows(sizeof(T) == 4, DP) == 32)
+        if ((int64_t)a.group * a.c.max_new > 16) return launch_shape<T, DP, 2, 4>(a, stream);
     if constexpr (DP <= 128)
         if (a.waves == 8) return launch_shape<T, DP, 1, 8>(a, stream);
     launch_shape<T, DP, 1, 4>(a, stream);

@@ -659,6 +659,44 @@ def test_more_rows_than_a_tile_and_than_the_weights_take_at_a_time(decay):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [64, 80, 128, 256])
+@pytest.mark.parametrize("lengths,new", [([300, 1, 40], 1), ([300, 33, 40], 9), ([5000], 2), ([2000], 9)])
+@pytest.mark.parametrize("v_up,q_up,k_up", [(125, 0, 0), (0, 124, -60), (125, 0, 100), (125, 124, -60)])
+def test_values_queries_and_keys_up_to_the_end_of_their_range_in_the_cache(dtype, D, lengths, new, v_up, q_up, k_up):
+    """Powers of 2 on the values come out of the mean as they went in, and those on queries and keys go with the scale: what a sum of
+    hundreds of codes takes out of range is as near the definition as what none takes out of it.  Elements are below 4, so that 2^125
+    times a value is in range and the difference of two is; two results that are within a tolerance each differ by two of them."""
+    rng = np.random.default_rng(D + new)
+    H, Hkv = 4, 2
+    pool = Pool(lengths, Hkv, D, 64)
+    few = [min(new, n) for n in lengths]
+    vals = [[rounded(np.clip(rng.standard_normal((n, Hkv, D)) + rng.standard_normal((n, Hkv, 1)), -3.5, 3.5), dtype) for _ in range(2)] for n in lengths]
+    q = rounded(np.clip(rng.standard_normal((sum(few), H, D)), -3.5, 3.5), dtype)
+    pool.fill(vals, dtype)
+    base = run_cache(pool, q, few, dtype, D ** -0.5, 0.0).astype(np.float64)
+    check_cache(pool, vals, q, few, lengths, dtype, D ** -0.5, base, (0.0, 0.0))
+    weights = [pool.slots(pool.weight, s, n) for s, n in enumerate(lengths)]
+    pool.fill([[k * np.float32(2.0) ** k_up, v * np.float32(2.0) ** v_up] for k, v in vals], dtype)
+    scale = D ** -0.5 * 2.0 ** -(q_up + k_up)
+    got = run_cache(pool, q * np.float32(2.0) ** q_up, few, dtype, scale, 0.0).astype(np.float64)
+    assert np.isfinite(got).all()
+    at = offsets(few)
+    for s, n in enumerate(lengths):
+        (ck, sk, zk), (cv, sv, zv) = quantised(vals[s][0]), quantised(vals[s][1])
+        part = np.abs(q[at[s]:at[s + 1]]).astype(np.float64).sum(-1).max()
+        dot = part * (np.abs(zk) + 31 * sk).max() * D ** -0.5
+        share = D * 2.0 ** -23 * dot + (n / 8 + 64) * 2.0 ** -23
+        most = float((np.abs(zv) + 15 * sv).max())
+        tol = 2 * (2 * share * most + (n / 8 + 64) * 2.0 ** -23 * float((np.abs(zv) + 31 * sv).max()))
+        if dtype == BF16:
+            tol += 2 * 1.01 * 2.0 ** -8 * (7.5 * float(sv.max()) + np.abs(base[at[s]:at[s + 1]]))
+        assert np.all(np.abs(got[at[s]:at[s + 1]] * 2.0 ** -v_up - base[at[s]:at[s + 1]]) <= tol), s
+        now = pool.slots(pool.weight, s, n)
+        assert np.all(np.abs(now - weights[s]) <= 4 * share * weights[s] + 1e-30), s
+
+
+@gpu
 def test_sequences_may_share_the_pages_of_a_prefix():
     """... where no weights are kept: two sequences over the same first 64 tokens, each with its own behind them"""
     rng = np.random.default_rng(31)
