@@ -382,7 +382,8 @@ lora_status lora_merge(int32_t num_layers, int32_t n, int32_t k, int32_t rank, f
  * columns of one projection's output.  Query head h uses the keys and values of head h / (num_heads / num_kv_heads).
  * head_dim is 1 .. LORA_MAX_HEAD_DIM.  Pointers have to be aligned to an element; the kernels are fastest with 16 bytes, and
  * leading dimensions and head_dim multiples of 8 (fp32: 4): prompts of anything else take up to three times as long.
- * Outputs must not share memory with inputs.
+ * Outputs must not share memory with inputs or the cache's pages (LORA_ERR_INVALID_ARG, where rows are of one pitch or one of the
+ * two is in one piece); columns of one buffer may lie side by side.
  *
  * Scores, softmax and sums are held in 32 bits; in bf16 the softmax weights are rounded to bf16 for the product with the
  * values, as the output is.  Values may be as large as their type holds: no sum over tokens takes their mean out of range.

@@ -82,6 +82,13 @@ lora_status check_rows(const lora_cache* c, int32_t num_heads, int32_t num_token
     return LORA_OK;
 }
 
+// of the cache's pages
+bool share_bytes(const memory_rows& a, const lora_cache* c)
+{
+    const int64_t page = (int64_t)lora_cache_page_bytes(c->page_tokens, c->head_dim), most = INT64_MAX / 2 / page / c->num_kv_heads;
+    return c->num_pages > 0 && share_bytes(a, memory_rows(c->pages, 1, 1, std::min(c->num_pages, most) * c->num_kv_heads * page, 1));
+}
+
 cache_args args_of(const lora_cache* c, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr)
 {
     cache_args a{};
@@ -118,6 +125,10 @@ extern "C" lora_status lora_attention(lora_attention_plan* p, const void* q, int
     const size_t e = elem_bytes(p->dtype);
     if (!q || !o || ldq < q_row || ldo < q_row || misaligned(q, e) || misaligned(o, e)) return LORA_ERR_INVALID_ARG;
     if (p->num_keys > 0 && (!k || !v || ldk < kv_row || ldv < kv_row || misaligned(k, e) || misaligned(v, e))) return LORA_ERR_INVALID_ARG;
+    const memory_rows out(o, p->num_queries, ldo, q_row, e);
+    if (share_bytes(out, memory_rows(q, p->num_queries, ldq, q_row, e)) || share_bytes(out, memory_rows(k, p->num_keys, ldk, kv_row, e)) ||
+        share_bytes(out, memory_rows(v, p->num_keys, ldv, kv_row, e)))
+        return LORA_ERR_INVALID_ARG;
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const lora_status st = ensure_uploaded(p, stream);
     if (st != LORA_OK) return st;
@@ -135,6 +146,8 @@ extern "C" lora_status lora_cache_append(const lora_cache* c, int32_t dtype, int
     const int64_t row = (int64_t)c->num_kv_heads * c->head_dim;
     if (!k || !v || ldk < row || ldv < row || misaligned(k, elem_bytes(dtype)) || misaligned(v, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
     if (tiles_of_tokens(num_tokens) > most_workgroups(LORA_CACHE_APPEND_THREADS) / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
+    const memory_rows keys(k, num_tokens, ldk, row, elem_bytes(dtype)), values(v, num_tokens, ldv, row, elem_bytes(dtype));
+    if (share_bytes(keys, c) || share_bytes(values, c)) return LORA_ERR_INVALID_ARG;
     return status_of(launch_cache_append(args_of(c, num_tokens, std::min(max_new, num_tokens), d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -147,6 +160,8 @@ extern "C" lora_status lora_cache_read(const lora_cache* c, int32_t dtype, int32
     const int64_t row = (int64_t)c->num_kv_heads * c->head_dim;
     if (!k || !v || ldk < row || ldv < row || misaligned(k, elem_bytes(dtype)) || misaligned(v, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
     if (tiles_of_tokens(num_tokens) > most_workgroups(LORA_CACHE_READ_THREADS) / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
+    const memory_rows keys(k, num_tokens, ldk, row, elem_bytes(dtype)), values(v, num_tokens, ldv, row, elem_bytes(dtype));
+    if (share_bytes(keys, c) || share_bytes(values, c) || share_bytes(keys, values)) return LORA_ERR_INVALID_ARG;
     return status_of(launch_cache_read(args_of(c, num_tokens, std::min(max_new, num_tokens), d_indptr), dtype, k, ldk, v, ldv, static_cast<hipStream_t>(hip_stream)));
 }
 
@@ -178,6 +193,8 @@ extern "C" lora_status lora_cache_attention(const lora_cache* c, int32_t dtype, 
     if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
     const int64_t row = (int64_t)num_heads * c->head_dim;
     if (!q || !o || ldq < row || ldo < row || misaligned(q, elem_bytes(dtype)) || misaligned(o, elem_bytes(dtype))) return LORA_ERR_INVALID_ARG;
+    const memory_rows out(o, num_tokens, ldo, row, elem_bytes(dtype));
+    if (share_bytes(out, memory_rows(q, num_tokens, ldq, row, elem_bytes(dtype))) || share_bytes(out, c)) return LORA_ERR_INVALID_ARG;
     const cache_division v = divide_cache_attention(c, num_heads, num_tokens, max_new, weights);
     if (v.total > 0 && (!workspace || workspace_bytes < v.total || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
     const int64_t rows = (int64_t)num_heads / c->num_kv_heads * max_new, tile = cache_tile_rows(dtype == LORA_F32, c->head_dim), row_tiles = (rows + tile - 1) / tile;

@@ -45,6 +45,19 @@ struct attention_instance {
 // aligned: rows and heads of the call are to 16 bytes; pitch: the greater of the bytes between rows of k and between rows of v
 attention_instance choose_attention(int32_t dtype, int32_t head_dim, int32_t most_rows, bool aligned, int64_t pitch);
 
+// Rows in memory: `width` bytes each, `pitch` apart
+struct memory_rows {
+    int64_t at, rows, pitch, width;
+    memory_rows(const void* p, int64_t rows_, int64_t ld, int64_t width_, size_t element)
+        : at((int64_t)reinterpret_cast<uintptr_t>(p)), rows(rows_), pitch(ld * (int64_t)element), width(width_ * (int64_t)element) {}
+    bool one_piece() const { return rows == 1 || pitch == width; }
+    int64_t end() const { return at + (rows - 1) * pitch + width; }
+};
+
+// Whether an output's rows and an input's have bytes in common.  Columns of one buffer, side by side in each of its rows, have
+// not.  (Rows of two different pitches, neither of them in one piece, are not looked at.)
+bool share_bytes(const memory_rows& a, const memory_rows& b);
+
 // set by the device side, so that the host code of plans links without it
 extern void (*lora_attention_plan_device_release)(lora_attention_plan*);
 

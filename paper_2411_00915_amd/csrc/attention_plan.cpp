@@ -78,6 +78,21 @@ attention_instance choose_attention(int32_t dtype, int32_t head_dim, int32_t mos
     return {dims, keys, 1, fits(keys)};
 }
 
+bool share_bytes(const memory_rows& a, const memory_rows& b)
+{
+    if (a.rows < 1 || b.rows < 1 || a.end() <= b.at || b.end() <= a.at) return false;
+    auto one_in_rows = [](const memory_rows& x, const memory_rows& y) {       // y's first row that ends behind x's start, if it starts before x's end
+        const int64_t behind = x.at - y.at - y.width, i = behind < 0 ? 0 : y.rows == 1 ? 1 : behind / y.pitch + 1;
+        return i < y.rows && y.at + i * y.pitch < x.end();
+    };
+    if (a.one_piece()) return one_in_rows(a, b);
+    if (b.one_piece()) return one_in_rows(b, a);
+    if (a.pitch != b.pitch) return false;
+    const int64_t d = b.at - a.at, k = d >= 0 ? d / a.pitch : -((-d + a.pitch - 1) / a.pitch), ahead = d - k * a.pitch;      // b's row j is `ahead` behind a's row k + j
+    auto both = [&](int64_t n) { return std::max<int64_t>(0, -n) < std::min(b.rows, a.rows - n); };                        // some j with 0 <= n + j < a.rows
+    return (ahead < a.width && both(k)) || (ahead + b.width > a.pitch && both(k + 1));
+}
+
 extern "C" lora_status lora_attention_plan_create(const lora_attention_desc* d, lora_attention_plan** out)
 {
     if (out) *out = nullptr;

@@ -1275,6 +1275,59 @@ def test_an_append_of_too_many_threads_is_refused():
         assert e.value.status == B.LORA_ERR_UNSUPPORTED, heads
 
 
+def test_outputs_that_share_memory_with_inputs_are_refused():
+    plan = B.lora_attention_plan([0, 3, 10], [0, 3, 20], 4, 2, 64, BF16)               # 10 rows of 512 bytes, 20 of 256
+    base = 1 << 20
+
+    def refused(call):
+        with pytest.raises(B.LoraError) as e:
+            call()
+        assert e.value.status == B.LORA_ERR_INVALID_ARG
+
+    far = dict(q=base, ldq=256, k=base << 1, ldk=128, v=base << 2, ldv=128, o=base << 3, ldo=256, scale=1.0)
+    for f in (dict(o=base), dict(o=base + 9 * 512 + 510), dict(o=base - 9 * 512 - 510), dict(o=(base << 1) + 19 * 256), dict(o=(base << 2) - 9 * 512),
+              dict(o=base, ldo=512, ldq=512), dict(o=base + 512 - 2, ldo=512, ldq=512), dict(o=base + 1024 * 5 + 1024 - 510, ldo=512, ldq=512),      # same pitch
+              dict(o=base + 1024 - 510, ldo=512, ldq=512), dict(o=base - 1024 * 3 - 2, ldo=512, ldq=512), dict(o=(base << 1) + 130, ldo=4096, ldk=128),
+              dict(o=(base << 1) - 1024 * 9, ldo=512)):                                 # the last row alone meets the keys
+        refused(lambda: B.lora_attention(plan, **{**far, **f}, stream=0))
+    for f in (dict(k=base + 73000), dict(v=base), dict(k=base - 200), dict(v=1 << 22, k=(1 << 22) + 100)):
+        name = dict(k=4096, v=8192, **{n: 0 for n in ()})
+        name.update(f)
+        refused(lambda: B.lora_cache_read(fake(), BF16, 2, 1, None, name["k"], 128, name["v"], 128, stream=0))
+        if f != dict(v=1 << 22, k=(1 << 22) + 100):
+            refused(lambda: B.lora_cache_append(fake(), BF16, 2, 1, None, name["k"], 128, name["v"], 128, stream=0))
+    for q, o in ((4096, 4096), (4096, 4096 + 1022), (4096, base), (base + 200000, base + 199000), (4096, base - 1000)):
+        refused(lambda: B.lora_cache_attention(fake(), BF16, 4, 2, 1, None, q, 256, o, 256, 1.0, -1.0, 1 << 24, 1 << 30, stream=0))
+
+
+@gpu
+def test_outputs_may_lie_beside_inputs_in_the_rows_of_one_buffer():
+    rng = np.random.default_rng(6)
+    n, m, H, Hkv, D = 33, 50, 4, 2, 64
+    q, k, v = prompt_case(rng, [n], [m], H, Hkv, D, BF16)
+    width = (2 * H + 2 * Hkv) * D
+    rows = torch.zeros((m, width), dtype=torch.bfloat16, device=DEV)                   # q, o, k, v: of the last two, more rows
+    for x, first in ((q, 0), (k, 2 * H * D), (v, (2 * H + Hkv) * D)):
+        rows[:len(x), first:first + x.shape[1] * D] = to_device(x, BF16).view(len(x), -1)
+    plan = B.lora_attention_plan([0, n], [0, m], H, Hkv, D, BF16)
+    at = lambda first: rows.data_ptr() + 2 * first
+    B.lora_attention(plan, at(0), width, at(2 * H * D), width, at((2 * H + Hkv) * D), width, at(H * D), width, 0.125)
+    torch.cuda.synchronize()
+    o, tol, amount, _ = reference(q, k, v, 0.125, lambda i: i + m - n + 1)
+    check(rows[:n, H * D:2 * H * D].float().cpu().numpy().reshape(n, H, D), o, tol, amount, BF16)
+    assert (rows[n:, :2 * H * D] == 0).all()
+    plan.destroy()
+    # ... and one behind the other
+    both = torch.zeros((2 * n, H * D), dtype=torch.bfloat16, device=DEV)
+    both[:n] = to_device(q, BF16).view(n, -1)
+    kd, vd = to_device(k, BF16), to_device(v, BF16)
+    plan = B.lora_attention_plan([0, n], [0, m], H, Hkv, D, BF16)
+    B.lora_attention(plan, both, H * D, kd, Hkv * D, vd, Hkv * D, both[n:], H * D, 0.125)
+    torch.cuda.synchronize()
+    assert torch.equal(both[n:], rows[:n, H * D:2 * H * D])
+    plan.destroy()
+
+
 def test_bytes_of_a_page():
     assert [B.lora_cache_page_bytes(64, d) for d in (1, 64, 65, 128, 129, 256)] == [64 * 72, 64 * 72, 64 * 136, 64 * 136, 64 * 264, 64 * 264]
     assert [B.lora_cache_page_bytes(*a) for a in ((0, 64), (31, 64), (33, 64), (1056, 64), (64, 0), (64, 257), (-32, 64))] == [0] * 7
