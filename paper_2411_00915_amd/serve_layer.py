@@ -24,7 +24,9 @@ DEV = "cuda:0"
 
 
 class Projection:
-    """y = x W + s (x A_a) B_a for the requests' adapters: the weight, the factors and their pointer tables"""
+    """y = x W + s (x A_a) B_a for the requests' adapters: the weight, the factors and their pointer tables, and the plans of the last few
+    batches"""
+    KEPT = 8                                                    # plans: decode steps take one again and again, every prompt batch one of its own
 
     def __init__(self, k, n, ranks, scale, gen):
         def randn(*size, std):
@@ -39,7 +41,12 @@ class Projection:
     def __call__(self, x, lengths, adapters):
         """x [tokens, k] of requests of these lengths, each on its adapter"""
         key = (tuple(lengths), tuple(adapters))                # (a program plans once a batch, for all of its layers)
-        if key not in self.plans:
+        if key in self.plans:
+            self.plans[key] = self.plans.pop(key)              # (the latest used is last)
+        else:
+            if len(self.plans) >= self.KEPT:
+                torch.cuda.synchronize()                       # (a plan is given back when the work that uses it is through)
+                self.plans.pop(next(iter(self.plans)))[0].destroy()
             plan = B.lora_plan(sum(lengths), np.concatenate([[0], np.cumsum(lengths)]), adapters, self.ranks, self.scale, self.k, self.n, B.LORA_BF16)
             B.lora_plan_upload(plan)
             room = torch.empty(max(256, B.lora_plan_query(plan)[2]), dtype=torch.uint8, device=DEV)

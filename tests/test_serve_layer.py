@@ -86,6 +86,24 @@ def test_prompts_decode_steps_and_eviction():
     assert evictions == 2
 
 
+def test_plans_of_past_batches_are_given_back():
+    from paper_2411_00915_amd.serve_layer import DEV, Projection
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(3)
+    p = Projection(256, 256, [8, 16, 24], 2.0, gen)
+    x = torch.randn((9, 256), generator=gen, device=DEV).bfloat16()
+    batches = [([n, 9 - n], [n % 3, (n + 1) % 3]) for n in range(10)] + [([4, 5], [2, 0]), ([9], [1])]
+    first = [p(x, *b) for b in batches]
+    assert len(p.plans) == Projection.KEPT == len({plan.handle for plan, _ in p.plans.values()})
+    held = list(p.plans.values())
+    for b, y in zip(batches, first):
+        assert torch.equal(p(x, *b), y)
+    assert len(p.plans) == Projection.KEPT and list(p.plans)[-1] == ((9,), (1,))
+    assert any(not plan.handle for plan, _ in held)             # (destroyed)
+    p(x, *batches[-3])                                          # one that is held: it is now the last to go
+    assert list(p.plans)[-1] == tuple(map(tuple, batches[-3])) and len(p.plans) == Projection.KEPT
+
+
 def test_the_command_runs():
     from paper_2411_00915_amd import serve_layer
     assert serve_layer.main(["--requests", "3", "--prompt", "40", "--steps", "12", "--hidden", "256", "--heads", "4", "--kv-heads", "2", "--limit", "64",
