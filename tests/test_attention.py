@@ -697,6 +697,24 @@ def test_values_queries_and_keys_up_to_the_end_of_their_range_in_the_cache(dtype
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,new", [(2, 1), (8, 5)])
+@pytest.mark.parametrize("where", [slice(0, 200), slice(2500, 2530), slice(4990, 5000)])
+def test_large_values_in_one_piece_of_a_long_cache(dtype, H, new, where):
+    """... whose sums are taken smaller, beside pieces whose are not"""
+    rng = np.random.default_rng(where.start + new)
+    lengths, D = [5000, 40], 64
+    pool = Pool(lengths, 1, D, 64)
+    vals = tokens(rng, lengths, 1, D, dtype)
+    vals[0][1][where] = rounded(np.clip(vals[0][1][where], -3.5, 3.5) * 2.0 ** 120, dtype)
+    pool.fill(vals, dtype)
+    q = rounded(rng.standard_normal((2 * new, H, D)), dtype)
+    got = run_cache(pool, q, [new, new], dtype, 0.125, 0.0)
+    assert np.isfinite(got).all()
+    check_cache(pool, vals, q, [new, new], lengths, dtype, 0.125, got, (0.0, 0.0))
+
+
+@gpu
 def test_sequences_may_share_the_pages_of_a_prefix():
     """... where no weights are kept: two sequences over the same first 64 tokens, each with its own behind them"""
     rng = np.random.default_rng(31)
