@@ -23,12 +23,15 @@
 // weights before they are rounded.
 //
 // What bounds it, bf16: matrix cores and the softmax's vector instructions, which run beside each other only in part.  Two prompts
-// of 8192 tokens, 40 heads of 128: 1.32 ms, 1.04 PFLOP/s, matrix cores busy in 53 % of the cycles, vector units in 48 %, no bank
-// conflicts.  Four of 1024 tokens, 32 heads: 52 us, 0.66 PFLOP/s, with the last tiles' tail.  fp32: the matrix cores, a product of
-// which takes 64 cycles: 4096 tokens, 16 heads of 64, 152 us.  Rows that are not ALIGNED: 4096 tokens, 32 heads of 128, 125 us
-// against 63.
+// of 8192 tokens, 40 heads of 128: 1.35 ms, 1.02 PFLOP/s, matrix cores busy in 53 % of the cycles, vector units in 48 %, no bank
+// conflicts.  Four of 1024 tokens, 32 heads: 52 us, 0.66 PFLOP/s: the workgroups' order leaves places empty at the end.  fp32, a
+// product of which takes 64 cycles: four of 1024 tokens, 16 heads of 64, 139 us, 62 TFLOP/s, matrix cores busy in 38 %: all
+// workgroups have a place at once, and those with the most keys take as long as the whole.  Rows that are not ALIGNED: 4096
+// tokens, 32 heads of 128, 127 us against 64.
+// bf16 weights are rounded to bf16 because the matrix cores take both operands in one type; outputs are then 2.1e-3 from 64-bit
+// arithmetic (normwise), 1.6e-3 of which are the output's own rounding.
 // Why so: 32 queries are a product's width, and four wavefronts share what is in LDS; of 64 keys a tile there are half the barriers
-// and maxima (32: 1436 against 1315 us), and heads past 128 have room for 32.  Few queries leave wavefronts without work: the
+// and maxima (32: 1436 against 1315 us at the time), and heads past 128 have room for 32.  Few queries leave wavefronts without work: the
 // plan gives those other heads of the same keys, or, where the chip is not full anyway, KS of them share the tile's keys and add up
 // in the end (32 heads of 128 on 8, 8 x 20 queries behind 1000 keys: 20.6 -> 15.9 us; of 256 dims 41 -> 43: not there).
 namespace {

@@ -12,7 +12,7 @@
 // element.  A token's keys are one run of bytes in its page; its values are 16 pieces that lie beside those of the seven
 // tokens around it, so they pass through LDS and go 8 tokens at a time (4 bytes apart a lane, 32 bytes together).
 // Bound by memory where there are many tokens (8 heads of 128, bf16: 8192 tokens in 17 and out in 10 us, 84 MB, 3.1 TB/s; 64000 out
-// in 57, 332 MB, 5.8), by the chain offsets -> length -> page -> store where there are few (16 tokens: 5.4 in, 3.7 out).
+// in 51, 332 MB, 6.5), by the chain offsets -> length -> page -> store where there are few (16 tokens: 5.7 in, 3.8 out).
 namespace {
 
 constexpr int kTile = 32;                                   // (tiles_of_tokens)
@@ -287,7 +287,7 @@ bool rows_aligned(const void* k, int64_t ldk, const void* v, int64_t ldv, int32_
 // order: above it, all; equal to it, the first few.  A thread has four slots in a row at a time (one address, one load), 4 STEPS
 // in all, whose numbers stay in registers (STEPS 0: they are read again in every pass).  Many weights share their first bits,
 // the exponent's: a wavefront adds those of its first lane's bin in one go.  Bound by one compute unit's instructions: 32768
-// weights 26.5 us (a slot at a time: 54), 1300 of 512 heads 11.5 in all.
+// weights 26.3 us (a slot at a time: 54), 1300 of 512 heads 11.3 in all.
 __device__ __forceinline__ uint32_t order_of(float w)
 {
     if (w != w) return 0xffffffffu;
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(kSelectThreads) void cache_select_kernel(cache_args
 
 // Second step: the kept tokens' codes, words and weights, a workgroup kMoved of them of a head: three trips to memory (what is
 // kept, its pages, their contents).  64 at a time, values in the target's order: 64 caches of 1300 tokens to 1000, 8 heads of 128,
-// 42 us for 139 MB, 3.3 TB/s; with selection and the values read back 132 (32 at a time 136; 128: 132, but one cache of 32768
+// 50 us for 139 MB, 2.8 TB/s; with selection and the values read back 132 (32 at a time 136; 128: 132, but one cache of 32768
 // tokens to 4096 70 instead of 66).
 constexpr int kMoved = 64;
 template <int DP>

@@ -16,11 +16,12 @@
 // it is.  The wavefronts of a workgroup (four or eight) take turns at the blocks of 32 and meet in LDS at the end; long contexts
 // are split over workgroups as well, which a second launch joins.
 //
-// Bound by memory: 256 requests of 1024 tokens, 32 heads of 128, 224 us, 5.0 TB/s.  The codes come straight to LDS, a ring of
-// blocks for each wavefront: with registers as their target 343 us against 247 at the time, as the compiler then has too few
-// left to ask ahead (a ring of three at 128 dims costs a workgroup a compute unit: 280).  Few requests are bound by the chain
-// length -> page -> codes: 8 of 700 tokens 11.0 us.  Four tokens over 131072, 32 heads on 8, with accumulated weights: 46 us here, the scores written out for
-// them (67 MB beside 147) included, 22 in the launch that reads them back.
+// Bound by memory: 256 requests of 1024 tokens, 32 heads of 128, 223 us, 5.1 TB/s (vector units busy in 83 % of the cycles).
+// The codes come straight to LDS, a ring of blocks for each wavefront: with registers as their target 343 us against 247 at the
+// time, as the compiler then has too few left to ask ahead (a ring of three at 128 dims costs a workgroup a compute unit: 280).
+// Few requests are bound by the chain length -> page -> codes: 8 of 700 tokens 11.0 us.  Four tokens over 131072, 32 heads on 8,
+// with accumulated weights: 45 us here, the scores written out for them (67 MB beside 147) included, 20 in the launch that
+// reads them back.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -507,7 +508,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
 
 // What is left when all splits are done, in one launch: the first `rows` workgroups join the splits of a query row each, the others
 // add up accumulated weights, for which they join the statistics themselves (one token over 8 caches of 2000, 32 heads on 8: 21.6 us
-// in all with two launches, 18.9 with one).  Bound by the scores that it reads, 67 MB in 22 us for four tokens over 131072.
+// in all with two launches, 18.9 with one).  Bound by the scores that it reads, 67 MB in 20 us for four tokens over 131072.
 constexpr int kFinishThreads = LORA_CACHE_FINISH_THREADS, kFinishWaves = kFinishThreads / 64, kWeightSlots = 4 * kFinishThreads;
 
 // a row's splits: the wavefronts take turns at them
