@@ -223,7 +223,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     for (;;) {
     bool huge = false;
     int tid = threadIdx.x, D = c.head_dim, group = a.group;
-    asm volatile("" : "+v"(tid));                              // (opaque, so that nothing made of them is kept for another round)
+    asm volatile("" : "+v"(tid));                              // (opaque, so that nothing made of them is kept for another pass)
     asm volatile("" : "+s"(D), "+s"(group));
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), r = lane & 15, g = lane >> 4;
 #pragma unroll
