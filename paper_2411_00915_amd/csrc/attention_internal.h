@@ -65,7 +65,7 @@ extern void (*lora_attention_plan_device_release)(lora_attention_plan*);
 inline int32_t padded_head_dim(int32_t d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 // Query rows of a tile of the cache's attention, where there are more than 16.  fp32 and 256 dims: 32 rows in three terms are more
-// registers than there are (64 requests of 1000 tokens, 8 new ones, 16 heads on 4: 92 us with 32 rows, 72 with 16).
+// registers than there are (64 requests of 1000 tokens, 8 new ones, 16 heads on 4: 96 us with 32 rows, 66 with 16).
 constexpr int32_t cache_tile_rows(bool f32, int32_t head_dim) { return f32 && head_dim > 128 ? 16 : 32; }
 
 // how lora_cache_attention divides its work, from what the host knows; the workspace's parts follow from it

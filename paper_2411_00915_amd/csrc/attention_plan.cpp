@@ -177,17 +177,17 @@ cache_division divide_cache_attention(const lora_cache* c, int32_t num_heads, in
     v.row_tiles = (int32_t)((rows + 31) / 32);
     const int64_t wgs = (int64_t)c->num_seqs * c->num_kv_heads * v.row_tiles;
     // Long contexts are split where there are fewer workgroups than compute units: into 512, of at least 256 tokens (two blocks a
-    // wavefront; 512 where there are 128 workgroups already: 160 of 260 tokens 10.7 us in one piece, 18.4 in two); and, where the
+    // wavefront; 512 where there are 128 workgroups already: 160 of 260 tokens 7.8 us in one piece, 15.7 in two); and, where the
     // pieces keep 2048 tokens, beside which joining them costs little, into the 1024 that the chip holds at a time (12 requests of
-    // 20000 tokens, 8 heads: 63 us in six pieces, 57 in ten; 40 of 8000: 94 in one, 78 in four; where the workgroups fill the
+    // 20000 tokens, 8 heads: 62 us in six pieces, 55 in ten; 40 of 8000: 92 in one, 79 in four; where the workgroups fill the
     // compute units evenly it is the other way round: 8 of 8000, 32 heads, 50 in one and 55 in four).
     auto pieces = [&](int64_t total, int64_t tokens) {
         return std::min<int64_t>((total + wgs - 1) / std::max<int64_t>(wgs, 1), (c->max_length + tokens - 1) / tokens);
     };
     const int64_t splits = std::max<int64_t>(1, std::max(wgs < 256 ? pieces(512, wgs < 128 ? 256 : 512) : 1, pieces(1024, 2048)));
     // In one piece, and fewer than two workgroups a compute unit: eight wavefronts each (one tile of rows, heads of up to 128; 8
-    // requests of 700 tokens, 32 heads: 11.4 us with four, 10.3 with eight; with pieces to join it is the other way round, 11.6
-    // and 12.5 for one request of 2000).
+    // requests of 700 tokens, 32 heads: 11.7 us with four, 10.3 with eight; with pieces to join there is nothing in it, 11.2
+    // and 11.1 for one request of 2000, 55.5 and 56.4 for 12 of 20000).
     v.waves = splits == 1 && wgs < 512 && rows <= 16 && padded_head_dim(c->head_dim) <= 128 ? 8 : 4;
     v.split_tokens = (int32_t)std::max<int64_t>(128, ((c->max_length + splits - 1) / splits + 127) / 128 * 128);
     v.splits = (int32_t)std::max<int64_t>(1, ((int64_t)c->max_length + v.split_tokens - 1) / v.split_tokens);

@@ -16,11 +16,11 @@
 // it is.  The wavefronts of a workgroup (four or eight) take turns at the blocks of 32 and meet in LDS at the end; long contexts
 // are split over workgroups as well, which a second launch joins.
 //
-// Bound by memory: 256 requests of 1024 tokens, 32 heads of 128, 223 us, 5.1 TB/s (vector units busy in 83 % of the cycles).
+// Bound by memory: 256 requests of 1024 tokens, 32 heads of 128, 225 us, 5.0 TB/s (vector units busy in 80 % of the cycles).
 // The codes come straight to LDS, a ring of blocks for each wavefront: with registers as their target 343 us against 247 at the
 // time, as the compiler then has too few left to ask ahead (a ring of three at 128 dims costs a workgroup a compute unit: 280).
-// Few requests are bound by the chain length -> page -> codes: 8 of 700 tokens 11.0 us.  Four tokens over 131072, 32 heads on 8,
-// with accumulated weights: 45 us here, the scores written out for them (67 MB beside 147) included, 20 in the launch that
+// Few requests are bound by the chain length -> page -> codes: 8 of 700 tokens 11.1 us.  Four tokens over 131072, 32 heads on 8,
+// with accumulated weights: 39 us here, the scores written out for them (67 MB beside 147) included, 20 in the launch that
 // reads them back.
 #include <hip/hip_runtime.h>
 
@@ -183,6 +183,28 @@ __device__ __forceinline__ float max_of_rows(float x)
     return x;
 }
 
+// Dims d0 .. d0 + 7 of a query in key_operand's order; what is past the D that there are comes from among them.  No branch over the
+// lanes, so that all loads are on their way together.
+template <typename T>
+__device__ __forceinline__ void load_query(const T* p, int d0, int D, bool aligned, float* x)
+{
+    if (!aligned) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = elem<T>::load(p + min(d0 + (i >> 1) + 4 * (i & 1), D - 1));
+    } else if constexpr (sizeof(T) == 2) {
+        const uint4 u = ld16(p + min(d0, D - 8));
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = (i >> 1) + 4 * (i & 1);
+            x[i] = __uint_as_float(e & 1 ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
+        }
+    } else {
+        const float4 a = *reinterpret_cast<const float4*>(p + min(d0, D - 4)), b = *reinterpret_cast<const float4*>(p + min(d0 + 4, D - 4));
+        x[0] = a.x; x[1] = b.x; x[2] = a.y; x[3] = b.y; x[4] = a.z; x[5] = b.z; x[6] = a.w; x[7] = b.w;
+    }
+}
+
 template <typename T, int DP, int CT, bool KEEP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 : 2) void cache_attention_kernel(cache_attention_args a)
 {
@@ -218,10 +240,11 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     // 2^-48 times (a mean does not depend on that).
     float scale = a.scale, down = 1.f, lower = 0.f;
     bool careful = false;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(a.q) | (uintptr_t)((a.ldq | c.head_dim) * (int64_t)sizeof(T))) & 15) == 0;       // queries to 16 bytes
     if (threadIdx.x == 0) again = 0;
 #pragma unroll 1
     for (;;) {
-    bool huge = false;
+    float largest = 0.f;
     int tid = threadIdx.x, D = c.head_dim, group = a.group;
     asm volatile("" : "+v"(tid));                              // (opaque, so that nothing made of them is kept for another pass)
     asm volatile("" : "+s"(D), "+s"(group));
@@ -238,17 +261,13 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
         for (int s = 0; s < NS; ++s) {
             float x[8];
             const int d0 = (DP / 4) * g + 8 * s;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int d = d0 + (i >> 1) + 4 * (i & 1);     // (key_operand's order)
-                x[i] = elem<T>::load(p + min(d, D - 1)) * down;       // (no branch, so that all are on their way together)
-            }
+            load_query(p, d0, D, aligned, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int d = d0 + (i >> 1) + 4 * (i & 1);
-                if (!valid || d >= D) x[i] = 0.f;
+                x[i] = valid && d < D ? x[i] * down : 0.f;
                 sum += x[i];
-                huge |= fabsf(x[i]) > 0x1p114f;
+                largest = fmaxf(largest, fabsf(x[i]));
             }
             terms_of<TERMS>(x, q[ct][s]);
         }
@@ -258,7 +277,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
         start[ct] = -OFFSET * sum;
     }
 
-    if (__builtin_expect(down == 1.f && __ballot(huge) != 0, 0)) {
+    if (__builtin_expect(down == 1.f && __ballot(largest > 0x1p114f) != 0, 0)) {
         down = 0x1p-14f;
         scale *= 0x1p14f;
         continue;

@@ -646,6 +646,24 @@ def test_single_tokens_need_no_offsets_and_any_layout_will_do(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("D", [4, 8, 12, 64, 80, 100, 128, 200, 256])
+@pytest.mark.parametrize("new", [1, 9])
+def test_queries_of_any_alignment_give_the_same(dtype, D, new):
+    """16 bytes a lane where rows and heads allow it, element by element elsewhere"""
+    rng = np.random.default_rng(D)
+    lengths, H = [70, 200, 9], 4
+    pool = Pool(lengths, 2, D, 32, weight=False)
+    vals = tokens(rng, lengths, 2, D, dtype)
+    pool.fill(vals, dtype)
+    q = rounded(rng.standard_normal((3 * new, H, D)), dtype)
+    got = run_cache(pool, q, [new] * 3, dtype, 0.1)
+    check_cache(pool, vals, q, [new] * 3, lengths, dtype, 0.1, got)
+    for pad, shift in ((8, 0), (8, 8), (1, 0), (0, 1), (7, 3)):
+        assert np.array_equal(run_cache(pool, q, [new] * 3, dtype, 0.1, pad=pad, shift=shift), got), (pad, shift)
+
+
+@gpu
 @pytest.mark.parametrize("decay", [-1.0, 0.0])
 def test_more_rows_than_a_tile_and_than_the_weights_take_at_a_time(decay):
     rng = np.random.default_rng(14)
