@@ -1326,12 +1326,10 @@ def test_outputs_that_share_memory_with_inputs_are_refused():
               dict(o=base + 1024 - 510, ldo=512, ldq=512), dict(o=base - 1024 * 3 - 2, ldo=512, ldq=512), dict(o=(base << 1) + 130, ldo=4096, ldk=128),
               dict(o=(base << 1) - 1024 * 9, ldo=512)):                                 # the last row alone meets the keys
         refused(lambda: B.lora_attention(plan, **{**far, **f}, stream=0))
-    for f in (dict(k=base + 73000), dict(v=base), dict(k=base - 200), dict(v=1 << 22, k=(1 << 22) + 100)):
-        name = dict(k=4096, v=8192, **{n: 0 for n in ()})
-        name.update(f)
-        refused(lambda: B.lora_cache_read(fake(), BF16, 2, 1, None, name["k"], 128, name["v"], 128, stream=0))
-        if f != dict(v=1 << 22, k=(1 << 22) + 100):
-            refused(lambda: B.lora_cache_append(fake(), BF16, 2, 1, None, name["k"], 128, name["v"], 128, stream=0))
+    for k, v in ((base + 73000, 8192), (4096, base), (base - 200, 8192)):             # the pages
+        for call in (B.lora_cache_read, B.lora_cache_append):
+            refused(lambda: call(fake(), BF16, 2, 1, None, k, 128, v, 128, stream=0))
+    refused(lambda: B.lora_cache_read(fake(), BF16, 2, 1, None, (1 << 22) + 100, 128, 1 << 22, 128, stream=0))        # its two outputs
     for q, o in ((4096, 4096), (4096, 4096 + 1022), (4096, base), (base + 200000, base + 199000), (4096, base - 1000)):
         refused(lambda: B.lora_cache_attention(fake(), BF16, 4, 2, 1, None, q, 256, o, 256, 1.0, -1.0, 1 << 24, 1 << 30, stream=0))
 
