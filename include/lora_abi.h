@@ -444,7 +444,7 @@ typedef struct {
     void*          pages;          /* [num_pages][num_kv_heads] pages, 16-byte aligned */
     float*         weight;         /* accumulated weights [num_pages][num_kv_heads][page_tokens], or NULL: none kept */
     const int32_t* page_table;     /* [num_seqs][table_stride] */
-    int32_t*       length;         /* [num_seqs] tokens held, those of the call at hand included (written by lora_cache_evict only) */
+    int32_t*       length;         /* [num_seqs] tokens held, those of the call at hand included (of the cache's calls, only lora_cache_evict writes it) */
     int64_t        num_pages;
     int32_t        num_seqs;
     int32_t        table_stride;
@@ -499,6 +499,127 @@ lora_status lora_cache_attention(const lora_cache* cache, int32_t dtype, int32_t
  */
 lora_status lora_cache_evict(const lora_cache* source, const lora_cache* target, int32_t budget, int32_t recent, int32_t* kept,
                              void* hip_stream);
+
+/*
+ * PAGES.  Which page of the pool holds which part of which sequence, kept on the device: page tables, lengths and how many use a page, for
+ * all layers of a model at once (every layer's lora_cache has pages of its own and the same page_table and length).  The
+ * descriptor is the caller's and read during a call only; its pointers are device memory, and what they hold is read and
+ * written when the call runs, so that a captured graph replays with what they hold then.  A page may be named by the entries of
+ * several sequences (a prefix that they share, beams of one request); `users` says by how many.  A pool begins with users and
+ * length all 0.  A program may hold pages of its own by adding to their users.  Entries behind a sequence's last page are not
+ * looked at, and entries outside [0, num_pages) count as not there: they are not given back, shared or copied.
+ */
+typedef struct {
+    int32_t* page_table;           /* [num_seqs][table_stride] */
+    int32_t* length;               /* [num_seqs] tokens held */
+    int32_t* users;                /* [num_pages] entries that name the page; 0: it is free */
+    int64_t  num_pages;            /* (num_pages + num_seqs) * page_tokens < 2^31 */
+    int32_t  num_seqs;             /* at most 2^14 */
+    int32_t  table_stride;
+    int32_t  max_length;           /* no sequence is longer; <= table_stride * page_tokens, at most 2^30 */
+    int32_t  page_tokens;          /* multiple of 32, at most 1024 */
+} lora_pages;
+
+/* bytes of workspace of the two calls below, 256-byte aligned; nothing in it is kept from one call to the next */
+lora_status lora_pages_workspace(const lora_pages* pages, size_t* bytes);
+
+/*
+ * lora_pages_resize -- every sequence to the length that its request wants: wanted, device, [num_seqs].
+ *   shorter, or 0 (the request has ended): pages behind the new end lose a user, their entries become -1.
+ *   longer: new pages at the end; and where the page that the first new token goes to holds tokens already and has other users, a page
+ *       of its own in its place, which the caller fills by lora_cache_copy, layer by layer, before anything is appended.  (Where
+ *       all users of a page grow in this call, the one with the most tokens in it, of those the last, keeps it.)
+ *   equal: nothing.  Outside [0, max_length]: the sequence is left as it is, and not granted.
+ * Sequences are served in order, each wholly or not at all, until one needs more pages than are free (those given back in this call
+ * included): it, and all behind it that need a page, stay as they were and are not granted.  New pages are the free pages of the
+ * lowest numbers, in the order of the sequences, a copy before the pages at the end.
+ * granted: device, [num_seqs], 1 or 0 (NULL: not wanted).  indptr: device, [num_seqs + 1], offsets of the sequences' new tokens, packed
+ * one behind the other, as lora_cache_append takes them (NULL: not wanted).  Of every new token with a row below num_tokens: its
+ * sequence, its position in it and its slot in the pool, page * page_tokens + place (each NULL: not wanted; -1 as slot where the
+ * entry is not there); rows behind the last token are left as they were.  copies: device, [num_seqs][2], the page to copy and the page
+ * to fill, -1 and -1 where there is none (NULL: LORA_ERR_INVALID_ARG).  length, users and page_table are brought up to date.
+ * The outputs may not share memory with each other, nor with what the call reads.
+ * Deterministic: what the atomics add up are whole numbers.
+ */
+lora_status lora_pages_resize(const lora_pages* pages, const int32_t* wanted, int32_t num_tokens, int32_t* granted, int32_t* indptr,
+                              int32_t* token_seq, int32_t* token_position, int64_t* token_slot, int32_t* copies,
+                              void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * lora_pages_fork -- sequence s becomes what sequence parent[s] was (device, [num_seqs]; outside [0, num_seqs): empty), all at once: the
+ * same pages and the same length, so that nothing is copied, and users as that leaves them.  What grows from there gets pages of its own by
+ * lora_pages_resize.  Beams: parents as lora_beam_select gives them.
+ */
+lora_status lora_pages_fork(const lora_pages* pages, const int32_t* parent, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * lora_cache_copy -- page copies[i][0] of one layer's cache to page copies[i][1], all heads, codes, words and accumulated weights (where the cache keeps
+ * them); i < num_copies; copies: device.  Pairs with a page outside [0, num_pages), or of a page and itself, are passed over.
+ * No page may be written twice, or written and read.
+ */
+lora_status lora_cache_copy(const lora_cache* cache, int32_t num_copies, const int32_t* copies, void* hip_stream);
+
+/*
+ * BEAMS.  lora_beam_select -- the best continuations of num_groups requests of `beams` beams each.  Beam b of request g is row r = g * beams + b of
+ * logits [num_groups * beams, vocab] (dtype, rows ld elements apart, aligned to an element; fastest at 16 bytes) and has score[r], the
+ * sum of its tokens' log-probabilities.  Its continuation by token v is worth
+ *     score[r] + (logits[r, v] - log sum_u exp logits[r, u])
+ * and of all of a request's the num_out greatest are given, greatest first: equal ones by beam, then by logit, greater first, then by
+ * token.  What they are worth is compared in 64 bits and rounded once, to out_score; sums of exponentials are 64 bits, each exponential 32.
+ * out_parent: the beam's row (for lora_pages_fork, where num_out is beams), out_token; all [num_groups][num_out], device.
+ * A beam has ended where last_token[r] (device, [num_groups * beams]; NULL: none has) is end_token, unless that is negative: its row is not looked
+ * at, and its one continuation is end_token, worth score[r].  Tokens of logit -inf, and rows whose sum of exponentials or whose score
+ * is no finite number (a row of -inf alone, one with NaN or +inf, a beam that is not there with score -inf) have no continuation;
+ * where there are fewer than num_out in all, the rest is -inf, -1 and -1.
+ * beams 1 .. LORA_MAX_BEAMS, num_out 1 .. LORA_MAX_BEAMS, vocab 1 .. 2^24.  Deterministic.
+ * Outputs must not share memory with inputs.
+ */
+#define LORA_MAX_BEAMS 64
+lora_status lora_beam_workspace(int32_t num_groups, int32_t beams, int32_t vocab, int32_t num_out, size_t* bytes);
+lora_status lora_beam_select(int32_t dtype, int32_t num_groups, int32_t beams, int32_t vocab, const void* logits, int64_t ld,
+                             const float* score, const int32_t* last_token, int32_t end_token, int32_t num_out,
+                             float* out_score, int32_t* out_parent, int32_t* out_token, void* workspace, size_t workspace_bytes,
+                             void* hip_stream);
+
+/*
+ * ATTENTION OVER CHOSEN PAGES.  Of a long cache each query attends to a few pages of every kv head: those whose keys could give it the
+ * largest score, by bounds that are kept of every page beside the cache.
+ *
+ * lora_cache_digest -- bounds of the keys that the cache holds of every page with one of the last tokens (packed as lora_cache_append takes
+ * them), after they were appended.  With x[t][d] the values (lora_cache_read's in 32 bits) of the page's tokens t below the sequence's length:
+ *     step = fp32(greatest |x| * fp32(1/127)), 0 if below 2^-100
+ *     upper[d] = min(127, ceil(max_t x[t][d] / step)),  lower[d] = max(-127, floor(min_t x[t][d] / step))     (0 where step is 0)
+ * bounds: device, [num_pages][num_kv_heads][2][DP] int8, 16-byte aligned: upper, then lower, DP as in a page; steps: device, [num_pages][num_kv_heads] fp32.
+ * A page with NaN among its tokens, or a value past 32 bits, has NaN for its step.
+ */
+lora_status lora_cache_digest(const lora_cache* cache, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr,
+                              int8_t* bounds, float* steps, void* hip_stream);
+
+/*
+ * lora_cache_choose -- the pages that each token attends to: token i of n of a sequence of length L sees slots 0 .. L - n + i and so pages
+ * 0 .. m - 1.  Up to `budget` of them are chosen for every kv head, all where there are no more: the first `first`, the last `recent`, and
+ * of the others those with the greatest
+ *     max over the kv head's query heads h of  fp32(sum_d max(c[d], 0) upper[d] + min(c[d], 0) lower[d]) * unit_h  * step
+ *     unit_h = fp32(greatest |q| * fp32(1/127)), 0 if below 2^-100;  c[d] = rint(q[h][d] / unit_h)   (unit_h NaN where q is not finite)
+ * equal ones by lower number, NaN above all.  The sums are whole numbers and all else is rounded once in 32 bits, so the choice does not depend on how it
+ * is computed.  Pages that are not there are not chosen.  The order is that of q . k: meant for a scale above 0.
+ * chosen: device, [num_tokens][num_kv_heads][budget] numbers of pages of the sequence (columns of its page table), ascending, -1 behind them.
+ * budget >= 1; first, recent >= 0, first + recent <= budget.  workspace as for lora_cache_attention, bytes from lora_cache_choose_workspace.
+ */
+lora_status lora_cache_choose_workspace(const lora_cache* cache, int32_t num_tokens, int32_t max_new, size_t* bytes);
+lora_status lora_cache_choose(const lora_cache* cache, int32_t dtype, int32_t num_heads, int32_t num_tokens, int32_t max_new,
+                              const int32_t* d_indptr, const void* q, int64_t ldq, const int8_t* bounds, const float* steps, int32_t budget,
+                              int32_t first, int32_t recent, int32_t* chosen, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * lora_cache_attention_chosen -- lora_cache_attention (without weights) where token and kv head see the slots of the chosen pages alone, as far as the
+ * token sees them without a choice.  chosen as lora_cache_choose gives it, or the caller's own: any order, each page once; numbers outside
+ * [0, m) count as not there.  A token that sees no slot gets zeros.  workspace: bytes from lora_cache_chosen_workspace.
+ */
+lora_status lora_cache_chosen_workspace(const lora_cache* cache, int32_t num_heads, int32_t num_tokens, int32_t max_new, int32_t budget, size_t* bytes);
+lora_status lora_cache_attention_chosen(const lora_cache* cache, int32_t dtype, int32_t num_heads, int32_t num_tokens, int32_t max_new,
+                                        const int32_t* d_indptr, const void* q, int64_t ldq, void* o, int64_t ldo, float scale, int32_t budget,
+                                        const int32_t* chosen, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 const char* lora_status_str(lora_status s);
 

@@ -42,6 +42,7 @@ LORA_EXPAND_BY_ROUNDS = 1 << 30
 LORA_STATIC_V_BYTES = 16 << 20
 LORA_STATIC_MAX_GROUPS = 4096
 LORA_MAX_HEAD_DIM = 256
+LORA_MAX_BEAMS = 64
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 _f32p = ctypes.POINTER(ctypes.c_float)
@@ -91,6 +92,11 @@ class CacheDesc(ctypes.Structure):
                 ("page_tokens", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
+class PagesDesc(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("length", ctypes.c_void_p), ("users", ctypes.c_void_p), ("num_pages", ctypes.c_int64),
+                ("num_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("max_length", ctypes.c_int32), ("page_tokens", ctypes.c_int32)]
+
+
 _vp = ctypes.c_void_p
 _lib.lora_plan_create.restype = ctypes.c_int
 _lib.lora_plan_create.argtypes = [ctypes.POINTER(BatchDesc), ctypes.POINTER(_vp)]
@@ -131,6 +137,14 @@ _lib.lora_cache_page_bytes.restype = ctypes.c_size_t
 _lib.lora_cache_page_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32]
 _lib.lora_cache_workspace.restype = ctypes.c_int
 _lib.lora_cache_workspace.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+_lib.lora_pages_workspace.restype = ctypes.c_int
+_lib.lora_pages_workspace.argtypes = [_vp, ctypes.POINTER(ctypes.c_size_t)]
+_lib.lora_beam_workspace.restype = ctypes.c_int
+_lib.lora_beam_workspace.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+_lib.lora_cache_choose_workspace.restype = ctypes.c_int
+_lib.lora_cache_choose_workspace.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
+_lib.lora_cache_chosen_workspace.restype = ctypes.c_int
+_lib.lora_cache_chosen_workspace.argtypes = [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.POINTER(ctypes.c_size_t)]
 _lib.lora_status_str.restype = ctypes.c_char_p
 _lib.lora_status_str.argtypes = [ctypes.c_int]
 _lib.lora_tuning_set.restype = None
@@ -171,6 +185,8 @@ EXPORTED = ["lora_timing_begin", "lora_timing_end", "lora_timing_read", "lora_ke
             "lora_fused_forward", "lora_merge", "lora_status_str", "lora_tuning_set", "lora_tuning_get",
             "lora_attention_plan_create", "lora_attention_plan_destroy", "lora_attention_plan_upload", "lora_attention",
             "lora_cache_page_bytes", "lora_cache_append", "lora_cache_read", "lora_cache_workspace", "lora_cache_attention", "lora_cache_evict",
+            "lora_pages_workspace", "lora_pages_resize", "lora_pages_fork", "lora_cache_copy", "lora_beam_workspace", "lora_beam_select",
+            "lora_cache_digest", "lora_cache_choose_workspace", "lora_cache_choose", "lora_cache_chosen_workspace", "lora_cache_attention_chosen",
             "lora_tuning_table_set", "lora_tuning_table_get", "lora_probe", "lora_trace_set", "lora_trace_tick_khz"]
 
 TUNING_FIELDS = ["shrink_waves", "shrink_tb2_min_rows", "shrink_max_jb", "expand_wave_bytes",
@@ -507,6 +523,54 @@ def lora_cache_workspace(cache: Cache, num_heads, num_tokens, max_new, weights=F
     return int(n.value)
 
 
+class Pages:
+    """A lora_pages descriptor and the device tensors that it names (kept alive by it)."""
+
+    def __init__(self, desc: PagesDesc, page_table=None, length=None, users=None):
+        self.desc = desc
+        self.handle = ctypes.addressof(desc)
+        self.page_table, self.length, self.users = page_table, length, users
+
+
+def lora_pages(page_table, length, users, page_tokens, max_length) -> Pages:
+    """Descriptor over device tensors of int32: page_table [num_seqs, table_stride], length [num_seqs], users [num_pages]."""
+    import torch
+    for name, x in (("page_table", page_table), ("length", length), ("users", users)):
+        if x.dtype != torch.int32 or not x.is_contiguous():
+            raise ValueError(f"{name}: a contiguous tensor of int32")
+    if page_table.dim() != 2 or length.dim() != 1 or users.dim() != 1 or page_table.shape[0] != length.shape[0]:
+        raise ValueError("page_table [num_seqs, table_stride], length [num_seqs], users [num_pages]")
+    desc = PagesDesc(_ptr(page_table), _ptr(length), _ptr(users), int(users.shape[0]), int(length.shape[0]), int(page_table.shape[1]), int(max_length),
+                     int(page_tokens))
+    return Pages(desc, page_table, length, users)
+
+
+def _workspace(function, *arguments) -> int:
+    n = ctypes.c_size_t()
+    _check(getattr(_lib, function)(*arguments, ctypes.byref(n)), function)
+    return int(n.value)
+
+
+def lora_pages_workspace(pages: Pages) -> int:
+    """Bytes that lora_pages_resize and lora_pages_fork need"""
+    return _workspace("lora_pages_workspace", pages.handle)
+
+
+def lora_beam_workspace(num_groups, beams, vocab, num_out) -> int:
+    """Bytes that lora_beam_select needs with these arguments"""
+    return _workspace("lora_beam_workspace", int(num_groups), int(beams), int(vocab), int(num_out))
+
+
+def lora_cache_choose_workspace(cache: Cache, num_tokens, max_new) -> int:
+    """Bytes that lora_cache_choose needs with these arguments"""
+    return _workspace("lora_cache_choose_workspace", cache.handle, int(num_tokens), int(max_new))
+
+
+def lora_cache_chosen_workspace(cache: Cache, num_heads, num_tokens, max_new, budget) -> int:
+    """Bytes that lora_cache_attention_chosen needs with these arguments"""
+    return _workspace("lora_cache_chosen_workspace", cache.handle, int(num_heads), int(num_tokens), int(max_new), int(budget))
+
+
 def _first_stream():
     """torch's current stream, and the functions that give the current device and a device's current stream once torch is
     initialised"""
@@ -547,3 +611,21 @@ _calls.bind_attention(*(_address(f) for f in (_lib.lora_attention_plan_upload, _
 (lora_attention_plan_upload, lora_attention, lora_cache_append, lora_cache_read, lora_cache_attention, lora_cache_evict) = (
     _calls.lora_attention_plan_upload, _calls.lora_attention, _calls.lora_cache_append, _calls.lora_cache_read, _calls.lora_cache_attention,
     _calls.lora_cache_evict)
+
+_calls.bind_sequences(*(_address(f) for f in (_lib.lora_pages_resize, _lib.lora_pages_fork, _lib.lora_cache_copy, _lib.lora_beam_select, _lib.lora_cache_digest,
+                                              _lib.lora_cache_choose, _lib.lora_cache_attention_chosen)))
+
+# lora_pages_resize(pages, d_wanted, num_tokens, d_granted, d_indptr, d_token_seq, d_token_position, d_token_slot, d_copies, workspace,
+#     workspace_bytes, stream=None),
+# lora_pages_fork(pages, d_parent, workspace, workspace_bytes, stream=None),
+# lora_cache_copy(cache, num_copies, d_copies, stream=None),
+# lora_beam_select(dtype, num_groups, beams, vocab, logits, ld, d_score, d_last_token, end_token, num_out, d_out_score, d_out_parent, d_out_token,
+#     workspace, workspace_bytes, stream=None),
+# lora_cache_digest(cache, num_tokens, max_new, d_indptr, d_bounds, d_steps, stream=None),
+# lora_cache_choose(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, d_bounds, d_steps, budget, first, recent, d_chosen, workspace,
+#     workspace_bytes, stream=None),
+# lora_cache_attention_chosen(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, o, ldo, scale, budget, d_chosen, workspace,
+#     workspace_bytes, stream=None)
+(lora_pages_resize, lora_pages_fork, lora_cache_copy, lora_beam_select, lora_cache_digest, lora_cache_choose, lora_cache_attention_chosen) = (
+    _calls.lora_pages_resize, _calls.lora_pages_fork, _calls.lora_cache_copy, _calls.lora_beam_select, _calls.lora_cache_digest, _calls.lora_cache_choose,
+    _calls.lora_cache_attention_chosen)

@@ -18,7 +18,8 @@ CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 OBJ_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["planner.cpp", "kernels_general.hip", "kernels_tiled.hip", "kernels_stream.hip", "kernels_gemm.hip", "kernels_gemm_small.hip", "kernels_gemm_mid.hip", "kernels_any.hip",
-           "attention_plan.cpp", "attention.hip", "kernels_attention.hip", "kernels_cache.hip", "kernels_cache_attention.hip", "abi.hip", "timing.hip", "probe.hip"]
+           "attention_plan.cpp", "attention.hip", "kernels_attention.hip", "kernels_cache.hip", "kernels_cache_attention.hip", "kernels_choose.hip",
+           "sequences.hip", "kernels_pages.hip", "kernels_beam.hip", "abi.hip", "timing.hip", "probe.hip"]
 
 HIP_FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-Wall", "-Wno-unused-function",
              "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

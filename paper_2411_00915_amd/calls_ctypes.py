@@ -12,6 +12,11 @@ _ATTENTION_PROTOTYPES = [ctypes.CFUNCTYPE(ctypes.c_int, *a) for a in (
     (_P, _P), (_P, _P, _L, _P, _L, _P, _L, _P, _L, _F, _P), (_P, _I, _I, _I, _P, _P, _L, _P, _L, _P), (_P, _I, _I, _I, _P, _P, _L, _P, _L, _P),
     (_P, _I, _I, _I, _I, _P, _P, _L, _P, _L, _F, _F, _P, _Z, _P), (_P, _P, _I, _I, _P, _P))]
 
+_SEQUENCE_PROTOTYPES = [ctypes.CFUNCTYPE(ctypes.c_int, *a) for a in (
+    (_P, _P, _I, _P, _P, _P, _P, _P, _P, _P, _Z, _P), (_P, _P, _P, _Z, _P), (_P, _I, _P, _P),
+    (_I, _I, _I, _I, _P, _L, _P, _P, _I, _I, _P, _P, _P, _P, _Z, _P), (_P, _I, _I, _P, _P, _P, _P),
+    (_P, _I, _I, _I, _I, _P, _P, _L, _P, _P, _I, _I, _I, _P, _P, _Z, _P), (_P, _I, _I, _I, _I, _P, _P, _L, _P, _L, _F, _I, _P, _P, _Z, _P))]
+
 
 def bind(check, first_stream, *addresses):
     """As that of _calls: check(status, name) raises; first_stream()[0] is torch's current stream; the functions' addresses in
@@ -103,3 +108,46 @@ def lora_cache_attention(cache, dtype, num_heads, num_tokens, max_new, d_indptr,
 
 def lora_cache_evict(cache, target, budget, recent, d_kept, stream=None):
     _check(_evict(cache.handle, target.handle, int(budget), int(recent), _ptr(d_kept), _stream(stream)), "lora_cache_evict")
+
+
+def bind_sequences(*addresses):
+    """As that of _calls: the functions' addresses in the order pages_resize, pages_fork, cache_copy, beam_select, cache_digest,
+    cache_choose, cache_attention_chosen"""
+    global _resize, _fork, _copy, _beam_select, _digest, _choose, _attention_chosen
+    _resize, _fork, _copy, _beam_select, _digest, _choose, _attention_chosen = (prototype(address) for prototype, address in zip(_SEQUENCE_PROTOTYPES, addresses))
+
+
+def lora_pages_resize(pages, d_wanted, num_tokens, d_granted, d_indptr, d_token_seq, d_token_position, d_token_slot, d_copies, workspace, workspace_bytes, stream=None):
+    _check(_resize(pages.handle, _ptr(d_wanted), int(num_tokens), _ptr(d_granted), _ptr(d_indptr), _ptr(d_token_seq), _ptr(d_token_position), _ptr(d_token_slot),
+                   _ptr(d_copies), _ptr(workspace), int(workspace_bytes), _stream(stream)), "lora_pages_resize")
+
+
+def lora_pages_fork(pages, d_parent, workspace, workspace_bytes, stream=None):
+    _check(_fork(pages.handle, _ptr(d_parent), _ptr(workspace), int(workspace_bytes), _stream(stream)), "lora_pages_fork")
+
+
+def lora_cache_copy(cache, num_copies, d_copies, stream=None):
+    _check(_copy(cache.handle, int(num_copies), _ptr(d_copies), _stream(stream)), "lora_cache_copy")
+
+
+def lora_beam_select(dtype, num_groups, beams, vocab, logits, ld, d_score, d_last_token, end_token, num_out, d_out_score, d_out_parent, d_out_token, workspace,
+                     workspace_bytes, stream=None):
+    _check(_beam_select(int(dtype), int(num_groups), int(beams), int(vocab), _ptr(logits), int(ld), _ptr(d_score), _ptr(d_last_token), int(end_token),
+                        int(num_out), _ptr(d_out_score), _ptr(d_out_parent), _ptr(d_out_token), _ptr(workspace), int(workspace_bytes), _stream(stream)),
+           "lora_beam_select")
+
+
+def lora_cache_digest(cache, num_tokens, max_new, d_indptr, d_bounds, d_steps, stream=None):
+    _check(_digest(cache.handle, int(num_tokens), int(max_new), _ptr(d_indptr), _ptr(d_bounds), _ptr(d_steps), _stream(stream)), "lora_cache_digest")
+
+
+def lora_cache_choose(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, d_bounds, d_steps, budget, first, recent, d_chosen, workspace,
+                      workspace_bytes, stream=None):
+    _check(_choose(cache.handle, int(dtype), int(num_heads), int(num_tokens), int(max_new), _ptr(d_indptr), _ptr(q), int(ldq), _ptr(d_bounds), _ptr(d_steps),
+                   int(budget), int(first), int(recent), _ptr(d_chosen), _ptr(workspace), int(workspace_bytes), _stream(stream)), "lora_cache_choose")
+
+
+def lora_cache_attention_chosen(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, o, ldo, scale, budget, d_chosen, workspace, workspace_bytes,
+                                stream=None):
+    _check(_attention_chosen(cache.handle, int(dtype), int(num_heads), int(num_tokens), int(max_new), _ptr(d_indptr), _ptr(q), int(ldq), _ptr(o), int(ldo),
+                             float(scale), int(budget), _ptr(d_chosen), _ptr(workspace), int(workspace_bytes), _stream(stream)), "lora_cache_attention_chosen")

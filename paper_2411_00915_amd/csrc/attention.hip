@@ -7,6 +7,7 @@
 
 #include "kernels.h"
 #include "kernels_attention.h"
+#include "kernels_choose.h"
 
 namespace {
 bool misaligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
@@ -236,4 +237,165 @@ extern "C" lora_status lora_cache_evict(const lora_cache* source, const lora_cac
     if (heads > most_workgroups(LORA_CACHE_SELECT_THREADS) || heads > most_workgroups(LORA_CACHE_MOVE_THREADS) / (budget / 32 + 1)) return LORA_ERR_UNSUPPORTED;
     return status_of(launch_cache_evict(args_of(source, 0, 0, nullptr), args_of(target, 0, 0, nullptr), target->length, budget, recent, kept,
                                         static_cast<hipStream_t>(hip_stream)));
+}
+
+extern "C" lora_status lora_cache_copy(const lora_cache* c, int32_t num_copies, const int32_t* copies, void* hip_stream)
+{
+    const lora_status st = check_cache(c);
+    if (st != LORA_OK) return st;
+    if (num_copies < 0 || misaligned(copies, 4) || (num_copies > 0 && !copies)) return LORA_ERR_INVALID_ARG;
+    if (num_copies == 0 || c->num_seqs == 0) return LORA_OK;
+    if (num_copies > most_workgroups(LORA_CACHE_COPY_THREADS) / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
+    return status_of(launch_cache_copy(args_of(c, 0, 0, nullptr), num_copies, copies, static_cast<hipStream_t>(hip_stream)));
+}
+
+namespace {
+// bounds and steps of every page; what is written may not be what is read
+lora_status check_digest(const lora_cache* c, const int8_t* bounds, const float* steps)
+{
+    if (!bounds || !steps || misaligned(bounds, 16) || misaligned(steps, 4)) return LORA_ERR_INVALID_ARG;
+    const int64_t heads = c->num_pages * c->num_kv_heads, row = 2 * (int64_t)padded_head_dim(c->head_dim);
+    const memory_rows b(bounds, 1, 1, heads * row, 1), s(steps, 1, 1, heads, 4);
+    return share_bytes(b, c) || share_bytes(s, c) || share_bytes(b, s) ? LORA_ERR_INVALID_ARG : LORA_OK;
+}
+
+// tokens, one by one: as many workgroups of `threads` for each kv head, `more` each
+lora_status check_single(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new, int64_t threads, int64_t more)
+{
+    if (num_heads < 1 || num_heads % c->num_kv_heads != 0) return LORA_ERR_INVALID_ARG;
+    if ((int64_t)num_tokens * num_heads > INT32_MAX || (int64_t)c->num_seqs * max_new > INT32_MAX / num_heads) return LORA_ERR_UNSUPPORTED;
+    return (int64_t)c->num_seqs * max_new * c->num_kv_heads > most_workgroups(threads) / std::max<int64_t>(1, more) ? LORA_ERR_UNSUPPORTED : LORA_OK;
+}
+
+// pages of the longest sequence, to whole 32s
+int64_t key_stride(const lora_cache* c) { return ((int64_t)(c->max_length + c->page_tokens - 1) / c->page_tokens + 31) / 32 * 32; }
+size_t choose_bytes(const lora_cache* c, int32_t num_tokens)
+{
+    return key_stride(c) > LORA_CACHE_CHOOSE_NEAR ? ((size_t)num_tokens * c->num_kv_heads * (size_t)key_stride(c) * 4 + 255) / 256 * 256 : 0;
+}
+}  // namespace
+
+extern "C" lora_status lora_cache_digest(const lora_cache* c, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr, int8_t* bounds, float* steps,
+                                         void* hip_stream)
+{
+    lora_status st = check_tokens(c, LORA_BF16, num_tokens, max_new, d_indptr);
+    if (st != LORA_OK) return st;
+    if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0 || c->num_pages == 0) return LORA_OK;
+    st = check_digest(c, bounds, steps);
+    if (st != LORA_OK) return st;
+    max_new = std::min(max_new, num_tokens);
+    const int64_t pages = digest_pages(max_new, c->page_tokens);
+    if ((int64_t)c->num_seqs * c->num_kv_heads > most_workgroups(64) / pages - 4) return LORA_ERR_UNSUPPORTED;
+    return status_of(launch_cache_digest(args_of(c, num_tokens, max_new, d_indptr), bounds, steps, static_cast<hipStream_t>(hip_stream)));
+}
+
+extern "C" lora_status lora_cache_choose_workspace(const lora_cache* c, int32_t num_tokens, int32_t max_new, size_t* bytes)
+{
+    if (!bytes) return LORA_ERR_INVALID_ARG;
+    *bytes = 0;
+    const lora_status st = check_tokens(c, LORA_BF16, num_tokens, max_new, nullptr);
+    if (st != LORA_OK) return st;
+    if ((int64_t)num_tokens * c->num_kv_heads > ((int64_t)1 << 40) / std::max<int64_t>(1, key_stride(c))) return LORA_ERR_UNSUPPORTED;
+    if (num_tokens > 0 && max_new > 0 && c->num_seqs > 0) *bytes = choose_bytes(c, num_tokens);
+    return LORA_OK;
+}
+
+extern "C" lora_status lora_cache_choose(const lora_cache* c, int32_t dtype, int32_t num_heads, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr,
+                                         const void* q, int64_t ldq, const int8_t* bounds, const float* steps, int32_t budget, int32_t first, int32_t recent,
+                                         int32_t* chosen, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    lora_status st = check_tokens(c, dtype, num_tokens, max_new, d_indptr);
+    if (st != LORA_OK) return st;
+    if (budget < 1 || first < 0 || recent < 0 || (int64_t)first + recent > budget) return LORA_ERR_INVALID_ARG;
+    max_new = std::min(max_new, num_tokens);
+    st = check_single(c, num_heads, num_tokens, max_new, LORA_CACHE_CHOOSE_THREADS, 1);
+    if (st != LORA_OK) return st;
+    if ((int64_t)num_tokens * c->num_kv_heads > ((int64_t)1 << 40) / std::max<int64_t>(budget, key_stride(c))) return LORA_ERR_UNSUPPORTED;
+    if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
+    const int64_t row = (int64_t)num_heads * c->head_dim;
+    if (!q || ldq < row || misaligned(q, elem_bytes(dtype)) || !chosen || misaligned(chosen, 4)) return LORA_ERR_INVALID_ARG;
+    st = check_digest(c, bounds, steps);
+    if (st != LORA_OK) return st;
+    const memory_rows out(chosen, 1, 1, (int64_t)num_tokens * c->num_kv_heads * budget, 4);
+    const int64_t heads = c->num_pages * c->num_kv_heads;
+    if (share_bytes(out, memory_rows(q, num_tokens, ldq, row, elem_bytes(dtype))) || share_bytes(out, c) || share_bytes(out, memory_rows(steps, 1, 1, heads, 4)) ||
+        share_bytes(out, memory_rows(bounds, 1, 1, heads * 2 * padded_head_dim(c->head_dim), 1)))
+        return LORA_ERR_INVALID_ARG;
+    const size_t bytes = choose_bytes(c, num_tokens);
+    if (bytes > 0 && (!workspace || workspace_bytes < bytes || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
+    choose_args a{};
+    a.c = args_of(c, num_tokens, max_new, d_indptr);
+    a.q = q;
+    a.ldq = ldq;
+    a.group = num_heads / c->num_kv_heads;
+    a.budget = budget;
+    a.first = first;
+    a.recent = recent;
+    a.bounds = bounds;
+    a.steps = steps;
+    a.chosen = chosen;
+    a.keys = bytes > 0 ? static_cast<uint32_t*>(workspace) : nullptr;
+    a.key_stride = key_stride(c);
+    return status_of(launch_cache_choose(a, dtype, static_cast<hipStream_t>(hip_stream)));
+}
+
+extern "C" lora_status lora_cache_chosen_workspace(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new, int32_t budget, size_t* bytes)
+{
+    if (!bytes) return LORA_ERR_INVALID_ARG;
+    *bytes = 0;
+    lora_status st = check_tokens(c, LORA_BF16, num_tokens, max_new, nullptr);
+    if (st != LORA_OK) return st;
+    if (budget < 1) return LORA_ERR_INVALID_ARG;
+    if (budget > LORA_ATTENTION_MAX_ROWS / c->page_tokens) return LORA_ERR_UNSUPPORTED;
+    max_new = std::min(max_new, num_tokens);
+    st = check_single(c, num_heads, num_tokens, max_new, 256, 1);
+    if (st != LORA_OK) return st;
+    if (num_tokens > 0 && max_new > 0 && c->num_seqs > 0) *bytes = divide_chosen_attention(c, num_heads, num_tokens, max_new, budget).total;
+    return LORA_OK;
+}
+
+extern "C" lora_status lora_cache_attention_chosen(const lora_cache* c, int32_t dtype, int32_t num_heads, int32_t num_tokens, int32_t max_new,
+                                                   const int32_t* d_indptr, const void* q, int64_t ldq, void* o, int64_t ldo, float scale, int32_t budget,
+                                                   const int32_t* chosen, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    lora_status st = check_tokens(c, dtype, num_tokens, max_new, d_indptr);
+    if (st != LORA_OK) return st;
+    if (!std::isfinite(scale) || budget < 1) return LORA_ERR_INVALID_ARG;
+    if (budget > LORA_ATTENTION_MAX_ROWS / c->page_tokens) return LORA_ERR_UNSUPPORTED;
+    max_new = std::min(max_new, num_tokens);
+    st = check_single(c, num_heads, num_tokens, max_new, 256, 1);
+    if (st != LORA_OK) return st;
+    if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
+    const int64_t row = (int64_t)num_heads * c->head_dim;
+    const size_t e = elem_bytes(dtype);
+    if (!q || !o || ldq < row || ldo < row || misaligned(q, e) || misaligned(o, e) || !chosen || misaligned(chosen, 4)) return LORA_ERR_INVALID_ARG;
+    const memory_rows out(o, num_tokens, ldo, row, e);
+    if (share_bytes(out, memory_rows(q, num_tokens, ldq, row, e)) || share_bytes(out, c) ||
+        share_bytes(out, memory_rows(chosen, 1, 1, (int64_t)num_tokens * c->num_kv_heads * budget, 4)))
+        return LORA_ERR_INVALID_ARG;
+    const cache_division v = divide_chosen_attention(c, num_heads, num_tokens, max_new, budget);
+    if (v.total > 0 && (!workspace || workspace_bytes < v.total || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
+    const int64_t group = num_heads / c->num_kv_heads, tile = group > 16 ? cache_tile_rows(dtype == LORA_F32, c->head_dim) : 16, row_tiles = (group + tile - 1) / tile;
+    st = check_single(c, num_heads, num_tokens, max_new, 64 * v.waves, v.splits * row_tiles);
+    if (st != LORA_OK) return st;
+    char* const w = static_cast<char*>(workspace);
+    cache_attention_args a{};
+    a.c = args_of(c, num_tokens, max_new, d_indptr);
+    a.q = q;
+    a.o = o;
+    a.ldq = ldq;
+    a.ldo = ldo;
+    a.num_heads = num_heads;
+    a.group = (int32_t)group;
+    a.scale = scale;
+    a.decay = -1.f;
+    a.row_tiles = (int32_t)row_tiles;
+    a.splits = v.splits;
+    a.split_tokens = v.split_tokens;
+    a.waves = v.waves;
+    a.stats = v.splits > 1 ? reinterpret_cast<float2*>(w + v.stats) : nullptr;
+    a.partial = v.splits > 1 ? reinterpret_cast<float*>(w + v.partial) : nullptr;
+    a.chosen = chosen;
+    a.budget = budget;
+    return status_of(launch_cache_attention(a, dtype, static_cast<hipStream_t>(hip_stream)));
 }

@@ -21,7 +21,7 @@ struct attention_tile {
 
 // Threads of a workgroup, and how many workgroups of them a launch holds: fewer than 2^32 threads in all
 enum { LORA_ATTENTION_THREADS = 256, LORA_CACHE_APPEND_THREADS = 320, LORA_CACHE_READ_THREADS = 256, LORA_CACHE_FINISH_THREADS = 512, LORA_CACHE_SELECT_THREADS = 1024,
-       LORA_CACHE_MOVE_THREADS = 256 };
+       LORA_CACHE_MOVE_THREADS = 256, LORA_CACHE_COPY_THREADS = 256 };
 constexpr int64_t most_workgroups(int64_t threads) { return (((int64_t)1 << 32) - 1) / threads; }
 
 struct lora_attention_plan {
@@ -75,3 +75,5 @@ struct cache_division {
     int64_t score_stride;
 };
 cache_division divide_cache_attention(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new, bool weights);
+// the same of lora_cache_attention_chosen: every token for itself, over `budget` pages
+cache_division divide_chosen_attention(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new, int32_t budget);

@@ -201,3 +201,12 @@ cache_division divide_cache_attention(const lora_cache* c, int32_t num_heads, in
     v.total = off;
     return v;
 }
+
+cache_division divide_chosen_attention(const lora_cache* c, int32_t num_heads, int32_t num_tokens, int32_t max_new, int32_t budget)
+{
+    // as many sequences as there are tokens, and as long as what one of them attends to
+    lora_cache tokens = *c;
+    tokens.num_seqs = (int32_t)std::min<int64_t>(num_tokens, (int64_t)c->num_seqs * max_new);
+    tokens.max_length = budget * c->page_tokens;
+    return divide_cache_attention(&tokens, num_heads, num_tokens, 1, false);
+}

@@ -35,6 +35,16 @@ struct attention_library {
     decltype(&lora_cache_evict) evict;
 } attention_lib;
 
+struct sequence_library {
+    decltype(&lora_pages_resize) resize;
+    decltype(&lora_pages_fork) fork;
+    decltype(&lora_cache_copy) copy;
+    decltype(&lora_beam_select) beam_select;
+    decltype(&lora_cache_digest) digest;
+    decltype(&lora_cache_choose) choose;
+    decltype(&lora_cache_attention_chosen) attention_chosen;
+} sequence_lib;
+
 PyObject* check = nullptr;                 // check(status, name) raises
 PyObject* first_stream = nullptr;          // torch.cuda.current_stream() by itself: initialises torch's side
 PyObject *get_device = nullptr, *get_stream = nullptr;
@@ -356,6 +366,117 @@ SIGNATURE(lora_cache_evict)
     CALL_OF(attention_lib, evict(cache, target, (int32_t)budget, (int32_t)recent, static_cast<int32_t*>(kept), stream))
 }
 
+SIGNATURE(lora_pages_resize)
+{
+    ARGS(11, "pages", "d_wanted", "num_tokens", "d_granted", "d_indptr", "d_token_seq", "d_token_position", "d_token_slot", "d_copies", "workspace",
+         "workspace_bytes", "stream")
+    const lora_pages* pages;
+    int64_t num_tokens, bytes;
+    void *wanted, *granted, *indptr, *seq, *position, *slot, *copies, *workspace, *stream;
+    if (!handle(a[0], &pages) || !address(a[1], &wanted) || !integer(a[2], &num_tokens) || !address(a[3], &granted) || !address(a[4], &indptr) ||
+        !address(a[5], &seq) || !address(a[6], &position) || !address(a[7], &slot) || !address(a[8], &copies) || !address(a[9], &workspace) ||
+        !integer(a[10], &bytes) || !stream_of(a[11], &stream))
+        return nullptr;
+    CALL_OF(sequence_lib, resize(pages, static_cast<const int32_t*>(wanted), (int32_t)num_tokens, static_cast<int32_t*>(granted), static_cast<int32_t*>(indptr),
+                                 static_cast<int32_t*>(seq), static_cast<int32_t*>(position), static_cast<int64_t*>(slot), static_cast<int32_t*>(copies),
+                                 workspace, (size_t)bytes, stream))
+}
+
+SIGNATURE(lora_pages_fork)
+{
+    ARGS(4, "pages", "d_parent", "workspace", "workspace_bytes", "stream")
+    const lora_pages* pages;
+    int64_t bytes;
+    void *parent, *workspace, *stream;
+    if (!handle(a[0], &pages) || !address(a[1], &parent) || !address(a[2], &workspace) || !integer(a[3], &bytes) || !stream_of(a[4], &stream)) return nullptr;
+    CALL_OF(sequence_lib, fork(pages, static_cast<const int32_t*>(parent), workspace, (size_t)bytes, stream))
+}
+
+SIGNATURE(lora_cache_copy)
+{
+    ARGS(3, "cache", "num_copies", "d_copies", "stream")
+    const lora_cache* cache;
+    int64_t num_copies;
+    void *copies, *stream;
+    if (!handle(a[0], &cache) || !integer(a[1], &num_copies) || !address(a[2], &copies) || !stream_of(a[3], &stream)) return nullptr;
+    CALL_OF(sequence_lib, copy(cache, (int32_t)num_copies, static_cast<const int32_t*>(copies), stream))
+}
+
+SIGNATURE(lora_beam_select)
+{
+    ARGS(15, "dtype", "num_groups", "beams", "vocab", "logits", "ld", "d_score", "d_last_token", "end_token", "num_out", "d_out_score", "d_out_parent",
+         "d_out_token", "workspace", "workspace_bytes", "stream")
+    int64_t dtype, num_groups, beams, vocab, ld, end_token, num_out, bytes;
+    void *logits, *score, *last, *out_score, *out_parent, *out_token, *workspace, *stream;
+    if (!integer(a[0], &dtype) || !integer(a[1], &num_groups) || !integer(a[2], &beams) || !integer(a[3], &vocab) || !address(a[4], &logits) ||
+        !integer(a[5], &ld) || !address(a[6], &score) || !address(a[7], &last) || !integer(a[8], &end_token) || !integer(a[9], &num_out) ||
+        !address(a[10], &out_score) || !address(a[11], &out_parent) || !address(a[12], &out_token) || !address(a[13], &workspace) || !integer(a[14], &bytes) ||
+        !stream_of(a[15], &stream))
+        return nullptr;
+    CALL_OF(sequence_lib, beam_select((int32_t)dtype, (int32_t)num_groups, (int32_t)beams, (int32_t)vocab, logits, ld, static_cast<const float*>(score),
+                                      static_cast<const int32_t*>(last), (int32_t)end_token, (int32_t)num_out, static_cast<float*>(out_score),
+                                      static_cast<int32_t*>(out_parent), static_cast<int32_t*>(out_token), workspace, (size_t)bytes, stream))
+}
+
+SIGNATURE(lora_cache_digest)
+{
+    ARGS(6, "cache", "num_tokens", "max_new", "d_indptr", "d_bounds", "d_steps", "stream")
+    const lora_cache* cache;
+    int64_t num_tokens, max_new;
+    void *indptr, *bounds, *steps, *stream;
+    if (!handle(a[0], &cache) || !integer(a[1], &num_tokens) || !integer(a[2], &max_new) || !address(a[3], &indptr) || !address(a[4], &bounds) ||
+        !address(a[5], &steps) || !stream_of(a[6], &stream))
+        return nullptr;
+    CALL_OF(sequence_lib, digest(cache, (int32_t)num_tokens, (int32_t)max_new, static_cast<const int32_t*>(indptr), static_cast<int8_t*>(bounds),
+                                 static_cast<float*>(steps), stream))
+}
+
+SIGNATURE(lora_cache_choose)
+{
+    ARGS(16, "cache", "dtype", "num_heads", "num_tokens", "max_new", "d_indptr", "q", "ldq", "d_bounds", "d_steps", "budget", "first", "recent", "d_chosen",
+         "workspace", "workspace_bytes", "stream")
+    const lora_cache* cache;
+    int64_t dtype, num_heads, num_tokens, max_new, ldq, budget, first, recent, bytes;
+    void *indptr, *q, *bounds, *steps, *chosen, *workspace, *stream;
+    if (!handle(a[0], &cache) || !integer(a[1], &dtype) || !integer(a[2], &num_heads) || !integer(a[3], &num_tokens) || !integer(a[4], &max_new) ||
+        !address(a[5], &indptr) || !address(a[6], &q) || !integer(a[7], &ldq) || !address(a[8], &bounds) || !address(a[9], &steps) || !integer(a[10], &budget) ||
+        !integer(a[11], &first) || !integer(a[12], &recent) || !address(a[13], &chosen) || !address(a[14], &workspace) || !integer(a[15], &bytes) ||
+        !stream_of(a[16], &stream))
+        return nullptr;
+    CALL_OF(sequence_lib, choose(cache, (int32_t)dtype, (int32_t)num_heads, (int32_t)num_tokens, (int32_t)max_new, static_cast<const int32_t*>(indptr), q, ldq,
+                                 static_cast<const int8_t*>(bounds), static_cast<const float*>(steps), (int32_t)budget, (int32_t)first, (int32_t)recent,
+                                 static_cast<int32_t*>(chosen), workspace, (size_t)bytes, stream))
+}
+
+SIGNATURE(lora_cache_attention_chosen)
+{
+    ARGS(15, "cache", "dtype", "num_heads", "num_tokens", "max_new", "d_indptr", "q", "ldq", "o", "ldo", "scale", "budget", "d_chosen", "workspace",
+         "workspace_bytes", "stream")
+    const lora_cache* cache;
+    int64_t dtype, num_heads, num_tokens, max_new, ldq, ldo, budget, bytes;
+    float scale;
+    void *indptr, *q, *o, *chosen, *workspace, *stream;
+    if (!handle(a[0], &cache) || !integer(a[1], &dtype) || !integer(a[2], &num_heads) || !integer(a[3], &num_tokens) || !integer(a[4], &max_new) ||
+        !address(a[5], &indptr) || !address(a[6], &q) || !integer(a[7], &ldq) || !address(a[8], &o) || !integer(a[9], &ldo) || !real(a[10], &scale) ||
+        !integer(a[11], &budget) || !address(a[12], &chosen) || !address(a[13], &workspace) || !integer(a[14], &bytes) || !stream_of(a[15], &stream))
+        return nullptr;
+    CALL_OF(sequence_lib, attention_chosen(cache, (int32_t)dtype, (int32_t)num_heads, (int32_t)num_tokens, (int32_t)max_new,
+                                           static_cast<const int32_t*>(indptr), q, ldq, o, ldo, scale, (int32_t)budget, static_cast<const int32_t*>(chosen),
+                                           workspace, (size_t)bytes, stream))
+}
+
+// bind_sequences(addresses of the library's functions in the order of `sequence_library`)
+PyObject* bind_sequences(PyObject*, PyObject* args)
+{
+    unsigned long long p[7];
+    if (!PyArg_ParseTuple(args, "KKKKKKK", &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6])) return nullptr;
+    sequence_lib = sequence_library{reinterpret_cast<decltype(sequence_library::resize)>(p[0]),      reinterpret_cast<decltype(sequence_library::fork)>(p[1]),
+                                    reinterpret_cast<decltype(sequence_library::copy)>(p[2]),        reinterpret_cast<decltype(sequence_library::beam_select)>(p[3]),
+                                    reinterpret_cast<decltype(sequence_library::digest)>(p[4]),      reinterpret_cast<decltype(sequence_library::choose)>(p[5]),
+                                    reinterpret_cast<decltype(sequence_library::attention_chosen)>(p[6])};
+    Py_RETURN_NONE;
+}
+
 // bind_attention(addresses of the library's functions in the order of `attention_library`)
 PyObject* bind_attention(PyObject*, PyObject* args)
 {
@@ -393,6 +514,7 @@ PyObject* bind(PyObject*, PyObject* args)
 PyMethodDef methods[] = {
     {"bind", bind, METH_VARARGS, nullptr},
     {"bind_attention", bind_attention, METH_VARARGS, nullptr},
+    {"bind_sequences", bind_sequences, METH_VARARGS, nullptr},
     METHOD(lora_plan_upload, "(plan, stream=None)"),
     METHOD(lora_shrink, "(plan, x, ldx, d_At_ptrs, v, stream=None)"),
     METHOD(lora_expand, "(plan, v, d_Bt_ptrs, y, ldy, beta=1.0, stream=None)"),
@@ -408,6 +530,17 @@ PyMethodDef methods[] = {
     METHOD(lora_cache_attention,
            "(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, o, ldo, scale, decay, workspace, workspace_bytes, stream=None)"),
     METHOD(lora_cache_evict, "(cache, target, budget, recent, d_kept, stream=None)"),
+    METHOD(lora_pages_resize,
+           "(pages, d_wanted, num_tokens, d_granted, d_indptr, d_token_seq, d_token_position, d_token_slot, d_copies, workspace, workspace_bytes, stream=None)"),
+    METHOD(lora_pages_fork, "(pages, d_parent, workspace, workspace_bytes, stream=None)"),
+    METHOD(lora_cache_copy, "(cache, num_copies, d_copies, stream=None)"),
+    METHOD(lora_beam_select,
+           "(dtype, num_groups, beams, vocab, logits, ld, d_score, d_last_token, end_token, num_out, d_out_score, d_out_parent, d_out_token, workspace, workspace_bytes, stream=None)"),
+    METHOD(lora_cache_digest, "(cache, num_tokens, max_new, d_indptr, d_bounds, d_steps, stream=None)"),
+    METHOD(lora_cache_choose,
+           "(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, d_bounds, d_steps, budget, first, recent, d_chosen, workspace, workspace_bytes, stream=None)"),
+    METHOD(lora_cache_attention_chosen,
+           "(cache, dtype, num_heads, num_tokens, max_new, d_indptr, q, ldq, o, ldo, scale, budget, d_chosen, workspace, workspace_bytes, stream=None)"),
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -41,6 +41,8 @@ struct cache_attention_args {
     float* partial;              // [num_tokens * num_heads][splits][head_dim], where splits > 1
     float* scores;               // [num_tokens * num_heads][score_stride], where weights are wanted
     int64_t score_stride;
+    const int32_t* chosen;       // [num_tokens][kv_heads][budget] pages, or null: all
+    int32_t budget;              // (splits and split_tokens are then of a token's budget * page_tokens slots)
 };
 
 // The cache's tokens go in and out in tiles of 32 packed rows, a workgroup one of a head
@@ -49,5 +51,6 @@ inline int64_t tiles_of_tokens(int64_t tokens) { return (tokens + 31) / 32; }
 hipError_t launch_cache_append(const cache_args& c, int32_t dtype, const void* k, int64_t ldk, const void* v, int64_t ldv, hipStream_t stream);
 hipError_t launch_cache_read(const cache_args& c, int32_t dtype, void* k, int64_t ldk, void* v, int64_t ldv, hipStream_t stream);
 hipError_t launch_cache_attention(const cache_attention_args& a, int32_t dtype, hipStream_t stream);
+hipError_t launch_cache_copy(const cache_args& c, int32_t num_copies, const int32_t* copies, hipStream_t stream);
 hipError_t launch_cache_evict(const cache_args& source, const cache_args& target, int32_t* target_length, int32_t budget, int32_t recent, int32_t* kept,
                               hipStream_t stream);

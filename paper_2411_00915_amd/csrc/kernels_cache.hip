@@ -275,6 +275,22 @@ __global__ __launch_bounds__(LORA_CACHE_READ_THREADS) void cache_read_kernel(cac
     }
 }
 
+// A page of one head to another page: bound by memory
+__global__ __launch_bounds__(LORA_CACHE_COPY_THREADS) void cache_copy_kernel(cache_args c, const int32_t* copies)
+{
+    const int head = blockIdx.x % c.kv_heads, i = blockIdx.x / c.kv_heads, tid = threadIdx.x;
+    const int64_t source = copies[2 * (int64_t)i], target = copies[2 * (int64_t)i + 1];
+    if (source < 0 || source >= c.num_pages || target < 0 || target >= c.num_pages || source == target) return;
+    const int64_t from = source * c.kv_heads + head, to = target * c.kv_heads + head;
+    const uint4* const p = reinterpret_cast<const uint4*>(c.pages + from * c.page_bytes);
+    uint4* const q = reinterpret_cast<uint4*>(c.pages + to * c.page_bytes);
+    const int count = (int)(c.page_bytes / 16);
+#pragma unroll 4
+    for (int n = tid; n < count; n += LORA_CACHE_COPY_THREADS) q[n] = p[n];
+    if (c.weight)
+        for (int n = tid; n < c.page_tokens; n += LORA_CACHE_COPY_THREADS) c.weight[to * c.page_tokens + n] = c.weight[from * c.page_tokens + n];
+}
+
 bool rows_aligned(const void* k, int64_t ldk, const void* v, int64_t ldv, int32_t head_dim, int32_t dtype)
 {
     const uintptr_t es = dtype == LORA_F32 ? 4 : 2;
@@ -561,5 +577,11 @@ hipError_t launch_cache_evict(const cache_args& c, const cache_args& to, int32_t
     const dim3 grid((uint32_t)(c.num_seqs * c.kv_heads * tiles));
 #define MOVE(DP, UNUSED) LORA_LAUNCH(LORA_K_CACHE_MOVE, (cache_move_kernel<DP>), grid, dim3(LORA_CACHE_MOVE_THREADS), 0, stream, c, to, budget, tiles, kept)
     BY_HEAD_DIM(MOVE, )
+    return hipGetLastError();
+}
+
+hipError_t launch_cache_copy(const cache_args& c, int32_t num_copies, const int32_t* copies, hipStream_t stream)
+{
+    LORA_LAUNCH(LORA_K_CACHE_COPY, cache_copy_kernel, dim3((uint32_t)((int64_t)num_copies * c.kv_heads)), dim3(LORA_CACHE_COPY_THREADS), 0, stream, c, copies);
     return hipGetLastError();
 }

@@ -205,7 +205,8 @@ __device__ __forceinline__ void load_query(const T* p, int d0, int D, bool align
     }
 }
 
-template <typename T, int DP, int CT, bool KEEP, int WAVES>
+// CHOSEN: a token at a time, over the pages that it is given; its blocks are counted along that list, and `number`ed by where they are
+template <typename T, int DP, int CT, bool KEEP, int WAVES, bool CHOSEN>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 1 ? 4 : 2) void cache_attention_kernel(cache_attention_args a)
 {
     constexpr bool EXACT = sizeof(T) == 4;
@@ -222,15 +223,22 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     id /= c.kv_heads;
     const int rt = id % a.row_tiles;
     id /= a.row_tiles;
-    const int split = id % a.splits, seq = id / a.splits;
-    const cache_rows rows = rows_of(c, seq);
+    const int split = id % a.splits, seq = CHOSEN ? id / a.splits / c.max_new : id / a.splits;
+    cache_rows rows = rows_of(c, seq);
+    int held = length_of(c, seq);
+    if constexpr (CHOSEN) {                                    // (as a sequence of its own, whose last token it is)
+        const int i = id / a.splits % c.max_new;
+        if (i >= rows.count) return;
+        held = max(0, held - rows.count + i + 1);
+        rows = cache_rows{rows.first + i, 1};
+    }
+    const int length = held;
     const int R = min(rows.count, c.max_new) * a.group, row0 = rt * (16 * CT);      // query rows: token major, then the group's heads
     if (row0 >= R) return;
-    const int length = length_of(c, seq);
     // what a query row sees: slots below seen(row)
     auto seen = [&](int row) { return max(0, length - rows.count + row / a.group + 1); };
     const int least = seen(row0), most = seen(min(R, row0 + 16 * CT) - 1);
-    const int t0 = split * a.split_tokens, t1 = min(most, t0 + a.split_tokens);
+    const int t0 = split * a.split_tokens, t1 = min(CHOSEN ? a.budget * c.page_tokens : most, t0 + a.split_tokens);
 
     op16 q[CT][NS][TERMS];
     float qsum[CT], start[CT];
@@ -298,8 +306,19 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     const int blocks_a_page = c.page_tokens >> 5, last = (t1 + 31) >> 5;
     typedef const __attribute__((address_space(4))) int32_t* constants;         // (nothing writes the table while the kernel runs)
     const constants table = (constants)(uintptr_t)(c.page_table + (int64_t)seq * c.table_stride);
+    const constants chosen = (constants)(uintptr_t)(a.chosen + ((int64_t)rows.first * c.kv_heads + head) * a.budget);
+    int number = 0;                                            // of the block that was asked for last
     auto page_at = [&](int b) -> const unsigned char* {        // null: not there
-        const int64_t p = table[b / blocks_a_page];
+        int n = b / blocks_a_page;
+        number = b;
+        if constexpr (CHOSEN) {
+            const int place = b - n * blocks_a_page;
+            n = chosen[n];
+            if (n < 0 || n >= (length + c.page_tokens - 1) / c.page_tokens) return nullptr;
+            number = n * blocks_a_page + place;
+            if (32 * number >= length) return nullptr;
+        }
+        const int64_t p = table[n];
         return p < 0 || p >= c.num_pages ? nullptr : c.pages + (p * c.kv_heads + head) * c.page_bytes;
     };
     const code_bits bits;
@@ -442,11 +461,12 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     const block_offsets<DP> off(c.page_tokens, lane);
     char* const ring = lds + wave * (RING * block_lds<DP>::BYTES);
     const uint32_t ring_at = __builtin_amdgcn_readfirstlane(lds_address(ring));
-    const int full = min(last, least >> 5);                    // blocks that every row sees
-    int queue[RING], slot = 0;                                 // blocks in their order; >= last: none
+    const int full = CHOSEN ? least >> 5 : min(last, least >> 5);      // blocks that every row sees
+    int queue[RING], slot = 0;                                 // numbers of blocks in their order, or NONE
+    constexpr int NONE = 0x7fffffff;
     auto ask = [&](int place) {                                // the next block into a place of the ring
         const unsigned char* const page = find();
-        const int found = b;
+        const int found = page ? number : NONE;
         if (page) fetch_block<DP>(page, c.page_tokens, at, off, ring_at + place * block_lds<DP>::BYTES);
         b += WAVES;
         return found;
@@ -456,16 +476,24 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
     auto turn = [&](auto masked) {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");     // (the block before this one is read: its place is free)
         queue[RING - 1] = ask(slot == 0 ? RING - 1 : slot - 1);
-        if (queue[RING - 1] < last) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * block_lds<DP>::COUNT) : "memory");
+        if (queue[RING - 1] != NONE) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((RING - 1) * block_lds<DP>::COUNT) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         compute(queue[0], ring + slot * block_lds<DP>::BYTES, masked);
 #pragma unroll
         for (int i = 0; i < RING - 1; ++i) queue[i] = queue[i + 1];
         slot = slot == RING - 1 ? 0 : slot + 1;
     };
-    while (queue[0] < full) turn(std::false_type{});
+    if constexpr (CHOSEN) {                                    // (in the order of the list, which need not be the blocks')
 #pragma unroll 1
-    while (queue[0] < last) turn(std::true_type{});
+        while (queue[0] != NONE) {
+            if (queue[0] < full) turn(std::false_type{});
+            else turn(std::true_type{});
+        }
+    } else {
+        while (queue[0] < full) turn(std::false_type{});
+#pragma unroll 1
+        while (queue[0] != NONE) turn(std::true_type{});
+    }
 
     bool wild = false;
     // the wavefronts' sums meet, column tile by column tile
@@ -638,15 +666,16 @@ template <typename T, int DP, int CT, int WAVES>
 void launch_shape(const cache_attention_args& a, hipStream_t stream)
 {
     const dim3 grid((uint32_t)((int64_t)a.c.num_seqs * a.c.kv_heads * a.splits * a.row_tiles)), block(64 * WAVES);
-    if (a.scores) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, true, WAVES>), grid, block, 0, stream, a);
-    else LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, false, WAVES>), grid, block, 0, stream, a);
+    if (a.chosen) LORA_LAUNCH(LORA_K_CACHE_ATTENTION_CHOSEN, (cache_attention_kernel<T, DP, CT, false, WAVES, true>), dim3(grid.x * (uint32_t)a.c.max_new), block, 0, stream, a);
+    else if (a.scores) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, true, WAVES, false>), grid, block, 0, stream, a);
+    else LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, false, WAVES, false>), grid, block, 0, stream, a);
 }
 
 template <typename T, int DP>
 void launch_main(const cache_attention_args& a, hipStream_t stream)
 {
     if constexpr (cache_tile_rows(sizeof(T) == 4, DP) == 32)
-        if ((int64_t)a.group * a.c.max_new > 16) return launch_shape<T, DP, 2, 4>(a, stream);
+        if ((int64_t)a.group * (a.chosen ? 1 : a.c.max_new) > 16) return launch_shape<T, DP, 2, 4>(a, stream);
     if constexpr (DP <= 128)
         if (a.waves == 8) return launch_shape<T, DP, 1, 8>(a, stream);
     launch_shape<T, DP, 1, 4>(a, stream);

@@ -1,0 +1,26 @@
+// Launch interface of the pages' bounds and of the choice among them (kernels_choose.hip).
+#pragma once
+#include "kernels_attention.h"
+
+enum { LORA_CACHE_DIGEST_THREADS = 256, LORA_CACHE_CHOOSE_THREADS = 512 };
+
+// pages that hold some of n tokens in a row, at most
+inline int32_t digest_pages(int32_t n, int32_t page_tokens) { return (int32_t)(((int64_t)n + 2 * page_tokens - 2) / page_tokens); }
+
+struct choose_args {
+    cache_args c;
+    const void* q;
+    int64_t ldq;
+    int32_t group, budget, first, recent;
+    const int8_t* bounds;
+    const float* steps;
+    int32_t* chosen;
+    uint32_t* keys;          // workspace: [num_tokens][kv_heads][key_stride]; null: in LDS
+    int64_t key_stride;
+};
+
+// pages of the longest sequence, whose keys LDS holds up to (beside 9 KB of queries and counts)
+constexpr int32_t LORA_CACHE_CHOOSE_NEAR = 12288;
+
+hipError_t launch_cache_digest(const cache_args& c, int8_t* bounds, float* steps, hipStream_t stream);
+hipError_t launch_cache_choose(const choose_args& a, int32_t dtype, hipStream_t stream);

@@ -41,6 +41,16 @@ enum lora_kernel_id {
     LORA_K_CACHE_FINISH,
     LORA_K_CACHE_SELECT,
     LORA_K_CACHE_MOVE,
+    LORA_K_CACHE_COPY,
+    LORA_K_CACHE_DIGEST,
+    LORA_K_CACHE_CHOOSE,
+    LORA_K_CACHE_ATTENTION_CHOSEN,
+    LORA_K_PAGES_GIVE_BACK,
+    LORA_K_PAGES_DECIDE,
+    LORA_K_PAGES_WRITE,
+    LORA_K_PAGES_FORK,
+    LORA_K_BEAM_ROWS,
+    LORA_K_BEAM_JOIN,
     LORA_K_PROBE_EMPTY,
     LORA_K_PROBE_READ,
     LORA_K_PROBE_MFMA,
