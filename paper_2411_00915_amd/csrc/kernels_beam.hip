@@ -64,261 +64,452 @@ __device__ __forceinline__ N wave_max(N x)
     return x;
 }
 
-// exp(d), d <= 0
-__device__ __forceinline__ float exp_of(float d)
-{
-    constexpr float LOG2E = 1.44269504088896340736f, LOG2E_LOW = 1.92596299112661746887e-8f, LN2 = 0.69314718055994530942f;
-    d = fmaxf(d, -200.f);                      // (-inf among them)
-    const float hi = d * LOG2E, lo = __builtin_fmaf(d, LOG2E, -hi) + d * LOG2E_LOW;
-    const float e = __builtin_amdgcn_exp2f(hi);
-    return __builtin_fmaf(e, lo * LN2, e);
-}
-
-// eight tokens from `token` on; -inf behind the row's end
-template <typename T>
-__device__ __forceinline__ void load8(const T* row, int token, int vocab, float* x)
-{
-    struct __attribute__((packed, aligned(sizeof(T)))) eight { T v[8]; };
-    if (token + 8 <= vocab) {
-        const eight u = *reinterpret_cast<const eight*>(row + token);
+// V tokens of a lane, 16 bytes of them in a row, the next 1024 bytes on, as they lie in memory
+template <typename T, int V>
+struct lane_words {
+    static constexpr int EACH = 16 / sizeof(T), LOADS = V / EACH;
+    uint32_t w[4 * LOADS];
+    // (offsets of 32 bits from the row: one register, and the row's in scalar ones)
+    __device__ __forceinline__ void load(const T* row, uint32_t token)
+    {
+        struct __attribute__((packed, aligned(sizeof(T)))) words { uint32_t w[4]; };
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if constexpr (sizeof(T) == 2) x[i] = bf16_to_f32(u.v[i]);
-            else x[i] = u.v[i];
-    } else
+        for (int i = 0; i < LOADS; ++i) {
+            const words u = *reinterpret_cast<const words*>(reinterpret_cast<const char*>(row) + (token * (uint32_t)sizeof(T) + 1024u * i));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = token + i < vocab ? elem<T>::load(row + token + i) : -INFINITY;
-}
+            for (int e = 0; e < 4; ++e) w[4 * i + e] = u.w[e];
+        }
+    }
+    __device__ __forceinline__ float operator()(int i) const
+    {
+        if constexpr (sizeof(T) == 2) return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+        else return __uint_as_float(w[i]);
+    }
+};
 
 // Is (x, i) before (y, j): the greater logit, of equal ones the lower token
 __device__ __forceinline__ bool before(float x, int i, float y, int j) { return x > y || (x == y && i < j); }
 
-template <typename T, int V>
-__global__ __launch_bounds__(BEAM_THREADS) void beam_rows_kernel(beam_args a)
+// the greatest number of BITS bits that no fewer than `wanted` lanes reach; 0 where there are too few
+template <int BITS>
+__device__ __forceinline__ uint32_t reached(uint32_t mine, int wanted)
 {
-    __shared__ beam_entry held[kWaves][kHeld];
-    __shared__ beam_entry best[kWaves][kMost];
-    __shared__ beam_sum sums[kWaves];
-    const int split = blockIdx.x % a.splits, row = blockIdx.x / a.splits, M = a.num_out;
-    if (a.last_token && a.end_token >= 0 && a.last_token[row] == a.end_token) return;         // (beam_join_kernel does not look at it)
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const T* const logits = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
-    const int start = split * (BEAM_THREADS * V) + wave * (64 * V) + 8 * lane;         // of the lane's first eight; the next are 512 on
-    auto token_of = [&](int i) { return start + i / 8 * 512 + i % 8; };
-    float x[V];
-#pragma unroll
-    for (int i = 0; i < V; i += 8) load8(logits, token_of(i), a.vocab, x + i);
-    float top = x[0];
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        top = fmaxf(top, x[i]);
-        bad |= !(x[i] < INFINITY);
-    }
-    // the bound: as many lanes as wanted have a logit that is not below it (its upper 16 bits are enough: all that is not below is looked at)
-    const uint32_t mine = order_of(top) >> 16;
     uint32_t bound = 0;
 #pragma unroll
-    for (int bit = 15; bit >= 0; --bit) {
+    for (int bit = BITS - 1; bit >= 0; --bit) {
         const uint32_t t = bound | 1u << bit;
-        if (__popcll(__ballot(mine >= t)) >= M) bound = t;
+        if (__popcll(__ballot(mine >= t)) >= wanted) bound = t;
     }
+    return bound;
+}
+
+// A wavefront's candidates in LDS, and the exponentials of all else
+constexpr float LOG2E = 1.44269504088896340736f;
+struct wave_state {
+    beam_entry* held;          // [kHeld]; the first `summed` are in `sum` already
+    int count, summed;
+    float bound;               // what is below it is no candidate; of what is equal, what is not before bound_token
+    int bound_token;
+    double sum;                // of exp(logit - ref), this lane's part
+    double ref;                // about the bound, or above it
+    // exp(x - ref) is exp2(x LOG2E - less_of), as ref is less_of / LOG2E; but past 1e9, where less_of is too coarse, exp2((x - less_of) LOG2E)
+    float less_of;
+    bool far;
+    template <bool FAR>
+    __device__ __forceinline__ float fast(float x) const
+    {
+        return __builtin_amdgcn_exp2f(FAR ? (x - less_of) * LOG2E : __builtin_fmaf(x, LOG2E, -less_of));
+    }
+};
+
+__device__ __forceinline__ void raise_ref(wave_state& s, float to)
+{
+    const bool far = !(fabsf(to) < 1e9f);
+    const float less_of = far ? to : to * LOG2E;
+    const double ref = far ? (double)to : (double)less_of / (double)LOG2E;
+    if (ref > s.ref) {
+        s.sum = s.sum == 0.0 ? 0.0 : s.sum * exp(s.ref - ref);
+        s.ref = ref;
+        s.less_of = less_of;
+        s.far = far;
+    }
+}
+
+// Those of the candidates that are not in the sum into it
+__device__ __forceinline__ void add_held(wave_state& s, int lane)
+{
+    float top = -INFINITY;
+    for (int i = s.summed + lane; i < s.count; i += 64) top = fmaxf(top, s.held[i].logit);
     top = wave_max(top);
-    bad = __ballot(bad) != 0;
-    const float ref = fabsf(top) < INFINITY ? top : 0.f;
-    double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) sum += (double)exp_of(x[i] - ref);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    if (lane == 0) sums[wave] = beam_sum{sum, ref, bad};
-    // what is not below it (and is a number that can be chosen)
-    const uint32_t least = bound << 16;
-    int count = 0;
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-        const bool is = order_of(x[i]) >= least && x[i] > -INFINITY;
-        const uint64_t mask = __ballot(is);
-        if (mask == 0) continue;
-        const int at = lanes_before(mask, count);
-        if (is && at < kHeld) held[wave][at] = beam_entry{x[i], token_of(i)};
-        count += __popcll(mask);
-    }
-    if (lane < M) best[wave][lane] = beam_entry{-INFINITY, -1};
+    if (fabsf(top) < INFINITY) raise_ref(s, top);
+    for (int i = s.summed + lane; i < s.count; i += 64) s.sum += exp((double)s.held[i].logit - s.ref);
+    s.summed = s.count;
+}
+
+// LDS is full: the best num_out of the candidates are kept, and the last of them is the bound
+__device__ __forceinline__ void keep_best(wave_state& s, int M, int lane)
+{
     wave_sync();
-    if (count <= kHeld) {
-        for (int i = lane; i < count; i += 64) {
-            const beam_entry e = held[wave][i];
-            int rank = 0;
-            for (int j = 0; j < count; ++j) {
-                const beam_entry o = held[wave][j];
-                rank += before(o.logit, o.token, e.logit, e.token);
-            }
-            if (rank < M) best[wave][rank] = e;
-        }
-    } else {
-        // more equal ones than that: one after the other
-        float past = INFINITY;
-        int past_token = -1;
-        for (int n = 0; n < M; ++n) {
-            float most = -INFINITY;
-            int token = 0x7fffffff;
+    add_held(s, lane);
+    beam_entry mine[kHeld / 64];
+    int rank[kHeld / 64];
+#pragma unroll
+    for (int n = 0; n < kHeld / 64; ++n) {
+        mine[n] = s.held[min(n * 64 + lane, s.count - 1)];
+        rank[n] = n * 64 + lane < s.count ? 0 : M;
+    }
+    for (int j = 0; j < s.count; ++j) {
+        const beam_entry o = s.held[j];
+#pragma unroll
+        for (int n = 0; n < kHeld / 64; ++n) rank[n] += before(o.logit, o.token, mine[n].logit, mine[n].token);
+    }
+    wave_sync();
+#pragma unroll
+    for (int n = 0; n < kHeld / 64; ++n)
+        if (rank[n] < M) s.held[rank[n]] = mine[n];
+    wave_sync();
+    if (s.count >= M) {
+        const beam_entry last = s.held[M - 1];
+        s.bound = last.logit;
+        s.bound_token = last.token;
+        raise_ref(s, s.bound);
+    }
+    s.count = s.summed = min(s.count, M);
+}
+
+// the number whose upper 16 bits in the order of numbers these are, the rest 0; NaN where there is none
+__device__ __forceinline__ float number_of(uint32_t upper)
+{
+    const uint32_t u = upper << 16;
+    return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u);
+}
+__device__ __forceinline__ void raise_bound(wave_state& s, float to)
+{
+    if (to > s.bound && to < INFINITY) {
+        s.bound = to;
+        s.bound_token = 0x7fffffff;
+        raise_ref(s, to);
+    }
+}
+
+// Raises the bound by up to 64 candidates: num_out of them are not below it, or in every wavefront its share (`bounds`: what they have
+// found so far; it only rises, so an old number does as well)
+__device__ __forceinline__ void raise_by_held(wave_state& s, int M, int wave, int lane, volatile uint32_t* bounds)
+{
+    wave_sync();
+    const uint32_t mine = lane < s.count ? order_of(s.held[lane].logit) >> 16 : 0u;
+    const uint32_t share = reached<16>(mine, (M + kWaves - 1) / kWaves);
+    if (lane == 0 && share > bounds[wave]) bounds[wave] = share;
+    uint32_t least = bounds[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) least = min(least, (uint32_t)bounds[w]);
+    least = max(least, reached<16>(mine, M));
+    raise_bound(s, number_of((uint32_t)__builtin_amdgcn_readfirstlane(least)));
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
+{
+    __shared__ beam_entry held[kWaves][kHeld];
+    __shared__ double sums[kWaves];
+    __shared__ double refs[kWaves];
+    __shared__ uint32_t bounds[kWaves];
+    __shared__ int counts[kWaves];
+    constexpr int UNIT = BEAM_THREADS * V, PART = 64 * V, EACH = lane_words<T, V>::EACH, ANY = 0x7fffffff;
+    const int split = blockIdx.x % a.splits, row = blockIdx.x / a.splits, M = a.num_out;
+    if (a.last_token && a.end_token >= 0 && a.last_token[row] == a.end_token) return;         // (beam_join_kernel does not look at it)
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const T* const logits = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
+    wave_state s{held[wave], 0, 0, -3.402823466e+38f, ANY, 0.0, -INFINITY, -3.402823466e+38f, true};      // (-inf is not chosen; NaN: the row is not)
+    const int begin = split * a.chunk, end = min(begin + a.chunk, a.vocab);
+    // The lane's first token of a unit.  A part that the row's end cuts is loaded from so far before its place, and what it has in common
+    // with the part before it is masked.
+    auto start_of = [&](int unit) { return max(min(unit + wave * PART, a.vocab - PART), 0) + EACH * lane; };
+    int look = 16;                                                 // candidates at which they are looked at for a better bound
+    lane_words<T, V> next;
+    if (V != BEAM_FEW || a.vocab >= PART) next.load(logits, start_of(begin));
+#pragma unroll 1
+    for (int unit = begin; unit < end; unit += UNIT) {
+        const int start = start_of(unit), first = unit + wave * PART;
+        auto token_of = [&](int i) { return start + i / EACH * (64 * EACH) + i % EACH; };
+        float x[V];
+        if (V != BEAM_FEW || a.vocab >= PART) {                    // (divide_beams: rows of many units have a part)
+#pragma unroll
+            for (int i = 0; i < V; ++i) x[i] = next(i);
+            if (unit + UNIT < end) next.load(logits, start_of(unit + UNIT));
+            if (first + PART > a.vocab)
+#pragma unroll
+                for (int i = 0; i < V; ++i) x[i] = token_of(i) >= first ? x[i] : -INFINITY;
+        } else {                                                   // (no branch over the lanes, so that all loads are on their way together)
 #pragma unroll
             for (int i = 0; i < V; ++i)
-                if (before(past, past_token, x[i], token_of(i)) && before(x[i], token_of(i), most, token)) {
-                    most = x[i];
-                    token = token_of(i);
-                }
+                x[i] = elem<T>::load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(logits) + (uint32_t)min(token_of(i), a.vocab - 1) * (uint32_t)sizeof(T)));
 #pragma unroll
-            for (int off = 32; off > 0; off >>= 1) {
-                const float y = __shfl_xor(most, off, 64);
-                const int j = __shfl_xor(token, off, 64);
-                if (before(y, j, most, token)) {
-                    most = y;
-                    token = j;
-                }
-            }
-            if (!(most > -INFINITY)) break;
-            if (lane == 0) best[wave][n] = beam_entry{most, token};
-            past = most;
-            past_token = token;
+            for (int i = 0; i < V; ++i) x[i] = token_of(i) < a.vocab && token_of(i) >= first ? x[i] : -INFINITY;
         }
-    }
-    __syncthreads();
-    // the workgroup's best, of the wavefronts'
-    beam_entry* const out = a.entries + ((int64_t)row * a.splits + split) * M;
-    if (tid < kWaves * M) {
-        const int w = tid / M;
-        const beam_entry e = best[w][tid - w * M];
-        int rank = 0, there = 0;
-        for (int v = 0; v < kWaves; ++v)
-            for (int j = 0; j < M; ++j) {
-                const beam_entry o = best[v][j];
-                if (o.token < 0) break;
-                ++there;
-                rank += before(o.logit, o.token, e.logit, e.token);
+        float top = x[0];
+#pragma unroll
+        for (int i = 1; i < V; ++i) top = fmaxf(top, x[i]);
+        // Bounds (the upper 16 bits do: all that is not below is looked at).  Of the first tokens two, of which the greater is taken: in
+        // every wavefront its share of num_out lanes have a logit that is not below the first, in this one num_out lanes one that is
+        // not below the second.  The second is what there is where another wavefront's part is masked or behind the row's end,
+        // and again where the first tokens were.
+        if (unit == begin) {
+            const uint32_t mine = order_of(top) >> 16, share = reached<16>(mine, (M + kWaves - 1) / kWaves);
+            uint32_t least = reached<16>(mine, M);
+            if (lane == 0) bounds[wave] = share;
+            __syncthreads();
+            uint32_t all = bounds[0];
+#pragma unroll
+            for (int w = 1; w < kWaves; ++w) all = min(all, bounds[w]);
+            raise_bound(s, number_of(max(least, all)));
+        } else if (__popcll(__ballot(top >= s.bound)) > M)
+            raise_bound(s, number_of(reached<16>(order_of(top) >> 16, M)));
+        // what is not below the bound goes to LDS, and is as good as masked here
+        const uint64_t lanes = __ballot(top >= s.bound);
+        if (lanes != 0) {
+            int hits = __popcll(lanes) * V;                        // at most
+            if (s.count + hits > kHeld) {
+                hits = 0;
+#pragma unroll
+                for (int i = 0; i < V; ++i) hits += __popcll(__ballot(x[i] >= s.bound));
             }
-        if (e.token >= 0 && rank < M) out[rank] = e;
-        if (tid < M && tid >= there) out[tid] = beam_entry{-INFINITY, -1};
-    }
-    if (tid == 0) {
-        beam_sum s = sums[0];
-        for (int w = 1; w < kWaves; ++w) {
-            const beam_sum o = sums[w];
-            if (o.bad || !(o.sum > 0.0) || !(s.sum > 0.0)) {   // (-inf alone has no place on the scale)
-                if (o.sum > 0.0) {
-                    s.sum = o.sum;
-                    s.top = o.top;
+            if (s.count + hits <= kHeld) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const bool is = x[i] >= s.bound;
+                    const uint64_t mask = __ballot(is);
+                    if (mask != 0) {
+                        if (is) s.held[lanes_before(mask, s.count)] = beam_entry{x[i], token_of(i)};
+                        s.count += __popcll(mask);
+                        x[i] = is ? -INFINITY : x[i];
+                    }
                 }
-                s.bad |= o.bad;
+                if (s.count >= look && s.count <= 64) {
+                    raise_by_held(s, M, wave, lane, bounds);
+                    look = s.count + 8;
+                }
+            } else {
+                // More than LDS holds (many equal ones): once more, 64 at a time
+#pragma unroll 1
+                for (int i = 0; i < V; ++i) {
+                    if (s.count > kHeld - 64) keep_best(s, M, lane);
+                    const int token = token_of(i);
+                    const float y = token < a.vocab && token >= first ? elem<T>::load(logits + token) : -INFINITY;
+                    const bool is = y > s.bound || (y == s.bound && token < s.bound_token);
+                    const uint64_t mask = __ballot(is);
+                    if (is) s.held[lanes_before(mask, s.count)] = beam_entry{y, token};
+                    s.count += __popcll(mask);
+                    s.sum += is ? 0.0 : (double)(s.far ? s.fast<true>(y) : s.fast<false>(y));
+                }
                 continue;
             }
-            const float ref_all = fmaxf(s.top, o.top);
-            s.sum = s.sum * exp((double)(s.top) - ref_all) + o.sum * exp((double)o.top - ref_all);
-            s.top = ref_all;
         }
-        a.sums[(int64_t)row * a.splits + split] = s;
+        // the exponentials of all else: eight in 32 bits, their sums in 64 (NaN is among these, and makes the sum NaN)
+        auto add = [&](auto far_) {
+#pragma unroll
+            for (int i = 0; i < V; i += 8) {
+                float part = 0.f;
+#pragma unroll
+                for (int e = i; e < i + 8; ++e) part += s.fast<decltype(far_)::value>(x[e]);
+                s.sum += (double)part;
+            }
+        };
+        if (__builtin_expect(__builtin_amdgcn_readfirstlane(s.far), 0)) add(std::true_type{});
+        else add(std::false_type{});
+    }
+    wave_sync();
+    add_held(s, lane);
+    if (s.count <= 64 && s.count > 0) raise_by_held(s, M, wave, lane, bounds);
+    double sum = s.sum;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    if (lane == 0) {
+        sums[wave] = sum;
+        refs[wave] = s.ref;
+    }
+    __syncthreads();
+    // What is left of the candidates, now that all wavefronts' bounds are there, to the front; then the workgroup's best in order
+    if (s.count > 0 && s.count <= 64) {
+        uint32_t all = bounds[0];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) all = min(all, bounds[w]);
+        raise_bound(s, number_of(all));
+        const beam_entry e = s.held[min(lane, s.count - 1)];
+        const bool is = lane < s.count && e.logit >= s.bound;
+        const uint64_t mask = __ballot(is);
+        wave_sync();
+        if (is) s.held[lanes_before(mask, 0)] = e;
+        s.count = __popcll(mask);
+    }
+    if (lane == 0) counts[wave] = s.count;
+    __syncthreads();
+    beam_entry* const out = a.entries + ((int64_t)row * a.splits + split) * M;
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all += counts[w];
+    for (int n = tid; n < all; n += BEAM_THREADS) {
+        int w = 0, at = n;
+        while (at >= counts[w]) at -= counts[w++];
+        const beam_entry e = held[w][at];
+        int rank = 0;
+        for (int v = 0; v < kWaves; ++v) {
+            const int there = counts[v];
+#pragma unroll 4
+            for (int j = 0; j < there; ++j) {
+                const beam_entry o = held[v][j];
+                rank += before(o.logit, o.token, e.logit, e.token);
+            }
+        }
+        if (rank < M) out[rank] = e;
+    }
+    if (tid < M && tid >= all) out[tid] = beam_entry{-INFINITY, -1};
+    if (wave == kWaves - 1) {
+        // the sums on one scale; one of nothing but -inf has no place on it
+        const double part = lane < kWaves ? sums[lane] : 0.0;
+        const bool some = part != 0.0;
+        const double ref = some ? refs[lane & (kWaves - 1)] : -INFINITY, scale = wave_max(ref);
+        double of_all = some ? part * exp(ref - scale) : 0.0;
+#pragma unroll
+        for (int off = kWaves / 2; off > 0; off >>= 1) of_all += __shfl_xor(of_all, off, 64);
+        if (lane == 0) a.sums[(int64_t)row * a.splits + split] = beam_sum{of_all, scale};
     }
 }
 
 // ---------------------------------------------------------------------------
-// A workgroup a request.  Candidates in tiles of a thread each; a wavefront puts its own in order by counting and keeps num_out of them,
-// which are put in order with the best so far.  A candidate: what it is worth, then what breaks ties, both greater is better, 0: none.
-constexpr int kJoinThreads = BEAM_JOIN_THREADS, kJoinWaves = kJoinThreads / 64;
+// A workgroup a request.  Again a bound first, by what every thread's best candidate is worth, and what is not below it put in order
+// by counting.  A candidate: what it is worth, then what breaks ties, both greater is better, 0: none.
+constexpr int kJoinThreads = BEAM_JOIN_THREADS, kJoinWaves = kJoinThreads / 64, kJoinHeld = 1024;
 struct __align__(16) candidate {
     uint64_t worth, tie;       // tie: 63 - beam, the logit's order, 2^24 - 1 - token
 };
 __device__ __forceinline__ bool better(const candidate& x, const candidate& y) { return x.worth > y.worth || (x.worth == y.worth && x.tie > y.tie); }
 
+// the upper bits of what it is worth, rounded to 32 bits: in the same order, but for equal ones
+__device__ __forceinline__ uint32_t about(const candidate& c) { return c.worth == 0 ? 0u : order_of((float)number_of(c.worth)) >> 12; }
+
 __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(beam_args a)
 {
-    __shared__ candidate pool[(kJoinWaves + 1) * kMost];       // the wavefronts' best, behind them the best so far
-    __shared__ candidate own[kJoinWaves][64];
+    __shared__ candidate pool[kJoinHeld];
+    __shared__ candidate best[kMost];
     __shared__ double worth[kMost], lse[kMost];
     __shared__ int state[kMost];                               // 0: no continuation, 1: from its logits, 2: has ended
+    __shared__ uint32_t bounds[kJoinThreads];
+    __shared__ int counter;
     const int group = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, M = a.num_out, B = a.beams;
     const int64_t row0 = (int64_t)group * B;
+    const int64_t all = (int64_t)a.splits * M * B;
+    if (tid == 0) counter = 0;
+    if (tid < M) best[tid] = candidate{0, 0};
     for (int b = wave; b < B; b += kJoinWaves) {
         const int64_t row = row0 + b;
         const float score = a.score[row];
         const bool ended = a.last_token && a.end_token >= 0 && a.last_token[row] == a.end_token;
-        double sum = 0.0;
-        float top = -INFINITY;
-        int bad = 0;
+        double sum = 0.0, ref = -INFINITY;
         if (!ended) {
             const beam_sum* const s = a.sums + row * a.splits;
-            for (int i = lane; i < a.splits; i += 64) {
-                if (s[i].sum > 0.0) top = fmaxf(top, s[i].top);
-                bad |= s[i].bad;
-            }
-            top = wave_max(top);
+            for (int i = lane; i < a.splits; i += 64) ref = fmax(ref, s[i].ref);           // (-inf where there is nothing)
+            ref = wave_max(ref);
             for (int i = lane; i < a.splits; i += 64)
-                if (s[i].sum > 0.0) sum += s[i].sum * exp((double)s[i].top - (double)top);
+                if (s[i].sum != 0.0) sum += s[i].sum * exp(s[i].ref - ref);
 #pragma unroll
             for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
-            bad = __ballot(bad != 0) != 0;
         }
         if (lane == 0) {
             const bool scored = fabsf(score) < INFINITY;
             worth[b] = (double)score;
-            lse[b] = sum > 0.0 ? (double)top + log(sum) : 0.0;
-            state[b] = !scored ? 0 : ended ? 2 : sum > 0.0 && !bad ? 1 : 0;
+            lse[b] = sum > 0.0 ? ref + log(sum) : 0.0;
+            state[b] = !scored ? 0 : ended ? 2 : sum > 0.0 && sum < INFINITY ? 1 : 0;
         }
     }
-    if (tid < M) pool[kJoinWaves * M + tid] = candidate{0, 0};
     __syncthreads();
-    const int64_t each = (int64_t)a.splits * M, all = each * B;
-    for (int64_t base = 0; base < all; base += kJoinThreads) {
-        const int64_t at = base + tid;
+    const int each = a.splits * M;                             // of a beam (2^24 tokens in pieces of 2048, 64 each: 2^19)
+    auto at = [&](int64_t n) {                                 // candidate n < all
+        const int b = (int)((uint32_t)n / (uint32_t)each), st = state[b];
+        const uint64_t tie = (uint64_t)(63 - b) << 56;
         candidate c{0, 0};
-        if (at < all) {
-            const int b = (int)(at / each), st = state[b];
-            const uint64_t tie = (uint64_t)(63 - b) << 56;
-            if (st == 1) {
-                const beam_entry e = a.entries[row0 * each + at];
-                if (e.token >= 0) {
-                    const double w = worth[b] + ((double)e.logit - lse[b]);
-                    c = candidate{order_of(w), tie | (uint64_t)order_of(e.logit) << 24 | (uint32_t)(0xffffff - e.token)};
-                }
-            } else if (st == 2 && at == b * each)
-                c = candidate{order_of(worth[b]), tie | (uint32_t)(0xffffff - a.end_token)};
-        }
-        // (as long as there is one among them that is better than the last of the best so far)
-        const candidate worst = pool[kJoinWaves * M + M - 1];
-        if (!__syncthreads_or(better(c, worst))) continue;
-        own[wave][lane] = c;
-        if (lane < M) pool[wave * M + lane] = candidate{0, 0};
-        wave_sync();
-        int rank = 0;
-        for (int j = 0; j < 64; ++j) rank += better(own[wave][j], c);
-        if (c.worth != 0 && rank < M) pool[wave * M + rank] = c;
-        __syncthreads();
-        const int count = (kJoinWaves + 1) * M;                // at most 576: a thread one or two
-        candidate mine[2] = {{0, 0}, {0, 0}};
-        int place[2] = {M, M};
+        if (st == 1) {
+            const beam_entry e = a.entries[row0 * each + n];
+            if (e.token >= 0)
+                c = candidate{order_of(worth[b] + ((double)e.logit - lse[b])), tie | (uint64_t)order_of(e.logit) << 24 | (uint32_t)(0xffffff - e.token)};
+        } else if (st == 2 && n == (int64_t)b * each)
+            c = candidate{order_of(worth[b]), tie | (uint32_t)(0xffffff - a.end_token)};
+        return c;
+    };
+    constexpr int KEPT = 4;                                    // of a thread's candidates, in registers
+    candidate kept[KEPT];
+    uint32_t mine = 0;
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int i = tid + n * kJoinThreads;
-            if (i >= count) continue;
-            mine[n] = pool[i];
-            if (mine[n].worth == 0) continue;
-            place[n] = 0;
-            for (int w = 0; w <= kJoinWaves; ++w)
-                for (int j = 0; j < M; ++j) {
-                    if (!better(pool[w * M + j], mine[n])) break;             // (in order)
-                    ++place[n];
-                }
-        }
-        __syncthreads();
-        if (tid < M) pool[kJoinWaves * M + tid] = candidate{0, 0};
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-            if (place[n] < M) pool[kJoinWaves * M + place[n]] = mine[n];
-        __syncthreads();
+    for (int i = 0; i < KEPT; ++i) {
+        const int64_t n = i * kJoinThreads + tid;
+        kept[i] = n < all ? at(n) : candidate{0, 0};
+        mine = max(mine, about(kept[i]));
     }
+    for (int64_t n = KEPT * kJoinThreads + tid; n < all; n += kJoinThreads) mine = max(mine, about(at(n)));
+    bounds[tid] = mine;
+    __syncthreads();
+    uint32_t bound = 0, theirs[kJoinWaves];                    // the greatest number that num_out threads reach; 0: there are fewer
+#pragma unroll
+    for (int w = 0; w < kJoinWaves; ++w) theirs[w] = bounds[w * 64 + lane];
+#pragma unroll 1
+    for (int bit = 19; bit >= 0; --bit) {
+        const uint32_t t = bound | 1u << bit;
+        int reached = 0;
+#pragma unroll
+        for (int w = 0; w < kJoinWaves; ++w) reached += __popcll(__ballot(theirs[w] >= t));
+        if (reached >= M) bound = t;
+    }
+    auto collect = [&](const candidate& c) {
+        const bool is = c.worth != 0 && about(c) >= bound;
+        const uint64_t mask = __ballot(is);
+        if (mask == 0) return;
+        int first = 0;
+        if (lane == 0) first = atomicAdd(&counter, __popcll(mask));
+        first = __builtin_amdgcn_readfirstlane(first);
+        const int place = lanes_before(mask, first);
+        if (is && place < kJoinHeld) pool[place] = c;          // (their order here does not matter: no two are equal)
+    };
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) collect(kept[i]);
+    for (int64_t base = KEPT * kJoinThreads; base < all; base += kJoinThreads) collect(base + tid < all ? at(base + tid) : candidate{0, 0});
+    __syncthreads();
+    const int count = counter;
+    if (count <= kJoinHeld) {
+#pragma unroll
+        for (int i = 0; i < kJoinHeld / kJoinThreads; ++i) {
+            const int n = i * kJoinThreads + tid;
+            if (n >= count) break;
+            const candidate c = pool[n];
+            int rank = 0;
+#pragma unroll 4
+            for (int j = 0; j < count; ++j) rank += better(pool[j], c);
+            if (rank < M) best[rank] = c;
+        }
+    } else {
+        // More: a tile of a thread each at a time, what is better than the last of the best so far put in order with them
+        for (int64_t base = 0; base < all; base += kJoinThreads) {
+            __syncthreads();
+            candidate c = base + tid < all ? at(base + tid) : candidate{0, 0};
+            if (!better(c, best[M - 1])) c = candidate{0, 0};
+            if (!__syncthreads_or(c.worth != 0)) continue;
+            pool[tid] = c;
+            if (tid < M) pool[kJoinThreads + tid] = best[tid];
+            __syncthreads();
+            const candidate old = tid < M ? best[tid] : candidate{0, 0};
+            int rank = 0, rank_old = 0;
+            for (int j = 0; j < kJoinThreads + M; ++j) {
+                const candidate o = pool[j];
+                rank += better(o, c);
+                rank_old += better(o, old);
+            }
+            __syncthreads();
+            if (c.worth != 0 && rank < M) best[rank] = c;
+            if (old.worth != 0 && rank_old < M) best[rank_old] = old;
+        }
+    }
+    __syncthreads();
     if (tid >= M) return;
-    const candidate c = pool[kJoinWaves * M + tid];
+    const candidate c = best[tid];
     const int64_t out = (int64_t)group * M + tid;
     a.out_score[out] = c.worth == 0 ? -INFINITY : (float)number_of(c.worth);
     a.out_parent[out] = c.worth == 0 ? -1 : (int32_t)(row0 + 63 - (int)(c.tie >> 56));
@@ -329,7 +520,7 @@ template <typename T>
 void launch_rows(const beam_args& a, hipStream_t stream)
 {
     const dim3 grid((uint32_t)((int64_t)a.num_groups * a.beams * a.splits));
-    if (a.chunk == BEAM_THREADS * BEAM_FEW) LORA_LAUNCH(LORA_K_BEAM_ROWS, (beam_rows_kernel<T, BEAM_FEW>), grid, dim3(BEAM_THREADS), 0, stream, a);
+    if (a.unit == BEAM_THREADS * BEAM_FEW) LORA_LAUNCH(LORA_K_BEAM_ROWS, (beam_rows_kernel<T, BEAM_FEW>), grid, dim3(BEAM_THREADS), 0, stream, a);
     else LORA_LAUNCH(LORA_K_BEAM_ROWS, (beam_rows_kernel<T, BEAM_MANY>), grid, dim3(BEAM_THREADS), 0, stream, a);
 }
 }  // namespace

@@ -43,34 +43,40 @@ hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream);
 hipError_t launch_pages_fork(const pages_args& p, const int32_t* parent, int32_t* workspace, hipStream_t stream);
 
 struct beam_sum {
-    double sum;              // of exp(logit - top)
-    float top;
-    int32_t bad;             // NaN or +inf among the logits
+    double sum, ref;         // of exp(logit - ref); no finite number where one of the logits is NaN or +inf
 };
 struct beam_entry {
     float logit;
     int32_t token;           // -1: none
 };
 
-// Beams.  A wavefront takes `chunk` / 4 tokens of a row
+// Beams.  A workgroup takes `chunk` tokens of a row, a unit at a time
 struct beam_args {
     const void* logits;
     int64_t ld;
     const float* score;
     const int32_t* last_token;
-    int32_t end_token, num_groups, beams, vocab, num_out, chunk, splits;
+    int32_t end_token, num_groups, beams, vocab, num_out, unit, chunk, splits;
     float* out_score;
     int32_t *out_parent, *out_token;
     beam_sum* sums;                 // workspace: [rows][splits]
     beam_entry* entries;            // workspace: [rows][splits][num_out], greatest first
 };
-constexpr int BEAM_THREADS = 256, BEAM_JOIN_THREADS = 512, BEAM_FEW = 8, BEAM_MANY = 32;      // (the last two: tokens a thread takes)
+constexpr int BEAM_THREADS = 256, BEAM_JOIN_THREADS = 512, BEAM_FEW = 8, BEAM_MANY = 16;      // (the last two: tokens a thread takes)
 
-// Chunks of a row: of 8192 tokens, or of 2048 where those would be fewer than two workgroups a compute unit
-inline void divide_beams(int64_t rows, int32_t vocab, int32_t* chunk, int32_t* splits)
+// Chunks of a row: units of 4096 tokens, or of 2048 where those would be fewer than two workgroups a compute unit; and as many units a
+// workgroup, one after the other, as leave four workgroups a compute unit (bounds carry on, and there is less to join)
+inline void divide_beams(int64_t rows, int32_t vocab, int32_t* unit, int32_t* chunk, int32_t* splits)
 {
-    constexpr int32_t many = BEAM_THREADS * BEAM_MANY, few = BEAM_THREADS * BEAM_FEW;
-    *chunk = rows * ((vocab + many - 1) / many) < 512 ? few : many;
+    const int32_t many = BEAM_THREADS * BEAM_MANY, few = BEAM_THREADS * BEAM_FEW, units = (vocab + many - 1) / many;
+    if (rows * units < 512 || vocab < many) {
+        *unit = *chunk = few;
+    } else {
+        const int64_t together = rows * units / 1024 < 1 ? 1 : rows * units / 1024 < units ? rows * units / 1024 : units;
+        const int32_t pieces = (int32_t)((units + together - 1) / together);
+        *unit = many;
+        *chunk = (units + pieces - 1) / pieces * many;             // (evenly)
+    }
     *splits = (vocab + *chunk - 1) / *chunk;
 }
 inline size_t beam_entries_offset(int64_t rows, int32_t splits) { return ((size_t)rows * splits * sizeof(beam_sum) + 255) / 256 * 256; }

@@ -106,8 +106,8 @@ lora_status check_beams(int32_t num_groups, int32_t beams, int32_t vocab, int32_
 {
     if (num_groups < 0 || beams < 1 || beams > LORA_MAX_BEAMS || vocab < 1 || vocab > 1 << 24 || num_out < 1 || num_out > LORA_MAX_BEAMS) return LORA_ERR_INVALID_ARG;
     if ((int64_t)num_groups * beams > LORA_ATTENTION_MAX_ROWS) return LORA_ERR_UNSUPPORTED;
-    int32_t chunk, splits;
-    divide_beams((int64_t)num_groups * beams, vocab, &chunk, &splits);
+    int32_t unit, chunk, splits;
+    divide_beams((int64_t)num_groups * beams, vocab, &unit, &chunk, &splits);
     return (int64_t)num_groups * beams > most_workgroups(BEAM_THREADS) / splits || num_groups > most_workgroups(BEAM_JOIN_THREADS) ? LORA_ERR_UNSUPPORTED : LORA_OK;
 }
 }  // namespace
@@ -118,8 +118,8 @@ extern "C" lora_status lora_beam_workspace(int32_t num_groups, int32_t beams, in
     *bytes = 0;
     const lora_status st = check_beams(num_groups, beams, vocab, num_out);
     if (st != LORA_OK || num_groups == 0) return st;
-    int32_t chunk, splits;
-    divide_beams((int64_t)num_groups * beams, vocab, &chunk, &splits);
+    int32_t unit, chunk, splits;
+    divide_beams((int64_t)num_groups * beams, vocab, &unit, &chunk, &splits);
     *bytes = beam_workspace((int64_t)num_groups * beams, splits, num_out);
     return LORA_OK;
 }
@@ -139,7 +139,7 @@ extern "C" lora_status lora_beam_select(int32_t dtype, int32_t num_groups, int32
         return LORA_ERR_INVALID_ARG;
     beam_args a{};
     const int64_t rows = (int64_t)num_groups * beams, out = 4 * (int64_t)num_groups * num_out;
-    divide_beams(rows, vocab, &a.chunk, &a.splits);
+    divide_beams(rows, vocab, &a.unit, &a.chunk, &a.splits);
     const size_t need = beam_workspace(rows, a.splits, num_out);
     if (!workspace || workspace_bytes < need || misaligned(workspace, 256)) return LORA_ERR_WORKSPACE;
     if (ld > ((int64_t)1 << 60) / rows) return LORA_ERR_UNSUPPORTED;
