@@ -7,6 +7,7 @@
 #include <hip/hip_runtime.h>
 
 #include <climits>
+#include <type_traits>
 
 #include "device_util.h"
 #include "kernels_sequences.h"
@@ -16,6 +17,7 @@ namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kList = 8192;                    // free pages that are kept in LDS
+constexpr int kFew = 4;                        // tokens of a sequence that its thread writes down by itself (no more than a page has)
 constexpr int kChunk = 1024;                   // entries or tokens of a sequence that a wavefront writes down
 
 // how many lanes before this one are in the mask, on top of n
@@ -32,17 +34,37 @@ __device__ __forceinline__ int pages_of(const pages_args& p, int tokens) { retur
 __device__ __forceinline__ int length_at(const pages_args& p, int s) { return min(max(p.length[s], 0), p.max_length); }
 __device__ __forceinline__ bool known(const pages_args& p, int page) { return page >= 0 && page < p.num_pages; }
 
+// a lane's number and those of the lanes before it
+__device__ __forceinline__ int sum_upto(int n)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    // within rows of 16 lanes by 1, 2, 4 and 8, then the rows' last to the rows behind
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);
+#endif
+    return n;
+}
+__device__ __forceinline__ int64_t sum_upto(int64_t n)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+        const int64_t below = __shfl_up(n, off, 64);
+        if (lane >= off) n += below;
+    }
+    return n;
+}
+
 // exclusive prefix of a thread's number over the workgroup, and the sum
 template <typename N>
 __device__ __forceinline__ N prefix(N n, N* sums, N* total)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    N upto = n;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const N below = __shfl_up(upto, off, 64);
-        if (lane >= off) upto += below;
-    }
+    const N upto = sum_upto(n);
     __syncthreads();                           // (sums of the call before have been read)
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
@@ -66,24 +88,32 @@ __device__ __forceinline__ void give_back(const pages_args& p, int s, int e)
     *entry = -1;
 }
 
-// The first `most` free pages in order, by one workgroup: how many there are of them.  list[i] is written for i < that.
-__device__ __forceinline__ int64_t find_free(const pages_args& p, int64_t most, int32_t* list, int* sums)
+// The users of a lane's pages, LOADS times four in a row, 256 on
+struct __attribute__((packed, aligned(4))) four { int32_t x[4]; };
+template <int LOADS>
+__device__ __forceinline__ void load_users(const pages_args& p, int64_t mine, four* u)
 {
-    struct __attribute__((packed, aligned(4))) four { int32_t x[4]; };
-    constexpr int LOADS = 4, WAVE = LOADS * 256;               // pages of a wavefront at a time
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int64_t at = mine + 256 * i;
+        if (at + 4 <= p.num_pages) u[i] = *reinterpret_cast<const four*>(p.users + at);
+        else
+#pragma unroll
+            for (int c = 0; c < 4; ++c) u[i].x[c] = at + c < p.num_pages ? p.users[at + c] : 1;
+    }
+}
+
+// The first `most` free pages in order, by one workgroup: how many there are of them.  list[i] is written for i < that.  u: the users of
+// the first pages, where nothing has changed them (fresh)
+constexpr int kFreeLoads = 4, kFreeWave = kFreeLoads * 256;    // pages of a wavefront at a time
+__device__ __forceinline__ int64_t find_free(const pages_args& p, int64_t most, int32_t* list, int* sums, four* u, bool fresh)
+{
+    constexpr int LOADS = kFreeLoads;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     int64_t found = 0;
-    for (int64_t base = 0; base < p.num_pages && found < most; base += kWaves * WAVE) {
-        const int64_t mine = base + wave * WAVE + 4 * lane;
-        four u[LOADS];
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int64_t at = mine + 256 * i;
-            if (at + 4 <= p.num_pages) u[i] = *reinterpret_cast<const four*>(p.users + at);
-            else
-#pragma unroll
-                for (int c = 0; c < 4; ++c) u[i].x[c] = at + c < p.num_pages ? p.users[at + c] : 1;
-        }
+    for (int64_t base = 0; base < p.num_pages && found < most; base += kWaves * kFreeWave) {
+        const int64_t mine = base + wave * kFreeWave + 4 * lane;
+        if (base > 0 || !fresh) load_users<LOADS>(p, mine, u);
         int before[LOADS], count = 0;                          // of the lanes below, and of the loads before
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
@@ -118,47 +148,74 @@ __device__ __forceinline__ int64_t find_free(const pages_args& p, int64_t most, 
     return found < most ? found : most;
 }
 
-// a new token's sequence, position and slot
-__device__ __forceinline__ void write_token(const resize_args& a, int row, int s, int position)
+// the free page of that number, when part_first is where each part's begin: of the part it is in, the one of that place
+__device__ __forceinline__ int free_page(const resize_args& a, int number)
 {
-    if (row >= a.num_tokens) return;
-    if (a.token_seq) a.token_seq[row] = s;
-    if (a.token_position) a.token_position[row] = position;
-    if (a.token_slot) {
-        const int number = position / a.p.page_tokens, page = a.p.page_table[(int64_t)s * a.p.table_stride + number];
-        a.token_slot[row] = known(a.p, page) ? (int64_t)page * a.p.page_tokens + position - number * a.p.page_tokens : -1;
+    int lo = 0, hi = free_parts(a.p.num_pages);
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        (a.part_first[mid] <= number ? lo : hi) = mid;
     }
+    return a.list[(int64_t)lo * FREE_PART + number - a.part_first[lo]];
 }
 
-// One workgroup decides: a thread R sequences, thread by thread in each thousand.  ALL: R is 1, and nothing is left to another launch.
+// a new token's sequence, position and slot (row < num_tokens)
+__device__ __forceinline__ void write_token(const resize_args& a, int row, int s, int position, int page)
+{
+    if (a.token_seq) a.token_seq[row] = s;
+    if (a.token_position) a.token_position[row] = position;
+    if (a.token_slot) a.token_slot[row] = known(a.p, page) ? (int64_t)page * a.p.page_tokens + position % a.p.page_tokens : -1;
+}
+
+// What a sequence has and wants, and the page that it would write next where that holds tokens already and has other users (else -1)
+struct wish {
+    int from, to, last;
+    bool fits;                                 // the wanted length is one
+    int page;                                  // that it would write next, if that holds tokens already
+};
+__device__ __forceinline__ wish wish_of(const resize_args& a, int s)
+{
+    const int wanted = a.wanted[s], from = length_at(a.p, s);
+    const bool fits = wanted >= 0 && wanted <= a.p.max_length;
+    return wish{from, fits ? wanted : from, -1, fits, -1};
+}
+__device__ __forceinline__ void look_at_page(const pages_args& p, int s, wish& w)
+{
+    if (w.to <= w.from || w.from % p.page_tokens == 0) return;
+    w.page = p.page_table[(int64_t)s * p.table_stride + w.from / p.page_tokens];
+    if (known(p, w.page) && p.users[w.page] > 1) w.last = w.page;
+}
+
+// One workgroup decides: a thread R sequences in a row.  ALL: R is 1, and nothing is left to other launches.  Else the launch before has
+// left wishes where the grants go, and of each part of the pool the number of free pages.
 template <int R, bool ALL>
 __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
 {
-    __shared__ int64_t sums[kWaves];
+    __shared__ int64_t sums_[kWaves];
     __shared__ int counts[kWaves];
     __shared__ int32_t near[ALL ? kList : 1];
     __shared__ page_grant grants[ALL ? kThreads : 1];
     const pages_args& p = a.p;
-    const int tid = threadIdx.x, S = p.num_seqs, P = p.page_tokens;
-    int from[R], to[R], last[R];               // last: the page that holds the next token's place already, if it has other users
-    bool fits[R];                              // the wanted length is one
-    bool shorter = false;
+    const int tid = threadIdx.x, S = p.num_seqs, s0 = tid * R;
+    wish w[R];
+    bool shorter = false, some = false;
+    four users[ALL ? kFreeLoads : 1];          // (asked for before it is known that they are wanted)
+    if constexpr (ALL) load_users<kFreeLoads>(p, (int64_t)(tid >> 6) * kFreeWave + 4 * (tid & 63), users);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int s = r * kThreads + tid;
-        from[r] = to[r] = 0;
-        fits[r] = false;
-        last[r] = -1;
-        if (s >= S) continue;
-        const int wanted = a.wanted[s];
-        from[r] = length_at(p, s);
-        fits[r] = wanted >= 0 && wanted <= p.max_length;
-        to[r] = fits[r] ? wanted : from[r];
-        shorter |= to[r] < from[r];
+        w[r] = wish{0, 0, -1, false, -1};
+        if (s0 + r >= S) continue;
+        if constexpr (ALL) w[r] = wish_of(a, s0 + r);
+        else {
+            const page_grant g = a.grants[s0 + r];
+            w[r] = wish{g.from, g.to, g.first, g.row != 0, -1};
+        }
+        shorter |= w[r].to < w[r].from;
     }
     if constexpr (ALL) {
-        grants[tid] = page_grant{from[0], to[0], 0, 0};
-        if (__syncthreads_or(shorter)) {
+        grants[tid] = page_grant{w[0].from, w[0].to, 0, 0};
+        shorter = __syncthreads_or(shorter);
+        if (shorter) {
             const int entries = S * p.table_stride;
             for (int e = tid; e < entries; e += kThreads) {
                 const int s = e / p.table_stride, i = e - s * p.table_stride;
@@ -167,104 +224,144 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
             }
             __syncthreads();
         }
+        if (tid < S) look_at_page(p, tid, w[0]);
     }
-    // who shares the page that it would write
-    bool some = false;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int s = r * kThreads + tid;
-        if (to[r] <= from[r] || from[r] % P == 0) continue;
-        const int page = p.page_table[(int64_t)s * p.table_stride + from[r] / P];
-        if (known(p, page) && p.users[page] > 1) {
-            last[r] = page;
-            some = true;
-        }
-    }
-    if (__syncthreads_or(some)) {
-        // all of them leave it; where nobody stays, the one with the most tokens in it keeps it
+    for (int r = 0; r < R; ++r) some |= w[r].last >= 0;
+    some = __syncthreads_or(some);
+    if (some) {
+        // all of them leave the page; where nobody stays, the one with the most tokens in it keeps it
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (last[r] >= 0) atomicSub(p.users + last[r], 1);
+            if (w[r].last >= 0) atomicSub(p.users + w[r].last, 1);
         __syncthreads();
-        int key[R];
+        auto key_of = [&](int r) { return -1 - (w[r].from % p.page_tokens * LORA_PAGES_MAX_SEQS + s0 + r); };
+        // (read from the caches' common level: other wavefronts' atomics are there)
+        auto users_of = [&](int r) { return __hip_atomic_load(p.users + w[r].last, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            key[r] = -1 - (from[r] % P * LORA_PAGES_MAX_SEQS + r * kThreads + tid);
-            // (from the caches' common level: other wavefronts' atomics are there)
-            if (last[r] >= 0 && __hip_atomic_load(p.users + last[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) <= 0) atomicMin(p.users + last[r], key[r]);
-        }
+        for (int r = 0; r < R; ++r)
+            if (w[r].last >= 0 && users_of(r) <= 0) atomicMin(p.users + w[r].last, key_of(r));
         __syncthreads();
-        bool keeps[R];
+        uint32_t keeps = 0;
 #pragma unroll
-        for (int r = 0; r < R; ++r) keeps[r] = last[r] >= 0 && __hip_atomic_load(p.users + last[r], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == key[r];
+        for (int r = 0; r < R; ++r)
+            if (w[r].last >= 0 && users_of(r) == key_of(r)) keeps |= 1u << r;
         __syncthreads();
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (keeps[r]) {
-                atomicExch(p.users + last[r], 1);
-                last[r] = -1;
+            if (keeps >> r & 1) {
+                atomicExch(p.users + w[r].last, 1);
+                w[r].last = -1;
             }
         __syncthreads();
     }
-    // what each needs, and what all before it need
-    int64_t upto[R], total = 0;
-    int need[R];
+    // what each needs, and what all before it need.  (Of ALL's tables sums stay below 2^31.)
+    using sum_t = std::conditional_t<ALL, int, int64_t>;
+    sum_t* const sums = reinterpret_cast<sum_t*>(sums_);
+    auto need_of = [&](int r) { return w[r].to > w[r].from ? pages_of(p, w[r].to) - pages_of(p, w[r].from) + (w[r].last >= 0) : 0; };
+    sum_t mine = 0, total;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        need[r] = to[r] > from[r] ? pages_of(p, to[r]) - pages_of(p, from[r]) + (last[r] >= 0) : 0;
-        int64_t all;
-        upto[r] = total + prefix<int64_t>(need[r], sums, &all) + need[r];
-        total += all;
-    }
-    int32_t* const list = ALL && total <= kList ? near : a.list;
+    for (int r = 0; r < R; ++r) mine += need_of(r);
+    sum_t upto = prefix<sum_t>(mine, sums, &total);
+    int32_t* const list = ALL && total > kList ? a.list : near;
+    int64_t found = 0;
+    if constexpr (ALL) {
+        if (total > 0) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");         // (users have been changed by atomics, in the caches' common level)
+            if (shorter || some) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");      // (users have been changed by atomics, in the caches' common level)
 #endif
-    const int64_t found = total > 0 ? find_free(p, total, list, counts) : 0;
-    __syncthreads();
+            found = find_free(p, total, list, counts, users, !shorter && !some);
+            __syncthreads();
+        }
+    } else {
+        if (total > 0) {
+            // where each part's free pages begin among all
+            const int parts = free_parts(p.num_pages);
+            for (int base = 0; base < parts; base += kThreads) {
+                const int i = base + tid;
+                int all;
+                const int before = prefix<int>(i < parts ? a.part_first[i] : 0, counts, &all);
+                if (i < parts) a.part_first[i] = (int)found + before;
+                found += all;
+            }
+        }
+        __syncthreads();
+    }
     // who is served
-    int64_t rows = 0;
+    int64_t tokens = 0;
+    int first[R];
+    uint32_t served = 0;
+    bool more = false;                                         // than a thread writes down by itself, while others wait
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int s = r * kThreads + tid;
-        const bool served = need[r] == 0 || upto[r] <= found;
-        if (!served) to[r] = from[r];
-        int64_t all;
-        const int64_t row = rows + prefix<int64_t>(max(0, to[r] - from[r]), sums, &all);
-        rows += all;
+        const int need = need_of(r);
+        first[r] = (int)min((int64_t)upto, (int64_t)INT_MAX);  // (past INT_MAX: not served)
+        upto += need;
+        if (need == 0 || upto <= found) {
+            served |= 1u << r;
+            tokens += max(0, w[r].to - w[r].from);
+            more |= w[r].to - w[r].from > kFew;
+        }
+    }
+    sum_t rows;
+    int row;
+    if constexpr (ALL) {
+        more = __syncthreads_or(more);
+        row = prefix<int>((int)tokens, sums, &rows);
+    } else
+        row = (int)prefix<int64_t>(tokens, sums, &rows);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int s = s0 + r;
         if (s >= S) continue;
-        const int first = (int)min(upto[r] - need[r], (int64_t)INT_MAX);       // (past INT_MAX: not served)
-        const bool copy = last[r] >= 0 && served;
+        const bool is = served >> r & 1, copy = w[r].last >= 0 && is;
+        const int to = is ? w[r].to : w[r].from;
         int target = -1;
         if (copy) {
-            target = list[first];
-            atomicExch(p.users + target, 1);
-            p.page_table[(int64_t)s * p.table_stride + from[r] / P] = target;
-        } else if (last[r] >= 0)
-            atomicAdd(p.users + last[r], 1);   // it stays
-        a.copies[2 * (int64_t)s] = copy ? last[r] : -1;
+            target = ALL ? list[first[r]] : free_page(a, first[r]);
+            p.users[target] = 1;
+            p.page_table[(int64_t)s * p.table_stride + w[r].from / p.page_tokens] = target;
+        } else if (w[r].last >= 0)
+            atomicAdd(p.users + w[r].last, 1);                 // it stays
+        a.copies[2 * (int64_t)s] = copy ? w[r].last : -1;
         a.copies[2 * (int64_t)s + 1] = target;
-        if (a.granted) a.granted[s] = served && fits[r];
+        if (a.granted) a.granted[s] = is && w[r].fits;
+        const int after = row + max(0, to - w[r].from);
         if (a.indptr) {
-            a.indptr[s] = (int32_t)row;
-            if (s == S - 1) a.indptr[S] = (int32_t)row + max(0, to[r] - from[r]);
+            a.indptr[s] = row;
+            if (s == S - 1) a.indptr[S] = after;
         }
-        if (served && fits[r]) p.length[s] = to[r];
-        const page_grant g{from[r], to[r], first | (copy ? INT_MIN : 0), (int32_t)row};
+        if (is && w[r].fits) p.length[s] = to;
+        if constexpr (ALL) {
+            if (!more) {
+                // few tokens: at most one new page, and nothing that another thread has to know
+                const int have = pages_of(p, w[0].from), fresh = pages_of(p, to) > have ? list[first[0] + copy] : -1;
+                if (fresh >= 0) {
+                    p.users[fresh] = 1;
+                    p.page_table[(int64_t)s * p.table_stride + have] = fresh;
+                }
+                for (int i = row; i < min(after, a.num_tokens); ++i) {
+                    const int position = w[0].from + i - row;
+                    write_token(a, i, s, position, position / p.page_tokens >= have ? fresh : copy ? target : w[0].page);
+                }
+            }
+        }
+        const page_grant g{w[r].from, to, first[r] | (copy ? INT_MIN : 0), row};
         if constexpr (ALL) grants[tid] = g;
         else a.grants[s] = g;
+        row = after;
     }
     if constexpr (ALL) {
+        if (!more) return;
         __syncthreads();
         // new entries: the sequence of each new page, by halves
         const int given = (int)(total < found ? total : found);
-        auto search = [&](int n, auto start) { // the last sequence that starts at or before n
-            int lo = 0, hi = S;
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                (start(mid) <= n ? lo : hi) = mid;
-            }
-            return lo;
+        auto search = [&](int n, auto start) { // the last sequence that starts at or before n (steps alike for all, so that several searches run side by side)
+            int at = 0;
+#pragma unroll
+            for (int step = kThreads / 2; step > 0; step >>= 1)
+                if (at + step < S && start(at + step) <= n) at += step;
+            return at;
         };
         for (int n = tid; n < given; n += kThreads) {
             const int s = search(n, [&](int i) { return grants[i].first & INT_MAX; });
@@ -272,15 +369,26 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
             const int i = n - (g.first & INT_MAX) - (g.first < 0), e = pages_of(p, g.from) + i;
             if (i < 0 || g.to <= g.from || e >= pages_of(p, g.to)) continue;           // (a copy; pages that would not have been enough)
             p.page_table[(int64_t)s * p.table_stride + e] = list[n];
-            atomicExch(p.users + list[n], 1);
+            p.users[list[n]] = 1;
         }
         __syncthreads();
         const int most = (int)(rows < a.num_tokens ? rows : a.num_tokens);
-        if (a.token_seq || a.token_position || a.token_slot)
-            for (int n = tid; n < most; n += kThreads) {
-                const int s = search(n, [&](int i) { return grants[i].row; });
-                write_token(a, n, s, grants[s].from + n - grants[s].row);
+        if (!a.token_seq && !a.token_position && !a.token_slot) return;
+        constexpr int TOGETHER = 4;
+        for (int n0 = tid; n0 < most; n0 += TOGETHER * kThreads) {
+            int s[TOGETHER], page[TOGETHER], position[TOGETHER];
+#pragma unroll
+            for (int k = 0; k < TOGETHER; ++k) {
+                const int n = min(n0 + k * kThreads, most - 1);
+                s[k] = search(n, [&](int i) { return grants[i].row; });
+                position[k] = grants[s[k]].from + n - grants[s[k]].row;
             }
+#pragma unroll
+            for (int k = 0; k < TOGETHER; ++k) page[k] = p.page_table[(int64_t)s[k] * p.table_stride + position[k] / p.page_tokens];
+#pragma unroll
+            for (int k = 0; k < TOGETHER; ++k)
+                if (n0 + k * kThreads < most) write_token(a, n0 + k * kThreads, s[k], position[k], page[k]);
+        }
     }
 }
 
@@ -296,6 +404,54 @@ __global__ __launch_bounds__(256) void pages_give_back_kernel(resize_args a, int
     for (int e = first + lane; e < end; e += 64) give_back(p, s, e);
 }
 
+// Then every sequence's wish, and of every part of the pool the free pages in order, to the part's place in the list, and how many there are
+__global__ __launch_bounds__(256) void pages_look_kernel(resize_args a)
+{
+    __shared__ int sums[4];
+    const pages_args& p = a.p;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t id = (int64_t)blockIdx.x * 256 + tid;
+    if (id < p.num_seqs) {
+        wish w = wish_of(a, (int)id);
+        look_at_page(p, (int)id, w);
+        a.grants[id] = page_grant{w.from, w.to, w.last, w.fits};
+    }
+    const int64_t base = (int64_t)blockIdx.x * FREE_PART;
+    if (base >= p.num_pages) return;
+    constexpr int LOADS = FREE_PART / 1024;
+    const int64_t mine = base + wave * (LOADS * 256) + 4 * lane;
+    four u[LOADS];
+    load_users<LOADS>(p, mine, u);
+    int before[LOADS], count = 0;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        before[i] = count;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const uint64_t mask = __ballot(u[i].x[c] == 0);
+            before[i] = lanes_before(mask, before[i]);
+            count += __popcll(mask);
+        }
+    }
+    if (lane == 0) sums[wave] = count;
+    __syncthreads();
+    int first = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        first += w < wave ? sums[w] : 0;
+        all += sums[w];
+    }
+    int32_t* const list = a.list + base;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        int rank = first + before[i];
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (u[i].x[c] == 0) list[rank++] = (int32_t)(mine + 256 * i + c);
+    }
+    if (tid == 0) a.part_first[blockIdx.x] = all;
+}
+
 // Behind it: a wavefront a sequence and so many of its new entries and tokens.  A token's page is taken from where its entry comes from:
 // another wavefront may not have written the entry yet.
 __global__ __launch_bounds__(256) void pages_write_kernel(resize_args a, int chunks)
@@ -305,25 +461,21 @@ __global__ __launch_bounds__(256) void pages_write_kernel(resize_args a, int chu
     if (s >= p.num_seqs) return;
     const page_grant g = a.grants[s];
     if (g.to <= g.from) return;
-    const int have = pages_of(p, g.from), want = pages_of(p, g.to), P = p.page_tokens;
-    const int32_t* const list = a.list + (g.first & INT_MAX) + (g.first < 0);
+    const int have = pages_of(p, g.from), want = pages_of(p, g.to), P = p.page_tokens, first = (g.first & INT_MAX) + (g.first < 0);
     int32_t* const table = p.page_table + (int64_t)s * p.table_stride;
     for (int e = have + chunk * kChunk + lane; e < min(want, have + (chunk + 1) * kChunk); e += 64) {
-        const int page = list[e - have];
+        const int page = free_page(a, first + e - have);
         table[e] = page;
         p.users[page] = 1;
     }
-    if (!a.token_seq && !a.token_position && !a.token_slot) return;
-    const int end = min(g.to - g.from, (chunk + 1) * kChunk);
-    for (int i = chunk * kChunk + lane; i < end; i += 64) {
-        const int row = g.row + i, position = g.from + i, number = position / P;
-        if (row >= a.num_tokens) break;
-        if (a.token_seq) a.token_seq[row] = s;
-        if (a.token_position) a.token_position[row] = position;
-        if (a.token_slot) {
-            const int page = number < have ? table[number] : list[number - have];
-            a.token_slot[row] = known(p, page) ? (int64_t)page * P + position - number * P : -1;
-        }
+    const int begin = chunk * kChunk, end = min(min(g.to - g.from, begin + kChunk), a.num_tokens - g.row);
+    if ((!a.token_seq && !a.token_position && !a.token_slot) || begin >= end) return;
+    // the pages that these tokens are in, a lane one (1024 tokens lie in 33 at most)
+    const int first_number = (g.from + begin) / P, mine = first_number + lane;
+    const int held = mine >= want ? -1 : mine < have ? table[mine] : free_page(a, first + mine - have);
+    for (int i = begin + lane; i < begin + (end - begin + 63) / 64 * 64; i += 64) {
+        const int position = g.from + i, page = __shfl(held, position / P - first_number, 64);
+        if (i < end) write_token(a, g.row + i, s, position, page);
     }
 }
 
@@ -361,35 +513,26 @@ __device__ __forceinline__ int fork_length(const pages_args& p, const int32_t* p
     return from >= 0 && from < p.num_seqs ? length_at(p, from) : 0;
 }
 
-constexpr int kForkEntries = 32, kForkLengths = LORA_PAGES_MAX_SEQS / kThreads;
+constexpr int kForkEntries = 4;                // of a thread, where one workgroup does
 
+template <int E>
 __global__ __launch_bounds__(kThreads) void pages_fork_kernel(pages_args p, const int32_t* parent)
 {
     const int tid = threadIdx.x, entries = p.num_seqs * p.table_stride;
-    fork_entry f[kForkEntries];
-    int length[kForkLengths];
+    fork_entry f[E];
 #pragma unroll
-    for (int i = 0; i < kForkEntries; ++i) {
-        f[i] = fork_entry{-2, -1};
+    for (int i = 0; i < E; ++i) {
         const int at = i * kThreads + tid;
-        if (at < entries) f[i] = fork_of(p, parent, at / p.table_stride, at % p.table_stride);
+        f[i] = at < entries ? fork_of(p, parent, at / p.table_stride, at % p.table_stride) : fork_entry{-2, -1};
     }
-#pragma unroll
-    for (int i = 0; i < kForkLengths; ++i) {
-        const int s = i * kThreads + tid;
-        length[i] = s < p.num_seqs ? fork_length(p, parent, s) : 0;
-    }
+    const int length = tid < p.num_seqs ? fork_length(p, parent, tid) : 0;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kForkEntries; ++i) {
+    for (int i = 0; i < E; ++i) {
         const int at = i * kThreads + tid;
         if (at < entries) write_fork(p, at / p.table_stride, at % p.table_stride, f[i]);
     }
-#pragma unroll
-    for (int i = 0; i < kForkLengths; ++i) {
-        const int s = i * kThreads + tid;
-        if (s < p.num_seqs && parent[s] != s) p.length[s] = length[i];
-    }
+    if (tid < p.num_seqs && parent[tid] != tid) p.length[tid] = length;
 }
 
 // the two launches; the workspace: new rows, new lengths, old lengths
@@ -425,10 +568,13 @@ hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream)
         LORA_LAUNCH(LORA_K_PAGES_DECIDE, (pages_decide_kernel<1, true>), dim3(1), dim3(kThreads), 0, stream, a);
         return hipGetLastError();
     }
-    const int entries = (p.table_stride + kChunk - 1) / kChunk;
+    const int entries = (p.table_stride + kChunk - 1) / kChunk, looks = free_parts(p.num_pages) > (p.num_seqs + 255) / 256 ? free_parts(p.num_pages) : (p.num_seqs + 255) / 256;
     auto blocks = [&](int64_t chunks) { return dim3((uint32_t)((p.num_seqs * chunks + 3) / 4)); };
     LORA_LAUNCH(LORA_K_PAGES_GIVE_BACK, pages_give_back_kernel, blocks(entries), dim3(256), 0, stream, a, entries);
     hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    LORA_LAUNCH(LORA_K_PAGES_LOOK, pages_look_kernel, dim3((uint32_t)looks), dim3(256), 0, stream, a);
+    e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (p.num_seqs <= kThreads) LORA_LAUNCH(LORA_K_PAGES_DECIDE, (pages_decide_kernel<1, false>), dim3(1), dim3(kThreads), 0, stream, a);
     else if (p.num_seqs <= 4 * kThreads) LORA_LAUNCH(LORA_K_PAGES_DECIDE, (pages_decide_kernel<4, false>), dim3(1), dim3(kThreads), 0, stream, a);
@@ -444,8 +590,9 @@ hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream)
 hipError_t launch_pages_fork(const pages_args& p, const int32_t* parent, int32_t* workspace, hipStream_t stream)
 {
     const int64_t entries = (int64_t)p.num_seqs * p.table_stride, most = entries > p.num_seqs ? entries : p.num_seqs;
-    if (entries <= kForkEntries * kThreads) {
-        LORA_LAUNCH(LORA_K_PAGES_FORK, pages_fork_kernel, dim3(1), dim3(kThreads), 0, stream, p, parent);
+    if (p.num_seqs <= kThreads && entries <= kForkEntries * kThreads) {
+        if (entries <= kThreads) LORA_LAUNCH(LORA_K_PAGES_FORK, pages_fork_kernel<1>, dim3(1), dim3(kThreads), 0, stream, p, parent);
+        else LORA_LAUNCH(LORA_K_PAGES_FORK, pages_fork_kernel<kForkEntries>, dim3(1), dim3(kThreads), 0, stream, p, parent);
         return hipGetLastError();
     }
     const dim3 grid((uint32_t)((most + 255) / 256));

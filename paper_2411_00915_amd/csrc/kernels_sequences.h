@@ -18,6 +18,7 @@ struct page_grant {
     int32_t from, to;       // length before and after
     int32_t first;          // of its new pages in the list of free pages; bit 31: the first of them is a copy
     int32_t row;            // of its first new token
+    // (before the launch that decides: lengths held and wanted, the page that would be written and has other users or -1, and whether the wanted one is a length)
 };
 
 struct resize_args {
@@ -28,14 +29,20 @@ struct resize_args {
     int64_t* token_slot;
     int32_t* copies;
     page_grant* grants;     // workspace: [num_seqs]
-    int32_t* list;          // workspace: [num_pages] free pages, in order
+    int32_t* part_first;    // workspace: [free_parts]
+    int32_t* list;          // workspace: [num_pages] free pages in order, each part of the pool's at its place, or all from the start
 };
 
-// workspace of the two calls: grants and list; the new table, new and old lengths
-inline size_t pages_list_offset(int64_t num_seqs) { return ((size_t)num_seqs * sizeof(page_grant) + 255) / 256 * 256; }
+// Parts of the pool whose free pages a workgroup looks for
+constexpr int FREE_PART = 4096;
+constexpr int free_parts(int64_t num_pages) { return (int)((num_pages + FREE_PART - 1) / FREE_PART); }
+
+// workspace of the two calls: grants, parts and list; the new table, new and old lengths
+inline size_t pages_parts_offset(int64_t num_seqs) { return ((size_t)num_seqs * sizeof(page_grant) + 255) / 256 * 256; }
+inline size_t pages_list_offset(int64_t num_seqs, int64_t num_pages) { return pages_parts_offset(num_seqs) + ((size_t)free_parts(num_pages) * 4 + 255) / 256 * 256; }
 inline size_t pages_workspace(int64_t num_pages, int64_t num_seqs, int64_t table_stride)
 {
-    const size_t resize = pages_list_offset(num_seqs) + (size_t)num_pages * 4, fork = (size_t)num_seqs * (size_t)table_stride * 4 + (size_t)num_seqs * 8;
+    const size_t resize = pages_list_offset(num_seqs, num_pages) + (size_t)num_pages * 4, fork = (size_t)num_seqs * (size_t)table_stride * 4 + (size_t)num_seqs * 8;
     return ((resize > fork ? resize : fork) + 255) / 256 * 256;
 }
 

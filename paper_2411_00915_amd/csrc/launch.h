@@ -46,6 +46,7 @@ enum lora_kernel_id {
     LORA_K_CACHE_CHOOSE,
     LORA_K_CACHE_ATTENTION_CHOSEN,
     LORA_K_PAGES_GIVE_BACK,
+    LORA_K_PAGES_LOOK,
     LORA_K_PAGES_DECIDE,
     LORA_K_PAGES_WRITE,
     LORA_K_PAGES_FORK,

@@ -82,7 +82,7 @@ extern "C" lora_status lora_pages_resize(const lora_pages* p, const int32_t* wan
         return LORA_ERR_INVALID_ARG;
     char* const w = static_cast<char*>(workspace);
     const resize_args a{args_of(p), wanted, num_tokens, granted, indptr, token_seq, token_position, token_slot, copies, reinterpret_cast<page_grant*>(w),
-                        reinterpret_cast<int32_t*>(w + pages_list_offset(p->num_seqs))};
+                        reinterpret_cast<int32_t*>(w + pages_parts_offset(p->num_seqs)), reinterpret_cast<int32_t*>(w + pages_list_offset(p->num_seqs, p->num_pages))};
     return status_of(launch_pages_resize(a, static_cast<hipStream_t>(hip_stream)));
 }
 
