@@ -269,9 +269,10 @@ lora_status check_single(const lora_cache* c, int32_t num_heads, int32_t num_tok
 
 // pages of the longest sequence, to whole 32s
 int64_t key_stride(const lora_cache* c) { return ((int64_t)(c->max_length + c->page_tokens - 1) / c->page_tokens + 31) / 32 * 32; }
+int32_t pieces_of(const lora_cache* c, int32_t num_tokens) { return choose_pieces((int64_t)num_tokens * c->num_kv_heads, key_stride(c)); }
 size_t choose_bytes(const lora_cache* c, int32_t num_tokens)
 {
-    return key_stride(c) > LORA_CACHE_CHOOSE_NEAR ? ((size_t)num_tokens * c->num_kv_heads * (size_t)key_stride(c) * 4 + 255) / 256 * 256 : 0;
+    return key_stride(c) > LORA_CACHE_CHOOSE_NEAR || pieces_of(c, num_tokens) > 1 ? ((size_t)num_tokens * c->num_kv_heads * (size_t)key_stride(c) * 4 + 255) / 256 * 256 : 0;
 }
 }  // namespace
 
@@ -308,7 +309,7 @@ extern "C" lora_status lora_cache_choose(const lora_cache* c, int32_t dtype, int
     if (st != LORA_OK) return st;
     if (budget < 1 || first < 0 || recent < 0 || (int64_t)first + recent > budget) return LORA_ERR_INVALID_ARG;
     max_new = std::min(max_new, num_tokens);
-    st = check_single(c, num_heads, num_tokens, max_new, LORA_CACHE_CHOOSE_THREADS, 1);
+    st = check_single(c, num_heads, num_tokens, max_new, LORA_CACHE_CHOOSE_THREADS, pieces_of(c, num_tokens));
     if (st != LORA_OK) return st;
     if ((int64_t)num_tokens * c->num_kv_heads > ((int64_t)1 << 40) / std::max<int64_t>(budget, key_stride(c))) return LORA_ERR_UNSUPPORTED;
     if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
@@ -336,6 +337,8 @@ extern "C" lora_status lora_cache_choose(const lora_cache* c, int32_t dtype, int
     a.chosen = chosen;
     a.keys = bytes > 0 ? static_cast<uint32_t*>(workspace) : nullptr;
     a.key_stride = key_stride(c);
+    a.pieces = pieces_of(c, num_tokens);
+    a.piece_pages = (int32_t)((a.key_stride + a.pieces - 1) / a.pieces);
     return status_of(launch_cache_choose(a, dtype, static_cast<hipStream_t>(hip_stream)));
 }
 

@@ -40,6 +40,21 @@ __device__ __forceinline__ float wave_sum(float v)
     return v;
 }
 
+// a lane's number and those of the lanes before it
+__device__ __forceinline__ int wave_sum_upto(int n)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    // within rows of 16 lanes by 1, 2, 4 and 8, then the rows' last to the rows behind
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);
+#endif
+    return n;
+}
+
 // Loads straight to LDS: lane i's 16 bytes at base + off -> LDS byte address lds_base + 16 i (base and lds_base
 // wavefront-uniform).  Issued from inline assembly, so the waits for them are written out.  M0 carries the LDS address;
 // nothing else in the kernels that use this uses M0 (LDS instructions of gfx9 and later do not read it).

@@ -666,8 +666,10 @@ template <typename T, int DP, int CT, int WAVES>
 void launch_shape(const cache_attention_args& a, hipStream_t stream)
 {
     const dim3 grid((uint32_t)((int64_t)a.c.num_seqs * a.c.kv_heads * a.splits * a.row_tiles)), block(64 * WAVES);
-    if (a.chosen) LORA_LAUNCH(LORA_K_CACHE_ATTENTION_CHOSEN, (cache_attention_kernel<T, DP, CT, false, WAVES, true>), dim3(grid.x * (uint32_t)a.c.max_new), block, 0, stream, a);
-    else if (a.scores) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, true, WAVES, false>), grid, block, 0, stream, a);
+    if (a.chosen) {
+        const dim3 tokens((uint32_t)((int64_t)a.c.num_seqs * a.c.max_new * a.c.kv_heads * a.splits * a.row_tiles));
+        LORA_LAUNCH(LORA_K_CACHE_ATTENTION_CHOSEN, (cache_attention_kernel<T, DP, CT, false, WAVES, true>), tokens, block, 0, stream, a);
+    } else if (a.scores) LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, true, WAVES, false>), grid, block, 0, stream, a);
     else LORA_LAUNCH(LORA_K_CACHE_ATTENTION, (cache_attention_kernel<T, DP, CT, false, WAVES, false>), grid, block, 0, stream, a);
 }
 

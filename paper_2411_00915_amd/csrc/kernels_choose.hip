@@ -51,18 +51,37 @@ __global__ __launch_bounds__(256) void cache_digest_kernel(cache_args c, int8_t*
         high[e] = -INFINITY;
         low[e] = INFINITY;
     }
-#pragma unroll 4
-    for (int t = token; t < c.page_tokens; t += TOKENS) {
-        const int at = min(t, held - 1);                       // (those behind the last: the last once more)
-        const uint32_t codes = *reinterpret_cast<const uint32_t*>(base + at * (DP / 2) + 4 * word);
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(base + word_offset<DP>(c.page_tokens, at, 0));
-        const float step = __uint_as_float(w << 16), zero = __uint_as_float(w & 0xffff0000u);
-        wild |= !(fabsf(step) < INFINITY && fabsf(zero) < INFINITY);
+    // 32 tokens at a time, the next ones' loads on their way
+    constexpr int LOADS = 32 / TOKENS;
+    uint32_t codes[LOADS], words[LOADS];
+    auto load = [&](int first_token) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float x = (float)(codes >> (4 * e) & 15u) * step + zero;
-            high[e] = fmaxf(high[e], x);
-            low[e] = fminf(low[e], x);
+        for (int k = 0; k < LOADS; ++k) {
+            const int at = min(first_token + k * TOKENS + token, held - 1);        // (those behind the last: the last once more)
+            codes[k] = *reinterpret_cast<const uint32_t*>(base + at * (DP / 2) + 4 * word);
+            words[k] = *reinterpret_cast<const uint32_t*>(base + word_offset<DP>(c.page_tokens, at, 0));
+        }
+    };
+    load(0);
+#pragma unroll 1
+    for (int t = 0; t < held; t += 32) {
+        uint32_t now[LOADS], w[LOADS];
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            now[k] = codes[k];
+            w[k] = words[k];
+        }
+        if (t + 32 < held) load(t + 32);
+#pragma unroll
+        for (int k = 0; k < LOADS; ++k) {
+            const float step = __uint_as_float(w[k] << 16), zero = __uint_as_float(w[k] & 0xffff0000u);
+            wild |= !(fabsf(step) < INFINITY && fabsf(zero) < INFINITY);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float x = (float)(now[k] >> (4 * e) & 15u) * step + zero;
+                high[e] = fmaxf(high[e], x);
+                low[e] = fminf(low[e], x);
+            }
         }
     }
     float most = 0.f;
@@ -113,196 +132,319 @@ __device__ __forceinline__ uint32_t order_of(float x)
 // the greater, NaN above all
 __device__ __forceinline__ float greater(float x, float y) { return y > x || y != y ? y : x; }
 
-__device__ __forceinline__ int lanes_before(uint64_t mask, int n)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, (uint32_t)n));
-#else
-    return n;
-#endif
-}
-
 constexpr int kThreads = LORA_CACHE_CHOOSE_THREADS, kWaves = kThreads / 64;
 
+// 16 codes of a page's bounds, and what makes a score of them, for 16 pages a wavefront at a time, ROUNDS of them on their way together
+template <int DP>
+struct bounds_block {
+    static constexpr int NS = 2 * DP / 64, ROUNDS = DP == 256 ? 2 : 4, PAGES = ROUNDS * kWaves * 16;
+    int4v b[ROUNDS][NS];
+    float step[ROUNDS];
+    bool there[ROUNDS];
+
+    // pages first ... of `end`; what is not there is loaded from page 0
+    __device__ __forceinline__ void load(const choose_args& a, const int32_t* table, int head, int first, int end, int wave, int lane)
+    {
+        const cache_args& c = a.c;
+        int64_t at[ROUNDS];
+#pragma unroll
+        for (int u = 0; u < ROUNDS; ++u) {
+            const int n = first + (u * kWaves + wave) * 16 + (lane & 15);
+            const int page = n < end ? table[n] : -1;
+            there[u] = page >= 0 && page < c.num_pages;
+            at[u] = (int64_t)(there[u] ? page : 0) * c.kv_heads + head;
+        }
+#pragma unroll
+        for (int u = 0; u < ROUNDS; ++u) {
+            if (first + (u * kWaves + wave) * 16 >= end) continue;             // (the wavefront's 16 together)
+            const int8_t* const p = a.bounds + at[u] * (2 * DP) + 16 * (lane >> 4);
+#pragma unroll
+            for (int m = 0; m < NS; ++m) b[u][m] = *reinterpret_cast<const int4v*>(p + 64 * m);
+            step[u] = a.steps[at[u]];
+        }
+    }
+};
+
+// The queries' codes, parted by sign: 16 lanes a query, DP/16 dims each
 template <typename T, int DP>
-__global__ __launch_bounds__(kThreads) void cache_choose_kernel(choose_args a)
+struct query_codes {
+    static constexpr int E = DP / 16;
+    float x[E];
+    __device__ __forceinline__ void load(const choose_args& a, int row, int head, int h0, int tid)
+    {
+        const int D = a.c.head_dim, l = tid & 15, h = min(h0 + (tid >> 4 & 15), a.group - 1);
+        const T* const q = static_cast<const T*>(a.q) + (int64_t)row * a.ldq + (int64_t)(head * a.group + h) * D;
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = elem<T>::load(q + min(l * E + e, D - 1));
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = l * E + e < D ? x[e] : 0.f;
+    }
+    __device__ __forceinline__ void make(int8_t (*codes)[2 * DP], float* units, int tid) const
+    {
+        if (tid >= 256) return;
+        const int l = tid & 15, h = tid >> 4;
+        float most = 0.f, wild = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            most = fmaxf(most, fabsf(x[e]));
+            wild = __builtin_fmaf(x[e], 0.f, wild);
+        }
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) {
+            most = fmaxf(most, __shfl_xor(most, off, 16));
+            wild += __shfl_xor(wild, off, 16);
+        }
+        float unit = most * (1.f / 127.f);
+        if (unit < 0x1p-100f) unit = 0.f;
+        if (wild != 0.f) unit = __builtin_nanf("");
+        uint32_t up[(E + 3) / 4] = {}, down[(E + 3) / 4] = {};
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int v = unit > 0.f ? (int)fminf(fmaxf(rintf(x[e] / unit), -127.f), 127.f) : 0;
+            up[e / 4] |= (uint32_t)max(v, 0) << (8 * (e % 4));
+            down[e / 4] |= ((uint32_t)min(v, 0) & 255u) << (8 * (e % 4));
+        }
+#pragma unroll
+        for (int w = 0; w < E / 4; ++w) {
+            *reinterpret_cast<uint32_t*>(&codes[h][l * E + 4 * w]) = up[w];
+            *reinterpret_cast<uint32_t*>(&codes[h][DP + l * E + 4 * w]) = down[w];
+        }
+        if (l == 0) units[h] = unit;
+    }
+};
+
+// The budget-th largest of `pages` keys, and how many of its like are wanted, 8 bits at a time (workgroup)
+__device__ __forceinline__ void threshold_by_bins(const uint32_t* keys, int pages, int budget, int* bins, uint32_t* found, int tid, uint32_t* threshold, int* equal)
 {
-    constexpr int NS = 2 * DP / 64;                            // products of 64 codes
+    const int lane = tid & 63;
+    uint32_t prefix = 0;
+    int wanted = budget;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        for (int n = tid; n < 256; n += kThreads) bins[n] = 0;
+        __syncthreads();
+        const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
+        for (int n = tid; n < pages; n += kThreads) {
+            const uint32_t key = keys[n];
+            if ((key & mask) == prefix) atomicAdd(&bins[key >> shift & 255], 1);
+        }
+        __syncthreads();
+        if (tid < 64) {                                        // from the top: the bin in which the wanted number is reached
+            int mine[4], sum = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sum += mine[e] = bins[255 - (4 * lane + e)];
+            const int upto = wave_sum_upto(sum);
+            int above = upto - sum;
+            if (above < wanted && upto >= wanted)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (above < wanted && above + mine[e] >= wanted) {
+                        found[0] = prefix | (uint32_t)(255 - (4 * lane + e)) << shift;
+                        found[1] = wanted - above;
+                    }
+                    above += mine[e];
+                }
+        }
+        __syncthreads();
+        prefix = found[0];
+        wanted = (int)found[1];
+    }
+    *threshold = prefix;
+    *equal = wanted;
+}
+
+// The same of up to 64 N keys, by one wavefront, bit by bit, without a barrier; done as soon as as many as wanted are not below a number
+// (eight wavefronts, each for itself, are in each other's way in the scalar unit: 3.9 us for 400 keys)
+template <int N>
+__device__ __forceinline__ void threshold_by_bits(const uint32_t* keys, int pages, int budget, int lane, uint32_t* found)
+{
+    uint32_t k[N], t = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) k[i] = i * 64 + lane < pages ? keys[i * 64 + lane] : 0u;
+    int equal = -1;
+#pragma unroll 1
+    for (int bit = 31; bit >= 0; --bit) {
+        const uint32_t next = t | 1u << bit;
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) count += __popcll(__ballot(k[i] >= next));
+        if (count >= budget) t = next;
+        if (count == budget) {
+            --t;                                               // (all that are above it)
+            equal = 0;
+            break;
+        }
+    }
+    if (equal < 0) {
+        equal = budget;
+#pragma unroll
+        for (int i = 0; i < N; ++i) equal -= __popcll(__ballot(k[i] > t));
+    }
+    if (lane == 0) {
+        found[0] = t;
+        found[1] = (uint32_t)equal;
+    }
+}
+
+constexpr int kBoth = 0, kScores = 1, kChoice = 2;      // what a launch does: keys and choice; keys of a piece of the pages; the choice
+
+template <typename T, int DP, int WHAT>
+__global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void cache_choose_kernel(choose_args a)
+{
+    typedef bounds_block<DP> block;
+    constexpr int NS = block::NS;
     extern __shared__ __align__(16) uint32_t near[];           // keys of the pages, where they fit
-    __shared__ __align__(16) int8_t codes[16][2 * DP];
+    __shared__ __align__(16) int8_t codes[WHAT == kChoice ? 1 : 16][2 * DP];
     __shared__ float units[16];
     __shared__ int bins[256], counts[2][kWaves];
     __shared__ uint32_t found[2];
     const cache_args& c = a.c;
     int id = blockIdx.x;
+    const int piece = WHAT == kScores ? id % a.pieces : 0;
+    if constexpr (WHAT == kScores) id /= a.pieces;
     const int head = id % c.kv_heads;
     id /= c.kv_heads;
     const int i = id % c.max_new, s = id / c.max_new;
     const cache_rows rows = rows_of(c, s);
     if (i >= rows.count) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = rows.first + i;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), row = rows.first + i;
     const int sees = max(0, length_of(c, s) - rows.count + i + 1), pages = sees == 0 ? 0 : page_number(c, sees - 1) + 1;
     const int budget = a.budget, last = pages - a.recent;
-    int32_t* const out = a.chosen + ((int64_t)row * c.kv_heads + head) * budget;
     const int32_t* const table = c.page_table + (int64_t)s * c.table_stride;
-    auto page_at = [&](int n) -> int64_t {
-        const int64_t p = table[n];
-        return p < 0 || p >= c.num_pages ? -1 : p;
-    };
-    uint32_t* const keys = a.keys ? a.keys + ((int64_t)row * c.kv_heads + head) * a.key_stride : near;
+    uint32_t* const keys = WHAT != kBoth || a.keys ? a.keys + ((int64_t)row * c.kv_heads + head) * a.key_stride : near;
     const bool all = pages <= budget || c.num_pages == 0;      // no need to know their order
-    if (all) {
-        for (int n = tid; n < pages; n += kThreads) keys[n] = page_at(n) < 0 ? 0u : kForced;
-    } else {
-        for (int h0 = 0; h0 < a.group; h0 += 16) {
-            // the queries' codes: 16 lanes a query, DP/16 dims each
-            __syncthreads();
-            constexpr int E = DP / 16;
-            for (int h = tid >> 4; h < 16; h += kThreads / 16) {
-                const int l = tid & 15;
-                const T* const q = static_cast<const T*>(a.q) + (int64_t)row * a.ldq + (int64_t)(head * a.group + min(h0 + h, a.group - 1)) * c.head_dim;
-                float x[E], most = 0.f, wild = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int d = l * E + e;
-                    x[e] = d < c.head_dim ? elem<T>::load(q + d) : 0.f;
-                    most = fmaxf(most, fabsf(x[e]));
-                    wild = __builtin_fmaf(x[e], 0.f, wild);
+    if constexpr (WHAT != kChoice) {
+        const int begin = WHAT == kScores ? piece * a.piece_pages : 0, end = WHAT == kScores ? min(pages, begin + a.piece_pages) : pages;
+        if (all) {
+            for (int n = begin + tid; n < end; n += kThreads) keys[n] = table[n] < 0 || table[n] >= c.num_pages ? 0u : kForced;
+        } else if (begin < end) {
+            query_codes<T, DP> q;
+            block now;
+            q.load(a, row, head, 0, tid);                      // (asked for before the pages' bounds, and used while these are on their way)
+            now.load(a, table, head, begin, end, wave, lane);
+            for (int h0 = 0; h0 < a.group; h0 += 16) {
+                if (h0 > 0) {
+                    __syncthreads();
+                    q.load(a, row, head, h0, tid);
                 }
+                q.make(codes, units, tid);
+                __syncthreads();
+                const int r = lane & 15, g = lane >> 4;
+                int4v query[NS];
 #pragma unroll
-                for (int off = 8; off > 0; off >>= 1) {
-                    most = fmaxf(most, __shfl_xor(most, off, 16));
-                    wild += __shfl_xor(wild, off, 16);
-                }
-                float unit = most * (1.f / 127.f);
-                if (unit < 0x1p-100f) unit = 0.f;
-                if (wild != 0.f) unit = __builtin_nanf("");
+                for (int n = 0; n < NS; ++n) query[n] = *reinterpret_cast<const int4v*>(&codes[WHAT == kChoice ? 0 : r][64 * n + 16 * g]);
+                float unit[4];
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const int v = unit > 0.f ? (int)fminf(fmaxf(rintf(x[e] / unit), -127.f), 127.f) : 0;
-                    codes[h][l * E + e] = (int8_t)max(v, 0);
-                    codes[h][DP + l * E + e] = (int8_t)min(v, 0);
-                }
-                if (l == 0) units[h] = unit;
-            }
-            __syncthreads();
-            const int r = lane & 15, g = lane >> 4;
-            int4v query[NS];
+                for (int e = 0; e < 4; ++e) unit[e] = units[4 * g + e];
+                const int valid = a.group - h0 - 4 * g;        // of the lane's four rows
+                for (int first = begin; first < end; first += block::PAGES) {
+                    if (first > begin || h0 > 0) now.load(a, table, head, first, end, wave, lane);
 #pragma unroll
-            for (int n = 0; n < NS; ++n) query[n] = *reinterpret_cast<const int4v*>(&codes[r][64 * n + 16 * g]);
-            float unit[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) unit[e] = units[4 * g + e];
-            const int valid = a.group - h0 - 4 * g;            // of the lane's four rows
-            for (int n0 = wave * 16; n0 < pages; n0 += kWaves * 16) {
-                const int n = n0 + r;
-                const int64_t page = n < pages ? page_at(n) : -1, at = max(page, (int64_t)0) * c.kv_heads + head;
-                const int8_t* const p = a.bounds + at * (2 * DP) + 16 * g;
-                int4v b[NS];
-#pragma unroll
-                for (int m = 0; m < NS; ++m) b[m] = *reinterpret_cast<const int4v*>(p + 64 * m);
-                const float step = a.steps[at];
-                int4v sum = {0, 0, 0, 0};
+                    for (int u = 0; u < block::ROUNDS; ++u) {
+                        const int n = first + (u * kWaves + wave) * 16 + r;
+                        if (n - r >= end) continue;
+                        int4v sum = {0, 0, 0, 0};
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
-                for (int m = 0; m < NS; ++m) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(query[m], b[m], sum, 0, 0, 0);
+                        for (int m = 0; m < NS; ++m) sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(query[m], now.b[u][m], sum, 0, 0, 0);
 #endif
-                float most = -INFINITY;
+                        float most = -INFINITY;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (e < valid) most = greater(most, (float)sum[e] * unit[e]);
+                        most = greater(most, __shfl_xor(most, 16, 64));
+                        most = greater(most, __shfl_xor(most, 32, 64));
+                        if (g == 0 && n < end) {
+                            uint32_t key = !now.there[u] ? 0u : n < a.first || n >= last ? kForced : order_of(most * now.step[u]);
+                            if (h0 > 0) key = max(key, keys[n]);               // (products with a step not below 0 are in their order)
+                            keys[n] = key;
+                        }
+                    }
+                }
+            }
+        }
+        if constexpr (WHAT == kScores) return;
+        __syncthreads();
+    }
+    if constexpr (WHAT != kScores) {
+        uint32_t threshold = 1;
+        int equal = budget;                                    // (all that are there)
+        if (!all) {
+            if (pages <= 1024) {
+                if (wave == 0) {
+                    if (pages <= 256) threshold_by_bits<4>(keys, pages, budget, lane, found);
+                    else threshold_by_bits<16>(keys, pages, budget, lane, found);
+                }
+                __syncthreads();
+                threshold = found[0];
+                equal = (int)found[1];
+            } else
+                threshold_by_bins(keys, pages, budget, bins, found, tid, &threshold, &equal);
+        }
+        // in order, four pages a thread: above it, all; equal to it, the first few; a page that is not there never
+        int32_t* const out = a.chosen + ((int64_t)row * c.kv_heads + head) * budget;
+        int written = 0, same = 0;
+        for (int n0 = 0; n0 < pages; n0 += 4 * kThreads) {
+            uint32_t above = 0, like = 0;                      // of the thread's four
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int n = n0 + 4 * tid + e;
+                const uint32_t key = n < pages ? keys[n] : 0u;
+                above |= (uint32_t)(key > threshold) << e;
+                like |= (uint32_t)(key == threshold && key != 0) << e;
+            }
+            auto upto = [&](int n, int* into, int* base) {     // of the workgroup's threads before this one, on top of *base, which becomes all
+                const int mine = wave_sum_upto(n);
+                __syncthreads();
+                if (lane == 63) into[wave] = mine;
+                __syncthreads();
+                int before = *base + mine - n;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) {
+                    before += w < wave ? into[w] : 0;
+                    *base += into[w];
+                }
+                return before;
+            };
+            if (equal > 0) {
+                int before = upto(__popc(like), counts[0], &same);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    if (e < valid) most = greater(most, (float)sum[e] * unit[e]);
-                most = greater(most, __shfl_xor(most, 16, 64));
-                most = greater(most, __shfl_xor(most, 32, 64));
-                if (g == 0 && n < pages) {
-                    uint32_t key = page < 0 ? 0u : n < a.first || n >= last ? kForced : order_of(most * step);
-                    if (h0 > 0) key = max(key, keys[n]);       // (products with a step not below 0 are in their order)
-                    keys[n] = key;
-                }
-            }
-        }
-    }
-    __syncthreads();
-    // the budget-th largest key, and how many of its like are wanted
-    uint32_t threshold = 1;
-    int equal = budget;                                        // (all that are there)
-    if (!all) {
-        uint32_t prefix = 0;
-        int wanted = budget;
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int n = tid; n < 256; n += kThreads) bins[n] = 0;
-            __syncthreads();
-            const uint32_t mask = shift == 24 ? 0u : ~0u << (shift + 8);
-            for (int n = tid; n < pages; n += kThreads) {
-                const uint32_t key = keys[n];
-                if ((key & mask) == prefix) atomicAdd(&bins[key >> shift & 255], 1);
-            }
-            __syncthreads();
-            if (wave == 0) {                                   // from the top: the bin in which the wanted number is reached
-                int mine[4], sum = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sum += mine[e] = bins[255 - (4 * lane + e)];
-                int upto = sum;
-#pragma unroll
-                for (int off = 1; off < 64; off <<= 1) {
-                    const int above = __shfl_up(upto, off, 64);
-                    if (lane >= off) upto += above;
-                }
-                int above = upto - sum;
-                if (above < wanted && upto >= wanted)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (above < wanted && above + mine[e] >= wanted) {
-                            found[0] = prefix | (uint32_t)(255 - (4 * lane + e)) << shift;
-                            found[1] = wanted - above;
-                        }
-                        above += mine[e];
+                    if (like >> e & 1) {
+                        if (before < equal) above |= 1u << e;
+                        ++before;
                     }
             }
-            __syncthreads();
-            prefix = found[0];
-            wanted = (int)found[1];
+            int at = upto(__popc(above), counts[1], &written);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (above >> e & 1) {
+                    if (at < budget) out[at] = n0 + 4 * tid + e;
+                    ++at;
+                }
         }
-        threshold = prefix;
-        equal = wanted;
+        for (int n = written + tid; n < budget; n += kThreads) out[n] = -1;
     }
-    // in order: above it, all; equal to it, the first few; a page that is not there never
-    int written = 0, same = 0;
-    for (int n0 = 0; n0 < pages; n0 += kThreads) {
-        const uint32_t key = n0 + tid < pages ? keys[n0 + tid] : 0u;
-        const bool is_equal = key == threshold && key != 0, above = key > threshold;
-        const uint64_t equals = __ballot(is_equal);
-        __syncthreads();
-        if (lane == 0) counts[0][wave] = __popcll(equals);
-        __syncthreads();
-        int before = same;
-        for (int w = 0; w < kWaves; ++w) {
-            before += w < wave ? counts[0][w] : 0;
-            same += counts[0][w];
-        }
-        const bool is = above || (is_equal && lanes_before(equals, before) < equal);
-        const uint64_t mask = __ballot(is);
-        if (lane == 0) counts[1][wave] = __popcll(mask);
-        __syncthreads();
-        int at = written;
-        for (int w = 0; w < kWaves; ++w) {
-            at += w < wave ? counts[1][w] : 0;
-            written += counts[1][w];
-        }
-        at = lanes_before(mask, at);
-        if (is && at < budget) out[at] = n0 + tid;
-    }
-    for (int n = written + tid; n < budget; n += kThreads) out[n] = -1;
+}
+
+template <typename T, int DP>
+void launch_dims(const choose_args& a, hipStream_t stream)
+{
+    const uint32_t wgs = (uint32_t)((int64_t)a.c.num_seqs * a.c.max_new * a.c.kv_heads);
+    const dim3 block(kThreads);
+    if (a.pieces > 1) {
+        LORA_LAUNCH(LORA_K_CACHE_SCORES, (cache_choose_kernel<T, DP, kScores>), dim3(wgs * (uint32_t)a.pieces), block, 0, stream, a);
+        LORA_LAUNCH(LORA_K_CACHE_CHOOSE, (cache_choose_kernel<T, DP, kChoice>), dim3(wgs), block, 0, stream, a);
+    } else
+        LORA_LAUNCH(LORA_K_CACHE_CHOOSE, (cache_choose_kernel<T, DP, kBoth>), dim3(wgs), block, a.keys ? 0u : (uint32_t)a.key_stride * 4, stream, a);
 }
 
 template <typename T>
 hipError_t launch_choose(const choose_args& a, hipStream_t stream)
 {
-    const dim3 grid((uint32_t)((int64_t)a.c.num_seqs * a.c.max_new * a.c.kv_heads)), block(kThreads);
-    const uint32_t lds = a.keys ? 0u : (uint32_t)a.key_stride * 4;
     switch (padded_head_dim(a.c.head_dim)) {
-        case 64: LORA_LAUNCH(LORA_K_CACHE_CHOOSE, (cache_choose_kernel<T, 64>), grid, block, lds, stream, a); break;
-        case 128: LORA_LAUNCH(LORA_K_CACHE_CHOOSE, (cache_choose_kernel<T, 128>), grid, block, lds, stream, a); break;
-        default: LORA_LAUNCH(LORA_K_CACHE_CHOOSE, (cache_choose_kernel<T, 256>), grid, block, lds, stream, a);
+        case 64: launch_dims<T, 64>(a, stream); break;
+        case 128: launch_dims<T, 128>(a, stream); break;
+        default: launch_dims<T, 256>(a, stream);
     }
     return hipGetLastError();
 }

@@ -35,19 +35,7 @@ __device__ __forceinline__ int length_at(const pages_args& p, int s) { return mi
 __device__ __forceinline__ bool known(const pages_args& p, int page) { return page >= 0 && page < p.num_pages; }
 
 // a lane's number and those of the lanes before it
-__device__ __forceinline__ int sum_upto(int n)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    // within rows of 16 lanes by 1, 2, 4 and 8, then the rows' last to the rows behind
-    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, false);
-    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, false);
-    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, false);
-    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, false);
-    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);
-    n += __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);
-#endif
-    return n;
-}
+__device__ __forceinline__ int sum_upto(int n) { return wave_sum_upto(n); }
 __device__ __forceinline__ int64_t sum_upto(int64_t n)
 {
     const int lane = threadIdx.x & 63;

@@ -43,6 +43,7 @@ enum lora_kernel_id {
     LORA_K_CACHE_MOVE,
     LORA_K_CACHE_COPY,
     LORA_K_CACHE_DIGEST,
+    LORA_K_CACHE_SCORES,
     LORA_K_CACHE_CHOOSE,
     LORA_K_CACHE_ATTENTION_CHOSEN,
     LORA_K_PAGES_GIVE_BACK,

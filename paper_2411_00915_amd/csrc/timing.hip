@@ -24,7 +24,7 @@ const char* kNames[LORA_K_COUNT] = {"shrink_general_kernel", "expand_general_ker
                                     "delta_f32_kernel", "attention_tiled_kernel", "attention_tiled_kernel<unaligned>", "attention_tiled_kernel<shared>", "cache_append_kernel",
                                     "cache_read_kernel", "cache_attention_kernel", "cache_finish_kernel",
                                     "cache_select_kernel", "cache_move_kernel",
-                                    "cache_copy_kernel", "cache_digest_kernel", "cache_choose_kernel", "cache_attention_kernel<chosen>",
+                                    "cache_copy_kernel", "cache_digest_kernel", "cache_choose_kernel<scores>", "cache_choose_kernel", "cache_attention_kernel<chosen>",
                                     "pages_give_back_kernel", "pages_look_kernel", "pages_decide_kernel", "pages_write_kernel", "pages_fork_kernel", "beam_rows_kernel",
                                     "beam_join_kernel", "probe_empty_kernel", "probe_read_kernel", "probe_mfma_kernel"};
 long long* g_trace = nullptr;

@@ -241,7 +241,7 @@ def test_long_tables(lengths, max_length, budget):
     pool = Long(lengths, 2, D, 32, 300 if budget > 100 else 5000, 3, max_length)
     q = rng.standard_normal((len(lengths), 4, D)).astype(F)
     need = B.lora_cache_choose_workspace(pool.cache, len(lengths), 1)
-    assert (need > 0) == (-(-(max_length or max(lengths)) // 32) > 12288)
+    assert need > 0                                         # (few tokens: their pages' scores are of a launch of their own)
     got = run_choose(pool, q, [1] * len(lengths), F32, pool.bounds, pool.steps, budget, 1, 1, ptr=None)
     check_choice(pool, q, [1] * len(lengths), lengths, pool.bounds, pool.steps, budget, 1, 1, got)
 
