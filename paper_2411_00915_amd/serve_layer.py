@@ -4,12 +4,15 @@
                  lora_cache_attention of the last tokens (how much weight every cached token gets) -> lora_fused_forward (output)
     decode step  lora_fused_forward -> lora_cache_append -> lora_cache_attention (weights carried on) -> lora_fused_forward
     eviction     lora_cache_evict, where the caches have grown past their limit, into pages of their own
+    beams        lora_pages_resize (pages for the step's tokens) -> lora_cache_copy (of pages that beams shared) -> lora_fused_forward -> lora_cache_append ->
+                 lora_cache_attention, or lora_cache_digest, lora_cache_choose and lora_cache_attention_chosen -> lora_fused_forward -> lora_base_gemm (logits) ->
+                 lora_beam_select -> lora_pages_fork (every beam becomes its parent)
 
     python -m paper_2411_00915_amd.serve_layer [--requests 32] [--prompt 512] [--steps 64] [--hidden 4096] [--heads 32]
-                                               [--kv-heads 8] [--limit 600] [--budget 512]
+                                               [--kv-heads 8] [--limit 600] [--budget 512] [--beams 4] [--vocab 32000] [--chosen 0]
 
-prints microseconds per layer of the prompts, of a decode step and of an eviction.  Random weights; rotary positions, norms
-and the MLP are the program's own and left out here.
+prints microseconds per layer of the prompts, of a decode step and of an eviction, and of a step of beam search (chosen: pages that a token attends
+to, 0: all).  Random weights; rotary positions, norms and the MLP are the program's own and left out here.
 """
 import argparse
 import sys
@@ -160,9 +163,110 @@ class AttentionLayer:
         return kept
 
 
+class BeamLayer:
+    """The same layer for requests of several beams each, and the selection behind it.  Sequence r * beams + b is beam b of request r; tables, lengths and
+    free pages are the device's, so that a step needs no word from it."""
+
+    def __init__(self, hidden, heads, kv_heads, head_dim, ranks, requests, beams, limit, vocab, page=64, chosen=0, end_token=-1, scale=2.0, seed=0):
+        """limit: tokens that a beam may have; chosen: pages of its cache that a token attends to (0: all)"""
+        gen = torch.Generator(device=DEV)
+        gen.manual_seed(seed)
+        self.hidden, self.heads, self.kv_heads, self.head_dim, self.page = hidden, heads, kv_heads, head_dim, page
+        self.requests, self.beams, self.limit, self.vocab, self.chosen, self.end_token = requests, beams, limit, vocab, chosen, end_token
+        self.qkv = Projection(hidden, (heads + 2 * kv_heads) * head_dim, ranks, scale, gen)
+        self.out = Projection(heads * head_dim, hidden, ranks, scale, gen)
+        self.embedding = (torch.randn((vocab, hidden), generator=gen, device=DEV) * hidden ** -0.5).bfloat16()
+        rows, each = requests * beams, -(-limit // page)
+        count = rows * each                                     # (as many as beams that share nothing have)
+
+        def zeros(*size, dtype=torch.int32):
+            return torch.zeros(size, dtype=dtype, device=DEV)
+        self.table, self.length, self.users = zeros(rows, each), zeros(rows), zeros(count)
+        self.pages = B.lora_pages(self.table, self.length, self.users, page, limit)
+        store = zeros(count, kv_heads, B.lora_cache_page_bytes(page, head_dim), dtype=torch.uint8)
+        self.cache = B.lora_cache(store, self.table, self.length, page, kv_heads, head_dim, limit)
+        padded = 64 if head_dim <= 64 else 128 if head_dim <= 128 else 256
+        self.bounds, self.steps = zeros(count, kv_heads, 2, padded, dtype=torch.int8), zeros(count, kv_heads, dtype=torch.float32)
+        self.wanted, self.parent, self.token, self.granted, self.indptr = zeros(rows), zeros(rows), zeros(rows), zeros(rows), zeros(rows + 1)
+        self.copies, self.score = zeros(rows, 2), zeros(rows, dtype=torch.float32)
+        self.best = [zeros(rows, dtype=torch.float32), zeros(rows), zeros(rows)]
+        self.list = zeros(rows, kv_heads, max(chosen, 1))
+        need = [B.lora_pages_workspace(self.pages), B.lora_beam_workspace(requests, beams, vocab, beams), B.lora_beam_workspace(requests, 1, vocab, beams),
+                B.lora_cache_workspace(self.cache, heads, rows, 1)]
+        if chosen:
+            need += [B.lora_cache_choose_workspace(self.cache, rows, 1), B.lora_cache_chosen_workspace(self.cache, heads, rows, 1, chosen)]
+        self.room = zeros(max(256, *need), dtype=torch.uint8)
+
+    _parts = AttentionLayer._parts
+
+    def _grow(self, tokens):
+        """Pages for `tokens` new tokens; what shared pages hold, into the pages that take their place"""
+        B.lora_pages_resize(self.pages, self.wanted, tokens, self.granted, self.indptr, None, None, None, self.copies, self.room, self.room.numel())
+        B.lora_cache_copy(self.cache, len(self.copies), self.copies)
+
+    def _select(self, y, first=False):
+        """Logits of the rows' last tokens, and the best continuations: what the beams become, their tokens and scores.  first: one row a request"""
+        beams = 1 if first else self.beams
+        logits = torch.empty((len(y), self.vocab), dtype=torch.bfloat16, device=DEV)
+        B.lora_base_gemm(len(y), self.hidden, self.vocab, B.LORA_BF16, y, self.hidden, self.embedding, self.hidden, logits, self.vocab)
+        B.lora_beam_select(B.LORA_BF16, self.requests, beams, self.vocab, logits, self.vocab, self.score, None if first else self.token, self.end_token,
+                           self.beams, *self.best, self.room, self.room.numel())
+        self.logits = logits
+        score, parent, token = self.best
+        # (beams behind a request's first step all come of its one sequence)
+        self.parent.copy_(torch.where(parent >= 0, parent * self.beams, -1) if first else parent)
+        self.token.copy_(token)
+        self.score.copy_(score)
+        B.lora_pages_fork(self.pages, self.parent, self.room, self.room.numel())
+
+    def prompts(self, x, lengths, adapters):
+        """x [tokens, hidden], the requests' prompts one behind the other.  Afterwards every request has its first beams: token, score, parent"""
+        if max(lengths) > self.limit:
+            raise ValueError("a prompt is longer than the caches' limit")
+        self.adapters = [a for a in adapters for _ in range(self.beams)]
+        qkv = self.qkv(x, lengths, adapters)
+        q, k, v, ld = self._parts(qkv)
+        offsets = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+        plan = B.lora_attention_plan(offsets, None, self.heads, self.kv_heads, self.head_dim, B.LORA_BF16)
+        o = torch.empty((x.shape[0], self.heads * self.head_dim), dtype=torch.bfloat16, device=DEV)
+        B.lora_attention(plan, q, ld, k, ld, v, ld, o, o.shape[1], self.head_dim ** -0.5)
+        # (the requests that were here before are through: their pages come back in the same call)
+        self.wanted.zero_()
+        self._grow(0)
+        self.wanted.view(self.requests, self.beams)[:, 0] = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+        self._grow(x.shape[0])
+        B.lora_cache_append(self.cache, B.LORA_BF16, x.shape[0], max(lengths), self.indptr, k, ld, v, ld)
+        if self.chosen:
+            B.lora_cache_digest(self.cache, x.shape[0], max(lengths), self.indptr, self.bounds, self.steps)
+        y = self.out(o, lengths, adapters)
+        self.score.zero_()
+        self._select(y[torch.from_numpy(offsets[1:].astype(np.int64) - 1).to(DEV)].contiguous(), first=True)
+        torch.cuda.current_stream().synchronize()              # (the plan is given back when the work that uses it is through)
+        plan.destroy()
+
+    def step(self):
+        """The beams' last tokens through the layer, and the best of what may follow"""
+        S, H, D = self.requests * self.beams, self.heads, self.head_dim
+        torch.add(self.length, 1, out=self.wanted)
+        self._grow(S)
+        qkv = self.qkv(self.embedding[self.token.clamp_min(0)], [1] * S, self.adapters)
+        q, k, v, ld = self._parts(qkv)
+        B.lora_cache_append(self.cache, B.LORA_BF16, S, 1, self.indptr, k, ld, v, ld)
+        o = torch.zeros((S, H * D), dtype=torch.bfloat16, device=DEV)
+        if self.chosen:
+            B.lora_cache_digest(self.cache, S, 1, self.indptr, self.bounds, self.steps)
+            B.lora_cache_choose(self.cache, B.LORA_BF16, H, S, 1, self.indptr, q, ld, self.bounds, self.steps, self.chosen, min(1, self.chosen - 1), 1, self.list, self.room,
+                                self.room.numel())
+            B.lora_cache_attention_chosen(self.cache, B.LORA_BF16, H, S, 1, self.indptr, q, ld, o, H * D, D ** -0.5, self.chosen, self.list, self.room, self.room.numel())
+        else:
+            B.lora_cache_attention(self.cache, B.LORA_BF16, H, S, 1, self.indptr, q, ld, o, H * D, D ** -0.5, -1.0, self.room, self.room.numel())
+        self._select(self.out(o, [1] * S, self.adapters))
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser()
-    for name, value in (("requests", 32), ("prompt", 512), ("steps", 64), ("hidden", 4096), ("heads", 32), ("kv-heads", 8), ("limit", 600), ("budget", 512)):
+    for name, value in (("requests", 32), ("prompt", 512), ("steps", 64), ("hidden", 4096), ("heads", 32), ("kv-heads", 8), ("limit", 600), ("budget", 512),
+                        ("beams", 4), ("vocab", 32000), ("chosen", 0)):
         ap.add_argument("--" + name, type=int, default=value)
     args = ap.parse_args(argv)
     if args.hidden % args.heads:
@@ -190,6 +294,16 @@ def main(argv=None):
     evict = timed(layer.evict, 1)
     print(f"prompts of {sum(lengths)} tokens: {prompts:.0f} us a layer; {held / 1e6:.1f} MB of keys and values held")
     print(f"decode step of {args.requests} requests: {steps:.1f} us a layer, evictions at {args.limit} tokens among them; eviction: {evict:.0f} us")
+    if args.beams > 0:
+        del layer
+        search = BeamLayer(args.hidden, args.heads, args.kv_heads, args.hidden // args.heads, ranks, args.requests, args.beams, args.limit + args.steps + 2, args.vocab,
+                           chosen=args.chosen)
+        for _ in range(2):
+            prompts = timed(lambda: search.prompts(x, lengths, adapters), 1)
+        search.step()
+        steps = timed(search.step, args.steps)
+        print(f"beam search, {args.beams} beams, {args.vocab} tokens: prompts {prompts:.0f} us, a step {steps:.1f} us, layer, logits and selection; "
+              f"{int((search.users > 0).sum())} pages in use, named {int(search.users.sum())} times")
     return 0
 
 
