@@ -555,7 +555,7 @@ lora_status lora_pages_fork(const lora_pages* pages, const int32_t* parent, void
 /*
  * lora_cache_copy -- page copies[i][0] of one layer's cache to page copies[i][1], all heads, codes, words and accumulated weights (where the cache keeps
  * them); i < num_copies; copies: device.  Pairs with a page outside [0, num_pages), or of a page and itself, are passed over.
- * No page may be written twice, or written and read.
+ * No page may be written twice, or written and read.  (A cache without sequences: nothing is copied.)
  */
 lora_status lora_cache_copy(const lora_cache* cache, int32_t num_copies, const int32_t* copies, void* hip_stream);
 
@@ -590,7 +590,8 @@ lora_status lora_beam_select(int32_t dtype, int32_t num_groups, int32_t beams, i
  *     step = fp32(greatest |x| * fp32(1/127)), 0 if below 2^-100
  *     upper[d] = min(127, ceil(max_t x[t][d] / step)),  lower[d] = max(-127, floor(min_t x[t][d] / step))     (0 where step is 0)
  * bounds: device, [num_pages][num_kv_heads][2][DP] int8, 16-byte aligned: upper, then lower, DP as in a page; steps: device, [num_pages][num_kv_heads] fp32.
- * A page with NaN among its tokens, or a value past 32 bits, has NaN for its step.
+ * A page with NaN among its tokens, or a value past 32 bits, has NaN for its step.  Sequences that share such a page have to hold as much of
+ * it (pages that tokens are appended to are of one sequence, and full ones are).  bounds and steps must not share memory with the cache's pages.
  */
 lora_status lora_cache_digest(const lora_cache* cache, int32_t num_tokens, int32_t max_new, const int32_t* d_indptr,
                               int8_t* bounds, float* steps, void* hip_stream);

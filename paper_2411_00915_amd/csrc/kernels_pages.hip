@@ -556,7 +556,7 @@ hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream)
         LORA_LAUNCH(LORA_K_PAGES_DECIDE, (pages_decide_kernel<1, true>), dim3(1), dim3(kThreads), 0, stream, a);
         return hipGetLastError();
     }
-    const int entries = (p.table_stride + kChunk - 1) / kChunk, looks = free_parts(p.num_pages) > (p.num_seqs + 255) / 256 ? free_parts(p.num_pages) : (p.num_seqs + 255) / 256;
+    const int entries = p.table_stride < kChunk ? 1 : (p.table_stride + kChunk - 1) / kChunk, looks = free_parts(p.num_pages) > (p.num_seqs + 255) / 256 ? free_parts(p.num_pages) : (p.num_seqs + 255) / 256;
     auto blocks = [&](int64_t chunks) { return dim3((uint32_t)((p.num_seqs * chunks + 3) / 4)); };
     LORA_LAUNCH(LORA_K_PAGES_GIVE_BACK, pages_give_back_kernel, blocks(entries), dim3(256), 0, stream, a, entries);
     hipError_t e = hipGetLastError();

@@ -196,6 +196,29 @@ def test_ended_beams_stay(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("groups,vocab", [(2, 9000), (40, 65536 + 77)])
+@pytest.mark.parametrize("order", ["up", "down", "close", "close up", "steps", "late", "few"])
+@pytest.mark.parametrize("out", [5, 64])
+def test_orders_of_logits_that_bounds_do_not_help(dtype, groups, vocab, order, out):
+    """Growing and falling along the row; within one step of 16 bits of each other; equal in long runs; the first half masked; all but a few masked"""
+    rng, beams = np.random.default_rng(out), 4
+    rows, i = groups * beams, np.arange(vocab)
+    if order in ("up", "down"):
+        x = np.tile(i * 1e-3 * (1 if order == "up" else -1), (rows, 1)) + 0.3 * rng.random((rows, 1))
+    elif order.startswith("close"):
+        x = 1 + (i % 8191 if order == "close up" else rng.integers(0, 8191, (rows, vocab))) * 2.0 ** -21 + 0 * rng.random((rows, 1))
+    elif order == "steps":
+        x = np.floor(i / 3000) % 5 + 0 * rng.random((rows, 1))
+    else:
+        x = logits(rng, rows, vocab)
+        x[:, :vocab // 2] = -np.inf
+        if order == "few":
+            x[:, rng.permutation(vocab)[:vocab - 70]] = -np.inf
+    check(np.asarray(x, np.float32), scores(rng, rows), None, 0, beams, out, dtype)
+
+
+@gpu
 def test_the_largest_vocabulary():
     vocab = 1 << 24
     gen = torch.Generator(device=DEV)

@@ -222,6 +222,17 @@ def test_more_new_pages_than_are_kept_near():
 
 
 @gpu
+@pytest.mark.parametrize("S", [5, 1500])
+def test_a_table_without_entries_and_a_pool_without_pages(S):
+    st = State(S, 0, 3, 32)
+    st.resize(np.arange(S) % 2)                             # (nothing may be longer than 0)
+    st.fork(np.arange(S)[::-1])
+    st = State(S, 2, 0, 32)
+    st.resize(np.arange(S) % 40)
+    st.fork(np.arange(S)[::-1])
+
+
+@gpu
 def test_what_is_not_wanted_is_left_out():
     st = State(3, 4, 20, 32)
     wanted, copies = torch.tensor([40, 0, 70], dtype=torch.int32, device=DEV), torch.zeros(6, dtype=torch.int32, device=DEV)
