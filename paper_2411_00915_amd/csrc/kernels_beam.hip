@@ -108,8 +108,7 @@ constexpr float LOG2E = 1.44269504088896340736f;
 struct wave_state {
     beam_entry* held;          // [kHeld]; the first `summed` are in `sum` already
     int count, summed;
-    float bound;               // what is below it is no candidate; of what is equal, what is not before bound_token
-    int bound_token;
+    float bound;               // what is below it is no candidate
     double sum;                // of exp(logit - ref), this lane's part
     double ref;                // about the bound, or above it
     // exp(x - ref) is exp2(x LOG2E - less_of), as ref is less_of / LOG2E; but past 1e9, where less_of is too coarse, exp2((x - less_of) LOG2E)
@@ -146,7 +145,29 @@ __device__ __forceinline__ void add_held(wave_state& s, int lane)
     s.summed = s.count;
 }
 
-// LDS is full: the best num_out of the candidates are kept, and the last of them is the bound
+// numbers from their order
+__device__ __forceinline__ float number_of(uint32_t u) { return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u); }
+
+// (NaN and +inf raise nothing)
+__device__ __forceinline__ void raise_bound(wave_state& s, float to)
+{
+    if (to > s.bound && to < INFINITY) {
+        s.bound = to;
+        raise_ref(s, to);
+    }
+}
+
+// above a number; what is below the bound is then not above it, so that it is the reference of the exponentials
+__device__ __forceinline__ void raise_above(wave_state& s, float last)
+{
+    const float to = number_of(order_of(last) + 1);
+    if (to > s.bound && to < INFINITY) {
+        s.bound = to;
+        raise_ref(s, last);
+    }
+}
+
+// LDS is full: the best num_out of the candidates are kept.  What comes later has higher tokens, so it has to be above the last of them.
 __device__ __forceinline__ void keep_best(wave_state& s, int M, int lane)
 {
     wave_sync();
@@ -168,43 +189,50 @@ __device__ __forceinline__ void keep_best(wave_state& s, int M, int lane)
     for (int n = 0; n < kHeld / 64; ++n)
         if (rank[n] < M) s.held[rank[n]] = mine[n];
     wave_sync();
-    if (s.count >= M) {
-        const beam_entry last = s.held[M - 1];
-        s.bound = last.logit;
-        s.bound_token = last.token;
-        raise_ref(s, s.bound);
-    }
+    if (s.count >= M) raise_above(s, s.held[M - 1].logit);
     s.count = s.summed = min(s.count, M);
 }
 
-// the number whose upper 16 bits in the order of numbers these are, the rest 0; NaN where there is none
-__device__ __forceinline__ float number_of(uint32_t upper)
+// The same of four numbers a lane
+__device__ __forceinline__ uint32_t reached_of_four(const uint32_t* mine, int wanted)
 {
-    const uint32_t u = upper << 16;
-    return __uint_as_float(u >> 31 ? u & 0x7fffffffu : ~u);
-}
-__device__ __forceinline__ void raise_bound(wave_state& s, float to)
-{
-    if (to > s.bound && to < INFINITY) {
-        s.bound = to;
-        s.bound_token = 0x7fffffff;
-        raise_ref(s, to);
+    uint32_t bound = 0;
+#pragma unroll 1
+    for (int bit = 15; bit >= 0; --bit) {
+        const uint32_t t = bound | 1u << bit;
+        int count = 0;
+#pragma unroll
+        for (int n = 0; n < kHeld / 64; ++n) count += __popcll(__ballot(mine[n] >= t));
+        if (count >= wanted) bound = t;
     }
+    return bound;
 }
 
-// Raises the bound by up to 64 candidates: num_out of them are not below it, or in every wavefront its share (`bounds`: what they have
-// found so far; it only rises, so an old number does as well)
-__device__ __forceinline__ void raise_by_held(wave_state& s, int M, int wave, int lane, volatile uint32_t* bounds)
+// Raises the bound by the candidates: num_out of them are not below it, or in every wavefront its share (`bounds`: what they have
+// found so far; it only rises, so an old number does as well).  Returns the upper 16 bits of what it found.
+__device__ __forceinline__ uint32_t raise_by_held(wave_state& s, int M, int wave, int lane, volatile uint32_t* bounds)
 {
     wave_sync();
-    const uint32_t mine = lane < s.count ? order_of(s.held[lane].logit) >> 16 : 0u;
-    const uint32_t share = reached<16>(mine, (M + kWaves - 1) / kWaves);
-    if (lane == 0 && share > bounds[wave]) bounds[wave] = share;
-    uint32_t least = bounds[0];
+    const int part = (M + kWaves - 1) / kWaves;
+    uint32_t share, least;
+    if (s.count <= 64) {
+        const uint32_t mine = lane < s.count ? order_of(s.held[lane].logit) >> 16 : 0u;
+        share = reached<16>(mine, part);
+        least = reached<16>(mine, M);
+    } else {
+        uint32_t mine[kHeld / 64];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) least = min(least, (uint32_t)bounds[w]);
-    least = max(least, reached<16>(mine, M));
-    raise_bound(s, number_of((uint32_t)__builtin_amdgcn_readfirstlane(least)));
+        for (int n = 0; n < kHeld / 64; ++n) mine[n] = n * 64 + lane < s.count ? order_of(s.held[n * 64 + lane].logit) >> 16 : 0u;
+        share = reached_of_four(mine, part);
+        least = reached_of_four(mine, M);
+    }
+    if (lane == 0 && share > bounds[wave]) bounds[wave] = share;
+    uint32_t all = bounds[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) all = min(all, (uint32_t)bounds[w]);
+    least = (uint32_t)__builtin_amdgcn_readfirstlane(max(least, all));
+    raise_bound(s, number_of(least << 16));
+    return least;
 }
 
 template <typename T, int V>
@@ -215,12 +243,12 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
     __shared__ double refs[kWaves];
     __shared__ uint32_t bounds[kWaves];
     __shared__ int counts[kWaves];
-    constexpr int UNIT = BEAM_THREADS * V, PART = 64 * V, EACH = lane_words<T, V>::EACH, ANY = 0x7fffffff;
+    constexpr int UNIT = BEAM_THREADS * V, PART = 64 * V, EACH = lane_words<T, V>::EACH;
     const int split = blockIdx.x % a.splits, row = blockIdx.x / a.splits, M = a.num_out;
     if (a.last_token && a.end_token >= 0 && a.last_token[row] == a.end_token) return;         // (beam_join_kernel does not look at it)
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const T* const logits = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
-    wave_state s{held[wave], 0, 0, -3.402823466e+38f, ANY, 0.0, -INFINITY, -3.402823466e+38f, true};      // (-inf is not chosen; NaN: the row is not)
+    wave_state s{held[wave], 0, 0, -3.402823466e+38f, 0.0, -INFINITY, -3.402823466e+38f, true};      // (-inf is not chosen; NaN: the row is not)
     const int begin = split * a.chunk, end = min(begin + a.chunk, a.vocab);
     // The lane's first token of a unit.  A part that the row's end cuts is loaded from so far before its place, and what it has in common
     // with the part before it is masked.
@@ -262,9 +290,9 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
             uint32_t all = bounds[0];
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) all = min(all, bounds[w]);
-            raise_bound(s, number_of(max(least, all)));
+            raise_bound(s, number_of(max(least, all) << 16));
         } else if (__popcll(__ballot(top >= s.bound)) > M)
-            raise_bound(s, number_of(reached<16>(order_of(top) >> 16, M)));
+            raise_bound(s, number_of(reached<16>(order_of(top) >> 16, M) << 16));
         // what is not below the bound goes to LDS, and is as good as masked here
         const uint64_t lanes = __ballot(top >= s.bound);
         if (lanes != 0) {
@@ -273,6 +301,7 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
                 hits = 0;
 #pragma unroll
                 for (int i = 0; i < V; ++i) hits += __popcll(__ballot(x[i] >= s.bound));
+                if (s.count + hits > kHeld && s.count > kHeld - kMost) keep_best(s, M, lane);
             }
             if (s.count + hits <= kHeld) {
 #pragma unroll
@@ -285,24 +314,56 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
                         x[i] = is ? -INFINITY : x[i];
                     }
                 }
-                if (s.count >= look && s.count <= 64) {
+                if (s.count >= look) {
                     raise_by_held(s, M, wave, lane, bounds);
-                    look = s.count + 8;
+                    look = s.count + max(8, M / 2);
                 }
             } else {
-                // More than LDS holds (many equal ones): once more, 64 at a time
+                // More than LDS holds (many equal ones): the best num_out of these tokens alone.  All above the num_out-th largest number, and
+                // of those that are equal to it the first few; no later token that is equal to it will do.  (There are more than num_out.)
+                uint32_t limit = 0;
 #pragma unroll 1
-                for (int i = 0; i < V; ++i) {
-                    if (s.count > kHeld - 64) keep_best(s, M, lane);
-                    const int token = token_of(i);
-                    const float y = token < a.vocab && token >= first ? elem<T>::load(logits + token) : -INFINITY;
-                    const bool is = y > s.bound || (y == s.bound && token < s.bound_token);
-                    const uint64_t mask = __ballot(is);
-                    if (is) s.held[lanes_before(mask, s.count)] = beam_entry{y, token};
-                    s.count += __popcll(mask);
-                    s.sum += is ? 0.0 : (double)(s.far ? s.fast<true>(y) : s.fast<false>(y));
+                for (int bit = 31; bit >= 0; --bit) {
+                    const float next = number_of(limit | 1u << bit);
+                    int count = 0;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) count += __popcll(__ballot(x[i] >= next));
+                    if (count >= M) limit |= 1u << bit;
                 }
-                continue;
+                const float last = number_of(limit);
+                int left = M;
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const bool is = x[i] > last;
+                    const uint64_t mask = __ballot(is);
+                    if (is) s.held[lanes_before(mask, s.count)] = beam_entry{x[i], token_of(i)};
+                    s.count += __popcll(mask);
+                    left -= __popcll(mask);
+                    x[i] = is ? -INFINITY : x[i];
+                }
+#pragma unroll
+                for (int i = 0; i < V; i += EACH) {                // tokens go up along a lane's EACH, then along the lanes
+                    int place = 0, all = 0;
+#pragma unroll
+                    for (int e = i; e < i + EACH; ++e) {
+                        const uint64_t mask = __ballot(x[e] == last);
+                        place = lanes_before(mask, place);
+                        all += __popcll(mask);
+                    }
+#pragma unroll
+                    for (int e = i; e < i + EACH; ++e)
+                        if (x[e] == last) {
+                            if (place < left) {
+                                s.held[s.count + place] = beam_entry{x[e], token_of(e)};
+                                x[e] = -INFINITY;
+                            }
+                            ++place;
+                        }
+                    const int taken = min(all, left);
+                    s.count += taken;
+                    left -= taken;
+                }
+                raise_above(s, last);
             }
         }
         // the exponentials of all else: eight in 32 bits, their sums in 64 (NaN is among these, and makes the sum NaN)
@@ -320,7 +381,7 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
     }
     wave_sync();
     add_held(s, lane);
-    if (s.count <= 64 && s.count > 0) raise_by_held(s, M, wave, lane, bounds);
+    uint32_t limit = s.count > 0 ? raise_by_held(s, M, wave, lane, bounds) : 0u;
     double sum = s.sum;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
@@ -330,18 +391,21 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
     }
     __syncthreads();
     // What is left of the candidates, now that all wavefronts' bounds are there, to the front; then the workgroup's best in order
-    if (s.count > 0 && s.count <= 64) {
-        uint32_t all = bounds[0];
+    uint32_t shares = bounds[0];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) all = min(all, bounds[w]);
-        raise_bound(s, number_of(all));
-        const beam_entry e = s.held[min(lane, s.count - 1)];
-        const bool is = lane < s.count && e.logit >= s.bound;
+    for (int w = 1; w < kWaves; ++w) shares = min(shares, bounds[w]);
+    limit = max(limit, shares) << 16;                              // (not the bound, which may be above what is kept of equal ones)
+    int kept = 0;
+    for (int n = 0; n < s.count; n += 64) {                        // (what is moved goes no further back than it was)
+        const beam_entry e = s.held[min(n + lane, s.count - 1)];
+        const bool is = n + lane < s.count && order_of(e.logit) >= limit;
         const uint64_t mask = __ballot(is);
         wave_sync();
-        if (is) s.held[lanes_before(mask, 0)] = e;
-        s.count = __popcll(mask);
+        if (is) s.held[lanes_before(mask, kept)] = e;
+        kept += __popcll(mask);
+        wave_sync();
     }
+    s.count = kept;
     if (lane == 0) counts[wave] = s.count;
     __syncthreads();
     beam_entry* const out = a.entries + ((int64_t)row * a.splits + split) * M;
