@@ -418,9 +418,16 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
         const beam_entry e = held[w][at];
         int rank = 0;
         for (int v = 0; v < kWaves; ++v) {
-            const int there = counts[v];
-#pragma unroll 4
-            for (int j = 0; j < there; ++j) {
+            const int there = __builtin_amdgcn_readfirstlane(counts[v]);
+            int j = 0;
+            for (; j + 8 <= there; j += 8) {                       // (eight on their way together)
+                beam_entry o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = held[v][j + k];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) rank += before(o[k].logit, o[k].token, e.logit, e.token);
+            }
+            for (; j < there; ++j) {
                 const beam_entry o = held[v][j];
                 rank += before(o.logit, o.token, e.logit, e.token);
             }
@@ -537,7 +544,7 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(beam_args a)
     for (int i = 0; i < KEPT; ++i) collect(kept[i]);
     for (int64_t base = KEPT * kJoinThreads; base < all; base += kJoinThreads) collect(base + tid < all ? at(base + tid) : candidate{0, 0});
     __syncthreads();
-    const int count = counter;
+    const int count = __builtin_amdgcn_readfirstlane(counter);
     if (count <= kJoinHeld) {
 #pragma unroll
         for (int i = 0; i < kJoinHeld / kJoinThreads; ++i) {
@@ -545,8 +552,15 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(beam_args a)
             if (n >= count) break;
             const candidate c = pool[n];
             int rank = 0;
-#pragma unroll 4
-            for (int j = 0; j < count; ++j) rank += better(pool[j], c);
+            int j = 0;
+            for (; j + 8 <= count; j += 8) {                       // (eight on their way together)
+                candidate o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = pool[j + k];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) rank += better(o[k], c);
+            }
+            for (; j < count; ++j) rank += better(pool[j], c);
             if (rank < M) best[rank] = c;
         }
     } else {
