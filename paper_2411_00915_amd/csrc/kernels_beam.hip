@@ -1,13 +1,21 @@
 // Beam search's selection: the best continuations of a request's beams over the vocabulary (include/lora_abi.h, BEAMS).
 //
-// One pass over the logits.  A row's best num_out are enough, and of any part of a row its own best num_out: a wavefront keeps its part in
-// registers, adds up exp(logit - its largest), and finds its best by a bound, the num_out-th largest of its lanes' largest logits:
-// what is not below it are a few more than num_out, which are put in order by counting.  A second launch joins the parts: a row's log sum, and the
-// request's best of all that is left.
+// One pass over the logits.  A row's best num_out are enough, and of any part of a row its own best num_out.  A workgroup goes through its
+// part a unit of 4096 tokens at a time, 16 a lane in registers, the next unit's loads on their way.  It keeps a bound that num_out tokens
+// are known not to be below: at first the num_out-th largest of the lanes' largest logits (16 ballots find it), later of the candidates.
+// What is not below the bound goes to LDS, in the mean 33 of a wavefront's 16384 tokens for 16 candidates; everything else is in the sum
+// of exponentials and nowhere else: four instructions a token (fused multiply-add, exp2, sum, half a maximum) and one that takes it out of its
+// word.  Equal logits by the hundred, which no bound parts, have a path of their own: the num_out-th largest of a unit bit by bit, and
+// the first of those that are equal to it.  A second launch joins the parts: a row's log sum, and the request's best of what is left, again
+// by a bound over all threads and by counting.
 //
 // A row's candidates are in the logits' own order whatever is subtracted, but those of different beams meet within 1e-7 of each other
-// now and then, so the sums are 64 bits, and an exponential's argument has its rounding carried on (exp2 of the product's upper part,
-// times 1 + its lower part): what is left of an error is the hardware's exp2, one step of 32 bits, at random.
+// now and then.  So the candidates' exponentials, which are the largest, are 64 bits, and so are the sums; the others are the hardware's
+// exp2 of a product with log2(e) that is rounded once, eight of them added in 32 bits.  Measured: scores within 3e-8 of 64 bits.
+//
+// 64 requests of 8 beams over 131072 tokens, 16 candidates: 38 us and 7.4, 134 MB at 3.5 TB/s (vector instructions busy in 55 %; with all of
+// a part's 8192 tokens in registers and its own bound each 54 and 62; a bound that does not rise 320); four beams over 32000: 7.4 and 6.8,
+// the chain load -> bound -> exponentials -> candidates -> join.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

@@ -3,6 +3,10 @@
 // A key of the page has upper[d] >= k[d] >= lower[d], so q . k <= sum max(q[d], 0) upper[d] + min(q[d], 0) lower[d]: what the choice
 // orders pages by.  Bounds and queries are whole numbers of 8 bits, so the sums are exact whatever their order, and what follows is
 // one rounding each: the choice is the definition's, page by page, which a sum in floating point would not be.
+//
+// Bounds of 8192 tokens' pages, 8 heads of 128: 10 us, of which the trips offsets -> length -> table -> codes are most.  The choice for 8
+// requests of 8000 tokens, 8 kv heads: 6.8 us (lengths 0.6, table and bounds 2.4, products 1, threshold 1.8, writing 0.8); 32 of 16384,
+// 17 MB of bounds, 11; four tokens over 131072, in pieces: 7 and 7.4 (in one launch 32: a compute unit reads 512 KB in 21 us).
 #include <hip/hip_runtime.h>
 
 #include "cache_format.h"
@@ -15,7 +19,7 @@ typedef __attribute__((__vector_size__(4 * sizeof(int)))) int int4v;
 
 // ---------------------------------------------------------------------------
 // Bounds: a wavefront a page of one head.  A lane has 8 dims of every so-manieth token (DP/8 lanes a token), the lanes of the same dims
-// meet by exchange.  Bound by the instructions that take the codes apart.
+// meet by exchange.
 __device__ __forceinline__ float max_of_wave(float x)
 {
 #pragma unroll
@@ -117,8 +121,9 @@ __global__ __launch_bounds__(256) void cache_digest_kernel(cache_args c, int8_t*
 // ---------------------------------------------------------------------------
 // The choice: a workgroup a token and kv head.  Its queries' codes, parted by sign, are rows of a product with the pages' bounds as columns, 16
 // queries and 16 pages at a time, on the matrix cores in whole numbers; a column's greatest goes to LDS as a whole number in the
-// order of the scores (or to the workspace, where there are more pages than LDS holds).  Then the number of the last page chosen
-// is found 8 bits at a time, and the pages are written in order.
+// order of the scores (or to the workspace, where there are more pages than LDS holds, or several workgroups share a token's pages).  Then
+// the last page chosen is found, by one wavefront bit by bit (up to 256 pages: 1.8 us) or by all by bins (2.7; bit by bit 5.5 for 400), and the
+// pages are written in order.
 
 // scores in their order as whole numbers above 0; NaN above them, what is chosen in any case above all
 constexpr uint32_t kForced = 0xffffffffu, kNan = 0xfffffffeu;
@@ -134,10 +139,11 @@ __device__ __forceinline__ float greater(float x, float y) { return y > x || y !
 
 constexpr int kThreads = LORA_CACHE_CHOOSE_THREADS, kWaves = kThreads / 64;
 
-// 16 codes of a page's bounds, and what makes a score of them, for 16 pages a wavefront at a time, ROUNDS of them on their way together
+// 16 codes of a page's bounds, and what makes a score of them, for 16 pages a wavefront at a time, ROUNDS of them on their way together (four: 0.8 us
+// more for 125 pages, whose table entries are then asked for in vain)
 template <int DP>
 struct bounds_block {
-    static constexpr int NS = 2 * DP / 64, ROUNDS = DP == 256 ? 2 : 4, PAGES = ROUNDS * kWaves * 16;
+    static constexpr int NS = 2 * DP / 64, ROUNDS = 2, PAGES = ROUNDS * kWaves * 16;
     int4v b[ROUNDS][NS];
     float step[ROUNDS];
     bool there[ROUNDS];
@@ -369,11 +375,8 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void cache_choose_kern
         uint32_t threshold = 1;
         int equal = budget;                                    // (all that are there)
         if (!all) {
-            if (pages <= 1024) {
-                if (wave == 0) {
-                    if (pages <= 256) threshold_by_bits<4>(keys, pages, budget, lane, found);
-                    else threshold_by_bits<16>(keys, pages, budget, lane, found);
-                }
+            if (pages <= 256) {
+                if (wave == 0) threshold_by_bits<4>(keys, pages, budget, lane, found);
                 __syncthreads();
                 threshold = found[0];
                 equal = (int)found[1];
