@@ -1,11 +1,12 @@
 // Pages given out and taken back on the device, and sequences that become others' (include/lora_abi.h, PAGES).
 //
 // A call is a few thousand whole numbers, so it is bound by its chain of dependent trips to memory: wanted length -> table ->
-// users of the page written next -> free pages -> table -> slots.  Where the tables are small, one workgroup does all of it with barriers between
-// the steps, and a thread its sequence's tokens where none has more than four (16 requests a token each: 5 us, of which 0.9 a prefix over the
-// workgroup).  Else pages are given back by one launch, a second looks for shared pages and for the free ones of every 4096, one workgroup decides,
-// and a fourth launch writes tables and slots down (4096 requests, 287000 new tokens: 4, 4, 13 and 8 us; with one workgroup that looks
-// for the free pages too, 52 in place of 13 and 4).
+// users of the page written next -> free pages -> table -> slots.  Where the tables are small, one workgroup does all of it with barriers
+// between the steps, and a thread its sequence's tokens where none has more than four (16 requests a token each: 5 us, of which 0.9 a prefix
+// over the workgroup; 128 prompts, 8192 tokens: 10 us, and 14.5 with a lane's four tokens one behind the other and divisions by the page's size).
+// Else pages are given back by one launch, a second looks for shared pages and for the free ones of every 4096, one workgroup decides, and a
+// fourth launch writes tables and slots down (4096 requests, 287000 new tokens: 4, 4, 11 and 8 us; with one workgroup that looks for the free
+// pages too, 52 in place of 11 and 4).
 // What the atomics do (counts of users, the greatest of the keys of those that share a page) does not depend on their order.
 #include <hip/hip_runtime.h>
 
@@ -33,7 +34,14 @@ __device__ __forceinline__ int lanes_before(uint64_t mask, int n)
 #endif
 }
 
-__device__ __forceinline__ int pages_of(const pages_args& p, int tokens) { return (int)(((int64_t)tokens + p.page_tokens - 1) / p.page_tokens); }
+// the page that a place is in (pages are mostly powers of two), and pages that hold so many tokens (at most 2^30)
+__device__ __forceinline__ int page_number(const pages_args& p, int at)
+{
+    return (p.page_tokens & (p.page_tokens - 1)) == 0 ? at >> __builtin_ctz(p.page_tokens) : at / p.page_tokens;
+}
+__device__ __forceinline__ int pages_of(const pages_args& p, int tokens) { return page_number(p, tokens + p.page_tokens - 1); }
+// of the tokens in the page of the last: 0 where it is full
+__device__ __forceinline__ int tokens_inside(const pages_args& p, int tokens) { return tokens - page_number(p, tokens) * p.page_tokens; }
 __device__ __forceinline__ int length_at(const pages_args& p, int s) { return min(max(p.length[s], 0), p.max_length); }
 __device__ __forceinline__ bool known(const pages_args& p, int page) { return page >= 0 && page < p.num_pages; }
 
@@ -155,7 +163,7 @@ __device__ __forceinline__ void write_token(const resize_args& a, int row, int s
 {
     if (a.token_seq) a.token_seq[row] = s;
     if (a.token_position) a.token_position[row] = position;
-    if (a.token_slot) a.token_slot[row] = known(a.p, page) ? (int64_t)page * a.p.page_tokens + position % a.p.page_tokens : -1;
+    if (a.token_slot) a.token_slot[row] = known(a.p, page) ? (int64_t)page * a.p.page_tokens + tokens_inside(a.p, position) : -1;
 }
 
 // What a sequence has and wants, and the page that it would write next where that holds tokens already and has other users (else -1)
@@ -172,8 +180,8 @@ __device__ __forceinline__ wish wish_of(const resize_args& a, int s)
 }
 __device__ __forceinline__ void look_at_page(const pages_args& p, int s, wish& w)
 {
-    if (w.to <= w.from || w.from % p.page_tokens == 0) return;
-    w.page = p.page_table[(int64_t)s * p.table_stride + w.from / p.page_tokens];
+    if (w.to <= w.from || tokens_inside(p, w.from) == 0) return;
+    w.page = p.page_table[(int64_t)s * p.table_stride + page_number(p, w.from)];
     if (known(p, w.page) && p.users[w.page] > 1) w.last = w.page;
 }
 
@@ -226,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
         for (int r = 0; r < R; ++r)
             if (w[r].last >= 0) atomicSub(p.users + w[r].last, 1);
         __syncthreads();
-        auto key_of = [&](int r) { return -1 - (w[r].from % p.page_tokens * LORA_PAGES_MAX_SEQS + s0 + r); };
+        auto key_of = [&](int r) { return -1 - (tokens_inside(p, w[r].from) * LORA_PAGES_MAX_SEQS + s0 + r); };
         // (read from the caches' common level: other wavefronts' atomics are there)
         auto users_of = [&](int r) { return __hip_atomic_load(p.users + w[r].last, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
 #pragma unroll
@@ -311,7 +319,7 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
         if (copy) {
             target = ALL ? list[first[r]] : free_page(a, first[r]);
             p.users[target] = 1;
-            p.page_table[(int64_t)s * p.table_stride + w[r].from / p.page_tokens] = target;
+            p.page_table[(int64_t)s * p.table_stride + page_number(p, w[r].from)] = target;
         } else if (w[r].last >= 0)
             atomicAdd(p.users + w[r].last, 1);                 // it stays
         a.copies[2 * (int64_t)s] = copy ? w[r].last : -1;
@@ -333,7 +341,7 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
                 }
                 for (int i = row; i < min(after, a.num_tokens); ++i) {
                     const int position = w[0].from + i - row;
-                    write_token(a, i, s, position, position / p.page_tokens >= have ? fresh : copy ? target : w[0].page);
+                    write_token(a, i, s, position, page_number(p, position) >= have ? fresh : copy ? target : w[0].page);
                 }
             }
         }
@@ -346,16 +354,11 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
         if (!more) return;
         __syncthreads();
         // new entries: the sequence of each new page, by halves
-        const int given = (int)(total < found ? total : found);
-        auto search = [&](int n, auto start) { // the last sequence that starts at or before n (steps alike for all, so that several searches run side by side)
-            int at = 0;
-#pragma unroll
-            for (int step = kThreads / 2; step > 0; step >>= 1)
-                if (at + step < S && start(at + step) <= n) at += step;
-            return at;
-        };
+        const int given = (int)(total < found ? total : found), widest = S > 1 ? 1 << (31 - __builtin_clz(S - 1)) : 0;
         for (int n = tid; n < given; n += kThreads) {
-            const int s = search(n, [&](int i) { return grants[i].first & INT_MAX; });
+            int s = 0;                                         // the last sequence whose pages start at or before n
+            for (int step = widest; step > 0; step >>= 1)
+                if (s + step < S && (grants[s + step].first & INT_MAX) <= n) s += step;
             const page_grant g = grants[s];
             const int i = n - (g.first & INT_MAX) - (g.first < 0), e = pages_of(p, g.from) + i;
             if (i < 0 || g.to <= g.from || e >= pages_of(p, g.to)) continue;           // (a copy; pages that would not have been enough)
@@ -369,13 +372,17 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
         for (int n0 = tid; n0 < most; n0 += TOGETHER * kThreads) {
             int s[TOGETHER], page[TOGETHER], position[TOGETHER];
 #pragma unroll
-            for (int k = 0; k < TOGETHER; ++k) {
-                const int n = min(n0 + k * kThreads, most - 1);
-                s[k] = search(n, [&](int i) { return grants[i].row; });
-                position[k] = grants[s[k]].from + n - grants[s[k]].row;
-            }
+            for (int k = 0; k < TOGETHER; ++k) s[k] = 0;
+            for (int step = widest; step > 0; step >>= 1)
 #pragma unroll
-            for (int k = 0; k < TOGETHER; ++k) page[k] = p.page_table[(int64_t)s[k] * p.table_stride + position[k] / p.page_tokens];
+                for (int k = 0; k < TOGETHER; ++k) {           // (searches side by side)
+                    const int next = s[k] + step;
+                    if (next < S && grants[next].row <= n0 + k * kThreads) s[k] = next;
+                }
+#pragma unroll
+            for (int k = 0; k < TOGETHER; ++k) position[k] = min(grants[s[k]].from + n0 + k * kThreads - grants[s[k]].row, p.max_length - 1);
+#pragma unroll
+            for (int k = 0; k < TOGETHER; ++k) page[k] = p.page_table[(int64_t)s[k] * p.table_stride + page_number(p, position[k])];
 #pragma unroll
             for (int k = 0; k < TOGETHER; ++k)
                 if (n0 + k * kThreads < most) write_token(a, n0 + k * kThreads, s[k], position[k], page[k]);
@@ -452,7 +459,7 @@ __global__ __launch_bounds__(256) void pages_write_kernel(resize_args a, int chu
     if (s >= p.num_seqs) return;
     const page_grant g = a.grants[s];
     if (g.to <= g.from) return;
-    const int have = pages_of(p, g.from), want = pages_of(p, g.to), P = p.page_tokens, first = (g.first & INT_MAX) + (g.first < 0);
+    const int have = pages_of(p, g.from), want = pages_of(p, g.to), first = (g.first & INT_MAX) + (g.first < 0);
     int32_t* const table = p.page_table + (int64_t)s * p.table_stride;
     for (int e = have + chunk * kChunk + lane; e < min(want, have + (chunk + 1) * kChunk); e += 64) {
         const int page = free_page(a, first + e - have);
@@ -462,10 +469,10 @@ __global__ __launch_bounds__(256) void pages_write_kernel(resize_args a, int chu
     const int begin = chunk * kChunk, end = min(min(g.to - g.from, begin + kChunk), a.num_tokens - g.row);
     if ((!a.token_seq && !a.token_position && !a.token_slot) || begin >= end) return;
     // the pages that these tokens are in, a lane one (1024 tokens lie in 33 at most)
-    const int first_number = (g.from + begin) / P, mine = first_number + lane;
+    const int first_number = page_number(p, g.from + begin), mine = first_number + lane;
     const int held = mine >= want ? -1 : mine < have ? table[mine] : free_page(a, first + mine - have);
     for (int i = begin + lane; i < begin + (end - begin + 63) / 64 * 64; i += 64) {
-        const int position = g.from + i, page = __shfl(held, position / P - first_number, 64);
+        const int position = g.from + i, page = __shfl(held, page_number(p, position) - first_number, 64);
         if (i < end) write_token(a, g.row + i, s, position, page);
     }
 }
