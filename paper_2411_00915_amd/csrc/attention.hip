@@ -319,11 +319,14 @@ extern "C" lora_status lora_cache_choose(const lora_cache* c, int32_t dtype, int
     if (st != LORA_OK) return st;
     const memory_rows out(chosen, 1, 1, (int64_t)num_tokens * c->num_kv_heads * budget, 4);
     const int64_t heads = c->num_pages * c->num_kv_heads;
-    if (share_bytes(out, memory_rows(q, num_tokens, ldq, row, elem_bytes(dtype))) || share_bytes(out, c) || share_bytes(out, memory_rows(steps, 1, 1, heads, 4)) ||
-        share_bytes(out, memory_rows(bounds, 1, 1, heads * 2 * padded_head_dim(c->head_dim), 1)))
-        return LORA_ERR_INVALID_ARG;
+    auto reads = [&](const memory_rows& x) {
+        return share_bytes(x, memory_rows(q, num_tokens, ldq, row, elem_bytes(dtype))) || share_bytes(x, c) || share_bytes(x, memory_rows(steps, 1, 1, heads, 4)) ||
+               share_bytes(x, memory_rows(bounds, 1, 1, heads * 2 * padded_head_dim(c->head_dim), 1));
+    };
+    if (reads(out)) return LORA_ERR_INVALID_ARG;
     const size_t bytes = choose_bytes(c, num_tokens);
     if (bytes > 0 && (!workspace || workspace_bytes < bytes || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
+    if (const memory_rows room(workspace, 1, 1, (int64_t)bytes, 1); bytes > 0 && (share_bytes(room, out) || reads(room))) return LORA_ERR_INVALID_ARG;
     choose_args a{};
     a.c = args_of(c, num_tokens, max_new, d_indptr);
     a.q = q;
@@ -373,11 +376,14 @@ extern "C" lora_status lora_cache_attention_chosen(const lora_cache* c, int32_t 
     const size_t e = elem_bytes(dtype);
     if (!q || !o || ldq < row || ldo < row || misaligned(q, e) || misaligned(o, e) || !chosen || misaligned(chosen, 4)) return LORA_ERR_INVALID_ARG;
     const memory_rows out(o, num_tokens, ldo, row, e);
-    if (share_bytes(out, memory_rows(q, num_tokens, ldq, row, e)) || share_bytes(out, c) ||
-        share_bytes(out, memory_rows(chosen, 1, 1, (int64_t)num_tokens * c->num_kv_heads * budget, 4)))
-        return LORA_ERR_INVALID_ARG;
+    auto reads = [&](const memory_rows& x) {
+        return share_bytes(x, memory_rows(q, num_tokens, ldq, row, e)) || share_bytes(x, c) ||
+               share_bytes(x, memory_rows(chosen, 1, 1, (int64_t)num_tokens * c->num_kv_heads * budget, 4));
+    };
+    if (reads(out)) return LORA_ERR_INVALID_ARG;
     const cache_division v = divide_chosen_attention(c, num_heads, num_tokens, max_new, budget);
     if (v.total > 0 && (!workspace || workspace_bytes < v.total || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
+    if (const memory_rows room(workspace, 1, 1, (int64_t)v.total, 1); v.total > 0 && (share_bytes(room, out) || reads(room))) return LORA_ERR_INVALID_ARG;
     const int64_t group = num_heads / c->num_kv_heads, tile = group > 16 ? cache_tile_rows(dtype == LORA_F32, c->head_dim) : 16, row_tiles = (group + tile - 1) / tile;
     st = check_single(c, num_heads, num_tokens, max_new, 64 * v.waves, v.splits * row_tiles);
     if (st != LORA_OK) return st;

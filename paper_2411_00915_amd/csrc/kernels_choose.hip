@@ -6,7 +6,7 @@
 //
 // Bounds of 8192 tokens' pages, 8 heads of 128: 10 us, of which the trips offsets -> length -> table -> codes are most.  The choice for 8
 // requests of 8000 tokens, 8 kv heads: 6.8 us (lengths 0.6, table and bounds 2.4, products 1, threshold 1.8, writing 0.8); 32 of 16384,
-// 17 MB of bounds, 11; four tokens over 131072, in pieces: 7 and 7.4 (in one launch 32: a compute unit reads 512 KB in 21 us).
+// 17 MB of bounds, 11; four tokens over 131072, in pieces: 6.5 and 8 (in one launch 32: a compute unit reads 512 KB in 21 us).
 #include <hip/hip_runtime.h>
 
 #include "cache_format.h"

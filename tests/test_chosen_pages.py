@@ -544,6 +544,8 @@ def test_choices_are_refused():
     assert need == 4 * 2 * 18752 * 4 // 256 * 256 + 256 * (4 * 2 * 18752 * 4 % 256 > 0) and B.lora_cache_choose_workspace(cache(), 4, 1) == 0
     for f in (dict(workspace=None, workspace_bytes=need), dict(workspace=9 * MB + 16, workspace_bytes=need), dict(workspace=9 * MB, workspace_bytes=need - 1)):
         assert refused("choose", far, **f) == WORKSPACE, f
+    for at in (7 * MB, 4 * MB, 5 * MB, 6 * MB, 64 * MB):
+        assert refused("choose", far, workspace=at, workspace_bytes=need) == BAD, at
 
 
 def test_attention_is_refused():
@@ -557,6 +559,8 @@ def test_attention_is_refused():
     assert need > 0
     for f in (dict(workspace=None), dict(workspace=9 * MB + 16), dict(workspace_bytes=need - 1)):
         assert refused("attend", c, budget=64, **f) == WORKSPACE, f
+    for at in (8 * MB, 7 * MB, 6 * MB, 64 * MB):
+        assert refused("attend", c, budget=64, workspace=at) == BAD, at
 
 
 def test_the_definitions_by_hand():
