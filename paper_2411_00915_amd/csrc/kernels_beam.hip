@@ -253,7 +253,8 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
     __shared__ int counts[kWaves];
     constexpr int UNIT = BEAM_THREADS * V, PART = 64 * V, EACH = lane_words<T, V>::EACH;
     const int split = blockIdx.x % a.splits, row = blockIdx.x / a.splits, M = a.num_out;
-    if (a.last_token && a.end_token >= 0 && a.last_token[row] == a.end_token) return;         // (beam_join_kernel does not look at it)
+    const bool ends = a.last_token && a.end_token >= 0;
+    const int last = ends ? a.last_token[row] : 0;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const T* const logits = static_cast<const T*>(a.logits) + (int64_t)row * a.ld;
     wave_state s{held[wave], 0, 0, -3.402823466e+38f, 0.0, -INFINITY, -3.402823466e+38f, true};      // (-inf is not chosen; NaN: the row is not)
@@ -263,7 +264,8 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
     auto start_of = [&](int unit) { return max(min(unit + wave * PART, a.vocab - PART), 0) + EACH * lane; };
     int look = 16;                                                 // candidates at which they are looked at for a better bound
     lane_words<T, V> next;
-    if (V != BEAM_FEW || a.vocab >= PART) next.load(logits, start_of(begin));
+    if (V != BEAM_FEW || a.vocab >= PART) next.load(logits, start_of(begin));      // (on their way together with the last token)
+    if (ends && last == a.end_token) return;                       // (beam_join_kernel does not look at it)
 #pragma unroll 1
     for (int unit = begin; unit < end; unit += UNIT) {
         const int start = start_of(unit), first = unit + wave * PART;
@@ -480,16 +482,26 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(beam_args a)
     const int64_t all = (int64_t)a.splits * M * B;
     if (tid == 0) counter = 0;
     if (tid < M) best[tid] = candidate{0, 0};
+    // All that a row has, on its way together (of a beam that has ended, what was in the workspace: it is not used).
+    constexpr int KEPT = 4;                                    // of a thread's candidates, in registers
+    beam_entry near[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) near[i] = a.entries[row0 * a.splits * M + min((int64_t)(i * kJoinThreads + tid), all - 1)];
     for (int b = wave; b < B; b += kJoinWaves) {
         const int64_t row = row0 + b;
         const float score = a.score[row];
-        const bool ended = a.last_token && a.end_token >= 0 && a.last_token[row] == a.end_token;
+        const bool ends = a.last_token && a.end_token >= 0;
+        const int last = ends ? a.last_token[row] : 0;
+        const beam_sum* const s = a.sums + row * a.splits;
+        const beam_sum own = s[min(lane, a.splits - 1)];
+        const bool ended = ends && last == a.end_token;
         double sum = 0.0, ref = -INFINITY;
         if (!ended) {
-            const beam_sum* const s = a.sums + row * a.splits;
-            for (int i = lane; i < a.splits; i += 64) ref = fmax(ref, s[i].ref);           // (-inf where there is nothing)
+            ref = own.ref;                                     // (-inf where there is nothing)
+            for (int i = lane + 64; i < a.splits; i += 64) ref = fmax(ref, s[i].ref);
             ref = wave_max(ref);
-            for (int i = lane; i < a.splits; i += 64)
+            if (lane < a.splits && own.sum != 0.0) sum = own.sum * exp(own.ref - ref);
+            for (int i = lane + 64; i < a.splits; i += 64)
                 if (s[i].sum != 0.0) sum += s[i].sum * exp(s[i].ref - ref);
 #pragma unroll
             for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
@@ -503,25 +515,24 @@ __global__ __launch_bounds__(kJoinThreads) void beam_join_kernel(beam_args a)
     }
     __syncthreads();
     const int each = a.splits * M;                             // of a beam (2^24 tokens in pieces of 2048, 64 each: 2^19)
-    auto at = [&](int64_t n) {                                 // candidate n < all
+    auto made_of = [&](int64_t n, const beam_entry& e) {       // candidate n < all
         const int b = (int)((uint32_t)n / (uint32_t)each), st = state[b];
         const uint64_t tie = (uint64_t)(63 - b) << 56;
         candidate c{0, 0};
         if (st == 1) {
-            const beam_entry e = a.entries[row0 * each + n];
             if (e.token >= 0)
                 c = candidate{order_of(worth[b] + ((double)e.logit - lse[b])), tie | (uint64_t)order_of(e.logit) << 24 | (uint32_t)(0xffffff - e.token)};
         } else if (st == 2 && n == (int64_t)b * each)
             c = candidate{order_of(worth[b]), tie | (uint32_t)(0xffffff - a.end_token)};
         return c;
     };
-    constexpr int KEPT = 4;                                    // of a thread's candidates, in registers
+    auto at = [&](int64_t n) { return made_of(n, a.entries[row0 * each + n]); };
     candidate kept[KEPT];
     uint32_t mine = 0;
 #pragma unroll
     for (int i = 0; i < KEPT; ++i) {
         const int64_t n = i * kJoinThreads + tid;
-        kept[i] = n < all ? at(n) : candidate{0, 0};
+        kept[i] = n < all ? made_of(n, near[i]) : candidate{0, 0};
         mine = max(mine, about(kept[i]));
     }
     for (int64_t n = KEPT * kJoinThreads + tid; n < all; n += kJoinThreads) mine = max(mine, about(at(n)));
