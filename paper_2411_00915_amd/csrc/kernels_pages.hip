@@ -171,18 +171,21 @@ struct wish {
     int from, to, last;
     bool fits;                                 // the wanted length is one
     int page;                                  // that it would write next, if that holds tokens already
+    int users;                                 // of that page
 };
 __device__ __forceinline__ wish wish_of(const resize_args& a, int s)
 {
     const int wanted = a.wanted[s], from = length_at(a.p, s);
     const bool fits = wanted >= 0 && wanted <= a.p.max_length;
-    return wish{from, fits ? wanted : from, -1, fits, -1};
+    return wish{from, fits ? wanted : from, -1, fits, -1, 0};
 }
 __device__ __forceinline__ void look_at_page(const pages_args& p, int s, wish& w)
 {
     if (w.to <= w.from || tokens_inside(p, w.from) == 0) return;
     w.page = p.page_table[(int64_t)s * p.table_stride + page_number(p, w.from)];
-    if (known(p, w.page) && p.users[w.page] > 1) w.last = w.page;
+    if (!known(p, w.page)) return;
+    w.users = p.users[w.page];
+    if (w.users > 1) w.last = w.page;
 }
 
 // One workgroup decides: a thread R sequences in a row.  ALL: R is 1, and nothing is left to other launches.  Else the launch before has
@@ -202,12 +205,12 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
     if constexpr (ALL) load_users<kFreeLoads>(p, (int64_t)(tid >> 6) * kFreeWave + 4 * (tid & 63), users);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        w[r] = wish{0, 0, -1, false, -1};
+        w[r] = wish{0, 0, -1, false, -1, 0};
         if (s0 + r >= S) continue;
         if constexpr (ALL) w[r] = wish_of(a, s0 + r);
         else {
             const page_grant g = a.grants[s0 + r];
-            w[r] = wish{g.from, g.to, g.first, g.row != 0, -1};
+            w[r] = wish{g.from, g.to, g.first, g.row != 0, -1, 0};
         }
         shorter |= w[r].to < w[r].from;
     }
@@ -228,13 +231,48 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
 #pragma unroll
     for (int r = 0; r < R; ++r) some |= w[r].last >= 0;
     some = __syncthreads_or(some);
-    if (some) {
-        // all of them leave the page; where nobody stays, the one with the most tokens in it keeps it
+    // all of them leave the page; where nobody stays, the one with the most tokens in it keeps it
+    auto key_of = [&](int r) { return -1 - (tokens_inside(p, w[r].from) * LORA_PAGES_MAX_SEQS + s0 + r); };
+    if constexpr (ALL) {
+        if (some) {
+            // They meet in LDS, by page (half the places stay empty, so that every search ends); users never go down to 0 here, so what has
+            // been asked for of the free pages stays right.
+            constexpr int PLACES = 2 * kThreads;
+            int* const pages = near, *const leave = near + PLACES, *const keeper = near + 2 * PLACES;
+            static_assert(3 * PLACES <= kList, "");
+            for (int i = tid; i < PLACES; i += kThreads) {
+                pages[i] = -1;
+                leave[i] = 0;
+                keeper[i] = 0;
+            }
+            __syncthreads();
+            const int page = w[0].last;
+            int at = (int)((uint32_t)page * 0x9e3779b1u >> 21);
+            if (page >= 0) {
+                for (;;) {
+                    const int there = atomicCAS(pages + at, -1, page);
+                    if (there == -1 || there == page) break;
+                    at = at + 1 & PLACES - 1;
+                }
+                atomicAdd(leave + at, 1);
+                atomicMin(keeper + at, key_of(0));
+            }
+            __syncthreads();
+            if (page >= 0) {
+                const int gone = leave[at];
+                if (w[0].users <= gone && keeper[at] == key_of(0)) {
+                    if (w[0].users < gone) atomicAdd(p.users + page, gone - w[0].users);        // (fewer than name it: it is the one now)
+                    w[0].last = -1;
+                } else
+                    atomicSub(p.users + page, 1);
+            }
+            __syncthreads();                                   // (the list of free pages is in the same place)
+        }
+    } else if (some) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
             if (w[r].last >= 0) atomicSub(p.users + w[r].last, 1);
         __syncthreads();
-        auto key_of = [&](int r) { return -1 - (tokens_inside(p, w[r].from) * LORA_PAGES_MAX_SEQS + s0 + r); };
         // (read from the caches' common level: other wavefronts' atomics are there)
         auto users_of = [&](int r) { return __hip_atomic_load(p.users + w[r].last, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
 #pragma unroll
@@ -267,9 +305,9 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
     if constexpr (ALL) {
         if (total > 0) {
 #if defined(__HIP_DEVICE_COMPILE__)
-            if (shorter || some) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");      // (users have been changed by atomics, in the caches' common level)
+            if (shorter) __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");              // (users have been changed by atomics, in the caches' common level)
 #endif
-            found = find_free(p, total, list, counts, users, !shorter && !some);
+            found = find_free(p, total, list, counts, users, !shorter);
             __syncthreads();
         }
     } else {
