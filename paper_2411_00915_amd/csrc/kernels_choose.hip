@@ -5,7 +5,7 @@
 // one rounding each: the choice is the definition's, page by page, which a sum in floating point would not be.
 //
 // Bounds of 8192 tokens' pages, 8 heads of 128: 10 us, of which the trips offsets -> length -> table -> codes are most.  The choice for 8
-// requests of 8000 tokens, 8 kv heads: 6.8 us (lengths 0.6, table and bounds 2.4, products 1, threshold 1.8, writing 0.8); 32 of 16384,
+// requests of 8000 tokens, 8 kv heads: 6.2 us (lengths 0.6, table and bounds 2.4, products 1, the choice 2); 32 of 16384,
 // 17 MB of bounds, 11; four tokens over 131072, in pieces: 6.5 and 8 (in one launch 32: a compute unit reads 512 KB in 21 us).
 #include <hip/hip_runtime.h>
 
@@ -122,8 +122,8 @@ __global__ __launch_bounds__(256) void cache_digest_kernel(cache_args c, int8_t*
 // The choice: a workgroup a token and kv head.  Its queries' codes, parted by sign, are rows of a product with the pages' bounds as columns, 16
 // queries and 16 pages at a time, on the matrix cores in whole numbers; a column's greatest goes to LDS as a whole number in the
 // order of the scores (or to the workspace, where there are more pages than LDS holds, or several workgroups share a token's pages).  Then
-// the last page chosen is found, by one wavefront bit by bit (up to 256 pages: 1.8 us) or by all by bins (2.7; bit by bit 5.5 for 400), and the
-// pages are written in order.
+// the last page chosen is found and the pages are written in order: by one wavefront, bit by bit, without a barrier (up to 256 pages: 2 us; 5.5 for
+// 400), or by all, by bins (2.7 and 0.8).
 
 // scores in their order as whole numbers above 0; NaN above them, what is chosen in any case above all
 constexpr uint32_t kForced = 0xffffffffu, kNan = 0xfffffffeu;
@@ -258,37 +258,61 @@ __device__ __forceinline__ void threshold_by_bins(const uint32_t* keys, int page
     *equal = wanted;
 }
 
-// The same of up to 64 N keys, by one wavefront, bit by bit, without a barrier; done as soon as as many as wanted are not below a number
-// (eight wavefronts, each for itself, are in each other's way in the scalar unit: 3.9 us for 400 keys)
+// how many lanes before this one are in the mask, on top of n
+__device__ __forceinline__ int lanes_before(uint64_t mask, int n)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, (uint32_t)n));
+#else
+    return n;
+#endif
+}
+
+// The choice among up to 64 N keys, by one wavefront without a barrier: the budget-th largest bit by bit, done as soon as as many as wanted are not
+// below a number; then the pages in order.  (Eight wavefronts, each for itself, are in each other's way in the scalar unit: 3.9 us for 400 keys;
+// counts in lanes that are summed up across them, for up to 256 pages 0.4 us slower, for up to 512 0.6 than by bins.)
 template <int N>
-__device__ __forceinline__ void threshold_by_bits(const uint32_t* keys, int pages, int budget, int lane, uint32_t* found)
+__device__ __forceinline__ void choose_by_bits(const uint32_t* keys, int pages, int budget, bool all, int lane, int32_t* out)
 {
     uint32_t k[N], t = 0;
 #pragma unroll
     for (int i = 0; i < N; ++i) k[i] = i * 64 + lane < pages ? keys[i * 64 + lane] : 0u;
-    int equal = -1;
+    int equal = -1;                                            // of those that are t, so many are wanted
+    if (!all) {
 #pragma unroll 1
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t next = t | 1u << bit;
-        int count = 0;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t next = t | 1u << bit;
+            int count = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) count += __popcll(__ballot(k[i] >= next));
-        if (count >= budget) t = next;
-        if (count == budget) {
-            --t;                                               // (all that are above it)
-            equal = 0;
-            break;
+            for (int i = 0; i < N; ++i) count += __popcll(__ballot(k[i] >= next));
+            if (count >= budget) t = next;
+            if (count == budget) {
+                --t;                                           // (all that are above it)
+                equal = 0;
+                break;
+            }
+        }
+        if (equal < 0) {
+            equal = budget;
+#pragma unroll
+            for (int i = 0; i < N; ++i) equal -= __popcll(__ballot(k[i] > t));
         }
     }
-    if (equal < 0) {
-        equal = budget;
+    int at = 0, same = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) equal -= __popcll(__ballot(k[i] > t));
+    for (int i = 0; i < N; ++i) {
+        bool is = k[i] > t;
+        if (equal > 0) {
+            const bool like = k[i] == t && k[i] != 0;          // (0: a page that is not there)
+            const uint64_t mask = __ballot(like);
+            is |= like && lanes_before(mask, same) < equal;
+            same += __popcll(mask);
+        }
+        const uint64_t mask = __ballot(is);
+        if (is) out[lanes_before(mask, at)] = i * 64 + lane;
+        at += __popcll(mask);
     }
-    if (lane == 0) {
-        found[0] = t;
-        found[1] = (uint32_t)equal;
-    }
+    for (int n = at + lane; n < budget; n += 64) out[n] = -1;
 }
 
 constexpr int kBoth = 0, kScores = 1, kChoice = 2;      // what a launch does: keys and choice; keys of a piece of the pages; the choice
@@ -372,19 +396,15 @@ __global__ __launch_bounds__(kThreads, DP == 256 ? 2 : 4) void cache_choose_kern
         __syncthreads();
     }
     if constexpr (WHAT != kScores) {
+        int32_t* const out = a.chosen + ((int64_t)row * c.kv_heads + head) * budget;
+        if (pages <= 256) {
+            if (wave == 0) choose_by_bits<4>(keys, pages, budget, all, lane, out);
+            return;
+        }
         uint32_t threshold = 1;
         int equal = budget;                                    // (all that are there)
-        if (!all) {
-            if (pages <= 256) {
-                if (wave == 0) threshold_by_bits<4>(keys, pages, budget, lane, found);
-                __syncthreads();
-                threshold = found[0];
-                equal = (int)found[1];
-            } else
-                threshold_by_bins(keys, pages, budget, bins, found, tid, &threshold, &equal);
-        }
+        if (!all) threshold_by_bins(keys, pages, budget, bins, found, tid, &threshold, &equal);
         // in order, four pages a thread: above it, all; equal to it, the first few; a page that is not there never
-        int32_t* const out = a.chosen + ((int64_t)row * c.kv_heads + head) * budget;
         int written = 0, same = 0;
         for (int n0 = 0; n0 < pages; n0 += 4 * kThreads) {
             uint32_t above = 0, like = 0;                      // of the thread's four
