@@ -317,12 +317,11 @@ def test_calls_are_refused():
 
 
 def test_the_workspace_holds_every_piece():
-    """Sums of 16 bytes and num_out candidates of 8 for every chunk of a row"""
-    for groups, beams, vocab, out in ((1, 1, 1, 1), (1, 4, 32000, 8), (64, 8, 131072, 16), (100, 6, 8192, 3), (100, 6, 8193, 64)):
-        rows = groups * beams
-        chunk = 2048 if rows * -(-vocab // 8192) < 512 else 8192
-        pieces = rows * -(-vocab // chunk)
-        assert B.lora_beam_workspace(groups, beams, vocab, out) == -(-(-(-pieces * 16 // 256) * 256 + pieces * out * 8) // 256) * 256
+    """Sums of 16 bytes and num_out candidates of 8 for every piece of a row: 2048 tokens, or as many times 4096 as leave four pieces a compute unit"""
+    for groups, beams, vocab, out, pieces in ((1, 1, 1, 1, 1), (1, 4, 32000, 8, 16), (64, 8, 131072, 16, 2), (100, 6, 8192, 3, 2), (100, 6, 8193, 64, 3), (1000, 2, 20000, 4, 1),
+                                              (64, 4, 50021, 4, 5), (600, 1, 4095, 7, 2)):
+        pieces *= groups * beams
+        assert B.lora_beam_workspace(groups, beams, vocab, out) == -(-(-(-pieces * 16 // 256) * 256 + pieces * out * 8) // 256) * 256, (groups, beams, vocab)
 
 
 def test_the_definition_by_hand():
