@@ -13,7 +13,7 @@
 // now and then.  So the candidates' exponentials, which are the largest, are 64 bits, and so are the sums; the others are the hardware's
 // exp2 of a product with log2(e) that is rounded once, eight of them added in 32 bits.  Measured: scores within 3e-8 of 64 bits.
 //
-// 64 requests of 8 beams over 131072 tokens, 16 candidates: 38 us and 7.4, 134 MB at 3.5 TB/s (vector instructions busy in 55 %; with all of
+// 64 requests of 8 beams over 131072 tokens, 16 candidates: 37 us and 7, 134 MB at 3.6 TB/s (vector instructions busy in 53 %; with all of
 // a part's 8192 tokens in registers and its own bound each 54 and 62; a bound that does not rise 320); four beams over 32000: 7.4 and 6.8,
 // the chain load -> bound -> exponentials -> candidates -> join.
 #include <hip/hip_runtime.h>
