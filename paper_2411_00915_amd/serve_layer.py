@@ -223,6 +223,7 @@ class BeamLayer:
         """x [tokens, hidden], the requests' prompts one behind the other.  Afterwards every request has its first beams: token, score, parent"""
         if max(lengths) > self.limit:
             raise ValueError("a prompt is longer than the caches' limit")
+        self.longest = max(lengths)
         self.adapters = [a for a in adapters for _ in range(self.beams)]
         qkv = self.qkv(x, lengths, adapters)
         q, k, v, ld = self._parts(qkv)
@@ -245,7 +246,10 @@ class BeamLayer:
         plan.destroy()
 
     def step(self):
-        """The beams' last tokens through the layer, and the best of what may follow"""
+        """The beams' last tokens through the layer, and the best of what may follow.  Every beam gets a token, so there is none where one of them is at the limit"""
+        if self.longest >= self.limit:                          # (rows go by the sequences' new tokens: one that is not granted would shift those behind it)
+            raise ValueError("a beam is at the caches' limit")
+        self.longest += 1
         S, H, D = self.requests * self.beams, self.heads, self.head_dim
         torch.add(self.length, 1, out=self.wanted)
         self._grow(S)
