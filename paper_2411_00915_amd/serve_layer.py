@@ -221,6 +221,8 @@ class BeamLayer:
 
     def prompts(self, x, lengths, adapters):
         """x [tokens, hidden], the requests' prompts one behind the other.  Afterwards every request has its first beams: token, score, parent"""
+        if len(lengths) != self.requests or len(adapters) != self.requests or min(lengths) < 1 or sum(lengths) != len(x):
+            raise ValueError("a prompt of at least a token and an adapter for every request")
         if max(lengths) > self.limit:
             raise ValueError("a prompt is longer than the caches' limit")
         self.longest = max(lengths)

@@ -37,6 +37,17 @@ def test_no_step_beyond_the_limit(monkeypatch, chosen):
         assert made == []
 
 
+@pytest.mark.parametrize("rows,lengths,adapters", [(23, [20, 0, 3], [0, 0, 0]), (20, [20], [0, 0, 0]), (20, [20], [0]), (24, [20, 4], [0, 0]), (60, [20, 37, 3], [0, 0]),
+                                                   (59, [20, 37, 3], [0, 0, 0]), (61, [20, 37, 3], [0, 0, 0]), (61, [20, 41, 0], [0, 0, 0])])
+def test_prompts_that_do_not_fit_the_requests(monkeypatch, rows, lengths, adapters):
+    """An empty prompt has no last row (its neighbour's would be taken); one length would be every request's"""
+    made = quiet(monkeypatch)
+    search = layer(3, 2, 60)
+    with pytest.raises(ValueError, match="request"):
+        search.prompts(torch.zeros((rows, 64)), lengths, adapters)
+    assert made == []
+
+
 @pytest.mark.gpu
 def test_steps_up_to_the_limit():
     """Prompts of unequal lengths: every beam gets all of its tokens, and tables and lengths are as they were behind the refusal"""
