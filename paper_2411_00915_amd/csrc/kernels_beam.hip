@@ -165,14 +165,13 @@ __device__ __forceinline__ void raise_bound(wave_state& s, float to)
     }
 }
 
-// above a number; what is below the bound is then not above it, so that it is the reference of the exponentials
+// above a number; what is below the bound is then not above it, so that it is the reference of the exponentials (also of the largest
+// finite number, above which there is no bound)
 __device__ __forceinline__ void raise_above(wave_state& s, float last)
 {
     const float to = number_of(order_of(last) + 1);
-    if (to > s.bound && to < INFINITY) {
-        s.bound = to;
-        raise_ref(s, last);
-    }
+    if (to > s.bound && to < INFINITY) s.bound = to;
+    if (last < INFINITY) raise_ref(s, last);
 }
 
 // LDS is full: the best num_out of the candidates are kept.  What comes later has higher tokens, so it has to be above the last of them.
