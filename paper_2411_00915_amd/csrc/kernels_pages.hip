@@ -22,7 +22,7 @@ namespace {
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
 constexpr int kList = 8192;                    // free pages that are kept in LDS
 constexpr int kFew = 4;                        // tokens of a sequence that its thread writes down by itself (no more than a page has)
-constexpr int kChunk = 1024;                   // entries or tokens of a sequence that a wavefront writes down
+constexpr int kChunk = PAGES_CHUNK;            // entries or tokens of a sequence that a wavefront writes down
 
 // how many lanes before this one are in the mask, on top of n
 __device__ __forceinline__ int lanes_before(uint64_t mask, int n)
@@ -599,12 +599,12 @@ __global__ __launch_bounds__(256) void pages_fork_write_kernel(pages_args p, con
 hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream)
 {
     const pages_args& p = a.p;
-    // One workgroup for all of it: 1024 sequences, and as many entries and tokens as it writes in the time of another launch
-    if (p.num_seqs <= kThreads && (int64_t)p.num_seqs * p.table_stride <= 32 * kThreads && a.num_tokens <= 16 * kThreads) {
+    static_assert(kThreads == 1024, "");                       // (one_workgroup_resizes)
+    if (one_workgroup_resizes(p.num_seqs, p.table_stride, a.num_tokens)) {
         LORA_LAUNCH(LORA_K_PAGES_DECIDE, (pages_decide_kernel<1, true>), dim3(1), dim3(kThreads), 0, stream, a);
         return hipGetLastError();
     }
-    const int entries = p.table_stride < kChunk ? 1 : (p.table_stride + kChunk - 1) / kChunk, looks = free_parts(p.num_pages) > (p.num_seqs + 255) / 256 ? free_parts(p.num_pages) : (p.num_seqs + 255) / 256;
+    const int entries = (int)entry_chunks(p.table_stride), looks = free_parts(p.num_pages) > (p.num_seqs + 255) / 256 ? free_parts(p.num_pages) : (p.num_seqs + 255) / 256;
     auto blocks = [&](int64_t chunks) { return dim3((uint32_t)((p.num_seqs * chunks + 3) / 4)); };
     LORA_LAUNCH(LORA_K_PAGES_GIVE_BACK, pages_give_back_kernel, blocks(entries), dim3(256), 0, stream, a, entries);
     hipError_t e = hipGetLastError();
@@ -617,8 +617,7 @@ hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream)
     else LORA_LAUNCH(LORA_K_PAGES_DECIDE, (pages_decide_kernel<16, false>), dim3(1), dim3(kThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    const bool tokens = a.token_seq || a.token_position || a.token_slot;
-    const int rows = tokens ? (int)(((int64_t)(a.num_tokens < p.max_length ? a.num_tokens : p.max_length) + kChunk - 1) / kChunk) : 0, chunks = rows > entries ? rows : entries;
+    const int chunks = (int)write_chunks(p.table_stride, p.max_length, a.num_tokens, a.token_seq || a.token_position || a.token_slot);
     LORA_LAUNCH(LORA_K_PAGES_WRITE, pages_write_kernel, blocks(chunks), dim3(256), 0, stream, a, chunks);
     return hipGetLastError();
 }

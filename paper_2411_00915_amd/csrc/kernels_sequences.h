@@ -46,6 +46,20 @@ inline size_t pages_workspace(int64_t num_pages, int64_t num_seqs, int64_t table
     return ((resize > fork ? resize : fork) + 255) / 256 * 256;
 }
 
+// Whether one workgroup does all of a resize: 1024 sequences, and as many entries and tokens as it writes in the time of another launch
+inline bool one_workgroup_resizes(int64_t num_seqs, int64_t table_stride, int64_t num_tokens)
+{
+    return num_seqs <= 1024 && num_seqs * table_stride <= 32 * 1024 && num_tokens <= 16 * 1024;
+}
+// Else wavefronts of a sequence's entries, 1024 each, and of its new tokens, too, where these are wanted
+constexpr int PAGES_CHUNK = 1024;
+inline int64_t entry_chunks(int64_t table_stride) { return table_stride < PAGES_CHUNK ? 1 : (table_stride + PAGES_CHUNK - 1) / PAGES_CHUNK; }
+inline int64_t write_chunks(int64_t table_stride, int64_t max_length, int64_t num_tokens, bool tokens)
+{
+    const int64_t rows = tokens ? ((num_tokens < max_length ? num_tokens : max_length) + PAGES_CHUNK - 1) / PAGES_CHUNK : 0, entries = entry_chunks(table_stride);
+    return rows > entries ? rows : entries;
+}
+
 hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream);
 hipError_t launch_pages_fork(const pages_args& p, const int32_t* parent, int32_t* workspace, hipStream_t stream);
 

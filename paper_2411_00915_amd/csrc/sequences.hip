@@ -80,6 +80,9 @@ extern "C" lora_status lora_pages_resize(const lora_pages* p, const int32_t* wan
     if (share_any({{granted, 4 * S}, {indptr, 4 * S + 4}, {token_seq, 4 * T}, {token_position, 4 * T}, {token_slot, 8 * T}, {copies, 8 * S}, {workspace, (int64_t)need},
                    {p->page_table, 4 * S * p->table_stride}, {p->length, 4 * S}, {p->users, 4 * p->num_pages}, {wanted, 4 * S}}, 10))
         return LORA_ERR_INVALID_ARG;
+    // (the last of its launches: refused before the first has changed anything)
+    if (!one_workgroup_resizes(S, p->table_stride, T) && S * write_chunks(p->table_stride, p->max_length, T, token_seq || token_position || token_slot) > most_workgroups(64) - 4)
+        return LORA_ERR_UNSUPPORTED;
     char* const w = static_cast<char*>(workspace);
     const resize_args a{args_of(p), wanted, num_tokens, granted, indptr, token_seq, token_position, token_slot, copies, reinterpret_cast<page_grant*>(w),
                         reinterpret_cast<int32_t*>(w + pages_parts_offset(p->num_seqs)), reinterpret_cast<int32_t*>(w + pages_list_offset(p->num_seqs, p->num_pages))};

@@ -1,0 +1,22 @@
+"""Resizes of pages at the ends of what the call takes, as test_pages.py has the others."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_2411_00915_amd import binding as B
+from test_pages import UNSUPPORTED, desc, status
+
+
+@pytest.mark.parametrize("field", ["d_token_seq", "d_token_position", "d_token_slot"])
+def test_a_last_launch_that_is_too_large_is_refused_before_the_first(field):
+    """2^14 sequences of 4200 pieces of 1024 tokens: 4.4e9 threads.  Where no token's number is wanted, and with fewer rows, launches are of the table's size"""
+    big = dict(page_table=1 << 40, num_seqs=1 << 14, table_stride=4200, max_length=4200 * 1024, page_tokens=1024)
+    p = B.Pages(desc(**big))
+    need = B.lora_pages_workspace(p)
+    rows = 4200 * 1024
+    none = dict(d_token_seq=None, d_token_position=None, d_token_slot=None)
+    fine = dict(d_wanted=1 << 41, d_granted=None, d_indptr=None, d_copies=1 << 42, workspace=1 << 43, workspace_bytes=need)
+    resize = lambda **f: status(lambda: B.lora_pages_resize(p, **{**fine, **none, **f}, stream=1))  # noqa: E731
+    assert resize(num_tokens=rows, **{field: 1 << 44}) == UNSUPPORTED
+    assert resize(num_tokens=2 ** 30, **{field: 1 << 44}) == UNSUPPORTED
+    assert resize(num_tokens=4096 * 1024, **{field: 1 << 44}) == UNSUPPORTED
