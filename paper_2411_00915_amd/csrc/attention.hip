@@ -267,6 +267,12 @@ lora_status check_single(const lora_cache* c, int32_t num_heads, int32_t num_tok
     return (int64_t)c->num_seqs * max_new * c->num_kv_heads > most_workgroups(threads) / std::max<int64_t>(1, more) ? LORA_ERR_UNSUPPORTED : LORA_OK;
 }
 
+// of lora_cache_attention_chosen: pieces are joined by a workgroup for each of the tokens' heads
+lora_status check_join(const lora_cache* c, int32_t num_heads, int32_t max_new, const cache_division& v)
+{
+    return v.splits > 1 && (int64_t)c->num_seqs * max_new > most_workgroups(LORA_CACHE_FINISH_THREADS) / num_heads ? LORA_ERR_UNSUPPORTED : LORA_OK;
+}
+
 // pages of the longest sequence, to whole 32s
 int64_t key_stride(const lora_cache* c) { return ((int64_t)(c->max_length + c->page_tokens - 1) / c->page_tokens + 31) / 32 * 32; }
 int32_t pieces_of(const lora_cache* c, int32_t num_tokens) { return choose_pieces((int64_t)num_tokens * c->num_kv_heads, key_stride(c)); }
@@ -356,8 +362,11 @@ extern "C" lora_status lora_cache_chosen_workspace(const lora_cache* c, int32_t 
     max_new = std::min(max_new, num_tokens);
     st = check_single(c, num_heads, num_tokens, max_new, 256, 1);
     if (st != LORA_OK) return st;
-    if (num_tokens > 0 && max_new > 0 && c->num_seqs > 0) *bytes = divide_chosen_attention(c, num_heads, num_tokens, max_new, budget).total;
-    return LORA_OK;
+    if (num_tokens == 0 || max_new == 0 || c->num_seqs == 0) return LORA_OK;
+    const cache_division v = divide_chosen_attention(c, num_heads, num_tokens, max_new, budget);
+    st = check_join(c, num_heads, max_new, v);
+    if (st == LORA_OK) *bytes = v.total;
+    return st;
 }
 
 extern "C" lora_status lora_cache_attention_chosen(const lora_cache* c, int32_t dtype, int32_t num_heads, int32_t num_tokens, int32_t max_new,
@@ -382,6 +391,8 @@ extern "C" lora_status lora_cache_attention_chosen(const lora_cache* c, int32_t 
     };
     if (reads(out)) return LORA_ERR_INVALID_ARG;
     const cache_division v = divide_chosen_attention(c, num_heads, num_tokens, max_new, budget);
+    st = check_join(c, num_heads, max_new, v);
+    if (st != LORA_OK) return st;
     if (v.total > 0 && (!workspace || workspace_bytes < v.total || misaligned(workspace, 256))) return LORA_ERR_WORKSPACE;
     if (const memory_rows room(workspace, 1, 1, (int64_t)v.total, 1); v.total > 0 && (share_bytes(room, out) || reads(room))) return LORA_ERR_INVALID_ARG;
     const int64_t group = num_heads / c->num_kv_heads, tile = group > 16 ? cache_tile_rows(dtype == LORA_F32, c->head_dim) : 16, row_tiles = (group + tile - 1) / tile;
