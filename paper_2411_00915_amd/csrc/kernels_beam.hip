@@ -215,31 +215,40 @@ __device__ __forceinline__ uint32_t reached_of_four(const uint32_t* mine, int wa
     return bound;
 }
 
-// Raises the bound by the candidates: num_out of them are not below it, or in every wavefront its share (`bounds`: what they have
-// found so far; it only rises, so an old number does as well).  Returns the upper 16 bits of what it found.
-__device__ __forceinline__ uint32_t raise_by_held(wave_state& s, int M, int wave, int lane, volatile uint32_t* bounds)
+// Raises the bound by the candidates: num_out of them are not below it.  Returns the upper 16 bits of what it found, and what the wavefront's
+// share of num_out are not below in *share, which only rises.
+__device__ __forceinline__ uint32_t raise_by_held(wave_state& s, int M, int lane, uint32_t* share)
 {
     wave_sync();
     const int part = (M + kWaves - 1) / kWaves;
-    uint32_t share, least;
+    uint32_t few, least;
     if (s.count <= 64) {
         const uint32_t mine = lane < s.count ? order_of(s.held[lane].logit) >> 16 : 0u;
-        share = reached<16>(mine, part);
+        few = reached<16>(mine, part);
         least = reached<16>(mine, M);
     } else {
         uint32_t mine[kHeld / 64];
 #pragma unroll
         for (int n = 0; n < kHeld / 64; ++n) mine[n] = n * 64 + lane < s.count ? order_of(s.held[n * 64 + lane].logit) >> 16 : 0u;
-        share = reached_of_four(mine, part);
+        few = reached_of_four(mine, part);
         least = reached_of_four(mine, M);
     }
-    if (lane == 0 && share > bounds[wave]) bounds[wave] = share;
-    uint32_t all = bounds[0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) all = min(all, (uint32_t)bounds[w]);
-    least = (uint32_t)__builtin_amdgcn_readfirstlane(max(least, all));
+    *share = max(*share, few);
     raise_bound(s, number_of(least << 16));
     return least;
+}
+
+// The least of the wavefronts' shares: num_out of the workgroup's candidates are not below it.  Behind a barrier, so that what a row's sum is
+// made of does not depend on who was first; slots[2], in turns, so that one barrier an exchange is enough.
+__device__ __forceinline__ uint32_t exchange(uint32_t (*slots)[kWaves], int turn, uint32_t share, int wave, int lane)
+{
+    uint32_t* const slot = slots[turn & 1];
+    if (lane == 0) slot[wave] = share;
+    __syncthreads();
+    uint32_t all = slot[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) all = min(all, slot[w]);
+    return all;
 }
 
 template <typename T, int V>
@@ -248,7 +257,7 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
     __shared__ beam_entry held[kWaves][kHeld];
     __shared__ double sums[kWaves];
     __shared__ double refs[kWaves];
-    __shared__ uint32_t bounds[kWaves];
+    __shared__ uint32_t slots[2][kWaves], shares[kWaves];
     __shared__ int counts[kWaves];
     constexpr int UNIT = BEAM_THREADS * V, PART = 64 * V, EACH = lane_words<T, V>::EACH;
     const int split = blockIdx.x % a.splits, row = blockIdx.x / a.splits, M = a.num_out;
@@ -262,6 +271,8 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
     // with the part before it is masked.
     auto start_of = [&](int unit) { return max(min(unit + wave * PART, a.vocab - PART), 0) + EACH * lane; };
     int look = 16;                                                 // candidates at which they are looked at for a better bound
+    int turn = 0, done = 0;                                        // exchanges and units so far
+    uint32_t share = 0;                                            // what the wavefront's share of num_out are not below
     lane_words<T, V> next;
     if (V != BEAM_FEW || a.vocab >= PART) next.load(logits, start_of(begin));      // (on their way together with the last token)
     if (ends && last == a.end_token) return;                       // (beam_join_kernel does not look at it)
@@ -292,14 +303,9 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
         // not below the second.  The second is what there is where another wavefront's part is masked or behind the row's end,
         // and again where the first tokens were.
         if (unit == begin) {
-            const uint32_t mine = order_of(top) >> 16, share = reached<16>(mine, (M + kWaves - 1) / kWaves);
-            uint32_t least = reached<16>(mine, M);
-            if (lane == 0) bounds[wave] = share;
-            __syncthreads();
-            uint32_t all = bounds[0];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) all = min(all, bounds[w]);
-            raise_bound(s, number_of(max(least, all) << 16));
+            const uint32_t mine = order_of(top) >> 16, least = reached<16>(mine, M);
+            share = reached<16>(mine, (M + kWaves - 1) / kWaves);
+            raise_bound(s, number_of(max(least, exchange(slots, turn++, share, wave, lane)) << 16));
         } else if (__popcll(__ballot(top >= s.bound)) > M)
             raise_bound(s, number_of(reached<16>(order_of(top) >> 16, M) << 16));
         // what is not below the bound goes to LDS, and is as good as masked here
@@ -324,7 +330,7 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
                     }
                 }
                 if (s.count >= look) {
-                    raise_by_held(s, M, wave, lane, bounds);
+                    raise_by_held(s, M, lane, &share);
                     look = s.count + max(8, M / 2);
                 }
             } else {
@@ -387,23 +393,28 @@ __global__ __launch_bounds__(BEAM_THREADS, 4) void beam_rows_kernel(beam_args a)
         };
         if (__builtin_expect(__builtin_amdgcn_readfirstlane(s.far), 0)) add(std::true_type{});
         else add(std::false_type{});
+        // Of shuffled logits as many are above the bound in the first units as in as many again.  (64 requests of 8 beams over 131072 tokens 46.6 us in
+        // all, with the shares found anew here 48.1, with no exchange behind the first unit 47.6, for 64 candidates 68, 71 and 94)
+        ++done;
+        if ((done & (done - 1)) == 0 && unit + UNIT < end) raise_bound(s, number_of(exchange(slots, turn++, share, wave, lane) << 16));
     }
     wave_sync();
     add_held(s, lane);
-    uint32_t limit = s.count > 0 ? raise_by_held(s, M, wave, lane, bounds) : 0u;
+    uint32_t limit = s.count > 0 ? raise_by_held(s, M, lane, &share) : 0u;
     double sum = s.sum;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 64);
     if (lane == 0) {
         sums[wave] = sum;
         refs[wave] = s.ref;
+        shares[wave] = share;
     }
     __syncthreads();
     // What is left of the candidates, now that all wavefronts' bounds are there, to the front; then the workgroup's best in order
-    uint32_t shares = bounds[0];
+    uint32_t least_share = shares[0];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) shares = min(shares, bounds[w]);
-    limit = max(limit, shares) << 16;                              // (not the bound, which may be above what is kept of equal ones)
+    for (int w = 1; w < kWaves; ++w) least_share = min(least_share, shares[w]);
+    limit = max(limit, least_share) << 16;                         // (not the bound, which may be above what is kept of equal ones)
     int kept = 0;
     for (int n = 0; n < s.count; n += 64) {                        // (what is moved goes no further back than it was)
         const beam_entry e = s.held[min(n + lane, s.count - 1)];

@@ -4,7 +4,8 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from test_beams import BF16, F32, TORCH, check, gpu, scores
+from paper_2411_00915_amd import binding as B
+from test_beams import BF16, DEV, F32, TORCH, check, gpu, scores
 
 
 @gpu
@@ -20,3 +21,32 @@ def test_many_logits_of_the_largest_finite_number(dtype, vocab, some, out, group
     for r, low in zip(range(len(x)), (1.0, -np.inf, top * (1 - torch.finfo(TORCH[dtype]).eps), -top)):
         x[r, rng.permutation(vocab)[: vocab - some]] = low
     check(x.astype(np.float32), scores(rng, len(x)), None, 0, beams, out, dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,groups,beams,vocab,out", [(BF16, 64, 8, 131072, 16), (F32, 64, 4, 50021, 4), (BF16, 200, 4, 60000, 8), (F32, 300, 4, 20001, 64), (BF16, 2, 4, 32000, 8)])
+def test_the_same_bits_again(dtype, groups, beams, vocab, out):
+    """Rows of several units a workgroup: scores, parents and tokens, and the sums that the second launch reads (two numbers of 64 bits for each piece of a row, at
+    the workspace's start), call after call, beside other work and on a stream of its own"""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(vocab)
+    x = (torch.randn((groups * beams, vocab), generator=gen, device=DEV) * 3).to(TORCH[dtype])
+    score = torch.rand(groups * beams, generator=gen, device=DEV) - 9
+    need = B.lora_beam_workspace(groups, beams, vocab, out)
+    pieces = next(n for n in range(1, 1 << 14) if need == -(-(-(-n * groups * beams * 16 // 256) * 256 + n * groups * beams * out * 8) // 256) * 256)
+    others, first = [torch.cuda.Stream(), torch.cuda.Stream()], None
+    side = torch.randn((2048, 2048), device=DEV)
+    torch.cuda.synchronize()
+    for i in range(24):
+        got = [torch.empty((groups, out), dtype=t, device=DEV) for t in (torch.float32, torch.int32, torch.int32)]
+        room = torch.zeros(need, dtype=torch.uint8, device=DEV)
+        torch.cuda.synchronize()
+        if i % 2:
+            with torch.cuda.stream(others[0]):
+                side = torch.tanh(side @ side)
+        with torch.cuda.stream(others[1] if i % 3 else torch.cuda.current_stream()):
+            B.lora_beam_select(dtype, groups, beams, vocab, x, vocab, score, None, 0, out, *got, room, need)
+        torch.cuda.synchronize()
+        bits = [got[0].view(torch.int32), got[1], got[2], room[: pieces * groups * beams * 16]]
+        first = bits if first is None else first
+        assert all(torch.equal(a, b) for a, b in zip(first, bits)), i
