@@ -428,6 +428,9 @@ __global__ __launch_bounds__(kThreads) void pages_decide_kernel(resize_args a)
     }
 }
 
+// No sequences: the end of their tokens
+__global__ void pages_none_kernel(int32_t* indptr) { indptr[0] = 0; }
+
 // Before the launch that decides: a wavefront a sequence and so many of its entries
 __global__ __launch_bounds__(256) void pages_give_back_kernel(resize_args a, int chunks)
 {
@@ -619,6 +622,12 @@ hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream)
     if (e != hipSuccess) return e;
     const int chunks = (int)write_chunks(p.table_stride, p.max_length, a.num_tokens, a.token_seq || a.token_position || a.token_slot);
     LORA_LAUNCH(LORA_K_PAGES_WRITE, pages_write_kernel, blocks(chunks), dim3(256), 0, stream, a, chunks);
+    return hipGetLastError();
+}
+
+hipError_t launch_pages_none(int32_t* indptr, hipStream_t stream)
+{
+    LORA_LAUNCH(LORA_K_PAGES_DECIDE, pages_none_kernel, dim3(1), dim3(1), 0, stream, indptr);
     return hipGetLastError();
 }
 

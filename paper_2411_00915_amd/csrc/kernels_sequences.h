@@ -61,6 +61,7 @@ inline int64_t write_chunks(int64_t table_stride, int64_t max_length, int64_t nu
 }
 
 hipError_t launch_pages_resize(const resize_args& a, hipStream_t stream);
+hipError_t launch_pages_none(int32_t* indptr, hipStream_t stream);
 hipError_t launch_pages_fork(const pages_args& p, const int32_t* parent, int32_t* workspace, hipStream_t stream);
 
 struct beam_sum {

@@ -72,7 +72,7 @@ extern "C" lora_status lora_pages_resize(const lora_pages* p, const int32_t* wan
     if (num_tokens < 0 || misaligned(wanted, 4) || misaligned(granted, 4) || misaligned(indptr, 4) || misaligned(token_seq, 4) || misaligned(token_position, 4) ||
         misaligned(token_slot, 8) || misaligned(copies, 4))
         return LORA_ERR_INVALID_ARG;
-    if (p->num_seqs == 0) return LORA_OK;
+    if (p->num_seqs == 0) return indptr ? status_of(launch_pages_none(indptr, static_cast<hipStream_t>(hip_stream))) : LORA_OK;
     if (!wanted || !copies) return LORA_ERR_INVALID_ARG;
     const size_t need = pages_workspace(p->num_pages, p->num_seqs, p->table_stride);
     if (!workspace || workspace_bytes < need || misaligned(workspace, 256)) return LORA_ERR_WORKSPACE;

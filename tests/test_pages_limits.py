@@ -4,7 +4,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2411_00915_amd import binding as B
-from test_pages import UNSUPPORTED, desc, status
+from test_pages import DEV, UNSUPPORTED, desc, gpu, status
 
 
 @pytest.mark.parametrize("field", ["d_token_seq", "d_token_position", "d_token_slot"])
@@ -20,3 +20,22 @@ def test_a_last_launch_that_is_too_large_is_refused_before_the_first(field):
     assert resize(num_tokens=rows, **{field: 1 << 44}) == UNSUPPORTED
     assert resize(num_tokens=2 ** 30, **{field: 1 << 44}) == UNSUPPORTED
     assert resize(num_tokens=4096 * 1024, **{field: 1 << 44}) == UNSUPPORTED
+
+
+@gpu
+def test_no_sequences_have_no_tokens():
+    """Offsets have one more number than there are sequences; also in a graph"""
+    p = B.Pages(desc(num_seqs=0, page_table=0, length=0, users=0))
+    out = torch.full((2,), 7, dtype=torch.int32, device=DEV)
+    call = lambda: B.lora_pages_resize(p, None, 5, None, out, None, None, None, None, None, 0)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    assert out.tolist() == [0, 7]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for value in (3, -1):
+        out.fill_(value)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert out.tolist() == [0, value]
