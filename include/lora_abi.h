@@ -567,7 +567,8 @@ lora_status lora_cache_copy(const lora_cache* cache, int32_t num_copies, const i
  * sum of its tokens' log-probabilities.  Its continuation by token v is worth
  *     score[r] + (logits[r, v] - log sum_u exp logits[r, u])
  * and of all of a request's the num_out greatest are given, greatest first: equal ones by beam, then by logit, greater first, then by
- * token.  What they are worth is compared in 64 bits and rounded once, to out_score; sums of exponentials are 64 bits, each exponential 32.
+ * token.  What they are worth is compared in 64 bits and rounded once, to out_score; sums of exponentials are 64 bits, each exponential 32,
+ * so that a row's log sum is off by at most (9 + 1.225 log(vocab)) 2^-24.
  * out_parent: the beam's row (for lora_pages_fork, where num_out is beams), out_token; all [num_groups][num_out], device.
  * A beam has ended where last_token[r] (device, [num_groups * beams]; NULL: none has) is end_token, unless that is negative: its row is not looked
  * at, and its one continuation is end_token, worth score[r].  Tokens of logit -inf, and rows whose sum of exponentials or whose score

@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2411_00915_amd import binding as B
-from test_beams import BF16, DEV, F32, TORCH, check, gpu, scores
+from test_beams import BF16, DEV, F32, TORCH, check, gpu, run, scores
 
 
 @gpu
@@ -50,3 +50,42 @@ def test_the_same_bits_again(dtype, groups, beams, vocab, out):
         bits = [got[0].view(torch.int32), got[1], got[2], room[: pieces * groups * beams * 16]]
         first = bits if first is None else first
         assert all(torch.equal(a, b) for a, b in zip(first, bits)), i
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vocab", [5000, 131072, 1 << 20])
+@pytest.mark.parametrize("floor", ["equal", "two", "spread"])
+def test_a_peak_over_a_floor(dtype, vocab, floor):
+    """One logit above all others, which together weigh as much as it, or far more, or less: the log sum is made of exponentials in 32 bits.
+
+    With u = 2^-24 and g the reference less the logit: the argument g log2(e) is rounded once (u of itself, so g u of the exponential), log2(e) in 32
+    bits is 0.224 u of itself off (0.224 g u), exp2 is off by 2 u, and of eight that are added the sum by 7 u.  The weighted mean of g is at most log(vocab): with
+    weights w = exp(-g) / Z it is the weights' entropy less log Z, and Z is 1 or more, as the largest logit is not below the reference.  So
+    a log sum is off by at most (9 + 1.225 log(vocab)) u; a score of it is rounded once more."""
+    rng = np.random.default_rng(vocab)
+    gaps, bases = np.arange(1.0, 17.0, 0.6180339887), np.array([4.0, -9.0, 0.0, 117.0])
+    if vocab > 1 << 17:
+        gaps = gaps[::4]
+    off = []
+    for base in bases:
+        x = np.full((len(gaps), vocab), base)
+        if floor == "two":
+            x[:, rng.permutation(vocab)[: vocab // 3]] -= 1.3
+        if floor == "spread":
+            x -= rng.random((1, vocab)) * 2
+        place = rng.integers(0, vocab, len(gaps))
+        x[np.arange(len(gaps)), place] = base + gaps
+        x = torch.from_numpy(x.astype(np.float32)).to(TORCH[dtype]).float().numpy()
+        got, parent, token = run(x, np.zeros(len(gaps), np.float32), None, 0, 1, 2, dtype)
+        x = x.astype(np.float64)
+        top = x.max(1, keepdims=True)
+        expect = x - top - np.log(np.exp(x - top).sum(1, keepdims=True))
+        rest = x.copy()
+        rest[np.arange(len(gaps)), place] = -np.inf
+        second = rest.argmax(1)
+        assert (token[:, 0] == place).all() and (token[:, 1] == second).all() and (parent == np.arange(len(gaps))[:, None]).all()
+        expect = np.take_along_axis(expect, np.stack([place, second], 1), 1)
+        off.append(np.abs(got - expect))
+        assert np.all(off[-1] <= (9 + 1.225 * np.log(vocab)) * 2.0 ** -24 + 2.0 ** -24 * np.abs(expect)), (base, off[-1].max())
+    print(f"{floor}, {vocab}: greatest difference of the peak's score {max(o[:, 0].max() for o in off):.2e}")
