@@ -557,7 +557,8 @@ lora_status lora_pages_fork(const lora_pages* pages, const int32_t* parent, void
 /*
  * lora_cache_copy -- page copies[i][0] of one layer's cache to page copies[i][1], all heads, codes, words and accumulated weights (where the cache keeps
  * them); i < num_copies; copies: device.  Pairs with a page outside [0, num_pages), or of a page and itself, are passed over.
- * No page may be written twice, or written and read.  (A cache without sequences: nothing is copied.)
+ * No page may be written twice, or written and read.  (A cache without sequences: nothing is copied.)  copies must not share memory with the
+ * cache's pages or weights.
  */
 lora_status lora_cache_copy(const lora_cache* cache, int32_t num_copies, const int32_t* copies, void* hip_stream);
 

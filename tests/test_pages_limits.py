@@ -4,7 +4,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2411_00915_amd import binding as B
-from test_pages import DEV, UNSUPPORTED, desc, gpu, status
+from test_pages import BAD, DEV, UNSUPPORTED, desc, gpu, status
 
 
 @pytest.mark.parametrize("field", ["d_token_seq", "d_token_position", "d_token_slot"])
@@ -20,6 +20,17 @@ def test_a_last_launch_that_is_too_large_is_refused_before_the_first(field):
     assert resize(num_tokens=rows, **{field: 1 << 44}) == UNSUPPORTED
     assert resize(num_tokens=2 ** 30, **{field: 1 << 44}) == UNSUPPORTED
     assert resize(num_tokens=4096 * 1024, **{field: 1 << 44}) == UNSUPPORTED
+
+
+def test_a_list_of_copies_in_the_cache_itself_is_refused():
+    """Five pairs, 40 bytes, around both ends of 100 pages of 8 heads, and of their weights"""
+    size = 100 * 8 * B.lora_cache_page_bytes(64, 128)
+    for weight in (None, 64 << 20):
+        c = B.Cache(B.CacheDesc(16 << 20, weight, 2 << 20, 3 << 20, 100, 4, 10, 640, 64, 8, 128))
+        places = [(16 << 20, size)] + ([(weight, 100 * 8 * 64 * 4)] if weight else [])
+        for at, n in places:
+            for copies in (at - 36, at, at + n // 2, at + n - 4):
+                assert status(lambda: B.lora_cache_copy(c, 5, copies, 1)) == BAD, (at, copies)
 
 
 @gpu
