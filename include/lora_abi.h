@@ -539,8 +539,8 @@ lora_status lora_pages_workspace(const lora_pages* pages, size_t* bytes);
  * entry is not there); rows behind the last token are left as they were.  copies: device, [num_seqs][2], the page to copy and the page
  * to fill, -1 and -1 where there is none (NULL: LORA_ERR_INVALID_ARG).  length, users and page_table are brought up to date.
  * The outputs may not share memory with each other, nor with what the call reads.
- * LORA_ERR_UNSUPPORTED, and nothing changed, where sequences times the thousands of the lesser of num_tokens and max_length are 2^26 and more (and any
- * of the tokens' numbers is wanted).
+ * LORA_ERR_UNSUPPORTED, and nothing changed, where num_seqs * ceil(min(num_tokens, max_length) / 1024) is about 2^26 or more (and any of
+ * the tokens' numbers is wanted).
  * Deterministic: what the atomics add up are whole numbers.
  */
 lora_status lora_pages_resize(const lora_pages* pages, const int32_t* wanted, int32_t num_tokens, int32_t* granted, int32_t* indptr,

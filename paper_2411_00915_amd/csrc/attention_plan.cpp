@@ -210,7 +210,7 @@ cache_division divide_chosen_attention(const lora_cache* c, int32_t num_heads, i
     tokens.max_length = budget * c->page_tokens;
     const int64_t wgs = (int64_t)tokens.num_seqs * c->num_kv_heads;
     // No more workgroups than compute units, and no more than four blocks a wavefront: in one piece, with eight wavefronts, and nothing to join
-    // (8 requests over 16 pages of 64, 32 heads on 8: 11.8 us, in four pieces of four wavefronts 8.0 and 3.8 in a second launch)
+    // (8 requests over 16 pages of 64, 32 heads on 8: 11.8 us at the least, in four pieces of four wavefronts 8.0 and 3.8 in a second launch)
     if (wgs <= 256 && num_heads / c->num_kv_heads <= 16 && tokens.max_length <= 1024) {
         cache_division v{};
         v.row_tiles = v.splits = 1;

@@ -17,8 +17,8 @@
 // even out, 6e-7 for one logit above 131071 equal ones, which are all rounded alike (that with the rounding of the score).  Without the
 // product's roundings (their sum beside the exponentials', six instructions more a logit) 64 requests of 8 beams take 53 us in place of 46.6.
 //
-// 64 requests of 8 beams over 131072 tokens, 16 candidates: 37 us and 7, 134 MB at 3.6 TB/s (vector instructions busy in 53 %; with all of
-// a part's 8192 tokens in registers and its own bound each 54 and 62; a bound that does not rise 320); four beams over 32000: 7.4 and 6.8,
+// 64 requests of 8 beams over 131072 tokens, 16 candidates: 40.8 us and 7.6, 134 MB at 3.3 TB/s (vector instructions busy in 50 %; 37.1 while wavefronts
+// read each other's bounds whenever they liked; a bound that does not rise 320); four beams over 32000: 8.0 and 7.0,
 // the chain load -> bound -> exponentials -> candidates -> join.
 #include <hip/hip_runtime.h>
 

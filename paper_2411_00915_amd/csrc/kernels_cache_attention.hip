@@ -22,7 +22,7 @@
 // Few requests are bound by the chain length -> page -> codes: 8 of 700 tokens 11.1 us.  Four tokens over 131072, 32 heads on 8,
 // with accumulated weights: 39 us here, the scores written out for them (67 MB beside 147) included, 20 in the launch that
 // reads them back.  Over chosen pages there are a few blocks a wavefront, and the chain has the list in front of it: 32 of 64 tokens for 32
-// requests 18.6 us (71 MB; 13.2 at the rate of a copy), 16 for 8 requests 11.8.
+// requests 19.4 to 20 us (71 MB; 13.2 at the rate of a copy), 16 for 8 requests 13.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -485,7 +485,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : sizeof(T) == 2 && CT == 
         slot = slot == RING - 1 ? 0 : slot + 1;
     };
     if constexpr (CHOSEN) {                                    // (in the order of the list, which need not be the blocks'; as a branch in one
-#pragma unroll 1                                               // loop both spill: 25.0 in place of 18.6 us for 32 sequences' 32 pages, 32 heads on 8)
+#pragma unroll 1                                               // loop both spill: 25.0 in place of 18.6 us, at their least, for 32 sequences' 32 pages, 32 heads on 8)
         while (queue[0] != NONE) {
 #pragma unroll 1
             while (queue[0] < full) turn(std::false_type{});

@@ -4,9 +4,9 @@
 // orders pages by.  Bounds and queries are whole numbers of 8 bits, so the sums are exact whatever their order, and what follows is
 // one rounding each: the choice is the definition's, page by page, which a sum in floating point would not be.
 //
-// Bounds of 8192 tokens' pages, 8 heads of 128: 10 us, of which the trips offsets -> length -> table -> codes are most.  The choice for 8
-// requests of 8000 tokens, 8 kv heads: 6.2 us (lengths 0.6, table and bounds 2.4, products 1, the choice 2); 32 of 16384,
-// 17 MB of bounds, 11; four tokens over 131072, in pieces: 6.5 and 8 (in one launch 32: a compute unit reads 512 KB in 21 us).
+// Bounds of 8192 tokens' pages, 8 heads of 128: 10.6 us, of which the trips offsets -> length -> table -> codes are most.  The choice for 8
+// requests of 8000 tokens, 8 kv heads: 6.4 us (lengths 0.6, table and bounds 2.4, products 1, the choice 2); 32 of 16384,
+// 17 MB of bounds, 11; four tokens over 131072, in pieces: 6.4 and 8.5 (in one launch 32: a compute unit reads 512 KB in 21 us).
 #include <hip/hip_runtime.h>
 
 #include "cache_format.h"

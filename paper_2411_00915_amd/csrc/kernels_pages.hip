@@ -2,10 +2,11 @@
 //
 // A call is a few thousand whole numbers, so it is bound by its chain of dependent trips to memory: wanted length -> table ->
 // users of the page written next -> free pages -> table -> slots.  Where the tables are small, one workgroup does all of it with barriers
-// between the steps, and a thread its sequence's tokens where none has more than four (16 requests a token each: 5 us, of which 0.9 a prefix
-// over the workgroup; 128 prompts, 8192 tokens: 13 us, 14.5 with a lane's tokens one behind the other and divisions by the page's size).
+// between the steps, and a thread its sequence's tokens where none has more than four (16 requests a token each: 4.7 us, of which 0.9 a prefix
+// over the workgroup; 128 prompts, 8192 tokens: 13.4 us, 14.5 with a lane's tokens one behind the other and divisions by the page's size).
 // Else pages are given back by one launch, a second looks for shared pages and for the free ones of every 4096, one workgroup decides, and a
-// fourth launch writes tables and slots down (4096 requests, 287000 new tokens: 4, 4, 11 and 8 us; with one workgroup that looks for the free
+// fourth launch writes tables and slots down (4096 requests, 287000 new tokens: 3.0, 4.2, 11.0 and 9.6 us; more than 4096 are 16 a thread, which it
+// holds in scratch memory, 238 registers of them: 53 us for 8192, 89 for 16384; with one workgroup that looks for the free
 // pages too, 52 in place of 11 and 4).
 // What the atomics do (counts of users, the greatest of the keys of those that share a page) does not depend on their order.
 #include <hip/hip_runtime.h>
