@@ -246,7 +246,8 @@ extern "C" lora_status lora_cache_copy(const lora_cache* c, int32_t num_copies, 
     if (num_copies < 0 || misaligned(copies, 4) || (num_copies > 0 && !copies)) return LORA_ERR_INVALID_ARG;
     if (num_copies == 0 || c->num_seqs == 0) return LORA_OK;
     if (num_copies > most_workgroups(LORA_CACHE_COPY_THREADS) / c->num_kv_heads) return LORA_ERR_UNSUPPORTED;
-    const memory_rows list(copies, 1, 1, 2 * (int64_t)num_copies, 4), weights(c->weight, 1, 1, c->num_pages * c->num_kv_heads * c->page_tokens, 4);
+    const int64_t slots = (int64_t)c->num_kv_heads * c->page_tokens;
+    const memory_rows list(copies, 1, 1, 2 * (int64_t)num_copies, 4), weights(c->weight, 1, 1, std::min(c->num_pages, INT64_MAX / 8 / slots) * slots, 4);
     if (share_bytes(list, c) || (c->weight && c->num_pages > 0 && share_bytes(list, weights))) return LORA_ERR_INVALID_ARG;
     return status_of(launch_cache_copy(args_of(c, 0, 0, nullptr), num_copies, copies, static_cast<hipStream_t>(hip_stream)));
 }
